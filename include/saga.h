@@ -80,7 +80,8 @@ typedef enum saga_status {
   SAGA_EINTERNAL = 6
 } saga_status;
 
-typedef enum saga_dtype { SAGA_F32 = 0, SAGA_BF16 = 1 } saga_dtype;
+/* SAGA_I8: 8-bit rows with a float32 scale each, only where a call names it. */
+typedef enum saga_dtype { SAGA_F32 = 0, SAGA_BF16 = 1, SAGA_I8 = 2 } saga_dtype;
 
 /* Gather reductions (Table I "Gather" column; the simple sum/mean/max
  * reductions and the attention reduction of Sec. 2 "Survey Result"). */
@@ -568,6 +569,131 @@ saga_status saga_apply_vertex(const saga_gemm_op* op, saga_cmat a, saga_cmat w,
                               saga_cmat a2, saga_cmat w2, const float* bias,
                               const float* bias2, saga_mat out, void* workspace,
                               size_t workspace_bytes, void* stream);
+
+/* ======================================================================
+ * ApplyVertex in 8-bit integers
+ * ======================================================================
+ * A row x of float values is held as whole numbers q and one scale s:
+ *     s = max(A / 127, 2^-126), A the row's largest magnitude (A / 127 rounded
+ *         to float32)
+ *     q_k = x_k / s rounded to the nearest whole number, ties to even
+ * so that x_k is about s q_k and |q_k| <= 127.  The quotient is judged exactly:
+ * the same row gives the same q and s in every call that quantises.  A row that
+ * holds a NaN or an infinity has s = NaN and q = 0 (every result of it is NaN).
+ *
+ * saga_quantize_rows: x: M x K (dtype f32 or bf16); q: M x K int8 (16-byte base
+ * and ld a multiple of 16; columns [K, ld) are not written); scale: float[M].
+ * K < 2^31.  Weights are quantised the same way, one output channel a row (the
+ * transpose of saga_apply_vertex's w).
+ *
+ * saga_apply_vertex_quant: the transform of saga_apply_vertex (mode PLAIN) on
+ * 8-bit rows of a and w, with a scale per vertex and one per channel:
+ *     out[i, j] = act(rs_i * (a_scale[i] * w_scale[j] * sum_k a[i, k] w[j, k]) + bias[j])
+ * rs_i = row_scale_deg ? (deg[i] > 0 ? deg[i]^-1/2 : 0) : 1.  The sums are exact
+ * (32-bit whole numbers), the rest is float32.
+ * a: M x K: a_dtype I8: 8-bit rows with a_scale[M]; F32 / BF16: float rows,
+ * which the call quantises as above (a_scale must be NULL).  w: N x K int8, one
+ * channel a row, w_scale[N] (both any values; -128 is allowed).  out: M x N,
+ * out_dtype F32 or BF16.  a, w and out: 16-byte base and row pitch, ld below
+ * 2^23 for a and w.  1 <= K <= 131071, N >= 1.
+ * Workspace: saga_apply_vertex_quant_workspace_size() bytes (0: none, may be
+ * NULL), 256-byte aligned, scratch afterwards, not overlapping any argument.
+ * Calls that share one workspace must be ordered.
+ * Errors: SAGA_EINVAL, SAGA_EUNSUPPORTED (K or ld too large), SAGA_EWORKSPACE,
+ * SAGA_EDEVICE. */
+saga_status saga_quantize_rows(int32_t dtype, saga_cmat x, saga_mat q, float* scale, void* stream);
+
+typedef struct saga_quant_op {
+  int32_t a_dtype;                /* SAGA_I8, SAGA_F32 or SAGA_BF16 */
+  int32_t out_dtype;              /* SAGA_F32 or SAGA_BF16 */
+  int32_t act;                    /* saga_act */
+  const int32_t* row_scale_deg;   /* nullable, int32[M] */
+} saga_quant_op;
+
+saga_status saga_apply_vertex_quant_workspace_size(const saga_quant_op* op, int64_t m, int64_t k,
+                                                   int64_t n, size_t* bytes);
+
+saga_status saga_apply_vertex_quant(const saga_quant_op* op, saga_cmat a, const float* a_scale,
+                                    saga_cmat w, const float* w_scale, const float* bias,
+                                    saga_mat out, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
+/* ======================================================================
+ * The end of a block in a deep network
+ * ======================================================================
+ * What stands between two blocks of a residual network (a block: a Gather or a
+ * whole layer), in one pass over the rows:
+ *     u = post(block)
+ *     y = x + res_scale * channel_scale * act(gate) * u
+ *     z = pre(y)
+ * norms:  NONE  v
+ *         RMS   v / sqrt(mean(v^2) + eps) * weight + bias
+ *         LAYER (v - mean) / sqrt(mean((v - mean)^2) + eps) * weight + bias
+ * over the F columns of a row, in float32 (weight, bias: nullable float[F];
+ * eps > 0, finite).  z is computed from y as summed, before y is rounded to its
+ * type.
+ * block, gate: M x F, dtype; gate is absent (1) if its ptr is NULL; gate_act is
+ * applied to it.  channel_scale: float[F], nullable (1).
+ * x (the residual stream): M x F, x_dtype; absent (0) if its ptr is NULL.
+ * y: M x F, x_dtype; may be absent, and may be x itself (same ptr and ld: the
+ * stream is updated in place).  z: M x F, absent if its ptr is NULL; type dtype,
+ * or int8 with its scales in z_scale[M] if z_scale is given (8-bit rows as
+ * saga_quantize_rows makes them, of the float32 values of z).  One of y and z
+ * is required.  dtype / x_dtype: F32 / F32, BF16 / BF16 or BF16 / F32.
+ * 1 <= F <= 16384.  All matrices: 16-byte base and row pitch.
+ * Errors: SAGA_EINVAL, SAGA_EUNSUPPORTED (F, types), SAGA_EDEVICE. */
+typedef enum saga_norm { SAGA_NORM_NONE = 0, SAGA_NORM_RMS = 1, SAGA_NORM_LAYER = 2 } saga_norm;
+
+typedef struct saga_norm_desc {
+  int32_t kind;          /* saga_norm */
+  float eps;
+  const float* weight;   /* nullable */
+  const float* bias;     /* nullable */
+} saga_norm_desc;
+
+typedef struct saga_block_op {
+  int32_t dtype;                 /* block, gate, z */
+  int32_t x_dtype;               /* x, y */
+  saga_norm_desc post, pre;
+  int32_t gate_act;              /* saga_act */
+  float res_scale;
+  const float* channel_scale;    /* nullable */
+} saga_block_op;
+
+saga_status saga_block_norm(const saga_block_op* op, saga_cmat block, saga_cmat gate, saga_cmat x,
+                            saga_mat y, saga_mat z, float* z_scale, void* stream);
+
+/* ======================================================================
+ * Answers: log probabilities of labels, entropy, top classes
+ * ======================================================================
+ * For every row x of logits (a vertex over its classes, or a query over the
+ * candidates of a link), with log p_j = x_j - log sum_i e^(x_i):
+ *     logp[i]           = log p of labels[i]; 0 for a label below 0 (unknown),
+ *                         NaN for one that is C or more
+ *     entropy[i]        = -sum_j p_j log p_j
+ *     top_index[i, 0..] = the top_k classes by logit, equal logits by class;
+ *     top_logp[i, 0..]    their log probabilities
+ * A logit of -inf is a class that is not allowed: it has p = 0 and is no
+ * alternative.  Where fewer than top_k classes are left the rest has index -1
+ * and log probability -inf.  A row with nothing left has logp -inf and entropy
+ * 0; a row with a NaN or +inf has NaN for all, and indices -1.
+ * logits: M x C (dtype f32 or bf16; 16-byte base and row pitch), 1 <= C <= 2^30.
+ * labels: int32[M], with logp: float[M] (both or neither); entropy: float[M],
+ * nullable; top_index: int32[M * top_k] and top_logp: float[M * top_k] (both if
+ * top_k > 0), 0 <= top_k <= 64.  One of the outputs is required.
+ * Workspace: saga_label_log_probs_workspace_size() bytes (0: none, may be NULL),
+ * 256-byte aligned, scratch afterwards, not overlapping any argument.  Calls that
+ * share one workspace must be ordered.
+ * Errors: SAGA_EINVAL, SAGA_EUNSUPPORTED (C), SAGA_EWORKSPACE, SAGA_EDEVICE. */
+#define SAGA_MAX_TOP 64
+
+saga_status saga_label_log_probs_workspace_size(int32_t dtype, int64_t m, int64_t c, int32_t top_k,
+                                                size_t* bytes);
+
+saga_status saga_label_log_probs(int32_t dtype, saga_cmat logits, const int32_t* labels,
+                                 float* logp, float* entropy, int32_t top_k, int32_t* top_index,
+                                 float* top_logp, void* workspace, size_t workspace_bytes,
+                                 void* stream);
 
 /* ======================================================================
  * One whole layer (Table I models)

@@ -516,6 +516,282 @@ saga_status run_gemm(const saga_gemm_op& op, const saga_cmat& a, const saga_cmat
 }
 
 // -------------------------------------------------------------------------
+// 8-bit products, block norms, label log probabilities
+// -------------------------------------------------------------------------
+struct Span {
+  const void* p;
+  size_t n;
+};
+Span span(const saga_cmat& m, size_t es) { return {m.ptr, mat_bytes(m.rows, m.cols, m.ld, es)}; }
+Span span(const saga_mat& m, size_t es) { return {m.ptr, mat_bytes(m.rows, m.cols, m.ld, es)}; }
+Span span(const void* p, int64_t n, size_t es) { return {p, n > 0 ? (size_t)n * es : 0}; }
+
+// no output overlaps an input or another output
+template <size_t NO, size_t NI>
+saga_status check_apart(const Span (&outs)[NO], const Span (&ins)[NI]) {
+  for (size_t i = 0; i < NO; ++i) {
+    for (const Span& in : ins)
+      if (range_overlap(outs[i].p, outs[i].n, in.p, in.n)) return fail(SAGA_EINVAL, "output overlaps an input");
+    for (size_t j = i + 1; j < NO; ++j)
+      if (range_overlap(outs[i].p, outs[i].n, outs[j].p, outs[j].n))
+        return fail(SAGA_EINVAL, "two outputs overlap");
+  }
+  return SAGA_OK;
+}
+
+// a vector of n 4-byte values
+saga_status check_vec(const void* p, int64_t n, bool need, const char* name) {
+  if (need && n > 0 && !p) return fail(SAGA_EINVAL, "%s: null pointer", name);
+  if ((uintptr_t)p % 4 != 0) return fail(SAGA_EINVAL, "%s: misaligned base", name);
+  return SAGA_OK;
+}
+
+// rows x cols within what address arithmetic and byte counts hold
+saga_status check_extent(int64_t rows, int64_t cols, int64_t ld, const char* name) {
+  if (rows < 0) return fail(SAGA_EINVAL, "%s: %lld rows", name, (long long)rows);
+  if (cols <= 0) return fail(SAGA_EINVAL, "%s: %lld columns", name, (long long)cols);
+  if (ld > 0 && rows > ((int64_t)1 << 58) / ld) return fail(SAGA_EINVAL, "%s: size out of range", name);
+  return SAGA_OK;
+}
+
+saga_status check_ws(void* ws, size_t ws_bytes, size_t need, const char* what) {
+  if (need == 0) return SAGA_OK;
+  if (!ws || ws_bytes < need)
+    return fail(SAGA_EWORKSPACE, "%s workspace: need %zu bytes, got %zu", what, need, ws ? ws_bytes : (size_t)0);
+  if ((uintptr_t)ws % 256 != 0) return fail(SAGA_EINVAL, "workspace must be 256-byte aligned");
+  return SAGA_OK;
+}
+
+bool float_dtype(int32_t t) { return t == SAGA_F32 || t == SAGA_BF16; }
+
+saga_status run_quantize_rows(int32_t dtype, const saga_cmat& x, const saga_mat& q, float* scale,
+                              hipStream_t st) {
+  if (!float_dtype(dtype)) return fail(SAGA_EINVAL, "bad dtype");
+  saga_status s = check_extent(x.rows, x.cols, std::max(x.ld, q.ld), "x");
+  if (s) return s;
+  if (x.cols > INT32_MAX) return fail(SAGA_EUNSUPPORTED, "x: %lld columns", (long long)x.cols);
+  if ((s = check_mat(x.ptr, x.rows, x.cols, x.ld, x.rows, x.cols, esize(dtype), true, "x"))) return s;
+  if ((s = check_mat(q.ptr, q.rows, q.cols, q.ld, x.rows, x.cols, 1, true, "q"))) return s;
+  if ((s = check_vec(scale, x.rows, true, "scale"))) return s;
+  const Span outs[] = {span(q, 1), span(scale, x.rows, 4)}, ins[] = {span(x, esize(dtype))};
+  if ((s = check_apart(outs, ins))) return s;
+  saga::QuantRowsArgs a;
+  a.dtype = dtype;
+  a.M = x.rows;
+  a.K = x.cols;
+  a.x = x.ptr;
+  a.ldx = x.ld;
+  a.q = static_cast<int8_t*>(q.ptr);
+  a.ldq = q.ld;
+  a.scale = scale;
+  const hipError_t e = saga::launch_quantize_rows(a, st);
+  return e == hipSuccess ? ok() : dev_fail(e, "quantize launch");
+}
+
+saga_status check_quant_op(const saga_quant_op& op, int64_t m, int64_t k, int64_t n) {
+  if (op.a_dtype != SAGA_I8 && !float_dtype(op.a_dtype)) return fail(SAGA_EINVAL, "bad a_dtype");
+  if (!float_dtype(op.out_dtype)) return fail(SAGA_EINVAL, "bad out_dtype");
+  if (op.act < SAGA_ACT_NONE || op.act > SAGA_ACT_TANH) return fail(SAGA_EINVAL, "bad activation");
+  if (m < 0 || k <= 0 || n <= 0) return fail(SAGA_EINVAL, "m must be >= 0, k and n > 0");
+  if (k > saga::kQuantMaxK) return fail(SAGA_EUNSUPPORTED, "8-bit product: k %lld too large", (long long)k);
+  if (n > INT32_MAX || m > ((int64_t)1 << 40)) return fail(SAGA_EUNSUPPORTED, "8-bit product: m or n too large");
+  return SAGA_OK;
+}
+
+// workspace: the rows quantised (ld whole 16 bytes), then their scales
+size_t quant_ws_bytes(const saga_quant_op& op, int64_t m, int64_t k, int64_t n) {
+  if (op.a_dtype == SAGA_I8 || m == 0) return 0;
+  return align256((size_t)m * round_up(k, 16)) + align256((size_t)m * 4);
+}
+
+saga_status run_quant(const saga_quant_op& op, const saga_cmat& a, const float* a_scale, const saga_cmat& w,
+                      const float* w_scale, const float* bias, const saga_mat& out, void* ws,
+                      size_t ws_bytes, hipStream_t st) {
+  const int64_t M = a.rows, K = a.cols, N = w.rows;
+  saga_status s = check_quant_op(op, M, K, N);
+  if (s) return s;
+  const bool i8 = op.a_dtype == SAGA_I8;
+  const size_t ea = i8 ? 1 : esize(op.a_dtype), eo = esize(op.out_dtype);
+  if ((s = check_extent(M, K, a.ld, "a"))) return s;
+  if ((s = check_extent(N, K, w.ld, "w"))) return s;
+  if ((s = check_extent(M, N, out.ld, "out"))) return s;
+  if ((s = check_mat(a.ptr, M, K, a.ld, M, K, ea, true, "a"))) return s;
+  if ((s = check_mat(w.ptr, N, w.cols, w.ld, N, K, 1, true, "w"))) return s;
+  if ((s = check_mat(out.ptr, out.rows, out.cols, out.ld, M, N, eo, true, "out"))) return s;
+  if (a.ld >= saga::kQuantMaxLd || w.ld >= saga::kQuantMaxLd)
+    return fail(SAGA_EUNSUPPORTED, "8-bit product: ld of a and w must be below 2^23");
+  if (!i8 && a_scale) return fail(SAGA_EINVAL, "a_scale is for 8-bit rows (a float a is quantised by the call)");
+  if ((s = check_vec(a_scale, M, i8, "a_scale"))) return s;
+  if ((s = check_vec(w_scale, N, true, "w_scale"))) return s;
+  if ((s = check_vec(bias, N, false, "bias"))) return s;
+  if ((s = check_vec(op.row_scale_deg, M, false, "row_scale_deg"))) return s;
+  const size_t need = quant_ws_bytes(op, M, K, N);
+  if ((s = check_ws(ws, ws_bytes, need, "apply_vertex_quant"))) return s;
+  const Span outs[] = {span(out, eo), Span{ws, need}};
+  const Span ins[] = {span(a, ea), span(w, 1), span(a_scale, M, 4), span(w_scale, N, 4), span(bias, N, 4),
+                      span(op.row_scale_deg, M, 4)};
+  if ((s = check_apart(outs, ins))) return s;
+  saga::QuantGemmArgs g;
+  g.M = M;
+  g.N = N;
+  g.K = K;
+  g.a = static_cast<const int8_t*>(a.ptr);
+  g.lda = a.ld;
+  g.a_scale = a_scale;
+  g.w = static_cast<const int8_t*>(w.ptr);
+  g.ldw = w.ld;
+  g.w_scale = w_scale;
+  g.bias = bias;
+  g.row_scale_deg = op.row_scale_deg;
+  g.act = op.act;
+  g.out_dtype = op.out_dtype;
+  g.out = out.ptr;
+  g.ldo = out.ld;
+  if (!i8 && M > 0) {
+    Carve c(ws, ws_bytes);
+    saga::QuantRowsArgs r;
+    r.dtype = op.a_dtype;
+    r.M = M;
+    r.K = K;
+    r.x = a.ptr;
+    r.ldx = a.ld;
+    r.ldq = round_up(K, 16);
+    r.q = static_cast<int8_t*>(c.take((size_t)M * r.ldq));
+    r.scale = static_cast<float*>(c.take((size_t)M * 4));
+    const hipError_t e = saga::launch_quantize_rows(r, st);
+    if (e != hipSuccess) return dev_fail(e, "quantize launch");
+    g.a = r.q;
+    g.lda = r.ldq;
+    g.a_scale = r.scale;
+  }
+  const hipError_t e = saga::launch_gemm_quant(g, st);
+  return e == hipSuccess ? ok() : dev_fail(e, "8-bit product launch");
+}
+
+saga_status check_norm(const saga_norm_desc& d, int64_t F, const char* name) {
+  if (d.kind < SAGA_NORM_NONE || d.kind > SAGA_NORM_LAYER) return fail(SAGA_EINVAL, "%s: bad norm", name);
+  if (d.kind != SAGA_NORM_NONE && !(d.eps > 0.0f && d.eps < 1e30f))
+    return fail(SAGA_EINVAL, "%s: eps must be > 0 and finite", name);
+  saga_status s = check_vec(d.weight, F, false, name);
+  return s ? s : check_vec(d.bias, F, false, name);
+}
+
+saga_status run_block_norm(const saga_block_op& op, const saga_cmat& block, const saga_cmat& gate,
+                           const saga_cmat& x, const saga_mat& y, const saga_mat& z, float* z_scale,
+                           hipStream_t st) {
+  const int64_t M = block.rows, F = block.cols;
+  if (!float_dtype(op.dtype) || !float_dtype(op.x_dtype)) return fail(SAGA_EINVAL, "bad dtype");
+  if (op.x_dtype == SAGA_BF16 && op.dtype == SAGA_F32)
+    return fail(SAGA_EUNSUPPORTED, "a bfloat16 stream takes bfloat16 blocks");
+  if (op.gate_act < SAGA_ACT_NONE || op.gate_act > SAGA_ACT_TANH) return fail(SAGA_EINVAL, "bad activation");
+  saga_status s;
+  const int64_t lds = std::max({block.ld, gate.ptr ? gate.ld : 0, x.ptr ? x.ld : 0, y.ptr ? y.ld : 0,
+                                z.ptr ? z.ld : 0});
+  if ((s = check_extent(M, F, lds, "block"))) return s;
+  if (F > saga::kBlockMaxF) return fail(SAGA_EUNSUPPORTED, "block norm: width %lld too large", (long long)F);
+  if ((s = check_norm(op.post, F, "post norm"))) return s;
+  if ((s = check_norm(op.pre, F, "pre norm"))) return s;
+  if ((s = check_vec(op.channel_scale, F, false, "channel_scale"))) return s;
+  const size_t e = esize(op.dtype), ex = esize(op.x_dtype), ez = z_scale ? 1 : e;
+  if ((s = check_mat(block.ptr, M, F, block.ld, M, F, e, true, "block"))) return s;
+  if (gate.ptr && (s = check_mat(gate.ptr, gate.rows, gate.cols, gate.ld, M, F, e, true, "gate"))) return s;
+  if (x.ptr && (s = check_mat(x.ptr, x.rows, x.cols, x.ld, M, F, ex, true, "x"))) return s;
+  if (y.ptr && (s = check_mat(y.ptr, y.rows, y.cols, y.ld, M, F, ex, true, "y"))) return s;
+  if (z.ptr && (s = check_mat(z.ptr, z.rows, z.cols, z.ld, M, F, ez, true, "z"))) return s;
+  if (M > 0 && !y.ptr && !z.ptr) return fail(SAGA_EINVAL, "neither y nor z is given");
+  if (z_scale && M > 0 && !z.ptr) return fail(SAGA_EINVAL, "z_scale without z");
+  if ((s = check_vec(z_scale, M, false, "z_scale"))) return s;
+  const bool in_place = y.ptr && y.ptr == x.ptr && y.ld == x.ld;
+  const Span outs[] = {y.ptr ? span(y, ex) : Span{nullptr, 0}, z.ptr ? span(z, ez) : Span{nullptr, 0},
+                       span(z_scale, M, 4)};
+  const Span none{nullptr, 0};
+  const Span ins[] = {span(block, e), gate.ptr ? span(gate, e) : none,
+                      x.ptr && !in_place ? span(x, ex) : none, span(op.post.weight, F, 4),
+                      span(op.post.bias, F, 4), span(op.pre.weight, F, 4), span(op.pre.bias, F, 4),
+                      span(op.channel_scale, F, 4)};
+  if ((s = check_apart(outs, ins))) return s;
+  saga::BlockArgs a;
+  memset(&a, 0, sizeof(a));
+  a.M = M;
+  a.F = (int)F;
+  a.dtype = op.dtype;
+  a.x_dtype = op.x_dtype;
+  a.block = block.ptr;
+  a.ld_block = block.ld;
+  a.gate = gate.ptr;
+  a.ld_gate = gate.ld;
+  a.x = x.ptr;
+  a.ld_x = x.ld;
+  a.y = y.ptr;
+  a.ld_y = y.ld;
+  a.z = z.ptr;
+  a.ld_z = z.ld;
+  a.z_scale = z_scale;
+  a.post_kind = op.post.kind;
+  a.pre_kind = op.pre.kind;
+  a.gate_act = op.gate_act;
+  a.post_eps = op.post.eps;
+  a.pre_eps = op.pre.eps;
+  a.res_scale = op.res_scale;
+  a.post_w = op.post.weight;
+  a.post_b = op.post.bias;
+  a.pre_w = op.pre.weight;
+  a.pre_b = op.pre.bias;
+  a.channel = op.channel_scale;
+  const hipError_t err = saga::launch_block_norm(a, st);
+  return err == hipSuccess ? ok() : dev_fail(err, "block norm launch");
+}
+
+saga_status check_labels(int32_t dtype, int64_t m, int64_t c, int32_t top_k) {
+  if (!float_dtype(dtype)) return fail(SAGA_EINVAL, "bad dtype");
+  if (top_k < 0 || top_k > SAGA_MAX_TOP) return fail(SAGA_EINVAL, "top_k must be 0 to %d", SAGA_MAX_TOP);
+  if (m < 0 || c <= 0) return fail(SAGA_EINVAL, "logits: %lld x %lld", (long long)m, (long long)c);
+  if (c > saga::kLabelsMaxC) return fail(SAGA_EUNSUPPORTED, "logits: %lld classes", (long long)c);
+  if (m > ((int64_t)1 << 40)) return fail(SAGA_EUNSUPPORTED, "logits: %lld rows", (long long)m);
+  return SAGA_OK;
+}
+
+saga_status run_labels(int32_t dtype, const saga_cmat& logits, const int32_t* labels, float* logp,
+                       float* entropy, int32_t top_k, int32_t* top_index, float* top_logp, void* ws,
+                       size_t ws_bytes, hipStream_t st) {
+  const int64_t M = logits.rows, C = logits.cols;
+  saga_status s = check_labels(dtype, M, C, top_k);
+  if (s) return s;
+  if ((s = check_extent(M, C, logits.ld, "logits"))) return s;
+  if ((s = check_mat(logits.ptr, M, C, logits.ld, M, C, esize(dtype), true, "logits"))) return s;
+  if (M > 0 && !labels != !logp) return fail(SAGA_EINVAL, "labels and logp: both or neither");
+  if ((s = check_vec(labels, M, false, "labels"))) return s;
+  if ((s = check_vec(logp, M, false, "logp"))) return s;
+  if ((s = check_vec(entropy, M, false, "entropy"))) return s;
+  if ((s = check_vec(top_index, M, top_k > 0, "top_index"))) return s;
+  if ((s = check_vec(top_logp, M, top_k > 0, "top_logp"))) return s;
+  if (M > 0 && !logp && !entropy && top_k == 0) return fail(SAGA_EINVAL, "no output is asked for");
+  const size_t need = saga::labels_workspace_bytes(dtype, M, C, top_k);
+  if ((s = check_ws(ws, ws_bytes, need, "label_log_probs"))) return s;
+  const int64_t MK = M * top_k;
+  const Span outs[] = {span(logp, M, 4), span(entropy, M, 4), span(top_index, MK, 4), span(top_logp, MK, 4),
+                       Span{ws, need}};
+  const Span ins[] = {span(logits, esize(dtype)), span(labels, M, 4)};
+  if ((s = check_apart(outs, ins))) return s;
+  saga::LabelArgs a;
+  memset(&a, 0, sizeof(a));
+  a.dtype = dtype;
+  a.M = M;
+  a.C = C;
+  a.logits = logits.ptr;
+  a.ld = logits.ld;
+  a.labels = labels;
+  a.logp = logp;
+  a.entropy = entropy;
+  a.top_k = top_k;
+  a.top_index = top_index;
+  a.top_logp = top_logp;
+  a.ws = ws;
+  const hipError_t e = saga::launch_label_log_probs(a, st);
+  return e == hipSuccess ? ok() : dev_fail(e, "label log probability launch");
+}
+
+// -------------------------------------------------------------------------
 // layers
 // -------------------------------------------------------------------------
 struct LayerPlanWs {
@@ -1646,6 +1922,75 @@ saga_status saga_apply_vertex(const saga_gemm_op* op, saga_cmat a, saga_cmat w, 
     if (!op) return fail(SAGA_EINVAL, "op is null");
     return run_gemm(*op, a, w, a2, w2, bias, bias2, out, workspace, workspace_bytes,
                     static_cast<hipStream_t>(stream));
+  } catch (...) {
+    return fail(SAGA_EINTERNAL, "exception");
+  }
+}
+
+saga_status saga_quantize_rows(int32_t dtype, saga_cmat x, saga_mat q, float* scale, void* stream) {
+  try {
+    return run_quantize_rows(dtype, x, q, scale, static_cast<hipStream_t>(stream));
+  } catch (...) {
+    return fail(SAGA_EINTERNAL, "exception");
+  }
+}
+
+saga_status saga_apply_vertex_quant_workspace_size(const saga_quant_op* op, int64_t m, int64_t k,
+                                                   int64_t n, size_t* bytes) {
+  try {
+    if (!op || !bytes) return fail(SAGA_EINVAL, "null argument");
+    saga_status s = check_quant_op(*op, m, k, n);
+    if (s) return s;
+    *bytes = quant_ws_bytes(*op, m, k, n);
+    return ok();
+  } catch (...) {
+    return fail(SAGA_EINTERNAL, "exception");
+  }
+}
+
+saga_status saga_apply_vertex_quant(const saga_quant_op* op, saga_cmat a, const float* a_scale,
+                                    saga_cmat w, const float* w_scale, const float* bias,
+                                    saga_mat out, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+  try {
+    if (!op) return fail(SAGA_EINVAL, "op is null");
+    return run_quant(*op, a, a_scale, w, w_scale, bias, out, workspace, workspace_bytes,
+                     static_cast<hipStream_t>(stream));
+  } catch (...) {
+    return fail(SAGA_EINTERNAL, "exception");
+  }
+}
+
+saga_status saga_block_norm(const saga_block_op* op, saga_cmat block, saga_cmat gate, saga_cmat x,
+                            saga_mat y, saga_mat z, float* z_scale, void* stream) {
+  try {
+    if (!op) return fail(SAGA_EINVAL, "op is null");
+    return run_block_norm(*op, block, gate, x, y, z, z_scale, static_cast<hipStream_t>(stream));
+  } catch (...) {
+    return fail(SAGA_EINTERNAL, "exception");
+  }
+}
+
+saga_status saga_label_log_probs_workspace_size(int32_t dtype, int64_t m, int64_t c, int32_t top_k,
+                                                size_t* bytes) {
+  try {
+    if (!bytes) return fail(SAGA_EINVAL, "null argument");
+    saga_status s = check_labels(dtype, m, c, top_k);
+    if (s) return s;
+    *bytes = saga::labels_workspace_bytes(dtype, m, c, top_k);
+    return ok();
+  } catch (...) {
+    return fail(SAGA_EINTERNAL, "exception");
+  }
+}
+
+saga_status saga_label_log_probs(int32_t dtype, saga_cmat logits, const int32_t* labels,
+                                 float* logp, float* entropy, int32_t top_k, int32_t* top_index,
+                                 float* top_logp, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+  try {
+    return run_labels(dtype, logits, labels, logp, entropy, top_k, top_index, top_logp, workspace,
+                      workspace_bytes, static_cast<hipStream_t>(stream));
   } catch (...) {
     return fail(SAGA_EINTERNAL, "exception");
   }

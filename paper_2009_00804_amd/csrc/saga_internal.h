@@ -191,6 +191,70 @@ bool gemm_streams(int dtype, int mode, int64_t M, int64_t N, int64_t K, int64_t 
 size_t stream_workspace_bytes(int64_t N, int64_t K, int64_t K2);
 hipError_t launch_gemm_stream(const GemmArgs& g, hipStream_t st);
 
+// ---- quant.hip: 8-bit rows and products ----
+struct QuantRowsArgs {
+  int dtype;
+  int64_t M, K;
+  const void* x; int64_t ldx;
+  int8_t* q; int64_t ldq;
+  float* scale;
+};
+hipError_t launch_quantize_rows(const QuantRowsArgs& a, hipStream_t st);
+
+struct QuantGemmArgs {
+  int64_t M, N, K;
+  const int8_t* a; int64_t lda;     // M x K
+  const float* a_scale;
+  const int8_t* w; int64_t ldw;     // N x K
+  const float* w_scale;
+  const float* bias;                // nullable
+  const int32_t* row_scale_deg;     // nullable
+  int act, out_dtype;
+  void* out; int64_t ldo;
+};
+constexpr int64_t kQuantMaxK = 131071;      // 128 * 128 k stays below 2^31
+constexpr int64_t kQuantMaxLd = 1 << 23;    // a tile's rows within 32-bit offsets
+hipError_t launch_gemm_quant(const QuantGemmArgs& g, hipStream_t st);
+
+// ---- block.hip ----
+constexpr int64_t kBlockMaxF = 16384;
+struct BlockArgs {
+  int64_t M;
+  int F, dtype, x_dtype;
+  const void* block; int64_t ld_block;
+  const void* gate; int64_t ld_gate;   // nullable
+  const void* x; int64_t ld_x;         // nullable
+  void* y; int64_t ld_y;               // nullable
+  void* z; int64_t ld_z;               // nullable
+  float* z_scale;                      // set: z is int8
+  int post_kind, pre_kind, gate_act;
+  float post_eps, pre_eps, res_scale;
+  const float *post_w, *post_b, *pre_w, *pre_b, *channel;  // nullable
+};
+hipError_t launch_block_norm(const BlockArgs& a, hipStream_t st);
+
+// ---- labels.hip ----
+struct LabelArgs {
+  int dtype;
+  int64_t M, C;
+  const void* logits; int64_t ld;
+  const int32_t* labels;    // with logp
+  float* logp;              // nullable
+  float* entropy;           // nullable
+  int top_k;
+  int32_t* top_index;       // M x top_k
+  float* top_logp;
+  void* ws;
+  // set by launch_label_log_probs: ranges of columns per row, and their results
+  int parts;
+  int64_t range;
+  float *part_stats, *part_value;
+  int32_t* part_index;
+};
+constexpr int64_t kLabelsMaxC = 1 << 30;
+size_t labels_workspace_bytes(int dtype, int64_t M, int64_t C, int top_k);
+hipError_t launch_label_log_probs(const LabelArgs& a, hipStream_t st);
+
 // ---- rel.hip ----
 constexpr int kRelTile = SAGA_REL_TILE;  // rows per grouped-GEMM tile
 constexpr int kRelMaxRelations = SAGA_REL_MAX_RELATIONS;

@@ -4,10 +4,15 @@
 workspace and output, so a forward pass enqueues kernels and nothing else.
 The two-layer models of the workloads (GCN: ReLU then raw output; GAT:
 concat + ELU then head mean) are sequences of such layers.
+
+``quantize_rows``, ``quant_linear``, ``block_norm`` and ``label_log_probs`` call
+the operators of a deep network on torch tensors; ``ResidualGCN`` is such a
+network, served with 8-bit transforms.
 """
 from __future__ import annotations
 
 import ctypes as C
+import functools
 
 import torch
 
@@ -123,3 +128,233 @@ def run(layers, x, edge_feat=None, stream=None):
     for l in layers:
         h = l(h, edge_feat=edge_feat, stream=stream)
     return h
+
+
+# --------------------------------------------------------------------------
+# operators of a deep network on torch tensors
+# --------------------------------------------------------------------------
+def _placed(f):
+    """Runs f on its first tensor's device and on ``stream`` (None: torch's
+    current stream of that device).  Outputs and workspaces are allocated there,
+    so calls on different streams or in different graphs share none."""
+    @functools.wraps(f)
+    def call(x, *args, stream=None, **kw):
+        if not x.is_cuda:
+            raise ValueError(f"{f.__name__}: tensors on the GPU are needed, got one on {x.device}")
+        if stream is None and x.device.index == torch.cuda.current_device():
+            return f(x, *args, **kw)
+        with torch.cuda.device(x.device), torch.cuda.stream(stream):
+            if torch.cuda.current_device() != x.device.index:
+                raise ValueError(f"{f.__name__}: the stream belongs to another device than {x.device}")
+            return f(x, *args, **kw)
+    return call
+
+
+def _matrix(t, name, like, dtypes, shape=None):
+    """saga_cmat of a 2-D tensor on the device of ``like``"""
+    if t is None:
+        return S.saga_cmat(None, 0, 0, 0)
+    if t.dim() != 2 or t.dtype not in dtypes or t.device != like.device:
+        raise ValueError(f"{name}: a 2-D tensor of {dtypes} on {like.device} is needed, got "
+                         f"{tuple(t.shape)} {t.dtype} on {t.device}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        raise ValueError(f"{name}: the columns of a row have to be neighbours")
+    return S.saga_cmat(t.data_ptr(), t.shape[0], t.shape[1], t.stride(0))
+
+
+def _vector(t, name, like, n, dtype=torch.float32):
+    """address of a contiguous vector of n values on the device of ``like``"""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != like.device or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: {n} contiguous values of {dtype} on {like.device} are needed, got "
+                         f"{tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _out(rows, cols, dtype, like):
+    """(view, saga_mat) of a new matrix with 16-byte rows"""
+    a = 16 // dtype.itemsize
+    ld = (cols + a - 1) // a * a
+    buf = torch.empty((rows, ld), dtype=dtype, device=like.device)
+    return (buf if ld == cols else buf[:, :cols]), S.saga_mat(buf.data_ptr(), rows, cols, ld)
+
+
+def _space(nbytes, like):
+    return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+
+
+_FLOATS = (torch.float32, torch.bfloat16)
+_NO_MAT = S.saga_mat(None, 0, 0, 0)
+
+
+@_placed
+def quantize_rows(x):
+    """(q, scale): the 8-bit rows of x and their float32 scales."""
+    cx = _matrix(x, "x", x, _FLOATS)
+    q, mq = _out(x.shape[0], x.shape[1], torch.int8, x)
+    scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    S.saga_quantize_rows(S.dtype_code(x.dtype), cx, mq, scale.data_ptr(), S.stream_handle())
+    return q, scale
+
+
+@_placed
+def quant_linear(x, w, w_scale, x_scale=None, bias=None, act="none", row_scale_deg=None, out_dtype=None):
+    """act(rs * (x w^T) + bias) in 8-bit integers: w and w_scale hold one output
+    channel a row; x is 8-bit rows with x_scale, or float rows that the call
+    quantises.  out_dtype: x's own, float32 for 8-bit rows."""
+    m, k = x.shape
+    i8 = x.dtype == torch.int8
+    if out_dtype is None:
+        out_dtype = torch.float32 if i8 else x.dtype
+    cx = _matrix(x, "x", x, (torch.int8,) if i8 else _FLOATS)
+    cw = _matrix(w, "w", x, (torch.int8,), (w.shape[0], k))
+    n = w.shape[0]
+    op = S.saga_quant_op(S.SAGA_I8 if i8 else S.dtype_code(x.dtype), S.dtype_code(out_dtype), S.ACT[act],
+                         _vector(row_scale_deg, "row_scale_deg", x, m, torch.int32))
+    out, mo = _out(m, n, out_dtype, x)
+    nbytes = S.saga_apply_vertex_quant_workspace_size(op, m, k, n)
+    ws = _space(nbytes, x)
+    S.saga_apply_vertex_quant(op, cx, _vector(x_scale, "x_scale", x, m), cw,
+                              _vector(w_scale, "w_scale", x, n), _vector(bias, "bias", x, n), mo,
+                              ws.data_ptr() if nbytes else None, nbytes, S.stream_handle())
+    return out
+
+
+@_placed
+def block_norm(block, x=None, *, post="none", post_weight=None, post_bias=None, gate=None, gate_act="none",
+               channel_scale=None, res_scale=1.0, pre="none", pre_weight=None, pre_bias=None, eps=1e-5,
+               quantize=False, in_place=False, x_dtype=None):
+    """(y, z, z_scale): y = x + res_scale * channel_scale * act(gate) * post(block)
+    and z = pre(y), quantised to 8-bit rows with z_scale if ``quantize`` (else
+    z_scale is None).  x_dtype: the type of y where there is no x; in_place: y is
+    written into x."""
+    m, f = block.shape
+    cb = _matrix(block, "block", block, _FLOATS)
+    if x is not None:
+        x_dtype = x.dtype
+    elif x_dtype is None:
+        x_dtype = block.dtype
+    cx = _matrix(x, "x", block, _FLOATS, block.shape)
+    cg = _matrix(gate, "gate", block, (block.dtype,), block.shape)
+    op = S.saga_block_op(
+        S.dtype_code(block.dtype), S.dtype_code(x_dtype),
+        S.saga_norm_desc(S.NORM[post], eps, _vector(post_weight, "post_weight", block, f),
+                         _vector(post_bias, "post_bias", block, f)),
+        S.saga_norm_desc(S.NORM[pre], eps, _vector(pre_weight, "pre_weight", block, f),
+                         _vector(pre_bias, "pre_bias", block, f)),
+        S.ACT[gate_act], res_scale, _vector(channel_scale, "channel_scale", block, f))
+    if in_place:
+        if x is None:
+            raise ValueError("in_place: there is no x")
+        y, my = x, S.saga_mat(cx.ptr, cx.rows, cx.cols, cx.ld)
+    else:
+        y, my = _out(m, f, x_dtype, block)
+    z, mz = _out(m, f, torch.int8 if quantize else block.dtype, block)
+    zs = torch.empty(m, dtype=torch.float32, device=block.device) if quantize else None
+    S.saga_block_norm(op, cb, cg, cx, my, mz, zs.data_ptr() if quantize else None, S.stream_handle())
+    return y, z, zs
+
+
+@_placed
+def label_log_probs(logits, labels=None, top_k=0, entropy=True):
+    """(logp, entropy, top_index, top_logp) of rows of logits; logp is None without
+    labels, entropy None if it is not asked for."""
+    m, c = logits.shape
+    cl = _matrix(logits, "logits", logits, _FLOATS)
+    code = S.dtype_code(logits.dtype)
+    at = _vector(labels, "labels", logits, m, torch.int32)
+    nbytes = S.saga_label_log_probs_workspace_size(code, m, c, top_k)
+    ws = _space(nbytes, logits)
+    dev = logits.device
+    lp = torch.empty(m, dtype=torch.float32, device=dev) if labels is not None else None
+    h = torch.empty(m, dtype=torch.float32, device=dev) if entropy else None
+    ti = torch.empty((m, top_k), dtype=torch.int32, device=dev)
+    tl = torch.empty((m, top_k), dtype=torch.float32, device=dev)
+    S.saga_label_log_probs(code, cl, at, lp.data_ptr() if labels is not None else None,
+                           h.data_ptr() if entropy else None, top_k, ti.data_ptr() if top_k else None,
+                           tl.data_ptr() if top_k else None, ws.data_ptr() if nbytes else None, nbytes,
+                           S.stream_handle())
+    return lp, h, ti, tl
+
+
+class ResidualGCN:
+    """A deep GCN with a gated residual stream, its transforms in 8-bit integers.
+
+        h = x W_in + b_in
+        per block:  z = pre(h) in 8 bits;  [v | g] = z [W | W_g] + [0 | b_g]
+                    m = relu(d_in^-1/2 A d_out^-1/2 v + b)
+                    h = h + res_scale * sigmoid(g) * post(m)
+        logits = norm(h) W_out + b_out
+
+    weights: W_in (F_in x F), b_in, blocks: a list of dicts with W, W_g (F x F),
+    b, b_g, pre, post (norm weights, F), then norm (F), W_out (F x classes), b_out;
+    float32 tensors or arrays.  The weights are quantised once, one scale per
+    output channel.  F is a multiple of 8.  The stream h is float32, blocks are
+    ``dtype``; both norms are RMS norms."""
+
+    def __init__(self, graph: S.Graph, weights: dict, dtype=torch.bfloat16, res_scale=1.0, eps=1e-5):
+        dev = graph.row_ptr.device
+        self.graph, self.dtype, self.res_scale, self.eps = graph, dtype, res_scale, eps
+
+        def vector(v):
+            return _dev(v, dev, torch.float32)
+
+        def transform(w, b):
+            rows = _dev(w, dev, torch.float32).t()
+            wide, _ = _out(rows.shape[0], rows.shape[1], torch.float32, rows)
+            return (*quantize_rows(wide.copy_(rows)), vector(b))
+
+        self.f = f = weights["blocks"][0]["W"].shape[0] if weights["blocks"] else weights["W_out"].shape[0]
+        if f % 8:
+            raise ValueError(f"the hidden width has to be a multiple of 8, got {f}")
+        self.first = transform(weights["W_in"], weights["b_in"])
+        self.blocks = []
+        for b in weights["blocks"]:
+            w, w_g = (_dev(b[k], dev, torch.float32) for k in ("W", "W_g"))
+            gate_bias = torch.cat([torch.zeros(f, device=dev), vector(b["b_g"])])
+            self.blocks.append(dict(both=transform(torch.cat([w, w_g], 1), gate_bias), bias=vector(b["b"]),
+                                    pre=vector(b["pre"]), post=vector(b["post"])))
+        self.norm = vector(weights["norm"])
+        self.last = transform(weights["W_out"], weights["b_out"])
+        self.op = S.saga_edge_op()
+        self.op.msg, self.op.reduce, self.op.dtype = S.SAGA_MSG_SRC_NORM, S.SAGA_RED_SUM, S.dtype_code(dtype)
+        self.op.heads, self.op.dst_norm, self.op.act = 1, 1, S.SAGA_ACT_RELU
+        self.ws_bytes = S.saga_gather_workspace_size(graph.plan, self.op, f)
+
+    def gather(self, v, bias):
+        """relu(d_in^-1/2 A d_out^-1/2 v + bias)"""
+        out, mo = _out(self.graph.num_dst, self.f, self.dtype, v)
+        ws = S.workspace(self.ws_bytes, v.device)
+        inputs = S.saga_edge_inputs()
+        inputs.src = S.cmat(v)
+        inputs.bias = bias.data_ptr()
+        S.saga_scatter_apply_edge_gather(self.graph.plan, self.op, inputs, mo, C.c_void_p(ws.data_ptr()),
+                                         ws.numel(), S.stream_handle())
+        return out
+
+    def logits(self, x):
+        """x: num_vertices x F_in (float32 or bfloat16) on the graph's device"""
+        if x.device != self.graph.row_ptr.device:
+            raise ValueError(f"x is on {x.device}, the graph on {self.graph.row_ptr.device}")
+        with torch.cuda.device(x.device):
+            w, ws, b = self.first
+            h = quant_linear(x, w, ws, bias=b, out_dtype=self.dtype)
+            norms = [blk["pre"] for blk in self.blocks] + [self.norm]
+            h, z, zs = block_norm(h, None, x_dtype=torch.float32, pre="rms", pre_weight=norms[0], eps=self.eps,
+                                  quantize=True)
+            for blk, norm in zip(self.blocks, norms[1:]):
+                w, ws, b = blk["both"]
+                vg = quant_linear(z, w, ws, x_scale=zs, bias=b, out_dtype=self.dtype)
+                m = self.gather(vg[:, :self.f], blk["bias"])
+                h, z, zs = block_norm(m, h, post="rms", post_weight=blk["post"], gate=vg[:, self.f:],
+                                      gate_act="sigmoid", res_scale=self.res_scale, pre="rms", pre_weight=norm,
+                                      eps=self.eps, quantize=True, in_place=True)
+            w, ws, b = self.last
+            return quant_linear(z, w, ws, x_scale=zs, bias=b)
+
+    def __call__(self, x, labels=None, top_k=1):
+        """(logp, entropy, top_index, top_logp) of every vertex"""
+        return label_log_probs(self.logits(x), labels, top_k)

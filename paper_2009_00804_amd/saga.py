@@ -21,17 +21,20 @@ LIB_PATH = os.path.join(_PKG, "libsaga.so")
 
 # enums (saga.h)
 SAGA_OK, SAGA_EINVAL, SAGA_EGRAPH, SAGA_EUNSUPPORTED, SAGA_EDEVICE, SAGA_EWORKSPACE, SAGA_EINTERNAL = range(7)
-SAGA_F32, SAGA_BF16 = 0, 1
+SAGA_F32, SAGA_BF16, SAGA_I8 = 0, 1, 2
 SAGA_RED_SUM, SAGA_RED_MEAN, SAGA_RED_MAX, SAGA_RED_SOFTMAX = range(4)
 SAGA_MSG_COPY, SAGA_MSG_SRC_NORM, SAGA_MSG_GAT, SAGA_MSG_GATED, SAGA_MSG_TYPED = range(5)
 SAGA_ACT_NONE, SAGA_ACT_RELU, SAGA_ACT_ELU, SAGA_ACT_SIGMOID, SAGA_ACT_TANH = range(5)
 SAGA_GEMM_PLAIN, SAGA_GEMM_CONCAT, SAGA_GEMM_GRU = range(3)
 (SAGA_LAYER_GCN, SAGA_LAYER_GAT, SAGA_LAYER_SAGE_POOL, SAGA_LAYER_GATED_GRU, SAGA_LAYER_SAGE_LSTM,
  SAGA_LAYER_RGCN) = range(6)
+SAGA_NORM_NONE, SAGA_NORM_RMS, SAGA_NORM_LAYER = range(3)
+SAGA_MAX_TOP = 64
 SAGA_REL_TILE = 128
 SAGA_REL_MAX_RELATIONS = 2048
 
 ACT = {"none": 0, "relu": 1, "elu": 2, "sigmoid": 3, "tanh": 4}
+NORM = {"none": 0, "rms": 1, "layer": 2}
 
 EXPORTS = [
     "saga_plan_workspace_size", "saga_plan_build", "saga_plan_build_split", "saga_plan_check",
@@ -43,6 +46,8 @@ EXPORTS = [
     "saga_rel_plan_workspace_size", "saga_rel_plan_build", "saga_rel_plan_check",
     "saga_rel_transform_workspace_size", "saga_rel_transform",
     "saga_apply_vertex_workspace_size", "saga_apply_vertex",
+    "saga_quantize_rows", "saga_apply_vertex_quant_workspace_size", "saga_apply_vertex_quant",
+    "saga_block_norm", "saga_label_log_probs_workspace_size", "saga_label_log_probs",
     "saga_layer_workspace_size", "saga_layer", "saga_trace_stages", "saga_sync_check",
     "saga_status_str", "saga_last_error", "saga_version",
 ]
@@ -116,6 +121,20 @@ class saga_gemm_op(C.Structure):
                 ("row_scale_deg", C.c_void_p), ("split_col", C.c_int32), ("tail", saga_mat)]
 
 
+class saga_quant_op(C.Structure):
+    _fields_ = [("a_dtype", C.c_int), ("out_dtype", C.c_int), ("act", C.c_int),
+                ("row_scale_deg", C.c_void_p)]
+
+
+class saga_norm_desc(C.Structure):
+    _fields_ = [("kind", C.c_int), ("eps", C.c_float), ("weight", C.c_void_p), ("bias", C.c_void_p)]
+
+
+class saga_block_op(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("x_dtype", C.c_int), ("post", saga_norm_desc), ("pre", saga_norm_desc),
+                ("gate_act", C.c_int), ("res_scale", C.c_float), ("channel_scale", C.c_void_p)]
+
+
 class saga_layer_desc(C.Structure):
     _fields_ = [
         ("kind", C.c_int), ("dtype", C.c_int), ("in_feat", C.c_int32), ("out_feat", C.c_int32),
@@ -179,6 +198,17 @@ def lib():
                                                  P(C.c_size_t)]),
         "saga_apply_vertex": (S, [P(saga_gemm_op), saga_cmat, saga_cmat, saga_cmat, saga_cmat, C.c_void_p,
                                   C.c_void_p, saga_mat, C.c_void_p, C.c_size_t, C.c_void_p]),
+        "saga_quantize_rows": (S, [C.c_int, saga_cmat, saga_mat, C.c_void_p, C.c_void_p]),
+        "saga_apply_vertex_quant_workspace_size": (S, [P(saga_quant_op), C.c_int64, C.c_int64, C.c_int64,
+                                                       P(C.c_size_t)]),
+        "saga_apply_vertex_quant": (S, [P(saga_quant_op), saga_cmat, C.c_void_p, saga_cmat, C.c_void_p,
+                                        C.c_void_p, saga_mat, C.c_void_p, C.c_size_t, C.c_void_p]),
+        "saga_block_norm": (S, [P(saga_block_op), saga_cmat, saga_cmat, saga_cmat, saga_mat, saga_mat,
+                                C.c_void_p, C.c_void_p]),
+        "saga_label_log_probs_workspace_size": (S, [C.c_int, C.c_int64, C.c_int64, C.c_int32,
+                                                    P(C.c_size_t)]),
+        "saga_label_log_probs": (S, [C.c_int, saga_cmat, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
         "saga_layer_workspace_size": (S, [P(saga_plan), P(saga_layer_desc), P(C.c_size_t)]),
         "saga_layer": (S, [P(saga_plan), P(saga_layer_desc), saga_cmat, saga_cmat, saga_mat, C.c_void_p,
                            C.c_size_t, C.c_void_p]),
@@ -352,6 +382,40 @@ def saga_apply_vertex(op, a, w, a2, w2, bias, bias2, out, workspace, ws_bytes, s
     return _check(lib().saga_apply_vertex(C.byref(op), a, w, a2, w2, bias, bias2, out, workspace,
                                           ws_bytes, stream),
                   "saga_apply_vertex")
+
+
+def saga_quantize_rows(dtype, x, q, scale, stream):
+    return _check(lib().saga_quantize_rows(dtype, x, q, scale, stream), "saga_quantize_rows")
+
+
+def saga_apply_vertex_quant_workspace_size(op, m, k, n):
+    out = C.c_size_t(0)
+    _check(lib().saga_apply_vertex_quant_workspace_size(C.byref(op), m, k, n, C.byref(out)),
+           "saga_apply_vertex_quant_workspace_size")
+    return out.value
+
+
+def saga_apply_vertex_quant(op, a, a_scale, w, w_scale, bias, out, workspace, ws_bytes, stream):
+    return _check(lib().saga_apply_vertex_quant(C.byref(op), a, a_scale, w, w_scale, bias, out, workspace,
+                                                ws_bytes, stream), "saga_apply_vertex_quant")
+
+
+def saga_block_norm(op, block, gate, x, y, z, z_scale, stream):
+    return _check(lib().saga_block_norm(C.byref(op), block, gate, x, y, z, z_scale, stream),
+                  "saga_block_norm")
+
+
+def saga_label_log_probs_workspace_size(dtype, m, c, top_k):
+    out = C.c_size_t(0)
+    _check(lib().saga_label_log_probs_workspace_size(dtype, m, c, top_k, C.byref(out)),
+           "saga_label_log_probs_workspace_size")
+    return out.value
+
+
+def saga_label_log_probs(dtype, logits, labels, logp, entropy, top_k, top_index, top_logp, workspace,
+                         ws_bytes, stream):
+    return _check(lib().saga_label_log_probs(dtype, logits, labels, logp, entropy, top_k, top_index,
+                                             top_logp, workspace, ws_bytes, stream), "saga_label_log_probs")
 
 
 def saga_trace_stages(events, markers=False):
