@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_device.h"
 #include "row_device.h"
@@ -127,6 +128,39 @@ __device__ __forceinline__ i32x4 mask_bytes(i32x4 v, int left) {
   return v;
 }
 
+// four neighbouring channels n.. of row m: scales, bias, activation, rounding
+__device__ __forceinline__ void store_quad(const QuantGemmArgs& g, int64_t m, int64_t n, i32x4 sum, float sa,
+                                           const float (&tw)[4], const float (&tb)[4]) {
+  float v[4];
+  const float rs = g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[m]) : 1.0f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[j] = (float)sum[j] * sa * tw[j] * rs;
+    if (g.bias) v[j] += tb[j];
+    v[j] = apply_act(g.act, v[j]);
+  }
+  if (g.out_dtype == SAGA_BF16) {
+    uint16_t* o = static_cast<uint16_t*>(g.out) + m * g.ldo + n;
+    if (n + 4 <= g.N) {
+      *reinterpret_cast<uint2*>(o) = make_uint2((uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
+                                                (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n + j < g.N) o[j] = f32_to_bf16(v[j]);
+    }
+  } else {
+    float* o = static_cast<float*>(g.out) + m * g.ldo + n;
+    if (n + 4 <= g.N) {
+      *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n + j < g.N) o[j] = v[j];
+    }
+  }
+}
+
 template <int WM, int WN, int MI, int NI>
 __global__ __launch_bounds__(64 * WM * WN) void k_gemm_quant(QuantGemmArgs g, int tiles_m,
                                                                             int tiles_n) {
@@ -182,83 +216,80 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm_quant(QuantGemmArgs g, in
       for (int r = 0; r < 16; ++r) acc[mi][ni][r] = 0;
 
   const int half = lane >> 5, lr = lane & 31;
+  uint32_t at[4];  // this lane's piece of each 32 k, in the row lr of a 32-row tile
+#pragma unroll
+  for (int s = 0; s < 4; ++s) at[s] = lr * 8 + ((2 * s + half) ^ ((lr >> 1) & 7));
   const auto frag = [&](const lds_uint4* st, int row0, int s) {
-    const int r = row0 + lr;
-    return *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(
-        st + r * 8 + ((2 * s + half) ^ ((r >> 1) & 7)));
+    return *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(st + row0 * 8 + at[s]);
   };
-  const auto step = [&](const lds_uint4* st, int s, int left) {
-    i32x4 a[MI], w[NI];
+  const auto chunk = [&](int c, auto whole) {
+    const lds_uint4* st = lds + (c & 1) * R::STAGE;
+    const lds_uint4* sa = st + wm * MI * 256;
+    const lds_uint4* sw = st + R::BM * 8 + wn * NI * 256;
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) a[mi] = frag(st, (wm * MI + mi) * 32, s);
+    for (int s = 0; s < 4; ++s) {
+      i32x4 a[MI], w[NI];
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni) {
-      w[ni] = frag(st, R::BM + (wn * NI + ni) * 32, s);
-      if (left < 128) w[ni] = mask_bytes(w[ni], left - (2 * s + half) * 16);
+      for (int ni = 0; ni < NI; ++ni) {
+        w[ni] = frag(sw, ni * 32, s);
+        if constexpr (!decltype(whole)::value) w[ni] = mask_bytes(w[ni], K - c * 128 - (2 * s + half) * 16);
+      }
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) a[mi] = frag(sa, mi * 32, s);
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni)
+          acc[mi][ni] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[ni], a[mi], acc[mi][ni], 0, 0, 0);
     }
-#pragma unroll
-    for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-      for (int ni = 0; ni < NI; ++ni)
-        acc[mi][ni] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[ni], a[mi], acc[mi][ni], 0, 0, 0);
   };
 
   issue(0);
-  for (int c = 0; c <= last; ++c) {
+  for (int c = 0; c < last; ++c) {
     wait_vm<0>();    // chunk c has landed
     ring_barrier();  // for every wave, and all are done with the other stage
-    if (c < last) issue(c + 1);
-    const lds_uint4* st = lds + (c & 1) * R::STAGE;
-    const int left = K - c * 128;
-    if (left >= 128) {
-#pragma unroll
-      for (int s = 0; s < 4; ++s) step(st, s, 128);
-    } else {
-      for (int s = 0; s * 32 < left; ++s) step(st, s, left);
-    }
+    issue(c + 1);
+    chunk(c, std::true_type{});
   }
+  wait_vm<0>();
+  ring_barrier();
+  chunk(last, std::false_type{});
+  ring_barrier();  // the stages are free
 
-  // lane: channels 8 q + 4 half + (0..3) of each 32, row lr
+  // Each 32 x 32 tile goes through 4 KB of LDS of this wave's own: a lane holds
+  // channels 8 q + 4 half + (0..3) of row lr, and takes back four channels of the
+  // rows lane / 8 + 8 i, so that stores cover whole pieces of rows.
+  lds_uint4* const mine = lds + wave * 256;
 #pragma unroll
-  for (int mi = 0; mi < MI; ++mi) {
-    const int64_t m = m0 + (wm * MI + mi) * 32 + lr;
-    if (m >= g.M) continue;
-    const float sa = g.a_scale[m];
-    const float rs = g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[m]) : 1.0f;
+  for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni)
+    for (int ni = 0; ni < NI; ++ni) {
+      asm volatile("" ::: "memory");
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int64_t n = n0 + (wn * NI + ni) * 32 + 8 * q + 4 * half;
-        float v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bool in_row = n + j < g.N;
-          v[j] = (float)acc[mi][ni][4 * q + j] * sa * (in_row ? g.w_scale[n + j] : 0.0f) * rs;
-          if (g.bias && in_row) v[j] += g.bias[n + j];
-          v[j] = apply_act(g.act, v[j]);
-        }
-        if (g.out_dtype == SAGA_BF16) {
-          uint16_t* o = static_cast<uint16_t*>(g.out) + m * g.ldo + n;
-          if (n + 4 <= g.N) {
-            *reinterpret_cast<uint2*>(o) =
-                make_uint2((uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
-                           (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16));
-          } else {
-            for (int j = 0; j < 4; ++j)
-              if (n + j < g.N) o[j] = f32_to_bf16(v[j]);
-          }
-        } else {
-          float* o = static_cast<float*>(g.out) + m * g.ldo + n;
-          if (n + 4 <= g.N) {
-            *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
-          } else {
-            for (int j = 0; j < 4; ++j)
-              if (n + j < g.N) o[j] = v[j];
-          }
-        }
+        const i32x16& v = acc[mi][ni];
+        *reinterpret_cast<__attribute__((address_space(3))) i32x4*>(mine + at[q]) =
+            i32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
       }
-  }
+      asm volatile("" ::: "memory");
+      const int p = lane & 7;
+      const int64_t n = n0 + (wn * NI + ni) * 32 + 4 * p;
+      float tw[4], tb[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        tw[j] = n + j < g.N ? g.w_scale[n + j] : 0.0f;
+        tb[j] = g.bias && n + j < g.N ? g.bias[n + j] : 0.0f;
+      }
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 3);
+        const int64_t m = m0 + (wm * MI + mi) * 32 + r;
+        const i32x4 v =
+            *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(mine + r * 8 + (p ^ ((r >> 1) & 7)));
+        if (m >= g.M || n >= g.N) continue;
+        store_quad(g, m, n, v, g.a_scale[m], tw, tb);
+      }
+    }
 }
 
 template <int WM, int WN, int MI, int NI>
