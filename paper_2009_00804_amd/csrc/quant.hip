@@ -14,7 +14,6 @@ namespace saga {
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) uint4 lds_uint4;
 
 constexpr int64_t kMostBlocks = 1 << 20;  // (a grid holds less than 2^32 threads)
@@ -102,19 +101,30 @@ hipError_t dispatch_rows(const QuantRowsArgs& a, hipStream_t st) {
 
 // --------------------------------------------------------------------------
 // product: a workgroup of WM x WN waves holds BM rows of a and BN rows of w, a
-// wave MI x NI tiles of 32 x 32 sums.  128 bytes of k a step, both operands
+// wave MI x NI tiles of 16 x 16 sums.  128 bytes of k a step, both operands
 // through two LDS stages filled by direct-to-LDS loads.  The 16-byte piece p of
-// row r lies at piece p ^ ((r >> 1) & 7), so that the 32 rows a fragment read
+// row r lies at piece p ^ ((r >> 1) & 7), so that the 16 rows a fragment read
 // touches fall on all banks.  The matrix instruction takes w as its first
 // operand: a lane then holds four neighbouring channels of one row.
 // --------------------------------------------------------------------------
-template <int WM, int WN, int MI, int NI>
+template <int WM, int WN, int MI, int NI, int KB, int ST>
 struct Tile {
   static constexpr int NW = WM * WN, THREADS = 64 * NW;
-  static constexpr int BM = 32 * MI * WM, BN = 32 * NI * WN;
-  static constexpr int STAGE = (BM + BN) * 8;  // 16-byte slots
-  static constexpr int LB = (BM + BN) / 8 / NW;  // loads a wave issues per stage, 8 rows each
-  static_assert((BM + BN) / 8 % NW == 0, "loads divide among the waves");
+  static constexpr int BM = 16 * MI * WM, BN = 16 * NI * WN;
+  static constexpr int PR = KB / 16;                            // 16-byte pieces of a row
+  static constexpr int STAGE = (BM + BN) * PR;                  // 16-byte slots
+  static constexpr int RL = 64 / PR;                            // rows a load instruction covers
+  static constexpr int GROUPS = (BM + BN) / RL;                 // load instructions per stage
+  static constexpr int LB = (GROUPS + NW - 1) / NW;             // of one wave
+  static constexpr int PH = KB / 64;                            // products' steps of 64 k
+  static constexpr int NP = 4 * NI;                             // 16-byte pieces of a wave's row of sums
+  static constexpr int SLOTS = ST * STAGE > NW * 16 * NP ? ST * STAGE : NW * 16 * NP;
+  static constexpr int LDS = SLOTS * 16 + (BM + 2 * BN) * 4;
+  static constexpr int WPE = 160 * 1024 / LDS * NW / 4;         // waves a SIMD that LDS has room for
+  // slot of piece p of row r: the 16 rows of a fragment read fall on all banks
+  __device__ __forceinline__ static int slot(int r, int p) {
+    return r * PR + (p ^ (PR == 8 ? (r >> 1) & 7 : (r >> 2) & 3));
+  }
 };
 
 // bytes past `left` cleared
@@ -130,14 +140,16 @@ __device__ __forceinline__ i32x4 mask_bytes(i32x4 v, int left) {
 
 // four neighbouring channels n.. of row m: scales, bias, activation, rounding
 __device__ __forceinline__ void store_quad(const QuantGemmArgs& g, int64_t m, int64_t n, i32x4 sum, float sa,
-                                           const float (&tw)[4], const float (&tb)[4]) {
+                                           const f32x4& tw, const f32x4& tb) {
   float v[4];
-  const float rs = g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[m]) : 1.0f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    v[j] = (float)sum[j] * sa * tw[j] * rs;
-    if (g.bias) v[j] += tb[j];
-    v[j] = apply_act(g.act, v[j]);
+  for (int j = 0; j < 4; ++j) v[j] = (float)sum[j] * sa * tw[j] + tb[j];
+  if (g.act == SAGA_ACT_RELU) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = v[j] > 0.0f ? v[j] : 0.0f;
+  } else if (g.act != SAGA_ACT_NONE) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = apply_act(g.act, v[j]);
   }
   if (g.out_dtype == SAGA_BF16) {
     uint16_t* o = static_cast<uint16_t*>(g.out) + m * g.ldo + n;
@@ -161,11 +173,14 @@ __device__ __forceinline__ void store_quad(const QuantGemmArgs& g, int64_t m, in
   }
 }
 
-template <int WM, int WN, int MI, int NI>
-__global__ __launch_bounds__(64 * WM * WN) void k_gemm_quant(QuantGemmArgs g, int tiles_m,
-                                                                            int tiles_n) {
-  typedef Tile<WM, WN, MI, NI> R;
-  __shared__ uint4 ring[2 * R::STAGE];
+template <int WM, int WN, int MI, int NI, int KB, int ST>
+__global__ __launch_bounds__(64 * WM * WN)
+__attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, KB, ST>::WPE))) void k_gemm_quant(QuantGemmArgs g,
+                                                                                         int tiles_m,
+                                                                                         int tiles_n) {
+  typedef Tile<WM, WN, MI, NI, KB, ST> R;
+  __shared__ uint4 ring[R::SLOTS];
+  __shared__ f32x4 scales[(R::BM + 2 * R::BN) / 4];  // of the rows, of the channels, and the bias
   // Workgroup w runs on XCD w % 8: every XCD gets a run of tiles, and in it eight
   // row tiles share each column tile.
   const int total = tiles_m * tiles_n, per = (total + kXcds - 1) / kXcds;
@@ -178,123 +193,194 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm_quant(QuantGemmArgs g, in
   const int wm = wave / WN, wn = wave % WN;
   lds_uint4* lds = (lds_uint4*)ring;
 
-  // this lane's share of the loads: row 8 (wave + j NW) + lane / 8 of the stage
+  // this lane's share of the loads: row RL (wave + j NW) + lane / PR of the stage
   // (rows past the last read the last one; their sums are not stored)
   const int8_t* const A = g.a + m0 * g.lda;
   const int8_t* const W = g.w + n0 * g.ldw;
-  const int K = (int)g.K, kmax = (K - 1) / 16 * 16, last = (K - 1) / 128;
+  const int K = (int)g.K, kmax = (K - 1) / 16 * 16, last = (K - 1) / KB;
   uint32_t off[R::LB];
   int piece[R::LB];
 #pragma unroll
   for (int j = 0; j < R::LB; ++j) {
-    const int r = 8 * (wave + j * R::NW) + (lane >> 3);
+    const int r = R::RL * (wave + j * R::NW) + lane / R::PR;
     const bool is_a = r < R::BM;
     const int rr = is_a ? (int)min((int64_t)r, g.M - 1 - m0) : (int)min((int64_t)(r - R::BM), g.N - 1 - n0);
+    piece[j] = (R::slot(r, lane % R::PR) % R::PR) * 16;
     off[j] = (uint32_t)rr * (uint32_t)(is_a ? g.lda : g.ldw);
-    piece[j] = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
   }
-  const auto issue = [&](int c) {
-    const uint32_t dst = (uint32_t)(uintptr_t)(lds + (c & 1) * R::STAGE);
-#pragma unroll
-    for (int j = 0; j < R::LB; ++j) {
-      const int grp = wave + j * R::NW;
-      const int8_t* base = grp * 8 < R::BM ? A : W;
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                   :
-                   : "s"(__builtin_amdgcn_readfirstlane(dst + grp * 1024)),
-                     "v"(off[j] + (uint32_t)min(c * 128 + piece[j], kmax)), "s"(base)
-                   : "memory", "m0");
-    }
+  // load j of chunk c; only the last chunk can reach past the rows' ends, where it
+  // reads their last piece again (masked before use)
+  const auto issue = [&](int c, int j) {
+    const int grp = wave + j * R::NW;
+    if (R::GROUPS % R::NW != 0 && grp >= R::GROUPS) return;
+    const int8_t* base = grp * R::RL < R::BM ? A : W;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds + (c % ST) * R::STAGE) + grp * 1024)),
+                   "v"(off[j] + (uint32_t)min(c * KB + piece[j], kmax)), "s"(base)
+                 : "memory", "m0");
   };
+#pragma unroll
+  for (int c = 0; c < ST; ++c)
+    if (c <= last)
+#pragma unroll
+      for (int j = 0; j < R::LB; ++j) issue(c, j);
+  {
+    float* sc = reinterpret_cast<float*>(scales);
+    for (int i = threadIdx.x; i < R::BM; i += R::THREADS) {
+      const int64_t m = min(m0 + i, g.M - 1);
+      sc[i] = g.a_scale[m] * (g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[m]) : 1.0f);
+    }
+    for (int i = threadIdx.x; i < R::BN; i += R::THREADS) {
+      const int64_t n = min(n0 + i, g.N - 1);
+      sc[R::BM + i] = g.w_scale[n];
+      sc[R::BM + R::BN + i] = g.bias ? g.bias[n] : 0.0f;
+    }
+  }
 
-  i32x16 acc[MI][NI];
+  i32x4 acc[MI][NI];
 #pragma unroll
   for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[mi][ni][r] = 0;
+    for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = i32x4{0, 0, 0, 0};
 
-  const int half = lane >> 5, lr = lane & 31;
-  uint32_t at[4];  // this lane's piece of each 32 k, in the row lr of a 32-row tile
+  const int quarter = lane >> 4, lr = lane & 15;
+  uint32_t at[R::PH];  // this lane's piece of each 64 k, in the row lr of a 16-row tile
 #pragma unroll
-  for (int s = 0; s < 4; ++s) at[s] = lr * 8 + ((2 * s + half) ^ ((lr >> 1) & 7));
-  const auto frag = [&](const lds_uint4* st, int row0, int s) {
-    return *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(st + row0 * 8 + at[s]);
+  for (int s = 0; s < R::PH; ++s) at[s] = R::slot(lr, 4 * s + quarter);
+
+  // Fragments of 64 k are read into one half of a and w while those in the other
+  // half are multiplied.
+  i32x4 a[2][MI], w[2][NI];
+  const auto read_w = [&](int c, int s, int b, int ni) {
+    w[b][ni] = *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(
+        lds + (c % ST) * R::STAGE + at[s] + (R::BM + (wn * NI + ni) * 16) * R::PR);
   };
-  const auto chunk = [&](int c, auto whole) {
-    const lds_uint4* st = lds + (c & 1) * R::STAGE;
-    const lds_uint4* sa = st + wm * MI * 256;
-    const lds_uint4* sw = st + R::BM * 8 + wn * NI * 256;
+  const auto read_a = [&](int c, int s, int b, int mi) {
+    a[b][mi] = *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(
+        lds + (c % ST) * R::STAGE + at[s] + (wm * MI + mi) * 16 * R::PR);
+  };
+  // Multiplies half b row tile by row tile; between the row tiles go the reads of
+  // the next fragments (chunk c, step s) and, where FILL, the loads of chunk `fill`:
+  // in one run either would hold up the products behind it.
+  const auto step = [&](auto fill_tag, int b, int c, int s, int fill) {
+    constexpr bool FILL = decltype(fill_tag)::value;
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      i32x4 a[MI], w[NI];
+    for (int mi = 0; mi < MI; ++mi) {
+      constexpr int WR = (NI + MI - 1) / MI;
 #pragma unroll
-      for (int ni = 0; ni < NI; ++ni) {
-        w[ni] = frag(sw, ni * 32, s);
-        if constexpr (!decltype(whole)::value) w[ni] = mask_bytes(w[ni], K - c * 128 - (2 * s + half) * 16);
+      for (int k = 0; k < WR; ++k)
+        if (mi * WR + k < NI) read_w(c, s, b ^ 1, mi * WR + k);
+      read_a(c, s, b ^ 1, mi);
+      if constexpr (FILL) {
+#pragma unroll
+        for (int j = 0; j < R::LB; ++j)
+          if (j * MI / R::LB == mi) issue(fill, j);
       }
 #pragma unroll
-      for (int mi = 0; mi < MI; ++mi) a[mi] = frag(sa, mi * 32, s);
+      for (int ni = 0; ni < NI; ++ni)
+        acc[mi][ni] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[b][ni], a[b][mi], acc[mi][ni], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // Chunk c, its first fragments in half b0.  Before its last step chunk c + 1 has
+  // to have landed, for every wave; every wave then has chunk c's fragments in
+  // registers, and chunk c + ST takes its stage.
+  const auto chunk = [&](auto fill_tag, int c, int b0) {
 #pragma unroll
-      for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-        for (int ni = 0; ni < NI; ++ni)
-          acc[mi][ni] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[ni], a[mi], acc[mi][ni], 0, 0, 0);
+    for (int s = 0; s < R::PH; ++s) {
+      const int b = (b0 + s) & 1;
+      if (s < R::PH - 1) {
+        step(std::false_type{}, b, c, s + 1, 0);
+      } else {
+        if constexpr (decltype(fill_tag)::value) wait_vm<(ST - 2) * R::LB>();
+        else wait_vm<0>();
+        ring_barrier();
+        step(fill_tag, b, c + 1, 0, c + ST);
+      }
     }
   };
 
-  issue(0);
-  for (int c = 0; c < last; ++c) {
-    wait_vm<0>();    // chunk c has landed
-    ring_barrier();  // for every wave, and all are done with the other stage
-    issue(c + 1);
-    chunk(c, std::true_type{});
-  }
   wait_vm<0>();
   ring_barrier();
-  chunk(last, std::false_type{});
+#pragma unroll
+  for (int ni = 0; ni < NI; ++ni) read_w(0, 0, 0, ni);
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi) read_a(0, 0, 0, mi);
+  constexpr int FLIP = R::PH & 1;  // a chunk of one step leaves the fragments in the other half
+  int c = 0;
+  for (; c + 1 + ST <= last; c += 2) {
+    chunk(std::true_type{}, c, 0);
+    chunk(std::true_type{}, c + 1, FLIP);
+  }
+  if (c + ST <= last) {
+    chunk(std::true_type{}, c, 0);
+    ++c;
+    if constexpr (FLIP) {
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) w[0][ni] = w[1][ni];
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) a[0][mi] = a[1][mi];
+    }
+  }
+  for (; c < last; ++c) {
+    chunk(std::false_type{}, c, 0);
+    if constexpr (FLIP) {
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) w[0][ni] = w[1][ni];
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) a[0][mi] = a[1][mi];
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < R::PH; ++s) {
+    const int b = s & 1;
+    if (s + 1 < R::PH) {
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) read_w(last, s + 1, b ^ 1, ni);
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) read_a(last, s + 1, b ^ 1, mi);
+    }
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) w[b][ni] = mask_bytes(w[b][ni], K - last * KB - (4 * s + quarter) * 16);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni)
+        acc[mi][ni] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[b][ni], a[b][mi], acc[mi][ni], 0, 0, 0);
+  }
   ring_barrier();  // the stages are free
 
-  // Each 32 x 32 tile goes through 4 KB of LDS of this wave's own: a lane holds
-  // channels 8 q + 4 half + (0..3) of row lr, and takes back four channels of the
-  // rows lane / 8 + 8 i, so that stores cover whole pieces of rows.
-  lds_uint4* const mine = lds + wave * 256;
+  // 16 rows at a time go through LDS of this wave's own: a lane holds channels
+  // 4 quarter + (0..3) of row lr, and takes back four channels of a row, so that
+  // a store covers whole rows of the wave's columns.
+  constexpr int NP = R::NP, ROWS = 64 / (NP < 64 ? NP : 64);
+  lds_uint4* const mine = lds + wave * 16 * NP;
+  const int p = lane % NP;
+  const int64_t n = n0 + (int64_t)wn * NI * 16 + 4 * p;
+  const f32x4 tw = scales[(R::BM + wn * NI * 16) / 4 + p], tb = scales[(R::BM + R::BN + wn * NI * 16) / 4 + p];
 #pragma unroll
-  for (int mi = 0; mi < MI; ++mi)
+  for (int mi = 0; mi < MI; ++mi) {
+    asm volatile("" ::: "memory");
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni) {
-      asm volatile("" ::: "memory");
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const i32x16& v = acc[mi][ni];
-        *reinterpret_cast<__attribute__((address_space(3))) i32x4*>(mine + at[q]) =
-            i32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-      }
-      asm volatile("" ::: "memory");
-      const int p = lane & 7;
-      const int64_t n = n0 + (wn * NI + ni) * 32 + 4 * p;
-      float tw[4], tb[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        tw[j] = n + j < g.N ? g.w_scale[n + j] : 0.0f;
-        tb[j] = g.bias && n + j < g.N ? g.bias[n + j] : 0.0f;
-      }
-#pragma unroll 1
-      for (int i = 0; i < 4; ++i) {
-        const int r = 8 * i + (lane >> 3);
-        const int64_t m = m0 + (wm * MI + mi) * 32 + r;
-        const i32x4 v =
-            *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(mine + r * 8 + (p ^ ((r >> 1) & 7)));
-        if (m >= g.M || n >= g.N) continue;
-        store_quad(g, m, n, v, g.a_scale[m], tw, tb);
-      }
+    for (int ni = 0; ni < NI; ++ni)
+      *reinterpret_cast<__attribute__((address_space(3))) i32x4*>(mine + lr * NP + ((ni * 4 + quarter) ^ (lr & (NP - 1)))) =
+          acc[mi][ni];
+    asm volatile("" ::: "memory");
+#pragma unroll 2
+    for (int i = 0; i < 16 / ROWS; ++i) {
+      const int r = i * ROWS + lane / NP, rr = (wm * MI + mi) * 16 + r;
+      const i32x4 v =
+          *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(mine + r * NP + (p ^ (r & (NP - 1))));
+      const float sa = reinterpret_cast<const float*>(scales)[rr];
+      if (m0 + rr < g.M && n < g.N) store_quad(g, m0 + rr, n, v, sa, tw, tb);
     }
+  }
 }
 
-template <int WM, int WN, int MI, int NI>
+template <int WM, int WN, int MI, int NI, int KB, int ST>
 hipError_t launch_tile(const QuantGemmArgs& g0, hipStream_t st) {
-  typedef Tile<WM, WN, MI, NI> R;
+  typedef Tile<WM, WN, MI, NI, KB, ST> R;
   const int64_t tn = (g0.N + R::BN - 1) / R::BN;
   const int64_t slice = std::max<int64_t>(1, kMostBlocks / tn) * R::BM;  // rows per launch
   for (int64_t m = 0; m < g0.M; m += slice) {
@@ -305,7 +391,7 @@ hipError_t launch_tile(const QuantGemmArgs& g0, hipStream_t st) {
     if (g.row_scale_deg) g.row_scale_deg += m;
     g.out = static_cast<char*>(g.out) + m * g.ldo * (g.out_dtype == SAGA_BF16 ? 2 : 4);
     const int64_t tm = (g.M + R::BM - 1) / R::BM, blocks = (tm * tn + kXcds - 1) / kXcds * kXcds;
-    hipLaunchKernelGGL((k_gemm_quant<WM, WN, MI, NI>), dim3((unsigned)blocks), dim3(R::THREADS), 0, st, g,
+    hipLaunchKernelGGL((k_gemm_quant<WM, WN, MI, NI, KB, ST>), dim3((unsigned)blocks), dim3(R::THREADS), 0, st, g,
                        (int)tm, (int)tn);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -322,11 +408,17 @@ hipError_t launch_quantize_rows(const QuantRowsArgs& a, hipStream_t st) {
 
 hipError_t launch_gemm_quant(const QuantGemmArgs& g, hipStream_t st) {
   if (g.M == 0) return hipSuccess;
-  if (g.N <= 32) return launch_tile<4, 1, 1, 1>(g, st);
-  if (g.N <= 64) return launch_tile<4, 1, 1, 2>(g, st);
+  if (g.N <= 16) return launch_tile<4, 1, 2, 1, 128, 2>(g, st);
+  if (g.N <= 32) return launch_tile<4, 1, 2, 2, 128, 2>(g, st);
+  if (g.N <= 64) return launch_tile<4, 1, 2, 4, 128, 2>(g, st);
+  // Long k over enough tiles for all CUs: 256 x 256 by 16 waves (us, against 128 x
+  // 128 by four, three workgroups a CU: 32768 x 4096 x 4096 510 / 675, 8192 x 4096
+  // x 4096 129 / 163).  Short k: 128 x 128, whose epilogues run beside another
+  // workgroup's products (40001 x 1024 x 1024 73 / 66, 16384 x 1024 x 4096 102 /
+  // 101).
   const int64_t large = ((g.M + 255) / 256) * ((g.N + 255) / 256);
-  if (large >= 256) return launch_tile<2, 4, 4, 2>(g, st);
-  return launch_tile<2, 2, 2, 2>(g, st);
+  if (large >= 256 && g.K >= 2048) return launch_tile<4, 4, 4, 4, 64, 4>(g, st);
+  return launch_tile<2, 2, 4, 4, 64, 3>(g, st);
 }
 
 }  // namespace saga
