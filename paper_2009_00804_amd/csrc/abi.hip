@@ -600,7 +600,7 @@ saga_status check_quant_op(const saga_quant_op& op, int64_t m, int64_t k, int64_
 
 // workspace: the rows quantised (ld whole 16 bytes), then their scales
 size_t quant_ws_bytes(const saga_quant_op& op, int64_t m, int64_t k, int64_t n) {
-  if (op.a_dtype == SAGA_I8 || m == 0) return 0;
+  if (op.a_dtype == SAGA_I8 || m == 0 || saga::quant_fuses(m, n, k)) return 0;
   return align256((size_t)m * round_up(k, 16)) + align256((size_t)m * 4);
 }
 
@@ -647,6 +647,10 @@ saga_status run_quant(const saga_quant_op& op, const saga_cmat& a, const float* 
   g.out_dtype = op.out_dtype;
   g.out = out.ptr;
   g.ldo = out.ld;
+  if (!i8 && saga::quant_fuses(M, N, K)) {
+    const hipError_t e = saga::launch_quant_fused(op.a_dtype, saga::QuantFloatArgs{g, a.ptr, a.ld}, st);
+    return e == hipSuccess ? ok() : dev_fail(e, "8-bit product launch");
+  }
   if (!i8 && M > 0) {
     Carve c(ws, ws_bytes);
     saga::QuantRowsArgs r;

@@ -21,16 +21,6 @@ constexpr int64_t kMostBlocks = 1 << 20;  // (a grid holds less than 2^32 thread
 // --------------------------------------------------------------------------
 // float rows to 8-bit rows; memory bounds it: a row is read once into registers
 // --------------------------------------------------------------------------
-template <int U>
-__device__ __forceinline__ uint32_t top_bits(const float (&v)[U][8]) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[u][j]) & 0x7fffffffu);
-  return top;
-}
-
 template <typename T, int G, int U>
 __global__ __launch_bounds__(RowGroup<G>::THREADS) void k_quantize_rows(QuantRowsArgs a) {
   typedef RowGroup<G> R;
@@ -40,14 +30,19 @@ __global__ __launch_bounds__(RowGroup<G>::THREADS) void k_quantize_rows(QuantRow
   for (int64_t row = blockIdx.x * (int64_t)R::ROWS + threadIdx.x / G; row < a.M;
        row += gridDim.x * (int64_t)R::ROWS) {
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-    float v[U][8];
+    Raw<T> v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) load_unit(x + col0 + u * 8 * G, K - col0 - u * 8 * G, v[u]);
-    const RowScale s = row_scale(R::template reduce<OpMaxU>(top_bits(v), red, turn));
+    for (int u = 0; u < U; ++u) v[u].load(x + col0 + u * 8 * G, K - col0 - u * 8 * G);
+    uint32_t top = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) top = max(top, v[u].top());
+    const RowScale s = row_scale(R::template reduce<OpMaxU>(top, red, turn));
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int col = col0 + u * 8 * G;
-      store_unit_i8(a.q + row * a.ldq + col, K - col, round_unit(v[u], s));
+      float f[8];
+      v[u].widen(f);
+      store_unit_i8(a.q + row * a.ldq + col, K - col, round_unit(f, s));
     }
     if (threadIdx.x % G == 0) a.scale[row] = s.s;
   }
@@ -62,16 +57,18 @@ __global__ __launch_bounds__(1024) void k_quantize_long(QuantRowsArgs a) {
   const int K = (int)a.K;
   for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-    float v[1][8];
+    Raw<T> v;
     uint32_t top = 0;
-    for (int col = threadIdx.x * 8; col < K; col += 8192) {
-      load_unit(x + col, K - col, v[0]);
-      top = max(top, top_bits(v));
+    for (int64_t col = threadIdx.x * 8; col < K; col += 8192) {
+      v.load(x + col, (int)(K - col));
+      top = max(top, v.top());
     }
     const RowScale s = row_scale(R::reduce<OpMaxU>(top, red, turn));
-    for (int col = threadIdx.x * 8; col < K; col += 8192) {
-      load_unit(x + col, K - col, v[0]);
-      store_unit_i8(a.q + row * a.ldq + col, K - col, round_unit(v[0], s));
+    for (int64_t col = threadIdx.x * 8; col < K; col += 8192) {
+      v.load(x + col, (int)(K - col));
+      float f[8];
+      v.widen(f);
+      store_unit_i8(a.q + row * a.ldq + col, K - col, round_unit(f, s));
     }
     if (threadIdx.x == 0) a.scale[row] = s.s;
   }
@@ -84,16 +81,20 @@ hipError_t launch_rows(const QuantRowsArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_quantize_rows<T, G, U>), dim3((unsigned)blocks), dim3(R::THREADS), 0, st, a);
   return hipGetLastError();
 }
+// 16 lanes a row while that takes few units a lane: less of a row's last unit is idle
 template <typename T>
 hipError_t dispatch_rows(const QuantRowsArgs& a, hipStream_t st) {
-  if (a.K <= 64) return launch_rows<T, 8, 1>(a, st);
   if (a.K <= 128) return launch_rows<T, 16, 1>(a, st);
-  if (a.K <= 256) return launch_rows<T, 32, 1>(a, st);
-  if (a.K <= 512) return launch_rows<T, 64, 1>(a, st);
-  if (a.K <= 1024) return launch_rows<T, 64, 2>(a, st);
-  if (a.K <= 2048) return launch_rows<T, 256, 1>(a, st);
-  if (a.K <= 4096) return launch_rows<T, 256, 2>(a, st);
-  if (a.K <= 8192) return launch_rows<T, 1024, 1>(a, st);
+  if (a.K <= 256) return launch_rows<T, 16, 2>(a, st);
+  if (a.K <= 384) return launch_rows<T, 16, 3>(a, st);
+  if (a.K <= 512) return launch_rows<T, 16, 4>(a, st);
+  if (a.K <= 640) return launch_rows<T, 16, 5>(a, st);
+  if (a.K <= 768) return launch_rows<T, 16, 6>(a, st);
+  if (a.K <= 1024) return launch_rows<T, 16, 8>(a, st);
+  if (a.K <= 1536) return launch_rows<T, 64, 3>(a, st);
+  if (a.K <= 2048) return launch_rows<T, 64, 4>(a, st);
+  if (a.K <= 4096) return launch_rows<T, 64, 8>(a, st);
+  if (a.K <= 8192) return launch_rows<T, 256, 4>(a, st);
   hipLaunchKernelGGL((k_quantize_long<T>), dim3((unsigned)std::min<int64_t>(a.M, kMostBlocks)), dim3(1024), 0, st,
                      a);
   return hipGetLastError();
@@ -399,11 +400,162 @@ hipError_t launch_tile(const QuantGemmArgs& g0, hipStream_t st) {
   return hipSuccess;
 }
 
+// --------------------------------------------------------------------------
+// float rows of up to kFusedK columns: a workgroup quantises BM rows into LDS and
+// multiplies them by all of w from there, so that the rows are read once and their
+// 8-bit form never leaves the CU.  Reading the rows bounds it while w has few
+// rows; two workgroups a CU, one reading while the other multiplies.
+//
+// Quantising: 16 lanes a row, four rows a wave and pass, U units a lane.  Rows lie
+// an odd number of 16-byte pieces apart, so that the 16 rows a fragment read
+// touches fall on all banks.  w's fragments come straight from memory (the second
+// level cache), kAhead steps ahead of their products.
+// --------------------------------------------------------------------------
+constexpr int kFusedK = 1248, kAhead = 4;
+
+__device__ __forceinline__ int fused_pitch(int K) { return ((K + 15) / 16) | 1; }  // in pieces
+
+template <typename T, int BM, int U, int WM, int WN, int NI>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void k_quant_fused(QuantFloatArgs f) {
+  constexpr int MI = BM / 16 / WM;
+  static_assert(WM * WN == 8 && MI * 16 * WM == BM, "eight waves");
+  extern __shared__ uint4 rows[];  // BM rows of `pitch` pieces, and four pieces that a last step may read
+  __shared__ float scales[BM];
+  const QuantGemmArgs& g = f.g;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int K = (int)g.K, pitch = fused_pitch(K), steps = (K + 63) / 64;
+  const int64_t m0 = blockIdx.x * (int64_t)BM;
+  char* const lds = reinterpret_cast<char*>(rows);
+
+  constexpr int RW = BM / 8;  // rows of a wave
+#pragma unroll 1
+  for (int r0 = 0; r0 < RW; r0 += 4) {
+    const int r = wave * RW + r0 + (lane >> 4), col0 = (lane & 15) * 8;
+    const int64_t m = min(m0 + r, g.M - 1);
+    const T* x = static_cast<const T*>(f.x) + m * f.ldx;
+    Raw<T> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u].load(x + col0 + u * 128, K - col0 - u * 128);
+    uint32_t top = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) top = max(top, v[u].top());
+    const RowScale s = row_scale(group_maxu<16>(top));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int col = col0 + u * 128;
+      float x8[8];
+      v[u].widen(x8);
+      if (col < pitch * 16) *reinterpret_cast<uint2*>(lds + r * pitch * 16 + col) = round_unit(x8, s);
+    }
+    if ((lane & 15) == 0) scales[r] = s.s * (g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[m]) : 1.0f);
+  }
+  __syncthreads();
+
+  const int wm = wave / WN, wn = wave % WN, quarter = lane >> 4, lr = lane & 15;
+  const uint4* const ar = rows + (wm * MI * 16 + lr) * pitch + quarter;
+  for (int64_t n0 = wn * NI * 16; n0 < g.N; n0 += WN * NI * 16) {
+    const int8_t* wr[NI];
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) wr[ni] = g.w + min(n0 + ni * 16 + lr, g.N - 1) * g.ldw + quarter * 16;
+    i32x4 acc[MI][NI], w[kAhead][NI];
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = i32x4{0, 0, 0, 0};
+    // (pieces past the rows' end read as 0: what lies behind a row in LDS then does not count)
+    const auto load = [&](int s, i32x4 (&o)[NI]) {
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) {
+        o[ni] = i32x4{0, 0, 0, 0};
+        if (s * 64 + quarter * 16 < K) o[ni] = *reinterpret_cast<const i32x4*>(wr[ni] + s * 64);
+      }
+    };
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) load(k, w[k]);
+    for (int s0 = 0; s0 < steps; s0 += kAhead) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (s0 + k < steps) {
+          i32x4 a[MI];
+#pragma unroll
+          for (int mi = 0; mi < MI; ++mi) a[mi] = *reinterpret_cast<const i32x4*>(ar + mi * 16 * pitch + (s0 + k) * 4);
+#pragma unroll
+          for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni)
+              acc[mi][ni] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[k][ni], a[mi], acc[mi][ni], 0, 0, 0);
+        }
+        load(s0 + k + kAhead, w[k]);
+      }
+    }
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+      const int64_t n = n0 + ni * 16 + quarter * 4;
+      if (n >= g.N) continue;
+      f32x4 tw, tb;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        tw[j] = n + j < g.N ? g.w_scale[n + j] : 0.0f;
+        tb[j] = g.bias && n + j < g.N ? g.bias[n + j] : 0.0f;
+      }
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) {
+        const int r = (wm * MI + mi) * 16 + lr;
+        if (m0 + r < g.M) store_quad(g, m0 + r, n, acc[mi][ni], scales[r], tw, tb);
+      }
+    }
+  }
+}
+
+template <typename T, int BM, int U>
+hipError_t launch_fused(const QuantFloatArgs& f0, hipStream_t st) {
+  const int64_t slice = kMostBlocks * BM;  // rows per launch
+  for (int64_t m = 0; m < f0.g.M; m += slice) {
+    QuantFloatArgs f = f0;
+    QuantGemmArgs& g = f.g;
+    g.M = std::min(slice, f0.g.M - m);
+    f.x = static_cast<const T*>(f.x) + m * f.ldx;
+    if (g.row_scale_deg) g.row_scale_deg += m;
+    g.out = static_cast<char*>(g.out) + m * g.ldo * (g.out_dtype == SAGA_BF16 ? 2 : 4);
+    const dim3 grid((unsigned)((g.M + BM - 1) / BM));
+    const size_t lds = ((size_t)BM * (((g.K + 15) / 16) | 1) + 4) * 16;
+    if (g.N <= 16) {
+      hipLaunchKernelGGL((k_quant_fused<T, BM, U, BM / 16, 128 / BM, 1>), grid, dim3(512), lds, st, f);
+    } else if (g.N <= 64) {
+      hipLaunchKernelGGL((k_quant_fused<T, BM, U, BM / 32, 256 / BM, 128 / BM == 1 ? 2 : 1>), grid, dim3(512), lds, st, f);
+    } else {
+      hipLaunchKernelGGL((k_quant_fused<T, BM, U, 2, 4, 2>), grid, dim3(512), lds, st, f);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+template <typename T>
+hipError_t dispatch_fused(const QuantFloatArgs& f, hipStream_t st) {
+  const int64_t k = f.g.K;
+  if (k <= 128) return launch_fused<T, 128, 1>(f, st);
+  if (k <= 256) return launch_fused<T, 128, 2>(f, st);
+  if (k <= 384) return launch_fused<T, 128, 3>(f, st);
+  if (k <= 512) return launch_fused<T, 128, 4>(f, st);
+  if (k <= 624) return launch_fused<T, 128, 5>(f, st);  // two workgroups' rows fill a CU's LDS
+  if (k <= 768) return launch_fused<T, 64, 6>(f, st);
+  if (k <= 1024) return launch_fused<T, 64, 8>(f, st);
+  return launch_fused<T, 64, 10>(f, st);
+}
+
 }  // namespace
 
 hipError_t launch_quantize_rows(const QuantRowsArgs& a, hipStream_t st) {
   if (a.M == 0) return hipSuccess;
   return a.dtype == SAGA_BF16 ? dispatch_rows<uint16_t>(a, st) : dispatch_rows<float>(a, st);
+}
+
+bool quant_fuses(int64_t M, int64_t N, int64_t K) { return K <= kFusedK && N <= 512; }
+
+hipError_t launch_quant_fused(int dtype, const QuantFloatArgs& f, hipStream_t st) {
+  if (f.g.M == 0) return hipSuccess;
+  return dtype == SAGA_BF16 ? dispatch_fused<uint16_t>(f, st) : dispatch_fused<float>(f, st);
 }
 
 hipError_t launch_gemm_quant(const QuantGemmArgs& g, hipStream_t st) {

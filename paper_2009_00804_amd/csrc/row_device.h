@@ -166,26 +166,104 @@ __device__ __forceinline__ RowScale row_scale(uint32_t amax) {
   if (r.bad) r.s = __uint_as_float(0x7fc00000u), r.inv = 0.0f;
   return r;
 }
-// x * inv is within 2^-23 of x / s, so its rounding is right or one next to a
-// half.  The remainder x - q s is then exact in float32 (a multiple of ulp(s),
-// at most about s / 2), and says on which side of the half x / s lies.
-__device__ __forceinline__ int round_q(float x, const RowScale& r) {
+// x * inv is within 2^-24 of x / s, so its rounding q is right or one next to a
+// half.  The remainder x - q s is then exact in float32 (a multiple of ulp(s), at
+// most about s / 2), and says on which side of the half x / s lies.
+__device__ __forceinline__ uint32_t round_exact(float x, const RowScale& r) {
   const float q = rintf(x * r.inv);
   const float e = fmaf(-q, r.s, x), d = 2.0f * fabsf(e);
   int k = (int)q;
   if (d > r.s || (d == r.s && (k & 1))) k += e > 0.0f ? 1 : -1;
-  return k;
+  return (uint32_t)k & 0xffu;
 }
+// 8 values to 8 bytes.  Added to 1.5 * 2^23 the product x * inv is rounded to a
+// whole number, ties to even, whose low byte is q; values further than 2e-5 from a
+// half (x / s is below 127.5: x * inv is within 8e-6 of it) are right as they are.
 __device__ __forceinline__ uint2 round_unit(const float (&x)[8], const RowScale& r) {
-  uint2 o = make_uint2(0u, 0u);
-  if (r.bad) return o;
+  constexpr float kWhole = 12582912.0f;
+  uint32_t t[8];
+  float far = 0.0f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    o.x |= (uint32_t)(round_q(x[j], r) & 0xff) << (8 * j);
-    o.y |= (uint32_t)(round_q(x[4 + j], r) & 0xff) << (8 * j);
+  for (int j = 0; j < 8; ++j) {
+    const float m = fmaf(x[j], r.inv, kWhole);
+    far = fmaxf(far, fabsf(fmaf(x[j], r.inv, kWhole - m)));
+    t[j] = __float_as_uint(m);
   }
-  return o;
+  if (far > 0.49998f) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[j] = round_exact(x[j], r);
+  }
+  uint32_t o[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t lo = __builtin_amdgcn_perm(t[4 * h + 1], t[4 * h], 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(t[4 * h + 3], t[4 * h + 2], 0x0c0c0400u);
+    o[h] = r.bad ? 0u : __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+  }
+  return make_uint2(o[0], o[1]);
 }
+
+// A unit as it lies in memory, columns past `left` cleared: half the registers of
+// its float32 values where it is bfloat16.
+template <typename T> struct Raw;
+template <> struct Raw<float> {
+  u32x4 v[2];
+  __device__ __forceinline__ void load(const float* p, int left) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      v[h] = u32x4{0u, 0u, 0u, 0u};
+      if (left > 4 * h) v[h] = *reinterpret_cast<const u32x4*>(p + 4 * h);
+    }
+    if (left > 0 && left < 8) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (left <= j) v[j / 4][j % 4] = 0u;
+    }
+  }
+  __device__ __forceinline__ uint32_t top() const {  // largest magnitude, as float32 bits
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, v[j / 4][j % 4] & 0x7fffffffu);
+    return m;
+  }
+  __device__ __forceinline__ void widen(float (&x)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(v[j / 4][j % 4]);
+  }
+};
+template <> struct Raw<uint16_t> {
+  u32x4 v;
+  __device__ __forceinline__ void load(const uint16_t* p, int left) {
+    v = u32x4{0u, 0u, 0u, 0u};
+    if (left > 0) v = *reinterpret_cast<const u32x4*>(p);
+    if (left > 0 && left < 8) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (left <= 2 * j) v[j] = 0u;
+        else if (left == 2 * j + 1) v[j] &= 0xffffu;
+      }
+    }
+  }
+  __device__ __forceinline__ uint32_t top() const {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t a = v[j] & 0x7fff7fffu;
+      u16x2 b;
+      __builtin_memcpy(&b, &a, 4);
+      m = __builtin_elementwise_max(m, b);
+    }
+    return (uint32_t)max(m[0], m[1]) << 16;
+  }
+  __device__ __forceinline__ void widen(float (&x)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = __uint_as_float(v[j] << 16);
+      x[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u);
+    }
+  }
+};
 
 }  // namespace
 }  // namespace saga

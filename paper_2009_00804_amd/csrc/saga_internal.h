@@ -215,6 +215,14 @@ struct QuantGemmArgs {
 constexpr int64_t kQuantMaxK = 131071;      // 128 * 128 k stays below 2^31
 constexpr int64_t kQuantMaxLd = 1 << 23;    // a tile's rows within 32-bit offsets
 hipError_t launch_gemm_quant(const QuantGemmArgs& g, hipStream_t st);
+// float rows quantised on the way, without a workspace (where quant_fuses); g.a,
+// g.lda and g.a_scale are not used
+struct QuantFloatArgs {
+  QuantGemmArgs g;
+  const void* x; int64_t ldx;
+};
+bool quant_fuses(int64_t M, int64_t N, int64_t K);
+hipError_t launch_quant_fused(int dtype, const QuantFloatArgs& f, hipStream_t st);
 
 // ---- block.hip ----
 constexpr int64_t kBlockMaxF = 16384;
