@@ -35,7 +35,10 @@ __global__ __launch_bounds__(RowGroup<G>::THREADS) void k_quantize_rows(QuantRow
     for (int u = 0; u < U; ++u) v[u].load(x + col0 + u * 8 * G, K - col0 - u * 8 * G);
     uint32_t top = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) top = max(top, v[u].top());
+    for (int u = 0; u < U; ++u) {
+      v[u].clear(K - col0 - u * 8 * G);
+      top = max(top, v[u].top());
+    }
     const RowScale s = row_scale(R::template reduce<OpMaxU>(top, red, turn));
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -61,11 +64,13 @@ __global__ __launch_bounds__(1024) void k_quantize_long(QuantRowsArgs a) {
     uint32_t top = 0;
     for (int64_t col = threadIdx.x * 8; col < K; col += 8192) {
       v.load(x + col, (int)(K - col));
+      v.clear((int)(K - col));
       top = max(top, v.top());
     }
     const RowScale s = row_scale(R::reduce<OpMaxU>(top, red, turn));
     for (int64_t col = threadIdx.x * 8; col < K; col += 8192) {
       v.load(x + col, (int)(K - col));
+      v.clear((int)(K - col));
       float f[8];
       v.widen(f);
       store_unit_i8(a.q + row * a.ldq + col, K - col, round_unit(f, s));
@@ -81,9 +86,15 @@ hipError_t launch_rows(const QuantRowsArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_quantize_rows<T, G, U>), dim3((unsigned)blocks), dim3(R::THREADS), 0, st, a);
   return hipGetLastError();
 }
-// 16 lanes a row while that takes few units a lane: less of a row's last unit is idle
+// 16 lanes a row where there are many rows: less of a row's last unit is idle.  Over
+// few rows a wave or workgroup a row: more lanes work at all.
 template <typename T>
 hipError_t dispatch_rows(const QuantRowsArgs& a, hipStream_t st) {
+  if (a.M <= 4096) {
+    if (a.K <= 512) return launch_rows<T, 64, 1>(a, st);
+    if (a.K <= 2048) return launch_rows<T, 256, 1>(a, st);
+    if (a.K <= 8192) return launch_rows<T, 1024, 1>(a, st);
+  }
   if (a.K <= 128) return launch_rows<T, 16, 1>(a, st);
   if (a.K <= 256) return launch_rows<T, 16, 2>(a, st);
   if (a.K <= 384) return launch_rows<T, 16, 3>(a, st);
@@ -416,9 +427,10 @@ constexpr int kFusedK = 1248, kAhead = 4;
 __device__ __forceinline__ int fused_pitch(int K) { return ((K + 15) / 16) | 1; }  // in pieces
 
 template <typename T, int BM, int U, int WM, int WN, int NI>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void k_quant_fused(QuantFloatArgs f) {
-  constexpr int MI = BM / 16 / WM;
-  static_assert(WM * WN == 8 && MI * 16 * WM == BM, "eight waves");
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(4))) void k_quant_fused(
+    QuantFloatArgs f) {
+  constexpr int MI = BM / 16 / WM, RW = BM / (WM * WN);  // RW: rows a wave quantises
+  static_assert(MI * 16 * WM == BM && RW % 4 == 0, "whole tiles and passes");
   extern __shared__ uint4 rows[];  // BM rows of `pitch` pieces, and four pieces that a last step may read
   __shared__ float scales[BM];
   const QuantGemmArgs& g = f.g;
@@ -427,27 +439,41 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void k
   const int64_t m0 = blockIdx.x * (int64_t)BM;
   char* const lds = reinterpret_cast<char*>(rows);
 
-  constexpr int RW = BM / 8;  // rows of a wave
-#pragma unroll 1
-  for (int r0 = 0; r0 < RW; r0 += 4) {
-    const int r = wave * RW + r0 + (lane >> 4), col0 = (lane & 15) * 8;
-    const int64_t m = min(m0 + r, g.M - 1);
-    const T* x = static_cast<const T*>(f.x) + m * f.ldx;
-    Raw<T> v[U];
+  // four rows a pass, the next pass's on their way while these are rounded
+  constexpr int PASSES = RW / 4;
+  Raw<T> v[2][U];
+  const auto load_pass = [&](int p) {
+    const int64_t m = min(m0 + wave * RW + p * 4 + (lane >> 4), g.M - 1);
+    const int col0 = (lane & 15) * 8;
+    const T* x = static_cast<const T*>(f.x) + m * f.ldx + col0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u].load(x + col0 + u * 128, K - col0 - u * 128);
+    for (int u = 0; u < U; ++u)
+      if (u * 128 < K) v[p & 1][u].load(x + u * 128, K - col0 - u * 128);
+  };
+  load_pass(0);
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    if (p + 1 < PASSES) load_pass(p + 1);
+    const int r = wave * RW + p * 4 + (lane >> 4), col0 = (lane & 15) * 8;
     uint32_t top = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) top = max(top, v[u].top());
+    for (int u = 0; u < U; ++u)
+      if (u * 128 < K) {
+        v[p & 1][u].clear(K - col0 - u * 128);
+        top = max(top, v[p & 1][u].top());
+      }
     const RowScale s = row_scale(group_maxu<16>(top));
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int col = col0 + u * 128;
-      float x8[8];
-      v[u].widen(x8);
-      if (col < pitch * 16) *reinterpret_cast<uint2*>(lds + r * pitch * 16 + col) = round_unit(x8, s);
+      if (u * 128 < K) {
+        const int col = col0 + u * 128;
+        float x8[8];
+        v[p & 1][u].widen(x8);
+        if (col < pitch * 16) *reinterpret_cast<uint2*>(lds + r * pitch * 16 + col) = round_unit(x8, s);
+      }
     }
-    if ((lane & 15) == 0) scales[r] = s.s * (g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[m]) : 1.0f);
+    if ((lane & 15) == 0)
+      scales[r] = s.s * (g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[min(m0 + r, g.M - 1)]) : 1.0f);
   }
   __syncthreads();
 
@@ -507,7 +533,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void k
   }
 }
 
-template <typename T, int BM, int U>
+template <typename T, int BM, int U, int WM, int WN, int NI>
 hipError_t launch_fused(const QuantFloatArgs& f0, hipStream_t st) {
   const int64_t slice = kMostBlocks * BM;  // rows per launch
   for (int64_t m = 0; m < f0.g.M; m += slice) {
@@ -517,31 +543,125 @@ hipError_t launch_fused(const QuantFloatArgs& f0, hipStream_t st) {
     f.x = static_cast<const T*>(f.x) + m * f.ldx;
     if (g.row_scale_deg) g.row_scale_deg += m;
     g.out = static_cast<char*>(g.out) + m * g.ldo * (g.out_dtype == SAGA_BF16 ? 2 : 4);
-    const dim3 grid((unsigned)((g.M + BM - 1) / BM));
     const size_t lds = ((size_t)BM * (((g.K + 15) / 16) | 1) + 4) * 16;
-    if (g.N <= 16) {
-      hipLaunchKernelGGL((k_quant_fused<T, BM, U, BM / 16, 128 / BM, 1>), grid, dim3(512), lds, st, f);
-    } else if (g.N <= 64) {
-      hipLaunchKernelGGL((k_quant_fused<T, BM, U, BM / 32, 256 / BM, 128 / BM == 1 ? 2 : 1>), grid, dim3(512), lds, st, f);
-    } else {
-      hipLaunchKernelGGL((k_quant_fused<T, BM, U, 2, 4, 2>), grid, dim3(512), lds, st, f);
-    }
+    hipLaunchKernelGGL((k_quant_fused<T, BM, U, WM, WN, NI>), dim3((unsigned)((g.M + BM - 1) / BM)),
+                       dim3(64 * WM * WN), lds, st, f);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
-template <typename T>
+// 64 rows by eight waves, each of all rows and 16 columns: w's fragments are loaded
+// once a workgroup (2^20 x 602 x 128 in bfloat16, us: 392; 128 rows 442; 128 rows by
+// 2 x 4 waves, which load them twice, 523; 64 rows by four waves of 32 columns 434).
+template <typename T, int U>
 hipError_t dispatch_fused(const QuantFloatArgs& f, hipStream_t st) {
-  const int64_t k = f.g.K;
-  if (k <= 128) return launch_fused<T, 128, 1>(f, st);
-  if (k <= 256) return launch_fused<T, 128, 2>(f, st);
-  if (k <= 384) return launch_fused<T, 128, 3>(f, st);
-  if (k <= 512) return launch_fused<T, 128, 4>(f, st);
-  if (k <= 624) return launch_fused<T, 128, 5>(f, st);  // two workgroups' rows fill a CU's LDS
-  if (k <= 768) return launch_fused<T, 64, 6>(f, st);
-  if (k <= 1024) return launch_fused<T, 64, 8>(f, st);
-  return launch_fused<T, 64, 10>(f, st);
+  if (f.g.N <= 32) return launch_fused<T, 64, U, 4, 2, 1>(f, st);
+  if (f.g.N <= 64) return launch_fused<T, 64, U, 2, 4, 1>(f, st);
+  return launch_fused<T, 64, U, 1, 8, 1>(f, st);
+}
+
+// --------------------------------------------------------------------------
+// few rows: 16 of them and 16 channels a workgroup, k divided among its eight
+// waves.  Every workgroup quantises the rows for itself (8-bit rows come straight
+// from memory): reading w over many CUs at once is what counts, and one launch.
+// --------------------------------------------------------------------------
+constexpr int kFewK = 4096;
+
+template <typename T>
+__global__ __launch_bounds__(512) void k_quant_few(QuantFloatArgs f) {
+  constexpr int NW = 8;
+  constexpr bool I8 = sizeof(T) == 1;
+  extern __shared__ uint4 rows[];  // 16 rows of `pitch` pieces, and four pieces that a last step may read
+  __shared__ float scales[16];
+  __shared__ i32x4 part[NW][64];
+  const QuantGemmArgs& g = f.g;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int quarter = lane >> 4, lr = lane & 15;
+  const int K = (int)g.K, pitch = fused_pitch(K), steps = (K + 63) / 64, per = (steps + NW - 1) / NW;
+  const int64_t m0 = blockIdx.y * (int64_t)16, n0 = blockIdx.x * (int64_t)16;
+  const int here = (int)min((int64_t)16, g.M - m0);
+  const int s0 = wave * per, s1 = min(steps, s0 + per);
+
+  const int8_t* const wr = g.w + min(n0 + lr, g.N - 1) * g.ldw + quarter * 16;
+  const auto load_w = [&](int s) {
+    i32x4 o = {0, 0, 0, 0};
+    if (s < s1 && s * 64 + quarter * 16 < K) o = *reinterpret_cast<const i32x4*>(wr + s * 64);
+    return o;
+  };
+  i32x4 w[kAhead], acc = {0, 0, 0, 0};
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) w[k] = load_w(s0 + k);
+
+  if constexpr (!I8) {
+    char* const lds = reinterpret_cast<char*>(rows);
+    for (int r = wave; r < here; r += NW) {
+      const T* x = static_cast<const T*>(f.x) + (m0 + r) * f.ldx;
+      uint32_t top = 0;
+      Raw<T> v;
+#pragma unroll 2
+      for (int col = lane * 8; col < K; col += 512) {
+        v.load(x + col, K - col);
+        v.clear(K - col);
+        top = max(top, v.top());
+      }
+      const RowScale s = row_scale(group_maxu<64>(top));
+#pragma unroll 2
+      for (int col = lane * 8; col < pitch * 16; col += 512) {
+        v.load(x + col, K - col);
+        v.clear(K - col);
+        float x8[8];
+        v.widen(x8);
+        *reinterpret_cast<uint2*>(lds + r * pitch * 16 + col) = round_unit(x8, s);
+      }
+      if (lane == 0) scales[r] = s.s;
+    }
+    __syncthreads();
+  }
+  // (rows past the last: another row's values, not stored)
+  const uint4* const al = rows + min(lr, here - 1) * pitch + quarter;
+  const int8_t* const ag = I8 ? g.a + (m0 + min(lr, here - 1)) * g.lda + quarter * 16 : nullptr;
+  for (int s = s0; s < s1; s += kAhead) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (s + k < s1) {
+        i32x4 a;
+        if constexpr (I8) {
+          // (a piece that reaches past K holds padding: cleared)
+          a = i32x4{0, 0, 0, 0};
+          const int left = K - (s + k) * 64 - quarter * 16;
+          if (left > 0) a = mask_bytes(*reinterpret_cast<const i32x4*>(ag + (s + k) * 64), left);
+        } else {
+          a = *reinterpret_cast<const i32x4*>(al + (s + k) * 4);
+        }
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[k], a, acc, 0, 0, 0);
+      }
+      w[k] = load_w(s + k + kAhead);
+    }
+  }
+  part[wave][lane] = acc;
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int k = 1; k < NW; ++k) acc += part[k][lane];
+  const int64_t m = m0 + lr, n = n0 + quarter * 4;
+  if (lr >= here || n >= g.N) return;
+  f32x4 tw, tb;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    tw[j] = n + j < g.N ? g.w_scale[n + j] : 0.0f;
+    tb[j] = g.bias && n + j < g.N ? g.bias[n + j] : 0.0f;
+  }
+  const float sa = I8 ? g.a_scale[m] : scales[lr];
+  store_quad(g, m, n, acc, sa * (g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[m]) : 1.0f), tw, tb);
+}
+
+template <typename T>
+hipError_t launch_few(const QuantFloatArgs& f, hipStream_t st) {
+  const size_t lds = sizeof(T) == 1 ? 0 : ((size_t)16 * (((f.g.K + 15) / 16) | 1) + 4) * 16;
+  hipLaunchKernelGGL((k_quant_few<T>), dim3((unsigned)((f.g.N + 15) / 16), (unsigned)((f.g.M + 15) / 16)), dim3(512),
+                     lds, st, f);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -551,15 +671,36 @@ hipError_t launch_quantize_rows(const QuantRowsArgs& a, hipStream_t st) {
   return a.dtype == SAGA_BF16 ? dispatch_rows<uint16_t>(a, st) : dispatch_rows<float>(a, st);
 }
 
-bool quant_fuses(int64_t M, int64_t N, int64_t K) { return K <= kFusedK && N <= 512; }
+// Which kernel takes a product (us, measured on bfloat16 or 8-bit rows).
+// k_quant_few while its workgroups and their steps are few: 8-bit rows against
+// 128 x 128 tiles 16 x 4096 x 4096 7 / 17, 64 x 4096 x 4096 18 / 21, 128 x 4096 x
+// 4096 34 / 21, 256 x 1024 x 1024 7 / 12; float rows, which every workgroup
+// quantises again, against two launches 16 x 4096 x 4096 17 / 27, 64 x 4096 x 4096
+// 42 / 31, 256 x 1024 x 1024 13 / 22, 200 x 1000 x 1000 12 / 23.
+bool quant_few(int64_t M, int64_t N, int64_t K, int64_t most) {
+  const int64_t wgs = ((M + 15) / 16) * ((N + 15) / 16);
+  return M <= 16384 && N <= 16384 && wgs <= 1024 && wgs * ((K + 63) / 64) <= most;
+}
+bool quant_few_float(int64_t M, int64_t N, int64_t K) { return K <= kFewK && quant_few(M, N, K, 32768); }
+// k_quant_fused while w is narrow, against two launches: 2^18 x 602 x 128 107 / 175,
+// 2000 x 602 x 128 13 / 19, 100000 x 602 x 256 60 / 76, x 512 96 / 106, x 1024 182 /
+// 163; over few rows its sweeps of 128 columns take too long (2000 x 1000 x 512 31 /
+// 24, 512 x 602 x 512 23 / 19).
+bool quant_fuses(int64_t M, int64_t N, int64_t K) {
+  return quant_few_float(M, N, K) || (K <= kFusedK && (N <= 128 || (N <= 512 && M >= 16384)));
+}
 
 hipError_t launch_quant_fused(int dtype, const QuantFloatArgs& f, hipStream_t st) {
   if (f.g.M == 0) return hipSuccess;
-  return dtype == SAGA_BF16 ? dispatch_fused<uint16_t>(f, st) : dispatch_fused<float>(f, st);
+  const bool bf = dtype == SAGA_BF16;
+  if (quant_few_float(f.g.M, f.g.N, f.g.K)) return bf ? launch_few<uint16_t>(f, st) : launch_few<float>(f, st);
+  if (f.g.K <= 640) return bf ? dispatch_fused<uint16_t, 5>(f, st) : dispatch_fused<float, 5>(f, st);
+  return bf ? dispatch_fused<uint16_t, 10>(f, st) : dispatch_fused<float, 10>(f, st);
 }
 
 hipError_t launch_gemm_quant(const QuantGemmArgs& g, hipStream_t st) {
   if (g.M == 0) return hipSuccess;
+  if (quant_few(g.M, g.N, g.K, 65536)) return launch_few<int8_t>(QuantFloatArgs{g, nullptr, 0}, st);
   if (g.N <= 16) return launch_tile<4, 1, 2, 1, 128, 2>(g, st);
   if (g.N <= 32) return launch_tile<4, 1, 2, 2, 128, 2>(g, st);
   if (g.N <= 64) return launch_tile<4, 1, 2, 4, 128, 2>(g, st);

@@ -203,8 +203,9 @@ __device__ __forceinline__ uint2 round_unit(const float (&x)[8], const RowScale&
   return make_uint2(o[0], o[1]);
 }
 
-// A unit as it lies in memory, columns past `left` cleared: half the registers of
-// its float32 values where it is bfloat16.
+// A unit as it lies in memory: half the registers of its float32 values where it is
+// bfloat16.  `clear` zeroes the columns past `left` (apart from `load`, so that it
+// does not wait for loads that are still under way).
 template <typename T> struct Raw;
 template <> struct Raw<float> {
   u32x4 v[2];
@@ -214,7 +215,9 @@ template <> struct Raw<float> {
       v[h] = u32x4{0u, 0u, 0u, 0u};
       if (left > 4 * h) v[h] = *reinterpret_cast<const u32x4*>(p + 4 * h);
     }
-    if (left > 0 && left < 8) {
+  }
+  __device__ __forceinline__ void clear(int left) {
+    if (left < 8) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         if (left <= j) v[j / 4][j % 4] = 0u;
@@ -236,7 +239,9 @@ template <> struct Raw<uint16_t> {
   __device__ __forceinline__ void load(const uint16_t* p, int left) {
     v = u32x4{0u, 0u, 0u, 0u};
     if (left > 0) v = *reinterpret_cast<const u32x4*>(p);
-    if (left > 0 && left < 8) {
+  }
+  __device__ __forceinline__ void clear(int left) {
+    if (left < 8) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (left <= 2 * j) v[j] = 0u;
