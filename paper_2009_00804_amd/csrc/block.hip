@@ -17,116 +17,183 @@
 namespace saga {
 namespace {
 
-constexpr int64_t kMostBlocks = 1 << 20;  // (a grid holds less than 2^32 threads)
+constexpr int64_t kMostBlocks = 2048;  // groups keep their vectors over many rows
 
+// A lane's share of a row: U units, unit u at column col0 + u * 8 * G.
 template <int G, int U>
-__device__ __forceinline__ void normalise(int kind, float eps, float inv_f, int col0, int F, float (&v)[U][8],
-                                          uint32_t* red, int& turn) {
+struct Share {
   typedef RowGroup<G> R;
-  if (kind == SAGA_NORM_LAYER) {
+  static constexpr int STEP = 8 * G;
+
+  // v / sqrt(mean v^2 + eps), for LAYER of v less its mean.  Columns past F are 0
+  // before and after.
+  __device__ __forceinline__ static void normalise(int kind, float eps, float inv_f, int left, float (&v)[U][8],
+                                                   uint32_t* red, int& turn) {
+    if (kind == SAGA_NORM_LAYER) {
+      float s = 0.0f;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += v[u][j];
+      const float mean = R::sum(s, red, turn) * inv_f;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[u][j] = j < left - u * STEP ? v[u][j] - mean : 0.0f;
+    }
     float s = 0.0f;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s += v[u][j];
-    const float mean = R::sum(s, red, turn) * inv_f;
+      for (int j = 0; j < 8; ++j) s = fmaf(v[u][j], v[u][j], s);
+    const float r = 1.0f / sqrtf(R::sum(s, red, turn) * inv_f + eps);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[u][j] = col0 + u * 8 * G + j < F ? v[u][j] - mean : 0.0f;
+      for (int j = 0; j < 8; ++j) v[u][j] *= r;
   }
-  float s = 0.0f;
+};
+
+// Gate activations, a few units in the last place off.  tanh: its series where
+// 1 - 2 / (e^2x + 1) would cancel (below 0.3 the first term left out is 5e-8 x).
+__device__ __forceinline__ float gate_value(int act, float x) {
+  switch (act) {
+    case SAGA_ACT_RELU: return x > 0.0f ? x : 0.0f;
+    case SAGA_ACT_ELU: return x > 0.0f ? x : expm1f(x);
+    case SAGA_ACT_SIGMOID: return __builtin_amdgcn_rcpf(1.0f + __expf(-x));
+    case SAGA_ACT_TANH: {
+      const float q = x * x;
+      const float p = fmaf(q, fmaf(q, fmaf(q, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f);
+      const float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__expf(2.0f * x) + 1.0f);
+      return q < 0.09f ? fmaf(x * q, p, x) : t;
+    }
+    default: return x;
+  }
+}
+
+// a lane's vector values at its columns, `other` where there is no vector, 0 past F
+template <int U, int STEP>
+__device__ __forceinline__ void load_vector(const float* w, float other, int col0, int left, float (&v)[U][8]) {
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = fmaf(v[u][j], v[u][j], s);
-  const float r = 1.0f / sqrtf(R::sum(s, red, turn) * inv_f + eps);
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[u][j] *= r;
-}
-
-// v = v * w + b on the unit's columns (w, b nullable)
-__device__ __forceinline__ void affine(const float* w, const float* b, int col, int F, float (&v)[8]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (col + j < F) {
-      if (w) v[j] *= w[col + j];
-      if (b) v[j] += b[col + j];
+    for (int j = 0; j < 8; ++j) {
+      const bool in_row = j < left - u * STEP;
+      v[u][j] = in_row ? (w ? w[col0 + u * STEP + j] : other) : 0.0f;
     }
 }
 
-template <typename XT, typename BT, int G, int U>
-__device__ __forceinline__ void block_row(const BlockArgs& a, int64_t row, uint32_t* red, int& turn) {
-  typedef RowGroup<G> R;
-  const int col0 = (threadIdx.x % G) * 8, F = a.F;
-  const float inv_f = 1.0f / (float)F;
-  float u[U][8], y[U][8];
-#pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int col = col0 + i * 8 * G;
-    load_unit(static_cast<const BT*>(a.block) + row * a.ld_block + col, F - col, u[i]);
-    if (a.x) {
-      load_unit(static_cast<const XT*>(a.x) + row * a.ld_x + col, F - col, y[i]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[i][j] = 0.0f;
-    }
-  }
-  if (a.post_kind != SAGA_NORM_NONE) normalise<G, U>(a.post_kind, a.post_eps, inv_f, col0, F, u, red, turn);
-#pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int col = col0 + i * 8 * G;
-    if (a.post_kind != SAGA_NORM_NONE) affine(a.post_w, a.post_b, col, F, u[i]);
-    affine(a.channel, nullptr, col, F, u[i]);
-    if (a.gate) {
-      float g[8];
-      load_unit(static_cast<const BT*>(a.gate) + row * a.ld_gate + col, F - col, g);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) u[i][j] *= apply_act(a.gate_act, g[j]);
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[i][j] = col + j < F ? fmaf(a.res_scale, u[i][j], y[i][j]) : 0.0f;
-    if (a.y) store_unit(static_cast<XT*>(a.y) + row * a.ld_y + col, F - col, y[i]);
-  }
-  if (!a.z) return;
-  if (a.pre_kind != SAGA_NORM_NONE) {
-    normalise<G, U>(a.pre_kind, a.pre_eps, inv_f, col0, F, y, red, turn);
-#pragma unroll
-    for (int i = 0; i < U; ++i) affine(a.pre_w, a.pre_b, col0 + i * 8 * G, F, y[i]);
-  }
-  if (a.z_scale) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(y[i][j]) & 0x7fffffffu);
-    const RowScale s = row_scale(R::template reduce<OpMaxU>(top, red, turn));
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int col = col0 + i * 8 * G;
-      store_unit_i8(static_cast<int8_t*>(a.z) + row * a.ld_z + col, F - col, round_unit(y[i], s));
-    }
-    if (threadIdx.x % G == 0) a.z_scale[row] = s.s;
-  } else {
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int col = col0 + i * 8 * G;
-      store_unit(static_cast<BT*>(a.z) + row * a.ld_z + col, F - col, y[i]);
-    }
-  }
-}
+template <typename XT, typename BT, int U>
+struct Inputs {
+  Raw<BT> block[U], gate[U];
+  Raw<XT> x[U];
+};
 
+// The vectors of a lane's columns stay in its registers for all rows of its group,
+// post's weights with the channel and residual scales taken in; a row's loads are
+// issued while the row before it is computed.
 template <typename XT, typename BT, int G, int U>
 __global__ __launch_bounds__(RowGroup<G>::THREADS) void k_block_norm(BlockArgs a) {
   typedef RowGroup<G> R;
+  typedef Share<G, U> H;
   __shared__ uint32_t red[2 * (G > 64 ? G / 64 : 1)];
   int turn = 0;
+  const int col0 = (threadIdx.x % G) * 8, left = a.F - col0;
+  const float inv_f = 1.0f / (float)a.F;
+  float aw[U][8], ab[U][8], pw[U][8], pb[U][8];
+  {
+    float ch[U][8];
+    load_vector<U, H::STEP>(a.channel, 1.0f, col0, left, ch);
+    load_vector<U, H::STEP>(a.post_kind != SAGA_NORM_NONE ? a.post_w : nullptr, 1.0f, col0, left, aw);
+    load_vector<U, H::STEP>(a.post_kind != SAGA_NORM_NONE ? a.post_b : nullptr, 0.0f, col0, left, ab);
+    load_vector<U, H::STEP>(a.pre_kind != SAGA_NORM_NONE ? a.pre_w : nullptr, 1.0f, col0, left, pw);
+    load_vector<U, H::STEP>(a.pre_kind != SAGA_NORM_NONE ? a.pre_b : nullptr, 0.0f, col0, left, pb);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        aw[u][j] *= ch[u][j] * a.res_scale;
+        ab[u][j] *= ch[u][j] * a.res_scale;
+      }
+  }
+  const int64_t stride = gridDim.x * (int64_t)R::ROWS;
+  int64_t row = blockIdx.x * (int64_t)R::ROWS + threadIdx.x / G;
+  Inputs<XT, BT, U> in;
+  const auto load = [&](int64_t r) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int col = col0 + u * H::STEP, l = left - u * H::STEP;
+      in.block[u].load(static_cast<const BT*>(a.block) + r * a.ld_block + col, l);
+      if (a.gate) in.gate[u].load(static_cast<const BT*>(a.gate) + r * a.ld_gate + col, l);
+      if (a.x) in.x[u].load(static_cast<const XT*>(a.x) + r * a.ld_x + col, l);
+    }
+  };
+  if (row < a.M) load(row);
   // (a row's lanes stay together: rows of several waves own their workgroup)
-  for (int64_t row = blockIdx.x * (int64_t)R::ROWS + threadIdx.x / G; row < a.M;
-       row += gridDim.x * (int64_t)R::ROWS)
-    block_row<XT, BT, G, U>(a, row, red, turn);
+  for (; row < a.M; row += stride) {
+    Inputs<XT, BT, U> now = in;
+    if (row + stride < a.M) load(row + stride);
+    float v[U][8], y[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      now.block[u].clear(left - u * H::STEP);
+      now.block[u].widen(v[u]);
+    }
+    if (a.post_kind != SAGA_NORM_NONE) H::normalise(a.post_kind, a.post_eps, inv_f, left, v, red, turn);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[u][j] = fmaf(v[u][j], aw[u][j], ab[u][j]);
+    if (a.gate) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float g[8];
+        now.gate[u].clear(left - u * H::STEP);
+        now.gate[u].widen(g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[u][j] *= gate_value(a.gate_act, g[j]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (a.x) {
+        now.x[u].clear(left - u * H::STEP);
+        now.x[u].widen(y[u]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[u][j] += v[u][j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[u][j] = v[u][j];
+      }
+      if (a.y)
+        store_unit(static_cast<XT*>(a.y) + row * a.ld_y + col0 + u * H::STEP, left - u * H::STEP, y[u]);
+    }
+    if (!a.z) continue;
+    if (a.pre_kind != SAGA_NORM_NONE) {
+      H::normalise(a.pre_kind, a.pre_eps, inv_f, left, y, red, turn);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[u][j] = fmaf(y[u][j], pw[u][j], pb[u][j]);
+    }
+    if (a.z_scale) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(y[u][j]) & 0x7fffffffu);
+      const RowScale s = row_scale(R::template reduce<OpMaxU>(top, red, turn));
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        store_unit_i8(static_cast<int8_t*>(a.z) + row * a.ld_z + col0 + u * H::STEP, left - u * H::STEP,
+                      round_unit(y[u], s));
+      if (threadIdx.x % G == 0) a.z_scale[row] = s.s;
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        store_unit(static_cast<BT*>(a.z) + row * a.ld_z + col0 + u * H::STEP, left - u * H::STEP, y[u]);
+    }
+  }
 }
 
 template <typename XT, typename BT, int G, int U>

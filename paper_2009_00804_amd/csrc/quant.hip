@@ -166,8 +166,7 @@ __device__ __forceinline__ void store_quad(const QuantGemmArgs& g, int64_t m, in
   if (g.out_dtype == SAGA_BF16) {
     uint16_t* o = static_cast<uint16_t*>(g.out) + m * g.ldo + n;
     if (n + 4 <= g.N) {
-      *reinterpret_cast<uint2*>(o) = make_uint2((uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
-                                                (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16));
+      *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)

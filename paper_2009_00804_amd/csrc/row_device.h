@@ -91,28 +91,10 @@ struct RowGroup {
 };
 
 // --------------------------------------------------------------------------
-// units: 8 columns of a row, columns past `left` read as 0.  A 16-byte piece
-// is touched only if its first column is in the row: the rest of it is padding
-// of the same 16 bytes.
+// units: 8 columns of a row.  A 16-byte piece is touched only if its first column
+// is in the row (`left` columns of it are): the rest of it is padding of the same
+// 16 bytes.
 // --------------------------------------------------------------------------
-__device__ __forceinline__ void load_unit(const float* p, int64_t left, float (&v)[8]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    if (left > 4 * h) x = *reinterpret_cast<const f32x4*>(p + 4 * h);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[4 * h + j] = left > 4 * h + j ? x[j] : 0.0f;
-  }
-}
-__device__ __forceinline__ void load_unit(const uint16_t* p, int64_t left, float (&v)[8]) {
-  u32x4 x = {0u, 0u, 0u, 0u};
-  if (left > 0) x = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    v[2 * j] = left > 2 * j ? __uint_as_float(x[j] << 16) : 0.0f;
-    v[2 * j + 1] = left > 2 * j + 1 ? __uint_as_float(x[j] & 0xffff0000u) : 0.0f;
-  }
-}
 __device__ __forceinline__ void store_unit(float* p, int64_t left, const float (&v)[8]) {
   if (left >= 8) {
     *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
@@ -123,12 +105,20 @@ __device__ __forceinline__ void store_unit(float* p, int64_t left, const float (
       if (j < left) p[j] = v[j];
   }
 }
+// two values rounded to bfloat16 (to nearest, ties to even; one instruction)
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 b = __builtin_convertvector((f32x2{lo, hi}), bf16x2);
+  uint32_t u;
+  __builtin_memcpy(&u, &b, 4);
+  return u;
+}
 __device__ __forceinline__ void store_unit(uint16_t* p, int64_t left, const float (&v)[8]) {
   if (left >= 8) {
     u32x4 w;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      w[j] = (uint32_t)f32_to_bf16(v[2 * j]) | ((uint32_t)f32_to_bf16(v[2 * j + 1]) << 16);
+    for (int j = 0; j < 4; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
     *reinterpret_cast<u32x4*>(p) = w;
   } else {
 #pragma unroll

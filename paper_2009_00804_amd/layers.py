@@ -182,6 +182,11 @@ def _out(rows, cols, dtype, like):
     return (buf if ld == cols else buf[:, :cols]), S.saga_mat(buf.data_ptr(), rows, cols, ld)
 
 
+def _stream(t):
+    """hipStream_t of torch's current stream on t's device"""
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
 def _space(nbytes, like):
     return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
 
@@ -196,7 +201,7 @@ def quantize_rows(x):
     cx = _matrix(x, "x", x, _FLOATS)
     q, mq = _out(x.shape[0], x.shape[1], torch.int8, x)
     scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-    S.saga_quantize_rows(S.dtype_code(x.dtype), cx, mq, scale.data_ptr(), S.stream_handle())
+    S.saga_quantize_rows(S.dtype_code(x.dtype), cx, mq, scale.data_ptr(), _stream(x))
     return q, scale
 
 
@@ -219,7 +224,7 @@ def quant_linear(x, w, w_scale, x_scale=None, bias=None, act="none", row_scale_d
     ws = _space(nbytes, x)
     S.saga_apply_vertex_quant(op, cx, _vector(x_scale, "x_scale", x, m), cw,
                               _vector(w_scale, "w_scale", x, n), _vector(bias, "bias", x, n), mo,
-                              ws.data_ptr() if nbytes else None, nbytes, S.stream_handle())
+                              ws.data_ptr() if nbytes else None, nbytes, _stream(x))
     return out
 
 
@@ -254,7 +259,7 @@ def block_norm(block, x=None, *, post="none", post_weight=None, post_bias=None, 
         y, my = _out(m, f, x_dtype, block)
     z, mz = _out(m, f, torch.int8 if quantize else block.dtype, block)
     zs = torch.empty(m, dtype=torch.float32, device=block.device) if quantize else None
-    S.saga_block_norm(op, cb, cg, cx, my, mz, zs.data_ptr() if quantize else None, S.stream_handle())
+    S.saga_block_norm(op, cb, cg, cx, my, mz, zs.data_ptr() if quantize else None, _stream(block))
     return y, z, zs
 
 
@@ -276,7 +281,7 @@ def label_log_probs(logits, labels=None, top_k=0, entropy=True):
     S.saga_label_log_probs(code, cl, at, lp.data_ptr() if labels is not None else None,
                            h.data_ptr() if entropy else None, top_k, ti.data_ptr() if top_k else None,
                            tl.data_ptr() if top_k else None, ws.data_ptr() if nbytes else None, nbytes,
-                           S.stream_handle())
+                           _stream(logits))
     return lp, h, ti, tl
 
 
