@@ -206,13 +206,18 @@ hipError_t launch(const BlockArgs& a, hipStream_t st) {
 
 template <typename XT, typename BT>
 hipError_t dispatch(const BlockArgs& a, hipStream_t st) {
+  // Lanes per row and units per lane (us, float32 stream, bfloat16 blocks): 200000 x
+  // 300 64 x 1 204, 32 x 2 217; 400000 x 256 32 x 1 260, 16 x 2 262; 100003 x 602 128
+  // x 1 185, 32 x 3 197, 64 x 2 218, 16 x 5 295; 131072 x 1024 128 x 1 340, 64 x 2
+  // 336; 65536 x 2048 256 x 1 370, 128 x 2 393; 32768 x 4096 512 x 1 347, 256 x 2
+  // 369, 1024 x 1 487; 16384 x 8192 1024 x 1 358, 512 x 2 379.
   if (a.F <= 64) return launch<XT, BT, 8, 1>(a, st);
   if (a.F <= 128) return launch<XT, BT, 16, 1>(a, st);
   if (a.F <= 256) return launch<XT, BT, 32, 1>(a, st);
   if (a.F <= 512) return launch<XT, BT, 64, 1>(a, st);
-  if (a.F <= 1024) return launch<XT, BT, 64, 2>(a, st);
+  if (a.F <= 1024) return launch<XT, BT, 128, 1>(a, st);
   if (a.F <= 2048) return launch<XT, BT, 256, 1>(a, st);
-  if (a.F <= 4096) return launch<XT, BT, 256, 2>(a, st);
+  if (a.F <= 4096) return launch<XT, BT, 512, 1>(a, st);
   if (a.F <= 8192) return launch<XT, BT, 1024, 1>(a, st);
   return launch<XT, BT, 1024, 2>(a, st);
 }

@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t group_maxu(uint32_t v) {
 // turn: the reductions so far)
 template <int G>
 struct RowGroup {
-  static constexpr int THREADS = G > 256 ? G : 256;
+  static constexpr int THREADS = G > 64 ? G : 256;  // (a row of several waves has barriers: it owns its workgroup)
   static constexpr int ROWS = THREADS / G;
 
   template <typename OP>
