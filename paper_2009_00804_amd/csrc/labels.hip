@@ -17,32 +17,45 @@ namespace {
 
 constexpr int64_t kMostBlocks = 1 << 20;  // (a grid holds less than 2^32 threads)
 constexpr float kNegInf = -__builtin_huge_valf();
+typedef volatile __attribute__((address_space(3))) float* lds_floats;
 
-// 16-byte piece of a row, columns past `left` read as -inf
+// 16-byte piece of a row as it lies in memory, and its values; of those past
+// `left` -inf
 template <typename T> struct Piece;
 template <> struct Piece<float> {
   static constexpr int N = 4;
-  __device__ __forceinline__ static void load(const float* p, int left, float* v) {
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    if (left > 0) x = *reinterpret_cast<const f32x4*>(p);
+  __device__ __forceinline__ static void widen(const u32x4& x, float* v) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = left > j ? x[j] : kNegInf;
+    for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(x[j]);
   }
   __device__ __forceinline__ static float one(const float* p) { return *p; }
 };
 template <> struct Piece<uint16_t> {
   static constexpr int N = 8;
-  __device__ __forceinline__ static void load(const uint16_t* p, int left, float* v) {
-    u32x4 x = {0u, 0u, 0u, 0u};
-    if (left > 0) x = *reinterpret_cast<const u32x4*>(p);
+  __device__ __forceinline__ static void widen(const u32x4& x, float* v) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      v[2 * j] = left > 2 * j ? __uint_as_float(x[j] << 16) : kNegInf;
-      v[2 * j + 1] = left > 2 * j + 1 ? __uint_as_float(x[j] & 0xffff0000u) : kNegInf;
+      v[2 * j] = __uint_as_float(x[j] << 16);
+      v[2 * j + 1] = __uint_as_float(x[j] & 0xffff0000u);
     }
   }
   __device__ __forceinline__ static float one(const uint16_t* p) { return bf16_to_f32(*p); }
 };
+template <typename T>
+__device__ __forceinline__ u32x4 load_piece(const T* p, int64_t left) {
+  u32x4 x = {0u, 0u, 0u, 0u};
+  if (left > 0) x = *reinterpret_cast<const u32x4*>(p);
+  return x;
+}
+template <typename T>
+__device__ __forceinline__ void widen_piece(const u32x4& x, int64_t left, float* v) {
+  Piece<T>::widen(x, v);
+  if (left < Piece<T>::N) {
+#pragma unroll
+    for (int j = 0; j < Piece<T>::N; ++j)
+      if (left <= j) v[j] = kNegInf;
+  }
+}
 
 // m, S and T of some columns.  Nothing but -inf: m = -inf, S = T = 0.  A NaN or
 // +inf among them makes S a NaN.
@@ -97,16 +110,23 @@ __device__ __forceinline__ Row row_of(const Stats& a) {
 __device__ __forceinline__ float log_prob(const Row& r, float x) {
   return r.bad ? __uint_as_float(0x7fc00000u) : r.empty ? kNegInf : x - r.m - r.log_s;
 }
-// logp and entropy of a row (one lane)
+// a row's label and the label's logit (0 if there is none), loaded ahead
+struct Label {
+  int32_t c;
+  float x;
+};
 template <typename T>
-__device__ __forceinline__ void write_row(const LabelArgs& a, int64_t row, const Row& r) {
+__device__ __forceinline__ Label load_label(const LabelArgs& a, int64_t row) {
+  Label l{-1, 0.0f};
   if (a.logp) {
-    const int32_t c = a.labels[row];
-    float lp = 0.0f;  // no label
-    if (c >= a.C) lp = __uint_as_float(0x7fc00000u);
-    else if (c >= 0) lp = log_prob(r, Piece<T>::one(static_cast<const T*>(a.logits) + row * a.ld + c));
-    a.logp[row] = lp;
+    l.c = a.labels[row];
+    if (l.c >= 0 && l.c < a.C) l.x = Piece<T>::one(static_cast<const T*>(a.logits) + row * a.ld + l.c);
   }
+  return l;
+}
+// logp and entropy of a row (one lane)
+__device__ __forceinline__ void write_row(const LabelArgs& a, int64_t row, const Row& r, const Label& l) {
+  if (a.logp) a.logp[row] = l.c < 0 ? 0.0f : l.c >= a.C ? __uint_as_float(0x7fc00000u) : log_prob(r, l.x);
   if (a.entropy) a.entropy[row] = r.entropy;
 }
 __device__ __forceinline__ void write_top(const LabelArgs& a, int64_t row, int k, const Row& r, float v, int c) {
@@ -126,7 +146,9 @@ __global__ __launch_bounds__(256) void k_labels_narrow(LabelArgs a) {
   const int g = threadIdx.x % G, col = g * P::N;
   for (int64_t row = blockIdx.x * (int64_t)ROWS + threadIdx.x / G; row < a.M; row += gridDim.x * (int64_t)ROWS) {
     float v[P::N];
-    P::load(static_cast<const T*>(a.logits) + row * a.ld + col, (int)(a.C - col), v);
+    const u32x4 raw = load_piece(static_cast<const T*>(a.logits) + row * a.ld + col, a.C - col);
+    const Label l = load_label<T>(a, row);
+    widen_piece<T>(raw, a.C - col, v);
     float top = v[0];
 #pragma unroll
     for (int j = 1; j < P::N; ++j) top = fmaxf(top, v[j]);
@@ -135,7 +157,7 @@ __global__ __launch_bounds__(256) void k_labels_narrow(LabelArgs a) {
     add_values(s, m, v);
     s = Stats{m, group_sum<G>(s.s), group_sum<G>(s.t)};
     const Row r = row_of(s);
-    if (g == 0) write_row<T>(a, row, r);
+    if (g == 0) write_row(a, row, r, l);
     for (int k = 0; k < a.top_k; ++k) {
       float best = v[0];
       int at = 0;
@@ -151,6 +173,106 @@ __global__ __launch_bounds__(256) void k_labels_narrow(LabelArgs a) {
       for (int j = 0; j < P::N; ++j)
         if (col + j == c) v[j] = kNegInf;
     }
+  }
+}
+
+// --------------------------------------------------------------------------
+// many rows of up to 64 columns: a lane a row, so that nothing is reduced between
+// lanes.  The top classes are kept in order by insertion, two instructions a value
+// and place for bfloat16: value and column make one whole number there.
+// --------------------------------------------------------------------------
+constexpr int kLaneC = 64;
+
+template <typename T, int K> struct TopList;
+template <int K> struct TopList<uint16_t, K> {
+  uint32_t t[K > 0 ? K : 1];
+  __device__ __forceinline__ TopList() {
+#pragma unroll
+    for (int k = 0; k < K; ++k) t[k] = 0x007fffffu;  // -inf
+  }
+  __device__ __forceinline__ void offer(float x, int col) {
+    const uint32_t u = __float_as_uint(x + 0.0f);  // (-0 counts as 0)
+    uint32_t key = ((u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) & 0xffff0000u) | (0xffffu - (uint32_t)col);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t m = max(t[k], key);
+      key = min(t[k], key);
+      t[k] = m;
+    }
+  }
+  __device__ __forceinline__ float value(int k) const {
+    const uint32_t h = t[k] & 0xffff0000u;
+    return __uint_as_float(h & 0x80000000u ? h ^ 0x80000000u : ~h & 0xffff0000u);
+  }
+  __device__ __forceinline__ int column(int k) const { return (int)(0xffffu - (t[k] & 0xffffu)); }
+};
+template <int K> struct TopList<float, K> {
+  float v[K > 0 ? K : 1];
+  int c[K > 0 ? K : 1];
+  __device__ __forceinline__ TopList() {
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = kNegInf, c[k] = -1;
+  }
+  __device__ __forceinline__ void offer(float x, int col) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const bool up = x > v[k];  // equal values stay behind those of lower columns
+      const float ov = v[k];
+      const int oc = c[k];
+      v[k] = up ? x : ov;
+      c[k] = up ? col : oc;
+      x = up ? ov : x;
+      col = up ? oc : col;
+    }
+  }
+  __device__ __forceinline__ float value(int k) const { return v[k]; }
+  __device__ __forceinline__ int column(int k) const { return c[k]; }
+};
+
+template <typename T, int K>
+__global__ __launch_bounds__(256) void k_labels_lane(LabelArgs a) {
+  typedef Piece<T> P;
+  constexpr int NP = kLaneC / P::N;
+  const int C = (int)a.C;
+  for (int64_t row = blockIdx.x * (int64_t)256 + threadIdx.x; row < a.M; row += gridDim.x * (int64_t)256) {
+    const T* x = static_cast<const T*>(a.logits) + row * a.ld;
+    u32x4 raw[NP];
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+      if (p * P::N < C) raw[p] = load_piece(x + p * P::N, C - p * P::N);
+    const Label l = load_label<T>(a, row);
+    TopList<T, K> best;
+    float m = kNegInf;
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+      if (p * P::N < C) {
+        float v[P::N];
+        widen_piece<T>(raw[p], C - p * P::N, v);
+#pragma unroll
+        for (int j = 0; j < P::N; ++j) {
+          m = fmaxf(m, v[j]);
+          best.offer(v[j], p * P::N + j);
+        }
+      }
+    Stats s{m, 0.0f, 0.0f};
+    const float mm = finite_top(m);
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+      if (p * P::N < C) {
+        float v[P::N];
+        widen_piece<T>(raw[p], C - p * P::N, v);
+#pragma unroll
+        for (int j = 0; j < P::N; ++j) {
+          const float d = v[j] - mm, e = __expf(d);
+          s.s += e;
+          s.t = fmaf(e, fmaxf(d, kFar), s.t);
+        }
+      }
+    const Row r = row_of(s);
+    write_row(a, row, r, l);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (k < a.top_k) write_top(a, row, k, r, best.value(k), best.column(k));
   }
 }
 
@@ -178,7 +300,23 @@ struct Best {
     const int uc = __shfl_up(c, 1, 64);
     v = lane < pos ? v : lane == pos ? x : uv;
     c = lane < pos ? c : lane == pos ? col : uc;
-    last = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), k - 1));
+    last = fmaxf(last, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), k - 1)));
+  }
+  // k or more values are at least x (uniform): smaller ones need not be looked at
+  __device__ __forceinline__ void at_least(float x) { last = fmaxf(last, below(x)); }
+  // the largest x that k or more lanes reach with `top`
+  __device__ __forceinline__ float reached(float top) const {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 64; ++i)
+      n += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top), i)) >= top ? 1 : 0;
+    return group_max<64>(n >= k ? top : kNegInf);
+  }
+  // the next smaller number
+  __device__ __forceinline__ static float below(float x) {
+    const uint32_t u = __float_as_uint(x);
+    if (x == 0.0f) return __uint_as_float(0x80000001u);
+    return x == kNegInf ? x : __uint_as_float(x > 0.0f ? u - 1u : u + 1u);
   }
   // one value a lane, columns in the order of the lanes
   __device__ __forceinline__ void offer(float x, int col) {
@@ -210,26 +348,52 @@ struct Best {
   }
 };
 
-// columns [c0, c1) of a row; c0 a multiple of a piece
+// Columns [c0, c1) of a row; c0 a multiple of a piece.  The next 32 columns a lane
+// are on their way while these are summed.  share: the waves of one row tell each
+// other (in shared) what they have reached (which only spares work: a value below what some
+// wave has top_k values of is none of the row's best).
 template <typename T>
-__device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1, Stats& s, Best& best) {
+__device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1, Stats& s, Best& best,
+                                             bool share, lds_floats shared) {
   typedef Piece<T> P;
-  constexpr int R = 16 / P::N * 2;  // 32 columns a lane at a time
-  const int lane = threadIdx.x & 63;
-  for (int64_t at = c0; at < c1; at += R * 64 * P::N) {
-    float v[R * P::N];
+  constexpr int R = 32 / P::N, TILE = 64 * 32;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  u32x4 next[R];
+  const auto load = [&](int64_t at) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int64_t col = at + (r * 64 + lane) * P::N;
-      P::load(x + col, (int)max((int64_t)0, min(c1 - col, (int64_t)P::N)), v + r * P::N);
+      next[r] = load_piece(x + col, c1 - col);
     }
+  };
+  if (c0 < c1) load(c0);
+  for (int64_t at = c0; at < c1; at += TILE) {
+    float v[32];
+    if (at + TILE <= c1) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) P::widen(next[r], v + r * P::N);
+    } else {
+#pragma unroll
+      for (int r = 0; r < R; ++r) widen_piece<T>(next[r], c1 - at - (r * 64 + lane) * P::N, v + r * P::N);
+    }
+    if (at + TILE < c1) load(at + TILE);
     float top = v[0];
 #pragma unroll
-    for (int i = 1; i < R * P::N; ++i) top = fmaxf(top, v[i]);
+    for (int i = 1; i < 32; ++i) top = fmaxf(top, v[i]);
     add_values(s, top, v);
-    if (__ballot(top > best.last)) {
+    if (best.k > 0) {
+      if (at == c0) best.at_least(best.reached(top));
+      if (share) {
+        float far = shared[0];
 #pragma unroll
-      for (int r = 0; r < R; ++r) best.offer<P::N>(v + r * P::N, (int)(at + (r * 64 + lane) * P::N));
+        for (int w = 1; w < 4; ++w) far = fmaxf(far, shared[w]);
+        best.last = fmaxf(best.last, far);
+      }
+      if (__ballot(top > best.last)) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) best.offer<P::N>(v + r * P::N, (int)(at + (r * 64 + lane) * P::N));
+        if (share && lane == 0) shared[wave] = Best::below(best.last);
+      }
     }
   }
 }
@@ -239,7 +403,7 @@ __device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1,
 // leaves its range's sums and best to k_labels_join.
 template <typename T>
 __global__ __launch_bounds__(256) void k_labels_wide(LabelArgs a) {
-  __shared__ float ls[3][4], lv[4][64];
+  __shared__ float ls[3][4], lv[4][64], reached[4];
   __shared__ int lc[4][64];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t units = a.M * a.parts;
@@ -251,9 +415,15 @@ __global__ __launch_bounds__(256) void k_labels_wide(LabelArgs a) {
     Stats s{kNegInf, 0.0f, 0.0f};
     Best best;
     best.clear(a.top_k);
+    if (a.parts == 4) {
+      if (lane == 0) reached[wave] = kNegInf;
+      __syncthreads();
+    }
+    const Label l = a.parts <= 4 && have ? load_label<T>(a, row) : Label{-1, 0.0f};
     if (have) {
       const int64_t c0 = part * a.range;
-      stream_range<T>(static_cast<const T*>(a.logits) + row * a.ld, c0, min((int64_t)a.C, c0 + a.range), s, best);
+      stream_range<T>(static_cast<const T*>(a.logits) + row * a.ld, c0, min(a.C, c0 + a.range), s, best,
+                      a.parts == 4, (lds_floats)reached);
       s = join_lanes<64>(s);
     }
     if (a.parts > 4) {
@@ -278,10 +448,10 @@ __global__ __launch_bounds__(256) void k_labels_wide(LabelArgs a) {
     }
     if (have && (a.parts == 1 || wave == 0)) {
       const Row r = row_of(s);
-      if (lane == 0) write_row<T>(a, row, r);
+      if (lane == 0) write_row(a, row, r, l);
       if (lane < a.top_k) write_top(a, row, lane, r, best.v, best.c);
     }
-    if (a.parts == 4) __syncthreads();  // the next row's waves write ls, lv and lc
+    if (a.parts == 4) __syncthreads();  // the next row's waves write to the same places
   }
 }
 
@@ -291,6 +461,7 @@ template <typename T>
 __global__ __launch_bounds__(64) void k_labels_join(LabelArgs a) {
   const int lane = threadIdx.x;
   for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
+    const Label l = load_label<T>(a, row);
     Stats s{kNegInf, 0.0f, 0.0f};
     for (int p = lane; p < a.parts; p += 64) {
       const float* q = a.part_stats + (row * a.parts + p) * 3;
@@ -303,12 +474,26 @@ __global__ __launch_bounds__(64) void k_labels_join(LabelArgs a) {
     Best best;
     best.clear(a.top_k);
     const int n = a.parts * a.top_k;
-    for (int i = 0; i < n; i += 64) {
-      const int64_t at = row * n + i + lane;
-      best.offer(i + lane < n ? a.part_value[at] : kNegInf, i + lane < n ? a.part_index[at] : -1);
+    if (n > 0) {
+      // every part's best comes first in it
+      float top = kNegInf;
+      for (int p = lane; p < a.parts; p += 64) top = fmaxf(top, a.part_value[(row * a.parts + p) * a.top_k]);
+      best.at_least(best.reached(top));
+      for (int i = 0; i < n; i += 256) {
+        float x[4];
+        int c[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int e = i + k * 64 + lane;
+          x[k] = e < n ? a.part_value[row * n + e] : kNegInf;
+          c[k] = e < n ? a.part_index[row * n + e] : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) best.offer(x[k], c[k]);
+      }
     }
     const Row r = row_of(s);
-    if (lane == 0) write_row<T>(a, row, r);
+    if (lane == 0) write_row(a, row, r, l);
     if (lane < a.top_k) write_top(a, row, lane, r, best.v, best.c);
   }
 }
@@ -335,6 +520,24 @@ hipError_t launch(LabelArgs a, hipStream_t st) {
   const auto rows = [&](int g) {
     return dim3((unsigned)std::min<int64_t>((a.M + 256 / g - 1) / (256 / g), kMostBlocks));
   };
+  // a lane a row from 16384 rows on: fewer do not fill the card
+  if (a.C <= kLaneC && a.M >= 16384 && a.top_k <= 8) {
+    const dim3 grid((unsigned)std::min<int64_t>((a.M + 255) / 256, kMostBlocks));
+    const auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
+      return hipGetLastError();
+    };
+    switch (a.top_k) {
+      case 0: return go(k_labels_lane<T, 0>);
+      case 1: return go(k_labels_lane<T, 1>);
+      case 2: return go(k_labels_lane<T, 2>);
+      case 3: return go(k_labels_lane<T, 3>);
+      case 4: return go(k_labels_lane<T, 4>);
+      case 5:
+      case 6: return go(k_labels_lane<T, 6>);
+      default: return go(k_labels_lane<T, 8>);
+    }
+  }
   if (a.C <= 8 * P::N) {
     hipLaunchKernelGGL((k_labels_narrow<T, 8>), rows(8), dim3(256), 0, st, a);
   } else if (a.C <= 16 * P::N) {
