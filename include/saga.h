@@ -680,12 +680,12 @@ saga_status saga_block_norm(const saga_block_op* op, saga_cmat block, saga_cmat 
  * logits: M x C (dtype f32 or bf16; 16-byte base and row pitch), 1 <= C <= 2^30.
  * labels: int32[M], with logp: float[M] (both or neither); entropy: float[M],
  * nullable; top_index: int32[M * top_k] and top_logp: float[M * top_k] (both if
- * top_k > 0), 0 <= top_k <= 64.  One of the outputs is required.
+ * top_k > 0), 0 <= top_k <= 32.  One of the outputs is required.
  * Workspace: saga_label_log_probs_workspace_size() bytes (0: none, may be NULL),
  * 256-byte aligned, scratch afterwards, not overlapping any argument.  Calls that
  * share one workspace must be ordered.
  * Errors: SAGA_EINVAL, SAGA_EUNSUPPORTED (C), SAGA_EWORKSPACE, SAGA_EDEVICE. */
-#define SAGA_MAX_TOP 64
+#define SAGA_MAX_TOP 32
 
 saga_status saga_label_log_probs_workspace_size(int32_t dtype, int64_t m, int64_t c, int32_t top_k,
                                                 size_t* bytes);

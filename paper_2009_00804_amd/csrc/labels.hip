@@ -17,7 +17,6 @@ namespace {
 
 constexpr int64_t kMostBlocks = 1 << 20;  // (a grid holds less than 2^32 threads)
 constexpr float kNegInf = -__builtin_huge_valf();
-typedef volatile __attribute__((address_space(3))) float* lds_floats;
 
 // 16-byte piece of a row as it lies in memory, and its values; of those past
 // `left` -inf
@@ -277,86 +276,135 @@ __global__ __launch_bounds__(256) void k_labels_lane(LabelArgs a) {
 }
 
 // --------------------------------------------------------------------------
-// longer rows: a wave streams a range of columns and keeps the best 64 so far
-// one a lane, in order
+// longer rows: a wave streams a range of columns and gathers in LDS what may be
+// among the best.  Every now and then the gathered values are ranked against each
+// other (by value, then column) and the best top_k kept in order; a value has to
+// exceed the last of them from then on.
 // --------------------------------------------------------------------------
-struct Best {
-  float v;     // this lane's entry
-  int c;
-  float last;  // entry top_k - 1: what a value has to exceed
-  int k;
+typedef volatile __attribute__((address_space(3))) float* lds_floats;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) u32x2 lds_pair;
+constexpr int kGather = 128;  // values a wave's list holds: SAGA_MAX_TOP kept ones of four waves
 
-  __device__ __forceinline__ void clear(int top_k) {
-    v = last = top_k > 0 ? kNegInf : __builtin_huge_valf();
-    c = -1;
-    k = top_k;
-  }
-  // x (uniform) > last; equal values are put behind those that are there, so
-  // they have to come in the order of their columns
-  __device__ __forceinline__ void put(float x, int col) {
-    const int lane = threadIdx.x & 63;
-    const int pos = __popcll(__ballot(v >= x));
-    const float uv = __shfl_up(v, 1, 64);
-    const int uc = __shfl_up(c, 1, 64);
-    v = lane < pos ? v : lane == pos ? x : uv;
-    c = lane < pos ? c : lane == pos ? col : uc;
-    last = fmaxf(last, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), k - 1)));
-  }
-  // k or more values are at least x (uniform): smaller ones need not be looked at
-  __device__ __forceinline__ void at_least(float x) { last = fmaxf(last, below(x)); }
-  // the largest x that k or more lanes reach with `top`
-  __device__ __forceinline__ float reached(float top) const {
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < 64; ++i)
-      n += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top), i)) >= top ? 1 : 0;
-    return group_max<64>(n >= k ? top : kNegInf);
-  }
-  // the next smaller number
-  __device__ __forceinline__ static float below(float x) {
-    const uint32_t u = __float_as_uint(x);
-    if (x == 0.0f) return __uint_as_float(0x80000001u);
-    return x == kNegInf ? x : __uint_as_float(x > 0.0f ? u - 1u : u + 1u);
-  }
-  // one value a lane, columns in the order of the lanes
-  __device__ __forceinline__ void offer(float x, int col) {
-    uint64_t hits = __ballot(x > last);
-    while (hits) {
-      const int l = __ffsll((unsigned long long)hits) - 1;
-      hits &= hits - 1;
-      const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l));
-      if (y > last) put(y, __builtin_amdgcn_readlane(col, l));
+// the next smaller number
+__device__ __forceinline__ float below(float x) {
+  const uint32_t u = __float_as_uint(x);
+  if (x == 0.0f) return __uint_as_float(0x80000001u);
+  return x == kNegInf ? x : __uint_as_float(x > 0.0f ? u - 1u : u + 1u);
+}
+// The largest x that k or more lanes reach with `top`: the largest of the lanes
+// left, again and again, while that is fewer steps than counting for every lane.
+__device__ __forceinline__ float reached_by(int k, float top) {
+  if (k <= 16) {
+    for (int n = 0;;) {
+      const float m = group_max<64>(top);
+      const uint64_t have = __ballot(top == m);
+      n += __popcll(have);
+      if (n >= k || m == kNegInf || have == 0) return m;
+      top = top == m ? kNegInf : top;
     }
   }
-  // N values a lane, in consecutive columns
-  template <int N>
-  __device__ __forceinline__ void offer(const float* x, int col) {
-    float top = x[0];
+  int n = 0;
 #pragma unroll
-    for (int j = 1; j < N; ++j) top = fmaxf(top, x[j]);
-    uint64_t hits = __ballot(top > last);
-    while (hits) {
-      const int l = __ffsll((unsigned long long)hits) - 1;
-      hits &= hits - 1;
-      const int c0 = __builtin_amdgcn_readlane(col, l);
+  for (int i = 0; i < 64; ++i)
+    n += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top), i)) >= top ? 1 : 0;
+  return group_max<64>(n >= k ? top : kNegInf);
+}
+
+struct Best {
+  lds_pair* list;  // (value, column): kGather + 4 places of this wave's own
+  int n, k;         // values gathered
+  float last;       // what a value has to exceed
+
+  __device__ __forceinline__ void clear(lds_pair* at, int top_k) {
+    list = at;
+    n = 0;
+    k = top_k;
+    last = top_k > 0 ? kNegInf : __builtin_huge_valf();
+  }
+  // Keeps the best k, in order.  Up to E values a lane; a value's place is the
+  // number of those before it.
+  template <int E>
+  __device__ __forceinline__ void rank() {
+    const int lane = threadIdx.x & 63;
+    float v[E];
+    int c[E], place[E];
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x[j]), l));
-        if (y > last) put(y, c0 + j);
+    for (int e = 0; e < E; ++e) {
+      u32x2 x = {0u, 0u};
+      if (e * 64 + lane < n) x = list[e * 64 + lane];
+      v[e] = __uint_as_float(x.x);
+      c[e] = (int)x.y;
+      place[e] = 0;
+    }
+    if (lane < 4) list[n + lane] = u32x2{__float_as_uint(kNegInf), 0x7fffffffu};  // before nothing
+    asm volatile("" ::: "memory");
+    for (int i = 0; i < n; i += 4) {
+      u32x2 x[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] = list[i + q];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float w = __uint_as_float(x[q].x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) place[e] += w > v[e] || (w == v[e] && (int)x[q].y < c[e]) ? 1 : 0;
       }
+    }
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (e * 64 + lane < n && place[e] < k) list[place[e]] = u32x2{__float_as_uint(v[e]), (uint32_t)c[e]};
+    asm volatile("" ::: "memory");
+  }
+  // keeps the best k; later columns are higher, so a value has to exceed the k-th
+  __device__ __forceinline__ void settle() {
+    if (n <= 64) rank<1>();
+    else rank<kGather / 64>();
+    n = min(n, k);
+    if (n == k) last = fmaxf(last, __uint_as_float(__builtin_amdgcn_readfirstlane(list[k - 1].x)));
+  }
+  // a value a lane, where there is room for all that count
+  __device__ __forceinline__ void add(float x, int col) {
+    const uint64_t m = __ballot(x > last);
+    if (m == 0) return;
+    const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+    if (x > last) list[at] = u32x2{__float_as_uint(x), (uint32_t)col};
+    n += __popcll(m);
+  }
+  // The k best of N values a lane (value i in column col_of(i), ascending with i),
+  // one after another: for tiles of which more count than there is room for, as
+  // where many are equal.
+  template <int N, typename F>
+  __device__ __forceinline__ void add_best(float (&x)[N], F col_of) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll 1
+    for (int r = 0; r < k; ++r) {
+      float best = x[0];
+      int at = 0;
+#pragma unroll
+      for (int i = 1; i < N; ++i)
+        if (x[i] > best) best = x[i], at = i;
+      const float most = group_max<64>(best);
+      if (!(most > last)) break;
+      const uint32_t col = ~group_maxu<64>(best == most ? ~(uint32_t)col_of(at) : 0u);
+      if (lane == 0) list[n] = u32x2{__float_as_uint(most), col};
+      ++n;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if ((uint32_t)col_of(i) == col) x[i] = kNegInf;
     }
   }
 };
 
-// Columns [c0, c1) of a row; c0 a multiple of a piece.  The next 32 columns a lane
-// are on their way while these are summed.  share: the waves of one row tell each
-// other (in shared) what they have reached (which only spares work: a value below what some
-// wave has top_k values of is none of the row's best).
-template <typename T>
-__device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1, Stats& s, Best& best,
-                                             bool share, lds_floats shared) {
+// Columns [c0, c1) of a row, NV values a lane at a time; c0 a multiple of a piece.
+// The next columns are on their way while these are summed.  share: the waves of
+// one row tell each other (in shared) what they have reached (which only spares
+// work: a value below what some wave has top_k values of is none of the row's best).
+template <typename T, int NV>
+__device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1, Stats& s, Best& best, bool share,
+                                             lds_floats shared) {
   typedef Piece<T> P;
-  constexpr int R = 32 / P::N, TILE = 64 * 32;
+  constexpr int R = NV / P::N, TILE = 64 * NV;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   u32x4 next[R];
   const auto load = [&](int64_t at) {
@@ -366,9 +414,10 @@ __device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1,
       next[r] = load_piece(x + col, c1 - col);
     }
   };
+  bool changed = false;
   if (c0 < c1) load(c0);
   for (int64_t at = c0; at < c1; at += TILE) {
-    float v[32];
+    float v[NV];
     if (at + TILE <= c1) {
 #pragma unroll
       for (int r = 0; r < R; ++r) P::widen(next[r], v + r * P::N);
@@ -379,10 +428,11 @@ __device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1,
     if (at + TILE < c1) load(at + TILE);
     float top = v[0];
 #pragma unroll
-    for (int i = 1; i < 32; ++i) top = fmaxf(top, v[i]);
+    for (int i = 1; i < NV; ++i) top = fmaxf(top, v[i]);
     add_values(s, top, v);
     if (best.k > 0) {
-      if (at == c0) best.at_least(best.reached(top));
+      // k lanes reach x: what is smaller need not be gathered
+      if (at == c0) best.last = fmaxf(best.last, below(reached_by(best.k, top)));
       if (share) {
         float far = shared[0];
 #pragma unroll
@@ -390,9 +440,24 @@ __device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1,
         best.last = fmaxf(best.last, far);
       }
       if (__ballot(top > best.last)) {
+        const auto col_of = [&](int i) { return (int)(at + (i / P::N * 64 + lane) * P::N + i % P::N); };
+        int count = 0;
 #pragma unroll
-        for (int r = 0; r < R; ++r) best.offer<P::N>(v + r * P::N, (int)(at + (r * 64 + lane) * P::N));
-        if (share && lane == 0) shared[wave] = Best::below(best.last);
+        for (int i = 0; i < NV; ++i) count += __popcll(__ballot(v[i] > best.last));
+        if (best.n + count <= kGather) {
+#pragma unroll
+          for (int i = 0; i < NV; ++i) best.add(v[i], col_of(i));
+        } else {
+          best.add_best(v, col_of);
+        }
+        asm volatile("" ::: "memory");
+        changed = true;
+      }
+      // ranked after the first columns and the last, and when there are many
+      if (changed && (at == c0 || at + TILE >= c1 || best.n >= min(64, best.k + 24))) {
+        best.settle();
+        changed = false;
+        if (share && lane == 0) shared[wave] = below(best.last);
       }
     }
   }
@@ -401,11 +466,13 @@ __device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1,
 // Workgroup: 4 waves.  parts == 1: four rows, one a wave.  parts == 4: one row,
 // its four ranges joined through LDS.  parts > 4 (a multiple of 4): every wave
 // leaves its range's sums and best to k_labels_join.
-template <typename T>
+template <typename T, int NV>
 __global__ __launch_bounds__(256) void k_labels_wide(LabelArgs a) {
-  __shared__ float ls[3][4], lv[4][64], reached[4];
-  __shared__ int lc[4][64];
+  __shared__ float ls[3][4], reached[4];
+  __shared__ u32x2 lists[4][kGather + 4];
+  __shared__ int ln[4];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  lds_pair* const list = (lds_pair*)lists[wave];
   const int64_t units = a.M * a.parts;
   for (int64_t u0 = blockIdx.x * (int64_t)4; u0 < units; u0 += gridDim.x * (int64_t)4) {
     const int64_t unit = u0 + wave;
@@ -414,7 +481,7 @@ __global__ __launch_bounds__(256) void k_labels_wide(LabelArgs a) {
     const int part = (int)(unit % a.parts);
     Stats s{kNegInf, 0.0f, 0.0f};
     Best best;
-    best.clear(a.top_k);
+    best.clear(list, a.top_k);
     if (a.parts == 4) {
       if (lane == 0) reached[wave] = kNegInf;
       __syncthreads();
@@ -422,43 +489,53 @@ __global__ __launch_bounds__(256) void k_labels_wide(LabelArgs a) {
     const Label l = a.parts <= 4 && have ? load_label<T>(a, row) : Label{-1, 0.0f};
     if (have) {
       const int64_t c0 = part * a.range;
-      stream_range<T>(static_cast<const T*>(a.logits) + row * a.ld, c0, min(a.C, c0 + a.range), s, best,
-                      a.parts == 4, (lds_floats)reached);
+      stream_range<T, NV>(static_cast<const T*>(a.logits) + row * a.ld, c0, min(a.C, c0 + a.range), s, best,
+                          a.parts == 4, (lds_floats)reached);
       s = join_lanes<64>(s);
     }
     if (a.parts > 4) {
       float* p = a.part_stats + unit * 3;
       if (lane == 0) p[0] = s.m, p[1] = s.s, p[2] = s.t;
       if (lane < a.top_k) {
-        a.part_value[unit * a.top_k + lane] = best.v;
-        a.part_index[unit * a.top_k + lane] = best.c;
+        const u32x2 x = lane < best.n ? list[lane] : u32x2{__float_as_uint(kNegInf), 0u};
+        a.part_value[unit * a.top_k + lane] = __uint_as_float(x.x);
+        a.part_index[unit * a.top_k + lane] = (int)x.y;
       }
       continue;
     }
     if (a.parts == 4) {
-      if (lane == 0) ls[0][wave] = s.m, ls[1][wave] = s.s, ls[2][wave] = s.t;
-      lv[wave][lane] = best.v;
-      lc[wave][lane] = best.c;
+      if (lane == 0) ls[0][wave] = s.m, ls[1][wave] = s.s, ls[2][wave] = s.t, ln[wave] = best.n;
       __syncthreads();
       if (wave == 0) {
         s = lane < 4 ? Stats{ls[0][lane], ls[1][lane], ls[2][lane]} : Stats{kNegInf, 0.0f, 0.0f};
         s = join_lanes<64>(s);
-        for (int w = 1; w < 4; ++w) best.offer(lane < a.top_k ? lv[w][lane] : kNegInf, lc[w][lane]);
+        if (a.top_k > 0) {
+          for (int w = 1; w < 4; ++w) {
+            const int n = __builtin_amdgcn_readfirstlane(ln[w]);
+            if (lane < n) list[best.n + lane] = ((lds_pair*)lists[w])[lane];
+            best.n += n;
+          }
+          asm volatile("" ::: "memory");
+          best.settle();
+        }
       }
     }
     if (have && (a.parts == 1 || wave == 0)) {
       const Row r = row_of(s);
       if (lane == 0) write_row(a, row, r, l);
-      if (lane < a.top_k) write_top(a, row, lane, r, best.v, best.c);
+      if (lane < a.top_k) {
+        const u32x2 x = lane < best.n ? list[lane] : u32x2{__float_as_uint(kNegInf), 0u};
+        write_top(a, row, lane, r, __uint_as_float(x.x), (int)x.y);
+      }
     }
     if (a.parts == 4) __syncthreads();  // the next row's waves write to the same places
   }
 }
 
-// a wave joins a row's parts: their columns ascend, and equal values of one part
-// lie in the order of their columns
+// a wave joins a row's parts: their columns ascend
 template <typename T>
 __global__ __launch_bounds__(64) void k_labels_join(LabelArgs a) {
+  __shared__ u32x2 lists[kGather + 4];
   const int lane = threadIdx.x;
   for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
     const Label l = load_label<T>(a, row);
@@ -472,107 +549,111 @@ __global__ __launch_bounds__(64) void k_labels_join(LabelArgs a) {
     }
     s = join_lanes<64>(s);
     Best best;
-    best.clear(a.top_k);
+    best.clear((lds_pair*)lists, a.top_k);
     const int n = a.parts * a.top_k;
     if (n > 0) {
       // every part's best comes first in it
       float top = kNegInf;
       for (int p = lane; p < a.parts; p += 64) top = fmaxf(top, a.part_value[(row * a.parts + p) * a.top_k]);
-      best.at_least(best.reached(top));
+      best.last = fmaxf(best.last, below(reached_by(a.top_k, top)));
       for (int i = 0; i < n; i += 256) {
         float x[4];
         int c[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int e = i + k * 64 + lane;
-          x[k] = e < n ? a.part_value[row * n + e] : kNegInf;
-          c[k] = e < n ? a.part_index[row * n + e] : -1;
+        for (int q = 0; q < 4; ++q) {
+          const int e = i + q * 64 + lane;
+          x[q] = e < n ? a.part_value[row * n + e] : kNegInf;
+          c[q] = e < n ? a.part_index[row * n + e] : -1;
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) best.offer(x[k], c[k]);
+        for (int q = 0; q < 4; ++q) {
+          best.add(x[q], c[q]);
+          asm volatile("" ::: "memory");
+          if (best.n > kGather - 64) best.settle();
+        }
       }
+      best.settle();
     }
     const Row r = row_of(s);
     if (lane == 0) write_row(a, row, r, l);
-    if (lane < a.top_k) write_top(a, row, lane, r, best.v, best.c);
+    if (lane < a.top_k) {
+      const u32x2 x = lane < best.n ? ((lds_pair*)lists)[lane] : u32x2{__float_as_uint(kNegInf), 0u};
+      write_top(a, row, lane, r, __uint_as_float(x.x), (int)x.y);
+    }
   }
 }
 
-// Waves per row: one where rows alone fill the card, a workgroup's four where
-// they do not, and so many workgroups that all CUs have some where there are few.
+// Values a lane takes at a time: 32, fewer where a row has no more.  Waves per row:
+// one where rows alone fill the card, a workgroup's four where they do not, and so
+// many workgroups that all CUs have some where there are few.
 struct Split {
   int parts;
   int64_t range;
 };
-template <typename T>
+inline int values_of(int64_t C) { return C <= 512 ? 8 : 16; }
 Split split_of(int64_t M, int64_t C) {
-  constexpr int64_t tile = 64 * 32;  // columns a wave takes at a time
+  const int64_t tile = 64 * values_of(C);  // columns a wave takes at a time
   const int64_t tiles = (C + tile - 1) / tile;
-  int64_t parts = tiles < 4 ? 1 : 4;
-  if (M < 1024 && tiles > 4) parts = std::min<int64_t>((tiles + 3) / 4, std::max<int64_t>(1, 1024 / M)) * 4;
-  const int64_t per = (tiles + parts - 1) / parts;
-  return Split{(int)parts, per * tile};
+  // four waves a row, more where those are few in all (up to 128, all of whose best
+  // k_labels_join reads: 8 x 262147, top 20: 27 us, with 264 waves a row 39)
+  const int64_t want = tiles < 4 ? 1 : std::min<int64_t>(128, std::max<int64_t>(4, 2048 / M));
+  const int64_t per = (tiles + want - 1) / want, parts = (tiles + per - 1) / per;
+  return Split{(int)(parts > 1 ? (parts + 3) / 4 * 4 : 1), per * tile};
+}
+// Rows a wave or less holds at once, whose top classes come one after another:
+// while that are few
+inline bool is_narrow(int64_t C, int top_k, int piece) {
+  return C <= 8 * piece || (C <= 64 * piece && top_k <= 8);
 }
 
 template <typename T>
 hipError_t launch(LabelArgs a, hipStream_t st) {
   typedef Piece<T> P;
-  const auto rows = [&](int g) {
-    return dim3((unsigned)std::min<int64_t>((a.M + 256 / g - 1) / (256 / g), kMostBlocks));
+  const auto go = [&](auto kernel, int64_t rows_per_wg) {
+    const int64_t blocks = std::min<int64_t>((a.M * a.parts + rows_per_wg - 1) / rows_per_wg, kMostBlocks);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    return hipGetLastError();
   };
+  a.parts = 1;
   // a lane a row from 16384 rows on: fewer do not fill the card
-  if (a.C <= kLaneC && a.M >= 16384 && a.top_k <= 8) {
-    const dim3 grid((unsigned)std::min<int64_t>((a.M + 255) / 256, kMostBlocks));
-    const auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
-      return hipGetLastError();
-    };
-    switch (a.top_k) {
-      case 0: return go(k_labels_lane<T, 0>);
-      case 1: return go(k_labels_lane<T, 1>);
-      case 2: return go(k_labels_lane<T, 2>);
-      case 3: return go(k_labels_lane<T, 3>);
-      case 4: return go(k_labels_lane<T, 4>);
-      case 5:
-      case 6: return go(k_labels_lane<T, 6>);
-      default: return go(k_labels_lane<T, 8>);
-    }
+  if (a.C <= kLaneC && a.M >= 16384 && a.top_k <= 32) {
+    const int k = a.top_k;
+    if (k == 0) return go(k_labels_lane<T, 0>, 256);
+    if (k == 1) return go(k_labels_lane<T, 1>, 256);
+    if (k == 2) return go(k_labels_lane<T, 2>, 256);
+    if (k == 3) return go(k_labels_lane<T, 3>, 256);
+    if (k <= 5) return go(k_labels_lane<T, 5>, 256);
+    if (k <= 8) return go(k_labels_lane<T, 8>, 256);
+    if (k <= 12) return go(k_labels_lane<T, 12>, 256);
+    if (k <= 20) return go(k_labels_lane<T, 20>, 256);
+    return go(k_labels_lane<T, 32>, 256);
   }
-  if (a.C <= 8 * P::N) {
-    hipLaunchKernelGGL((k_labels_narrow<T, 8>), rows(8), dim3(256), 0, st, a);
-  } else if (a.C <= 16 * P::N) {
-    hipLaunchKernelGGL((k_labels_narrow<T, 16>), rows(16), dim3(256), 0, st, a);
-  } else if (a.C <= 32 * P::N) {
-    hipLaunchKernelGGL((k_labels_narrow<T, 32>), rows(32), dim3(256), 0, st, a);
-  } else if (a.C <= 64 * P::N) {
-    hipLaunchKernelGGL((k_labels_narrow<T, 64>), rows(64), dim3(256), 0, st, a);
-  } else {
-    const Split sp = split_of<T>(a.M, a.C);
-    a.parts = sp.parts;
-    a.range = sp.range;
+  if (is_narrow(a.C, a.top_k, P::N)) {
+    if (a.C <= 8 * P::N) return go(k_labels_narrow<T, 8>, 32);
+    if (a.C <= 16 * P::N) return go(k_labels_narrow<T, 16>, 16);
+    if (a.C <= 32 * P::N) return go(k_labels_narrow<T, 32>, 8);
+    return go(k_labels_narrow<T, 64>, 4);
+  }
+  const Split sp = split_of(a.M, a.C);
+  a.parts = sp.parts;
+  a.range = sp.range;
+  if (a.parts > 4) {
     const int64_t units = a.M * a.parts;
-    if (a.parts > 4) {
-      char* ws = static_cast<char*>(a.ws);
-      a.part_stats = reinterpret_cast<float*>(ws);
-      a.part_value = a.part_stats + units * 3;
-      a.part_index = reinterpret_cast<int32_t*>(a.part_value + units * a.top_k);
-    }
-    hipLaunchKernelGGL((k_labels_wide<T>), dim3((unsigned)std::min<int64_t>((units + 3) / 4, kMostBlocks)),
-                       dim3(256), 0, st, a);
-    if (a.parts > 4) {
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
-      hipLaunchKernelGGL((k_labels_join<T>), dim3((unsigned)a.M), dim3(64), 0, st, a);
-    }
+    a.part_stats = static_cast<float*>(a.ws);
+    a.part_value = a.part_stats + units * 3;
+    a.part_index = reinterpret_cast<int32_t*>(a.part_value + units * a.top_k);
   }
+  const hipError_t e = values_of(a.C) == 8 ? go(k_labels_wide<T, 8>, 4) : go(k_labels_wide<T, 16>, 4);
+  if (e != hipSuccess || a.parts <= 4) return e;
+  hipLaunchKernelGGL((k_labels_join<T>), dim3((unsigned)a.M), dim3(64), 0, st, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t labels_workspace_bytes(int dtype, int64_t M, int64_t C, int top_k) {
-  if (M <= 0 || C <= 64 * (dtype == SAGA_BF16 ? 8 : 4)) return 0;
-  const Split sp = dtype == SAGA_BF16 ? split_of<uint16_t>(M, C) : split_of<float>(M, C);
+  if (M <= 0 || is_narrow(C, top_k, dtype == SAGA_BF16 ? 8 : 4)) return 0;
+  const Split sp = split_of(M, C);
   return sp.parts > 4 ? (size_t)M * sp.parts * (3 + 2 * (size_t)top_k) * 4 : 0;
 }
 

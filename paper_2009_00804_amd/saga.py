@@ -29,7 +29,7 @@ SAGA_GEMM_PLAIN, SAGA_GEMM_CONCAT, SAGA_GEMM_GRU = range(3)
 (SAGA_LAYER_GCN, SAGA_LAYER_GAT, SAGA_LAYER_SAGE_POOL, SAGA_LAYER_GATED_GRU, SAGA_LAYER_SAGE_LSTM,
  SAGA_LAYER_RGCN) = range(6)
 SAGA_NORM_NONE, SAGA_NORM_RMS, SAGA_NORM_LAYER = range(3)
-SAGA_MAX_TOP = 64
+SAGA_MAX_TOP = 32
 SAGA_REL_TILE = 128
 SAGA_REL_MAX_RELATIONS = 2048
 
