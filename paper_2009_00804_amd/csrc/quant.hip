@@ -131,6 +131,7 @@ struct Tile {
   static constexpr int PH = KB / 64;                            // products' steps of 64 k
   static constexpr int NP = 4 * NI;                             // 16-byte pieces of a wave's row of sums
   static constexpr int SLOTS = ST * STAGE > NW * 16 * NP ? ST * STAGE : NW * 16 * NP;
+  static_assert(ST == 2 || GROUPS % NW == 0, "a wait counts the same loads on every wave");
   static constexpr int LDS = SLOTS * 16 + (BM + 2 * BN) * 4;
   static constexpr int WPE = 160 * 1024 / LDS * NW / 4;         // waves a SIMD that LDS has room for
   // slot of piece p of row r: the 16 rows of a fragment read fall on all banks

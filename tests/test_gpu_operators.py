@@ -141,7 +141,11 @@ def check_product(got, want, mag, dtype):
 
 SIZES = [(1, 1, 1), (1, 1024, 1000), (2, 100, 70), (7, 602, 41), (16, 16, 16), (33, 17, 5), (31, 127, 32), (128, 128, 128),
          (129, 130, 257), (300, 602, 128), (513, 257, 41), (1000, 64, 33), (70, 4096, 65), (257, 1000, 300),
-         (64, 129, 64), (2000, 15, 129), (9, 5000, 700), (4099, 144, 4096), (3, 40000, 33)]
+         (64, 129, 64), (2000, 15, 129), (9, 5000, 700), (4099, 144, 4096), (3, 40000, 33),
+         # wider and longer than the kernel for few rows takes: every tile shape, fused and not
+         (17003, 130, 13), (17003, 1, 30), (20000, 257, 41), (17100, 602, 128), (16500, 64, 65), (9000, 640, 70),
+         (16390, 641, 100), (17000, 1248, 16), (16400, 1000, 300), (17001, 77, 500), (18000, 1249, 20),
+         (1300, 2100, 11008), (1290, 2048, 11010)]
 
 
 @pytest.mark.parametrize("m,k,n", SIZES)
@@ -163,6 +167,28 @@ def test_product_of_8bit_rows(m, k, n, out):
     check_product(got, want, mag, out)
 
 
+def test_float_product_leaves_what_is_not_its_own():
+    S = lib()
+    g = gen(6)
+    for m, k, n in [(5, 40, 13), (17000, 30, 29), (17001, 200, 75), (9001, 700, 10), (3000, 70, 130)]:
+        x = padded(torch.randint(-127, 128, (m, k), generator=g).float())
+        x[:, 0] = 127.0  # scale 1: the rows hold themselves
+        w = padded(torch.randint(-9, 9, (n, k), generator=g, dtype=torch.int8))
+        ws = torch.ones(n, device=device())
+        for dtype in FLOATS:
+            out = padded(torch.full((m + 2, n), 5.0), dtype, fill=7.0, extra=1)
+            op = S.saga_quant_op(S.SAGA_F32, S.dtype_code(dtype), 0, None)
+            nbytes = S.saga_apply_vertex_quant_workspace_size(op, m, k, n)
+            space = S.workspace(nbytes + 256, device())
+            space.fill_(33)
+            S.saga_apply_vertex_quant(op, S.cmat(x), None, S.cmat(w), ws.data_ptr(), None, S.mat(out, rows=m),
+                                      space.data_ptr() if nbytes else None, nbytes, S.stream_handle())
+            torch.cuda.synchronize()
+            assert torch.equal(out[:m].cpu(), (x.cpu().double() @ w.cpu().double().T).to(dtype))
+            assert bool((out[m:] == 5).all()) and bool((padding_of(out) == 7).all())
+            assert bool((space[nbytes:] == 33).all())
+
+
 @pytest.mark.parametrize("m,k,n", SIZES)
 @pytest.mark.parametrize("dtype", FLOATS)
 def test_product_of_float_rows(m, k, n, dtype):
@@ -180,7 +206,7 @@ def test_product_of_float_rows(m, k, n, dtype):
     check_product(got, want, mag, dtype)
 
 
-@pytest.mark.parametrize("m,n", [(1, 40), (130, 40)])
+@pytest.mark.parametrize("m,n", [(1, 40), (130, 40), (1500, 130)])
 def test_product_sums_reach_31_bits(m, n):
     L = LY()
     k = 131071
@@ -197,7 +223,8 @@ def test_product_leaves_what_is_not_its_own():
     """columns past N and rows past M keep what they held"""
     S = lib()
     g = gen(5)
-    for m, k, n in [(5, 40, 13), (200, 40, 75), (130, 200, 130)]:
+    for m, k, n in [(5, 40, 13), (200, 40, 75), (130, 200, 130), (20000, 40, 13), (17000, 30, 29), (17000, 200, 75),
+                    (3000, 70, 130)]:
         q = padded(torch.randint(-9, 9, (m, k), generator=g, dtype=torch.int8))
         w = padded(torch.randint(-9, 9, (n, k), generator=g, dtype=torch.int8))
         s, ws = torch.ones(m, device=device()), torch.ones(n, device=device())
