@@ -439,11 +439,14 @@ __device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1,
         for (int w = 1; w < 4; ++w) far = fmaxf(far, shared[w]);
         best.last = fmaxf(best.last, far);
       }
-      if (__ballot(top > best.last)) {
+      if (const uint64_t hits = __ballot(top > best.last)) {
         const auto col_of = [&](int i) { return (int)(at + (i / P::N * 64 + lane) * P::N + i % P::N); };
-        int count = 0;
+        int count = __popcll(hits) * NV;  // at most
+        if (best.n + count > kGather) {
+          count = 0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) count += __popcll(__ballot(v[i] > best.last));
+          for (int i = 0; i < NV; ++i) count += __popcll(__ballot(v[i] > best.last));
+        }
         if (best.n + count <= kGather) {
 #pragma unroll
           for (int i = 0; i < NV; ++i) best.add(v[i], col_of(i));
