@@ -400,30 +400,42 @@ struct Best {
 // The next columns are on their way while these are summed.  share: the waves of
 // one row tell each other (in shared) what they have reached (which only spares
 // work: a value below what some wave has top_k values of is none of the row's best).
+// Short rows (NV 8) are loaded 4 bytes a lane, so that all lanes hold some of them.
 template <typename T, int NV>
 __device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1, Stats& s, Best& best, bool share,
                                              lds_floats shared) {
   typedef Piece<T> P;
-  constexpr int R = NV / P::N, TILE = 64 * NV;
+  constexpr int W = NV > 8 ? P::N : 4 / (int)sizeof(T);  // values a load brings a lane
+  constexpr int R = NV / W, TILE = 64 * NV;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  u32x4 next[R];
+  typedef uint32_t words __attribute__((ext_vector_type(W * sizeof(T) / 4)));
+  words next[R];
   const auto load = [&](int64_t at) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int64_t col = at + (r * 64 + lane) * P::N;
-      next[r] = load_piece(x + col, c1 - col);
+      const int64_t col = at + (r * 64 + lane) * W;
+      next[r] = words(0u);
+      if (col < c1) next[r] = *reinterpret_cast<const words*>(x + col);
     }
   };
   bool changed = false;
   if (c0 < c1) load(c0);
   for (int64_t at = c0; at < c1; at += TILE) {
     float v[NV];
-    if (at + TILE <= c1) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) P::widen(next[r], v + r * P::N);
-    } else {
+    for (int r = 0; r < R; ++r) {
+      u32x4 piece = {0u, 0u, 0u, 0u};
+      if constexpr (W == P::N) piece = next[r];
+      else piece[0] = next[r][0];
+      float p[P::N];
+      P::widen(piece, p);
 #pragma unroll
-      for (int r = 0; r < R; ++r) widen_piece<T>(next[r], c1 - at - (r * 64 + lane) * P::N, v + r * P::N);
+      for (int j = 0; j < W; ++j) v[r * W + j] = p[j];
+    }
+    if (at + TILE > c1) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (at + (i / W * 64 + lane) * W + i % W >= c1) v[i] = kNegInf;
     }
     if (at + TILE < c1) load(at + TILE);
     float top = v[0];
@@ -440,7 +452,7 @@ __device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1,
         best.last = fmaxf(best.last, far);
       }
       if (const uint64_t hits = __ballot(top > best.last)) {
-        const auto col_of = [&](int i) { return (int)(at + (i / P::N * 64 + lane) * P::N + i % P::N); };
+        const auto col_of = [&](int i) { return (int)(at + (i / W * 64 + lane) * W + i % W); };
         int count = __popcll(hits) * NV;  // at most
         if (best.n + count > kGather) {
           count = 0;
