@@ -595,11 +595,11 @@ saga_status saga_apply_vertex(const saga_gemm_op* op, saga_cmat a, saga_cmat w,
  * which the call quantises as above (a_scale must be NULL).  w: N x K int8, one
  * channel a row, w_scale[N] (both any values; -128 is allowed).  out: M x N,
  * out_dtype F32 or BF16.  a, w and out: 16-byte base and row pitch, ld below
- * 2^23 for a and w.  1 <= K <= 131071, N >= 1.
+ * 2^23 for a and w.  1 <= K <= 131071, 1 <= N <= 2^28.
  * Workspace: saga_apply_vertex_quant_workspace_size() bytes (0: none, may be
  * NULL), 256-byte aligned, scratch afterwards, not overlapping any argument.
  * Calls that share one workspace must be ordered.
- * Errors: SAGA_EINVAL, SAGA_EUNSUPPORTED (K or ld too large), SAGA_EWORKSPACE,
+ * Errors: SAGA_EINVAL, SAGA_EUNSUPPORTED (K, N or ld too large), SAGA_EWORKSPACE,
  * SAGA_EDEVICE. */
 saga_status saga_quantize_rows(int32_t dtype, saga_cmat x, saga_mat q, float* scale, void* stream);
 
@@ -630,8 +630,8 @@ saga_status saga_apply_vertex_quant(const saga_quant_op* op, saga_cmat a, const 
  *         RMS   v / sqrt(mean(v^2) + eps) * weight + bias
  *         LAYER (v - mean) / sqrt(mean((v - mean)^2) + eps) * weight + bias
  * over the F columns of a row, in float32 (weight, bias: nullable float[F];
- * eps > 0, finite).  z is computed from y as summed, before y is rounded to its
- * type.
+ * eps > 0, finite).  The squares are summed in float32: rows of magnitudes from
+ * 2^60 on overflow.  z is computed from y as summed, before y is rounded to its type.
  * block, gate: M x F, dtype; gate is absent (1) if its ptr is NULL; gate_act is
  * applied to it.  channel_scale: float[F], nullable (1).
  * x (the residual stream): M x F, x_dtype; absent (0) if its ptr is NULL.

@@ -594,7 +594,7 @@ saga_status check_quant_op(const saga_quant_op& op, int64_t m, int64_t k, int64_
   if (op.act < SAGA_ACT_NONE || op.act > SAGA_ACT_TANH) return fail(SAGA_EINVAL, "bad activation");
   if (m < 0 || k <= 0 || n <= 0) return fail(SAGA_EINVAL, "m must be >= 0, k and n > 0");
   if (k > saga::kQuantMaxK) return fail(SAGA_EUNSUPPORTED, "8-bit product: k %lld too large", (long long)k);
-  if (n > INT32_MAX || m > ((int64_t)1 << 40)) return fail(SAGA_EUNSUPPORTED, "8-bit product: m or n too large");
+  if (n > saga::kQuantMaxN || m > ((int64_t)1 << 40)) return fail(SAGA_EUNSUPPORTED, "8-bit product: m or n too large");
   return SAGA_OK;
 }
 

@@ -213,6 +213,7 @@ struct QuantGemmArgs {
   void* out; int64_t ldo;
 };
 constexpr int64_t kQuantMaxK = 131071;      // 128 * 128 k stays below 2^31
+constexpr int64_t kQuantMaxN = 1 << 28;     // its column tiles fit one grid
 constexpr int64_t kQuantMaxLd = 1 << 23;    // a tile's rows within 32-bit offsets
 hipError_t launch_gemm_quant(const QuantGemmArgs& g, hipStream_t st);
 // float rows quantised on the way, without a workspace (where quant_fuses); g.a,

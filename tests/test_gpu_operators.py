@@ -628,6 +628,27 @@ def test_residual_gcn(dtype):
         assert torch.equal(a, b)
 
 
+def test_residual_gcn_captured():
+    """the whole network in a graph, replayed on new features"""
+    L = LY()
+    n, f_in, f = 500, 40, 64
+    gr, _, _ = small_graph(n, 5, 8)
+    net = L.ResidualGCN(gr, deep_weights(f_in, f, 9, 3, 6), res_scale=0.3)
+    x = padded(torch.randn(n, f_in, generator=gen(1)))
+    net(x, top_k=2)
+    torch.cuda.synchronize()
+    gph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gph):
+        got = net(x, top_k=2)
+    for turn in range(3):
+        x.copy_(torch.randn(n, f_in, generator=gen(2 + turn)).to(device()))
+        want = net(x, top_k=2)
+        torch.cuda.synchronize()
+        gph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got[1:], want[1:]))
+
+
 def everything(L, t):
     """one call of each operator on the tensors t"""
     out = [L.quant_linear(t["x"], t["w"], t["ws"], act="tanh")]
@@ -726,3 +747,31 @@ def test_largest_offsets():
     y, z, _ = L.block_norm(x, x, pre="rms", in_place=False)
     y3, z3, _ = L.block_norm(tail.to(device()), tail.to(device()), pre="rms")
     assert torch.equal(y[-3:], y3) and torch.equal(z[-3:], z3)
+
+
+def test_torch_entry_points_refuse():
+    """what the tensors themselves give away, and what the library answers"""
+    S, L = lib(), LY()
+    d = device()
+    x = torch.zeros(4, 32, device=d)
+    w, ws = torch.zeros(8, 32, dtype=torch.int8, device=d), torch.ones(8, device=d)
+    for f in (lambda: L.quant_linear(x.double(), w, ws), lambda: L.quant_linear(x, w.cpu(), ws),
+              lambda: L.quant_linear(x, w[:, :16], ws), lambda: L.quant_linear(x, w, ws[:4]),
+              lambda: L.quant_linear(x, w, ws, out_dtype=torch.float16),
+              lambda: L.quant_linear(x, w, ws, row_scale_deg=torch.ones(4, device=d)),
+              lambda: L.block_norm(x, x[:2]), lambda: L.block_norm(x, x.cpu()),
+              lambda: L.block_norm(x, gate=x.bfloat16()), lambda: L.block_norm(x, in_place=True),
+              lambda: L.block_norm(x, x, pre="rms", pre_weight=torch.ones(31, device=d)),
+              lambda: L.label_log_probs(x, torch.zeros(4, dtype=torch.int64, device=d)),
+              lambda: L.label_log_probs(x.t())):
+        with pytest.raises(ValueError):
+            f()
+    for f in (lambda: L.quant_linear(x, w, ws, x_scale=torch.ones(4, device=d)),          # float rows have no scale
+              lambda: L.quant_linear(x.to(torch.int8), w, ws),                          # 8-bit rows need one
+              lambda: L.quantize_rows(torch.zeros(4, 31, device=d)),                      # 124-byte rows
+              lambda: L.block_norm(x, x, pre="rms", eps=0.0), lambda: L.label_log_probs(x, top_k=33),
+              lambda: L.label_log_probs(x, entropy=False), lambda: L.quantize_rows(x[:1].expand(4, 32)),
+              lambda: L.block_norm(x, x.bfloat16(), pre="rms")):
+        with pytest.raises(S.SagaError):
+            f()
+    torch.cuda.synchronize()

@@ -86,6 +86,7 @@ def test_product_refusals(S):
     call(S.SAGA_EINVAL, "k and n", a=(A, 5, 0, 48))
     call(S.SAGA_EINVAL, "k and n", w=(D, 0, 40, 48))
     call(S.SAGA_EUNSUPPORTED, "too large", a=(A, 5, 131072, 131072), w=(D, 7, 131072, 131072))
+    call(S.SAGA_EUNSUPPORTED, "too large", w=(D, (1 << 28) + 1, 40, 48), out=(F, 5, (1 << 28) + 1, (1 << 28) + 4))
     call(S.SAGA_EUNSUPPORTED, "2^23", a=(A, 5, 40, 1 << 23))
     call(S.SAGA_EUNSUPPORTED, "2^23", w=(D, 7, 40, 1 << 23))
     call(S.SAGA_EINVAL, "shape", w=(D, 7, 41, 48))
@@ -101,16 +102,19 @@ def test_product_refusals(S):
     call(S.SAGA_EINVAL, "overlaps", out=(A, 5, 7, 8))
     call(S.SAGA_EINVAL, "overlaps", out=(D + 64, 5, 7, 8))
     call(S.SAGA_EINVAL, "overlaps", out=(E, 5, 7, 8))
-    # float rows: a workspace, and no scales
+    # float rows: no scales, and a workspace where a kernel of its own quantises them
     call(S.SAGA_EINVAL, "a_scale is for", a_dtype=0)
-    need = S.saga_apply_vertex_quant_workspace_size(S.saga_quant_op(0, 0, 0, None), 5, 40, 7)
-    assert need >= 5 * 48 + 5 * 4
-    call(S.SAGA_EWORKSPACE, "need", a_dtype=0, sa=None)
-    call(S.SAGA_EWORKSPACE, "need", a_dtype=0, sa=None, ws=G, nws=need - 1)
-    call(S.SAGA_EINVAL, "256", a_dtype=0, sa=None, ws=G + 16, nws=need)
-    call(S.SAGA_EINVAL, "overlap", a_dtype=0, sa=None, ws=F, nws=need)
-    call(S.SAGA_EINVAL, "overlap", a_dtype=0, sa=None, ws=A, nws=need)
-    call(S.SAGA_EINVAL, "overlap", a_dtype=0, sa=None, ws=D, nws=need)
+    m, k, n = 2000, 1300, 600
+    big = dict(a_dtype=0, sa=None, a=(A, m, k, 1312), w=(D, n, k, 1312), out=(F, m, n, 608))
+    need = S.saga_apply_vertex_quant_workspace_size(S.saga_quant_op(0, 0, 0, None), m, k, n)
+    assert need >= m * 1312 + m * 4
+    assert S.saga_apply_vertex_quant_workspace_size(S.saga_quant_op(2, 0, 0, None), m, k, n) == 0
+    call(S.SAGA_EWORKSPACE, "need", **big)
+    call(S.SAGA_EWORKSPACE, "need", **big, ws=G, nws=need - 1)
+    call(S.SAGA_EINVAL, "256", **big, ws=G + 16, nws=need)
+    call(S.SAGA_EINVAL, "overlap", **big, ws=F, nws=need)
+    call(S.SAGA_EINVAL, "overlap", **big, ws=A, nws=need)
+    call(S.SAGA_EINVAL, "overlap", **big, ws=D, nws=need)
     with pytest.raises(S.SagaError):
         S.saga_apply_vertex_quant_workspace_size(S.saga_quant_op(0, 0, 0, None), 5, 0, 7)
     assert S.lib().saga_apply_vertex_quant_workspace_size(None, 1, 1, 1, None) == S.SAGA_EINVAL
