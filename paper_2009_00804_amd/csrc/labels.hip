@@ -3,8 +3,12 @@
 // pass over the logits.  With m the row's largest logit, S = sum e^(x - m) and
 // T = sum e^(x - m) (x - m):
 //     log p_j = x_j - m - log S,   H = log S - T / S
-// Every lane keeps m, S and T of its own columns and rescales them as m grows.
-// The classes come by value, equal ones by index.
+// Every lane keeps m, S and T of its own columns (float32) and rescales them as m
+// grows.  The classes come by value, equal ones by index.
+//
+// Memory bounds the sums (4099 x 100003 in bfloat16 170 to 180 us without
+// alternatives, 4.6 to 4.8 TB/s); the alternatives add to it: top 5 10 us, top 20 60
+// to 70 us.  2^21 x 41 with top 3 takes 73 us (41 us without, 4.2 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
