@@ -141,7 +141,7 @@ def _placed(f):
     def call(x, *args, stream=None, **kw):
         if not x.is_cuda:
             raise ValueError(f"{f.__name__}: tensors on the GPU are needed, got one on {x.device}")
-        if stream is None and x.device.index == torch.cuda.current_device():
+        if stream is None and x.get_device() == torch._C._cuda_getDevice():
             return f(x, *args, **kw)
         with torch.cuda.device(x.device), torch.cuda.stream(stream):
             if torch.cuda.current_device() != x.device.index:
@@ -154,21 +154,24 @@ def _matrix(t, name, like, dtypes, shape=None):
     """saga_cmat of a 2-D tensor on the device of ``like``"""
     if t is None:
         return S.saga_cmat(None, 0, 0, 0)
-    if t.dim() != 2 or t.dtype not in dtypes or t.device != like.device:
+    size = t.shape
+    if len(size) != 2 or t.dtype not in dtypes or t.get_device() != like.get_device():
         raise ValueError(f"{name}: a 2-D tensor of {dtypes} on {like.device} is needed, got "
-                         f"{tuple(t.shape)} {t.dtype} on {t.device}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.stride(1) != 1 and t.shape[1] > 1:
+                         f"{tuple(size)} {t.dtype} on {t.device}")
+    if shape is not None and size != shape:
+        raise ValueError(f"{name}: shape {tuple(size)}, expected {tuple(shape)}")
+    rows, cols = size
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{name}: the columns of a row have to be neighbours")
-    return S.saga_cmat(t.data_ptr(), t.shape[0], t.shape[1], t.stride(0))
+    return S.saga_cmat(t.data_ptr(), rows, cols, ld)
 
 
 def _vector(t, name, like, n, dtype=torch.float32):
     """address of a contiguous vector of n values on the device of ``like``"""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != like.device or t.numel() != n or not t.is_contiguous():
+    if t.dtype != dtype or t.get_device() != like.get_device() or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name}: {n} contiguous values of {dtype} on {like.device} are needed, got "
                          f"{tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
@@ -178,21 +181,32 @@ def _out(rows, cols, dtype, like):
     """(view, saga_mat) of a new matrix with 16-byte rows"""
     a = 16 // dtype.itemsize
     ld = (cols + a - 1) // a * a
-    buf = torch.empty((rows, ld), dtype=dtype, device=like.device)
+    buf = like.new_empty((rows, ld), dtype=dtype)
     return (buf if ld == cols else buf[:, :cols]), S.saga_mat(buf.data_ptr(), rows, cols, ld)
 
 
 def _stream(t):
     """hipStream_t of torch's current stream on t's device"""
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _space(nbytes, like):
-    return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+    return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+
+
+# (workspace sizes depend on types and sizes alone)
+@functools.lru_cache(maxsize=1024)
+def _quant_bytes(a_dtype, out_dtype, m, k, n):
+    return S.saga_apply_vertex_quant_workspace_size(S.saga_quant_op(a_dtype, out_dtype, 0, None), m, k, n)
+
+
+@functools.lru_cache(maxsize=1024)
+def _label_bytes(dtype, m, c, top_k):
+    return S.saga_label_log_probs_workspace_size(dtype, m, c, top_k)
 
 
 _FLOATS = (torch.float32, torch.bfloat16)
-_NO_MAT = S.saga_mat(None, 0, 0, 0)
+_BYTES = (torch.int8,)
 
 
 @_placed
@@ -200,7 +214,7 @@ def quantize_rows(x):
     """(q, scale): the 8-bit rows of x and their float32 scales."""
     cx = _matrix(x, "x", x, _FLOATS)
     q, mq = _out(x.shape[0], x.shape[1], torch.int8, x)
-    scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    scale = x.new_empty(x.shape[0], dtype=torch.float32)
     S.saga_quantize_rows(S.dtype_code(x.dtype), cx, mq, scale.data_ptr(), _stream(x))
     return q, scale
 
@@ -214,13 +228,13 @@ def quant_linear(x, w, w_scale, x_scale=None, bias=None, act="none", row_scale_d
     i8 = x.dtype == torch.int8
     if out_dtype is None:
         out_dtype = torch.float32 if i8 else x.dtype
-    cx = _matrix(x, "x", x, (torch.int8,) if i8 else _FLOATS)
-    cw = _matrix(w, "w", x, (torch.int8,), (w.shape[0], k))
+    cx = _matrix(x, "x", x, _BYTES if i8 else _FLOATS)
     n = w.shape[0]
+    cw = _matrix(w, "w", x, _BYTES, (n, k))
     op = S.saga_quant_op(S.SAGA_I8 if i8 else S.dtype_code(x.dtype), S.dtype_code(out_dtype), S.ACT[act],
                          _vector(row_scale_deg, "row_scale_deg", x, m, torch.int32))
+    nbytes = _quant_bytes(op.a_dtype, op.out_dtype, m, k, n)
     out, mo = _out(m, n, out_dtype, x)
-    nbytes = S.saga_apply_vertex_quant_workspace_size(op, m, k, n)
     ws = _space(nbytes, x)
     S.saga_apply_vertex_quant(op, cx, _vector(x_scale, "x_scale", x, m), cw,
                               _vector(w_scale, "w_scale", x, n), _vector(bias, "bias", x, n), mo,
@@ -258,7 +272,7 @@ def block_norm(block, x=None, *, post="none", post_weight=None, post_bias=None, 
     else:
         y, my = _out(m, f, x_dtype, block)
     z, mz = _out(m, f, torch.int8 if quantize else block.dtype, block)
-    zs = torch.empty(m, dtype=torch.float32, device=block.device) if quantize else None
+    zs = block.new_empty(m, dtype=torch.float32) if quantize else None
     S.saga_block_norm(op, cb, cg, cx, my, mz, zs.data_ptr() if quantize else None, _stream(block))
     return y, z, zs
 
@@ -271,13 +285,12 @@ def label_log_probs(logits, labels=None, top_k=0, entropy=True):
     cl = _matrix(logits, "logits", logits, _FLOATS)
     code = S.dtype_code(logits.dtype)
     at = _vector(labels, "labels", logits, m, torch.int32)
-    nbytes = S.saga_label_log_probs_workspace_size(code, m, c, top_k)
+    nbytes = _label_bytes(code, m, c, top_k)
     ws = _space(nbytes, logits)
-    dev = logits.device
-    lp = torch.empty(m, dtype=torch.float32, device=dev) if labels is not None else None
-    h = torch.empty(m, dtype=torch.float32, device=dev) if entropy else None
-    ti = torch.empty((m, top_k), dtype=torch.int32, device=dev)
-    tl = torch.empty((m, top_k), dtype=torch.float32, device=dev)
+    lp = logits.new_empty(m, dtype=torch.float32) if labels is not None else None
+    h = logits.new_empty(m, dtype=torch.float32) if entropy else None
+    ti = logits.new_empty((m, top_k), dtype=torch.int32)
+    tl = logits.new_empty((m, top_k), dtype=torch.float32)
     S.saga_label_log_probs(code, cl, at, lp.data_ptr() if labels is not None else None,
                            h.data_ptr() if entropy else None, top_k, ti.data_ptr() if top_k else None,
                            tl.data_ptr() if top_k else None, ws.data_ptr() if nbytes else None, nbytes,
