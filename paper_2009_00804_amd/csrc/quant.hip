@@ -125,9 +125,9 @@ hipError_t dispatch_rows(const QuantRowsArgs& a, hipStream_t st) {
 // 32768 x 4096 x 4096 takes 510 us, 2150 TOPS: two thirds of what the instruction
 // reaches alone.  The products' units are busy half of the time; the barrier of
 // each stage and the two thirds of the CU's LDS bandwidth that fragments and loads
-// take stand against it.  Short k (40001 x 1024 x 1024 66 to 74 us, 1.2 POPS) is
-// bounded by the first loads and the epilogue of every tile, beside 2504 tiles in
-// 3.3 rounds of 768.
+// take stand against it.  Short k (40001 x 1024 x 1024 68 to 75 us, 1.2 POPS) is
+// bounded by the first loads and the epilogue of every tile, which nothing hides
+// with one workgroup a CU, and by 628 tiles in 2.5 rounds of 256.
 // --------------------------------------------------------------------------
 template <int WM, int WN, int MI, int NI, int KB, int ST>
 struct Tile {
@@ -719,13 +719,14 @@ hipError_t launch_gemm_quant(const QuantGemmArgs& g, hipStream_t st) {
   if (g.N <= 16) return launch_tile<4, 1, 2, 1, 128, 2>(g, st);
   if (g.N <= 32) return launch_tile<4, 1, 2, 2, 128, 2>(g, st);
   if (g.N <= 64) return launch_tile<4, 1, 2, 4, 128, 2>(g, st);
-  // Long k over enough tiles for all CUs: 256 x 256 by 16 waves (us, against 128 x
-  // 128 by four, three workgroups a CU: 32768 x 4096 x 4096 510 / 675, 8192 x 4096
-  // x 4096 129 / 163).  Short k: 128 x 128, whose epilogues run beside another
-  // workgroup's products (40001 x 1024 x 1024 73 / 66, 16384 x 1024 x 4096 102 /
-  // 101).
-  const int64_t large = ((g.M + 255) / 256) * ((g.N + 255) / 256);
-  if (large >= 256 && g.K >= 2048) return launch_tile<4, 4, 4, 4, 64, 4>(g, st);
+  // 256 x 256 by 16 waves, one workgroup a CU, where its tiles fill whole rounds of
+  // the CUs to four fifths (us, against 128 x 128 by four waves, three workgroups a
+  // CU: 32768 x 4096 x 4096 510 / 670, 16384 x 2048 x 1024, one round, 39 / 50, 16384
+  // x 1024 x 4096 96 / 107, 300000 x 128 x 512 117 / 132, 60000 x 600 x 2000 157 / 165,
+  // 40001 x 1024 x 1024, 0.82 of three rounds, 72 / 68 to 75; 5000 x 1024 x 4096, 0.63
+  // of two, 41 / 36; 20000 x 512 x 512, 0.62 of one, 18 / 17).
+  const int64_t large = ((g.M + 255) / 256) * ((g.N + 255) / 256), rounds = (large + 255) / 256;
+  if (large * 5 >= rounds * 256 * 4) return launch_tile<4, 4, 4, 4, 64, 4>(g, st);
   return launch_tile<2, 2, 4, 4, 64, 3>(g, st);
 }
 
