@@ -217,9 +217,12 @@ template <int K> struct TopList<float, K> {
     for (int k = 0; k < K; ++k) v[k] = kNegInf, c[k] = -1;
   }
   __device__ __forceinline__ void offer(float x, int col) {
+    // behind equal values, whose columns are lower; from there on all move by one,
+    // equal ones too
+    bool up = false;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const bool up = x > v[k];  // equal values stay behind those of lower columns
+      up = up || x > v[k];
       const float ov = v[k];
       const int oc = c[k];
       v[k] = up ? x : ov;

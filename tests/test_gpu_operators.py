@@ -527,6 +527,19 @@ def test_labels_many_rows(m, c, k, dtype):
     check_labels(*logits_for(m, c, dtype, m + c), k, dtype)
 
 
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("m,c,ks", [(16400, 41, (1, 2, 3, 5, 8, 12, 20, 32)), (17000, 64, (4, 19, 31)),
+                                    (3000, 60, (7, 32)), (700, 250, (8, 20)), (600, 1000, (10, 32)), (50, 5000, (20,))])
+def test_labels_equal_logits(m, c, ks, dtype):
+    """few distinct values: every place among the best is decided by the column"""
+    g = gen(m + c)
+    x = torch.randint(-4, 5, (m, c), generator=g).float() / 2
+    x[torch.rand(m, c, generator=g) < 0.1] = -float("inf")
+    to = torch.randint(0, c, (m,), generator=g, dtype=torch.int32)
+    for k in ks:
+        check_labels(x.to(dtype), to, k, dtype)
+
+
 def test_labels_some_outputs():
     L = LY()
     x, to = logits_for(20, 600, torch.float32, 1)
