@@ -452,28 +452,29 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(4)
   const int64_t m0 = blockIdx.x * (int64_t)BM;
   char* const lds = reinterpret_cast<char*>(rows);
 
-  // four rows a pass, the next pass's on their way while these are rounded
-  constexpr int PASSES = RW / 4;
-  Raw<T> v[2][U];
+  // four rows a pass, the next pass's on their way while these are rounded (where
+  // their registers have room for both)
+  constexpr int PASSES = RW / 4, NB = sizeof(T) * U <= 20 ? 2 : 1;
+  Raw<T> v[NB][U];
   const auto load_pass = [&](int p) {
     const int64_t m = min(m0 + wave * RW + p * 4 + (lane >> 4), g.M - 1);
     const int col0 = (lane & 15) * 8;
     const T* x = static_cast<const T*>(f.x) + m * f.ldx + col0;
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (u * 128 < K) v[p & 1][u].load(x + u * 128, K - col0 - u * 128);
+      if (u * 128 < K) v[p % NB][u].load(x + u * 128, K - col0 - u * 128);
   };
   load_pass(0);
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
-    if (p + 1 < PASSES) load_pass(p + 1);
+    if (p + 1 < PASSES && NB == 2) load_pass(p + 1);
     const int r = wave * RW + p * 4 + (lane >> 4), col0 = (lane & 15) * 8;
     uint32_t top = 0;
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (u * 128 < K) {
-        v[p & 1][u].clear(K - col0 - u * 128);
-        top = max(top, v[p & 1][u].top());
+        v[p % NB][u].clear(K - col0 - u * 128);
+        top = max(top, v[p % NB][u].top());
       }
     const RowScale s = row_scale(group_maxu<16>(top));
 #pragma unroll
@@ -481,12 +482,13 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(4)
       if (u * 128 < K) {
         const int col = col0 + u * 128;
         float x8[8];
-        v[p & 1][u].widen(x8);
+        v[p % NB][u].widen(x8);
         if (col < pitch * 16) *reinterpret_cast<uint2*>(lds + r * pitch * 16 + col) = round_unit(x8, s);
       }
     }
     if ((lane & 15) == 0)
       scales[r] = s.s * (g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[min(m0 + r, g.M - 1)]) : 1.0f);
+    if (p + 1 < PASSES && NB == 1) load_pass(p + 1);
   }
   __syncthreads();
 
@@ -496,13 +498,9 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(4)
     const int8_t* wr[NI];
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) wr[ni] = g.w + min(n0 + ni * 16 + lr, g.N - 1) * g.ldw + quarter * 16;
-    i32x4 acc[MI][NI], w[kAhead][NI];
-#pragma unroll
-    for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = i32x4{0, 0, 0, 0};
+    i32x4 w[kAhead][NI];
     // (pieces past the rows' end read as 0: what lies behind a row in LDS then does not count)
-    const auto load = [&](int s, i32x4 (&o)[NI]) {
+    const auto load_w = [&](int s, i32x4 (&o)[NI]) {
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni) {
         o[ni] = i32x4{0, 0, 0, 0};
@@ -510,7 +508,12 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(4)
       }
     };
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) load(k, w[k]);
+    for (int k = 0; k < kAhead; ++k) load_w(k, w[k]);
+    i32x4 acc[MI][NI];
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = i32x4{0, 0, 0, 0};
     for (int s0 = 0; s0 < steps; s0 += kAhead) {
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
@@ -524,7 +527,7 @@ __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(4)
             for (int ni = 0; ni < NI; ++ni)
               acc[mi][ni] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[k][ni], a[mi], acc[mi][ni], 0, 0, 0);
         }
-        load(s0 + k + kAhead, w[k]);
+        load_w(s0 + k + kAhead, w[k]);
       }
     }
 #pragma unroll
@@ -566,7 +569,9 @@ hipError_t launch_fused(const QuantFloatArgs& f0, hipStream_t st) {
 }
 // 64 rows by eight waves, each of all rows and 16 columns: w's fragments are loaded
 // once a workgroup (2^20 x 602 x 128 in bfloat16, us: 392; 128 rows 442; 128 rows by
-// 2 x 4 waves, which load them twice, 523; 64 rows by four waves of 32 columns 434).
+// 2 x 4 waves, which load them twice, 523; 64 rows by four waves of 32 columns 434;
+// w's first fragments loaded before the rows 423: their registers cost a workgroup a
+// CU).
 template <typename T, int U>
 hipError_t dispatch_fused(const QuantFloatArgs& f, hipStream_t st) {
   if (f.g.N <= 32) return launch_fused<T, 64, U, 4, 2, 1>(f, st);
@@ -709,6 +714,7 @@ hipError_t launch_quant_fused(int dtype, const QuantFloatArgs& f, hipStream_t st
   if (f.g.M == 0) return hipSuccess;
   const bool bf = dtype == SAGA_BF16;
   if (quant_few_float(f.g.M, f.g.N, f.g.K)) return bf ? launch_few<uint16_t>(f, st) : launch_few<float>(f, st);
+  if (f.g.K <= 128) return bf ? dispatch_fused<uint16_t, 1>(f, st) : dispatch_fused<float, 1>(f, st);
   if (f.g.K <= 640) return bf ? dispatch_fused<uint16_t, 5>(f, st) : dispatch_fused<float, 5>(f, st);
   return bf ? dispatch_fused<uint16_t, 10>(f, st) : dispatch_fused<float, 10>(f, st);
 }
@@ -726,7 +732,13 @@ hipError_t launch_gemm_quant(const QuantGemmArgs& g, hipStream_t st) {
   // 40001 x 1024 x 1024, 0.82 of three rounds, 72 / 68 to 75; 5000 x 1024 x 4096, 0.63
   // of two, 41 / 36; 20000 x 512 x 512, 0.62 of one, 18 / 17).
   const int64_t large = ((g.M + 255) / 256) * ((g.N + 255) / 256), rounds = (large + 255) / 256;
-  if (large * 5 >= rounds * 256 * 4) return launch_tile<4, 4, 4, 4, 64, 4>(g, st);
+  const int64_t cols = (g.N + 127) / 128, rows = (g.M + 127) / 128;
+  // (not where 128-wide tiles leave out a tenth or more of its columns: 2^20 x 602 x
+  // 128 263 / 361)
+  if (large * 5 >= rounds * 256 * 4 && (g.N + 255) / 256 * 20 <= cols * 11) return launch_tile<4, 4, 4, 4, 64, 4>(g, st);
+  // Too few of those for all CUs: 64 x 64, and seven stages on their way instead of
+  // two, as a workgroup's time is its loads' latency (4000 x 4000 x 300 15 / 31).
+  if (cols * rows <= 256) return launch_tile<2, 2, 2, 2, 64, 8>(g, st);
   return launch_tile<2, 2, 4, 4, 64, 3>(g, st);
 }
 
