@@ -692,22 +692,25 @@ hipError_t launch_quantize_rows(const QuantRowsArgs& a, hipStream_t st) {
 }
 
 // Which kernel takes a product (us, measured on bfloat16 or 8-bit rows).
-// k_quant_few while its workgroups and their steps are few: 8-bit rows against
-// 128 x 128 tiles 16 x 4096 x 4096 7 / 17, 64 x 4096 x 4096 18 / 21, 128 x 4096 x
-// 4096 34 / 21, 256 x 1024 x 1024 7 / 12; float rows, which every workgroup
-// quantises again, against two launches 16 x 4096 x 4096 17 / 27, 64 x 4096 x 4096
-// 42 / 31, 256 x 1024 x 1024 13 / 22, 200 x 1000 x 1000 12 / 23.
-bool quant_few(int64_t M, int64_t N, int64_t K, int64_t most) {
+// k_quant_few while its workgroups and their steps are few: 8-bit rows against 64 x
+// 64 tiles 16 x 1024 x 1024 3.5 / 5.2, 1000 x 600 x 100 4.2 / 5.1, 16 x 4096 x 4096
+// 6.9 / 9.1, 64 x 1024 x 1024 6.0 / 5.5, 64 x 4096 x 4096 18 / 10, 2000 x 130 x 300 5.8 /
+// 4.2; float rows, which every workgroup quantises again, against two launches 64 x
+// 1024 x 1024 7.0 / 9.5, 128 x 1024 x 1024 8.1 / 9.1, 256 x 1024 x 1024 13 / 9, 16 x 4096 x
+// 4096 16 / 13.
+bool quant_few(int64_t M, int64_t N, int64_t K, int64_t workgroups, int64_t steps) {
   const int64_t wgs = ((M + 15) / 16) * ((N + 15) / 16);
-  return M <= 16384 && N <= 16384 && wgs <= 1024 && wgs * ((K + 63) / 64) <= most;
+  return M <= 16384 && N <= 16384 && wgs <= workgroups && wgs * ((K + 63) / 64) <= steps;
 }
-bool quant_few_float(int64_t M, int64_t N, int64_t K) { return K <= kFewK && quant_few(M, N, K, 32768); }
-// k_quant_fused while w is narrow, against two launches: 2^18 x 602 x 128 107 / 175,
-// 2000 x 602 x 128 13 / 19, 100000 x 602 x 256 60 / 76, x 512 96 / 106, x 1024 182 /
-// 163; over few rows its sweeps of 128 columns take too long (2000 x 1000 x 512 31 /
-// 24, 512 x 602 x 512 23 / 19).
+bool quant_few_float(int64_t M, int64_t N, int64_t K) { return K <= kFewK && quant_few(M, N, K, 512, 8192); }
+// k_quant_fused while w is narrow, against two launches: 10000 x 602 x 128 14 / 17,
+// 40000 x 602 x 128 24 / 33, 2^18 x 602 x 128 107 / 175, 5000 x 128 x 128 5.5 / 7.4, 16384
+// x 602 x 256 18 / 26, 60000 x 1000 x 512 83 / 87, 100000 x 602 x 1024 182 / 163; over
+// few rows its sweeps of 128 columns, and of long rows the first, take too long
+// (2000 x 1000 x 512 31 / 24, 2000 x 602 x 128 12.5 / 10.4).
 bool quant_fuses(int64_t M, int64_t N, int64_t K) {
-  return quant_few_float(M, N, K) || (K <= kFusedK && (N <= 128 || (N <= 512 && M >= 16384)));
+  if (quant_few_float(M, N, K)) return true;
+  return K <= kFusedK && (N <= 128 ? M >= 4096 || K <= 128 : N <= 512 && M >= 16384);
 }
 
 hipError_t launch_quant_fused(int dtype, const QuantFloatArgs& f, hipStream_t st) {
@@ -721,10 +724,12 @@ hipError_t launch_quant_fused(int dtype, const QuantFloatArgs& f, hipStream_t st
 
 hipError_t launch_gemm_quant(const QuantGemmArgs& g, hipStream_t st) {
   if (g.M == 0) return hipSuccess;
-  if (quant_few(g.M, g.N, g.K, 65536)) return launch_few<int8_t>(QuantFloatArgs{g, nullptr, 0}, st);
-  if (g.N <= 16) return launch_tile<4, 1, 2, 1, 128, 2>(g, st);
-  if (g.N <= 32) return launch_tile<4, 1, 2, 2, 128, 2>(g, st);
-  if (g.N <= 64) return launch_tile<4, 1, 2, 4, 128, 2>(g, st);
+  if (quant_few(g.M, g.N, g.K, 448, 16384)) return launch_few<int8_t>(QuantFloatArgs{g, nullptr, 0}, st);
+  const int64_t cols = (g.N + 127) / 128, rows = (g.M + 127) / 128;
+  // Too few 128 x 128 tiles for all CUs: 64 x 64, and seven stages on their way
+  // instead of two, as a workgroup's time is its loads' latency (4000 x 4000 x 300 15 /
+  // 31).
+  if (cols * rows <= 256) return launch_tile<2, 2, 2, 2, 64, 8>(g, st);
   // 256 x 256 by 16 waves, one workgroup a CU, where its tiles fill whole rounds of
   // the CUs to four fifths (us, against 128 x 128 by four waves, three workgroups a
   // CU: 32768 x 4096 x 4096 510 / 670, 16384 x 2048 x 1024, one round, 39 / 50, 16384
@@ -732,13 +737,12 @@ hipError_t launch_gemm_quant(const QuantGemmArgs& g, hipStream_t st) {
   // 40001 x 1024 x 1024, 0.82 of three rounds, 72 / 68 to 75; 5000 x 1024 x 4096, 0.63
   // of two, 41 / 36; 20000 x 512 x 512, 0.62 of one, 18 / 17).
   const int64_t large = ((g.M + 255) / 256) * ((g.N + 255) / 256), rounds = (large + 255) / 256;
-  const int64_t cols = (g.N + 127) / 128, rows = (g.M + 127) / 128;
   // (not where 128-wide tiles leave out a tenth or more of its columns: 2^20 x 602 x
   // 128 263 / 361)
   if (large * 5 >= rounds * 256 * 4 && (g.N + 255) / 256 * 20 <= cols * 11) return launch_tile<4, 4, 4, 4, 64, 4>(g, st);
-  // Too few of those for all CUs: 64 x 64, and seven stages on their way instead of
-  // two, as a workgroup's time is its loads' latency (4000 x 4000 x 300 15 / 31).
-  if (cols * rows <= 256) return launch_tile<2, 2, 2, 2, 64, 8>(g, st);
+  if (g.N <= 16) return launch_tile<4, 1, 2, 1, 128, 2>(g, st);
+  if (g.N <= 32) return launch_tile<4, 1, 2, 2, 128, 2>(g, st);
+  if (g.N <= 64) return launch_tile<4, 1, 2, 4, 128, 2>(g, st);
   return launch_tile<2, 2, 4, 4, 64, 3>(g, st);
 }
 
