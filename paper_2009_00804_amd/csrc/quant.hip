@@ -580,6 +580,115 @@ hipError_t dispatch_fused(const QuantFloatArgs& f, hipStream_t st) {
 }
 
 // --------------------------------------------------------------------------
+// many short float rows (up to kShortK columns) by a w of up to 128 rows: w's
+// fragments fit a wave's registers, so a workgroup keeps them and takes tile after
+// tile of 64 rows, the next tile's rows on their way while this one is multiplied and
+// stored.  Two LDS buffers in turn: one barrier a tile.  2^20 x 128 x 128 in bfloat16
+// takes 137 us, 3.9 TB/s; the rounding and the stores of few bytes a row bound it
+// (x 40 channels 101 us, 3.5 TB/s).  Consecutive tiles for a workgroup, instead of every
+// 1024th: 142.
+// --------------------------------------------------------------------------
+constexpr int kShortK = 256;
+
+template <typename T, int U, int WM, int WN>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void k_quant_short(QuantFloatArgs f,
+                                                                                           int64_t tiles) {
+  constexpr int BM = 64, MI = BM / 16 / WM, STEPS = U * 2, PITCH = (U * 8) | 1;
+  static_assert(WM * WN == 8 && MI * 16 * WM == BM, "eight waves");
+  __shared__ uint4 rows[2][BM * PITCH + 4];
+  __shared__ float scales[2][BM];
+  const QuantGemmArgs& g = f.g;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int K = (int)g.K, quarter = lane >> 4, lr = lane & 15, wm = wave / WN, wn = wave % WN;
+
+  // (pieces past the rows' end are 0: what lies there in LDS then does not count)
+  const int64_t n = wn * 16 + quarter * 4;
+  const int8_t* const wr = g.w + min((int64_t)wn * 16 + lr, g.N - 1) * g.ldw + quarter * 16;
+  i32x4 w[STEPS];
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) {
+    w[k] = i32x4{0, 0, 0, 0};
+    if (k * 64 + quarter * 16 < K) w[k] = *reinterpret_cast<const i32x4*>(wr + k * 64);
+  }
+  f32x4 tw, tb;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    tw[j] = n + j < g.N ? g.w_scale[n + j] : 0.0f;
+    tb[j] = g.bias && n + j < g.N ? g.bias[n + j] : 0.0f;
+  }
+
+  Raw<T> v[2][U];  // two passes of four rows
+  const int col0 = (lane & 15) * 8;
+  const auto load = [&](int64_t t) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int64_t m = min(t * BM + wave * 8 + p * 4 + quarter, g.M - 1);
+      const T* x = static_cast<const T*>(f.x) + m * f.ldx + col0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[p][u].load(x + u * 128, K - col0 - u * 128);
+    }
+  };
+  int buf = 0;
+  load(blockIdx.x);
+  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x, buf ^= 1) {
+    char* const lds = reinterpret_cast<char*>(rows[buf]);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int r = wave * 8 + p * 4 + quarter;
+      uint32_t top = 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        v[p][u].clear(K - col0 - u * 128);
+        top = max(top, v[p][u].top());
+      }
+      const RowScale s = row_scale(group_maxu<16>(top));
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float x8[8];
+        v[p][u].widen(x8);
+        *reinterpret_cast<uint2*>(lds + r * PITCH * 16 + col0 + u * 128) = round_unit(x8, s);
+      }
+      if (lr == 0)
+        scales[buf][r] =
+            s.s * (g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[min(t * BM + r, g.M - 1)]) : 1.0f);
+    }
+    if (t + gridDim.x < tiles) load(t + gridDim.x);
+    ring_barrier();  // (leaves the loads under way; the other buffer's readers are past the last one)
+    const uint4* const ar = rows[buf] + (wm * MI * 16 + lr) * PITCH + quarter;
+    i32x4 acc[MI];
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) acc[mi] = i32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) {
+      if (k * 64 < K) {
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+          const i32x4 a = *reinterpret_cast<const i32x4*>(ar + mi * 16 * PITCH + k * 4);
+          acc[mi] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[k], a, acc[mi], 0, 0, 0);
+        }
+      }
+    }
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      const int r = (wm * MI + mi) * 16 + lr;
+      if (t * BM + r < g.M && n < g.N) store_quad(g, t * BM + r, n, acc[mi], scales[buf][r], tw, tb);
+    }
+  }
+}
+
+template <typename T, int U>
+hipError_t launch_short(const QuantFloatArgs& f, hipStream_t st) {
+  const int64_t tiles = (f.g.M + 63) / 64;
+  const auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(tiles, 1024)), dim3(512), 0, st, f, tiles);
+    return hipGetLastError();
+  };
+  if (f.g.N <= 32) return go(k_quant_short<T, U, 4, 2>);
+  if (f.g.N <= 64) return go(k_quant_short<T, U, 2, 4>);
+  return go(k_quant_short<T, U, 1, 8>);
+}
+
+// --------------------------------------------------------------------------
 // few rows: 16 of them and 16 channels a workgroup, k divided among its eight
 // waves.  Every workgroup quantises the rows for itself (8-bit rows come straight
 // from memory): reading w over many CUs at once is what counts, and one launch.
@@ -708,6 +817,17 @@ bool quant_few_float(int64_t M, int64_t N, int64_t K) { return K <= kFewK && qua
 // x 602 x 256 18 / 26, 60000 x 1000 x 512 83 / 87, 100000 x 602 x 1024 182 / 163; over
 // few rows its sweeps of 128 columns, and of long rows the first, take too long
 // (2000 x 1000 x 512 31 / 24, 2000 x 602 x 128 12.5 / 10.4).
+// k_quant_short from a tile for each of its 1024 workgroups on, against k_quant_fused: in
+// bfloat16 2^20 x 128 x 128 137 / 159, 2^20 x 100 x 32 93 / 106, 2^20 x 64 x 64 100 / 101,
+// 2^20 x 256 x 128 204 / 219, 65536 x 256 x 128 18.9 / 21.2; in float32 151 / 177, 95 / 98,
+// 89 / 98, 249 / 294, 19.7 / 22.9; 40000 x 256 x 128 15.6 / 14.9 in bfloat16, 14.1 / 16.3 in
+// float32.  Not where float32 rows of up to 128 columns go into output rows with gaps
+// between them, which make their lines' writes partial (2^20 x 128 x 41 153 / 132, x 44
+// 160 / 129, x 9 111 / 104; without gaps x 40 118 / 122; 400000 x 128 x 41 39 / 42, 2^20 x
+// 200 x 41 198 / 227; in bfloat16 2^20 x 128 x 41 108 / 118, x 44 104 / 118).
+bool quant_short(int dtype, const QuantGemmArgs& g) {
+  return g.K <= kShortK && g.N <= 128 && g.M >= 65536 && (dtype == SAGA_BF16 || g.K > 128 || g.ldo == g.N);
+}
 bool quant_fuses(int64_t M, int64_t N, int64_t K) {
   if (quant_few_float(M, N, K)) return true;
   return K <= kFusedK && (N <= 128 ? M >= 4096 || K <= 128 : N <= 512 && M >= 16384);
@@ -717,6 +837,10 @@ hipError_t launch_quant_fused(int dtype, const QuantFloatArgs& f, hipStream_t st
   if (f.g.M == 0) return hipSuccess;
   const bool bf = dtype == SAGA_BF16;
   if (quant_few_float(f.g.M, f.g.N, f.g.K)) return bf ? launch_few<uint16_t>(f, st) : launch_few<float>(f, st);
+  if (quant_short(dtype, f.g)) {
+    if (f.g.K <= 128) return bf ? launch_short<uint16_t, 1>(f, st) : launch_short<float, 1>(f, st);
+    return bf ? launch_short<uint16_t, 2>(f, st) : launch_short<float, 2>(f, st);
+  }
   if (f.g.K <= 128) return bf ? dispatch_fused<uint16_t, 1>(f, st) : dispatch_fused<float, 1>(f, st);
   if (f.g.K <= 640) return bf ? dispatch_fused<uint16_t, 5>(f, st) : dispatch_fused<float, 5>(f, st);
   return bf ? dispatch_fused<uint16_t, 10>(f, st) : dispatch_fused<float, 10>(f, st);

@@ -206,6 +206,44 @@ def test_product_of_float_rows(m, k, n, dtype):
     check_product(got, want, mag, dtype)
 
 
+@pytest.mark.parametrize("m", [65536, 131137])
+@pytest.mark.parametrize("k,n", [(1, 1), (13, 41), (64, 64), (100, 32), (127, 100), (128, 128), (129, 32), (200, 41), (256, 65),
+                                 (256, 128)])
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_product_of_many_short_rows(m, k, n, dtype):
+    """workgroups that take several tiles of rows; a row without a number, one of zeros,
+    the last row alone in its tile, and nothing written around the result"""
+    S = lib()
+    g = gen(m + k * 3 + n)
+    x = torch.randn(m, k, generator=g).to(dtype)
+    x[77], x[m - 3, k // 2] = 0, float("nan")
+    x[1::2] *= 300  # (a row that got a neighbour's scale would show)
+    q, s = rows_exact(torch.nan_to_num(x.double()))
+    w = torch.randint(-127, 128, (n, k), generator=g, dtype=torch.int8)
+    ws = (torch.rand(n, generator=g) + 0.1) / (30000 * k ** 0.5)
+    bias = torch.randn(n, generator=g) if n % 2 else None
+    deg = torch.randint(0, 9, (m,), generator=g, dtype=torch.int32) if k % 2 else None
+    want, mag = product_exact(q, s, w, ws, bias, "none", deg)
+    keep = torch.arange(m) != m - 3
+    wd, wsd = padded(w), ws.to(device())
+    bd, degd = (None if v is None else v.to(device()) for v in (bias, deg))
+    for out_dtype in FLOATS:
+        for extra in (0, 1):
+            xd = padded(x, extra=extra)
+            out = padded(torch.full((m + 70, n), 5.0), out_dtype, fill=7.0, extra=extra)
+            op = S.saga_quant_op(S.dtype_code(dtype), S.dtype_code(out_dtype), 0, None if deg is None else degd.data_ptr())
+            assert S.saga_apply_vertex_quant_workspace_size(op, m, k, n) == 0
+            S.saga_apply_vertex_quant(op, S.cmat(xd), None, S.cmat(wd), wsd.data_ptr(),
+                                      None if bias is None else bd.data_ptr(), S.mat(out, rows=m), None, 0,
+                                      S.stream_handle())
+            torch.cuda.synchronize()
+            assert bool(out[m - 3].isnan().all())
+            check_product(out[:m].cpu()[keep], want[keep], mag[keep], out_dtype)
+            assert bool((out[m:] == 5).all())
+            if out.stride(0) > n:
+                assert bool((padding_of(out) == 7).all())
+
+
 @pytest.mark.parametrize("m,n", [(1, 40), (130, 40), (1500, 130)])
 def test_product_sums_reach_31_bits(m, n):
     L = LY()
