@@ -673,9 +673,11 @@ saga_status saga_block_norm(const saga_block_op* op, saga_cmat block, saga_cmat 
  *     entropy[i]        = -sum_j p_j log p_j
  *     top_index[i, 0..] = the top_k classes by logit, equal logits by class;
  *     top_logp[i, 0..]    their log probabilities
- * in float32: the sums of e^(x - max) are good to a few 2^-24 of themselves, so
- * log p and the entropy are to about 1e-6 of 1 + their magnitude (a row that is
- * certain but for 1e-4 has four digits of its entropy).
+ * With D = sum_j p_j (max - x_j), the sums of e^(x - max) are good to 9 D + 54 units of
+ * 2^-24 of themselves, whatever C (terms are float32, sums over many of them float64):
+ * log p is good to that and a few 2^-24 of its own magnitude, the entropy to 1 + D times
+ * as much.  These are bounds; errors are about 1e-6 of 1 + the values' magnitude, and a row that
+ * is certain but for 1e-4 has four digits of its entropy.
  * A logit of -inf is a class that is not allowed: it has p = 0 and is no
  * alternative.  Where fewer than top_k classes are left the rest has index -1
  * and log probability -inf.  A row with nothing left has logp -inf and entropy

@@ -3,8 +3,9 @@
 // pass over the logits.  With m the row's largest logit, S = sum e^(x - m) and
 // T = sum e^(x - m) (x - m):
 //     log p_j = x_j - m - log S,   H = log S - T / S
-// Every lane keeps m, S and T of its own columns (float32) and rescales them as m
-// grows.  The classes come by value, equal ones by index.
+// Every lane keeps m, S and T of its own columns (terms in float32, sums over many of
+// them in float64) and rescales them as m grows.  The classes come by value, equal ones
+// by index.
 //
 // Memory bounds the sums (4099 x 100003 in bfloat16 170 to 180 us without
 // alternatives, 4.6 to 4.8 TB/s); the alternatives add to it: top 5 10 us, top 20 60
@@ -12,6 +13,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "row_device.h"
 #include "saga_internal.h"
@@ -74,20 +76,61 @@ __device__ __forceinline__ Stats about(const Stats& a, float mm) {
 }
 __device__ __forceinline__ float finite_top(float m) { return m == kNegInf ? 0.0f : m; }
 
-template <int NV>
-__device__ __forceinline__ void add_values(Stats& a, float top, const float (&v)[NV]) {
-  const float m = fmaxf(a.m, top), mm = finite_top(m);
-  Stats b = about(a, mm);
+// S and T of a few values about mm, in N chains of additions
+template <int N>
+struct Chains {
+  float s[N] = {}, t[N] = {};
+  // FIRST: nothing has been added yet
+  template <bool FIRST, int NV>
+  __device__ __forceinline__ void add(float mm, const float (&v)[NV]) {
+    static_assert(NV >= N, "a value for each chain");
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const float d = v[i] - mm, e = __expf(d);
-    b.s += e;
-    b.t = fmaf(e, fmaxf(d, kFar), b.t);
+    for (int i = 0; i < NV; ++i) {
+      const float d = v[i] - mm, e = __expf(d), far = fmaxf(d, kFar);
+      const bool first = FIRST && i < N;
+      s[i % N] = first ? e : s[i % N] + e;
+      t[i % N] = first ? e * far : fmaf(e, far, t[i % N]);
+    }
   }
-  a.s = b.s;
-  a.t = b.t;
-  a.m = m;
-}
+  __device__ __forceinline__ static float total(const float (&x)[N]) {
+    if constexpr (N == 2) return x[0] + x[1];
+    else return (x[0] + x[1]) + (x[2] + x[3]);
+  }
+};
+
+// m, S and T of a lane's columns, tile after tile.  A tile's terms are added in float32.
+// A is what the tiles' sums are held in: float where a row is one tile, else float64
+// (1 to 3 % of the time).  Added one by one to a float32 sum, terms of few distinct values round
+// to one side: rows of 2^18 classes and two values had log S off by 9e-6, of 2^22 by 2e-4.
+template <typename A>
+struct Sums {
+  float m = kNegInf;    // the largest value
+  float ref = kNegInf;  // what s and t are about
+  A s = 0, t = 0;
+
+  template <int NV>
+  __device__ __forceinline__ void add(float top, const float (&v)[NV]) {
+    m = fmaxf(m, top);
+    // Only a clearly larger value moves the sums: one that grows a little in every tile
+    // would round them every time.
+    if (m > ref + 2.0f) {
+      const float d = ref - m, c = __expf(d);
+      t = (A)c * (t + (A)fmaxf(d, kFar) * s);
+      s *= (A)c;
+      ref = m;
+    }
+    Chains<2> f;  // (of at most 8 additions)
+    f.template add<true>(finite_top(ref), v);
+    s += (A)f.total(f.s);
+    t += (A)f.total(f.t);
+  }
+  // over the wave's lanes
+  __device__ __forceinline__ Stats join() const {
+    const float most = group_max<64>(m);
+    const Stats b = about(Stats{ref, (float)s, (float)t}, finite_top(most));
+    return Stats{most, group_sum<64>(b.s), group_sum<64>(b.t)};
+  }
+};
 template <int G>
 __device__ __forceinline__ Stats join_lanes(const Stats& a) {
   const float m = group_max<G>(a.m);
@@ -155,11 +198,10 @@ __global__ __launch_bounds__(256) void k_labels_narrow(LabelArgs a) {
     float top = v[0];
 #pragma unroll
     for (int j = 1; j < P::N; ++j) top = fmaxf(top, v[j]);
-    Stats s{kNegInf, 0.0f, 0.0f};
     const float m = group_max<G>(top);
-    add_values(s, m, v);
-    s = Stats{m, group_sum<G>(s.s), group_sum<G>(s.t)};
-    const Row r = row_of(s);
+    Chains<2> f;
+    f.template add<true>(finite_top(m), v);
+    const Row r = row_of(Stats{m, group_sum<G>(f.total(f.s)), group_sum<G>(f.total(f.t))});
     if (g == 0) write_row(a, row, r, l);
     for (int k = 0; k < a.top_k; ++k) {
       float best = v[0];
@@ -260,21 +302,15 @@ __global__ __launch_bounds__(256) void k_labels_lane(LabelArgs a) {
           best.offer(v[j], p * P::N + j);
         }
       }
-    Stats s{m, 0.0f, 0.0f};
-    const float mm = finite_top(m);
+    Chains<4> f;
 #pragma unroll
     for (int p = 0; p < NP; ++p)
       if (p * P::N < C) {
         float v[P::N];
         widen_piece<T>(raw[p], C - p * P::N, v);
-#pragma unroll
-        for (int j = 0; j < P::N; ++j) {
-          const float d = v[j] - mm, e = __expf(d);
-          s.s += e;
-          s.t = fmaf(e, fmaxf(d, kFar), s.t);
-        }
+        f.template add<false>(finite_top(m), v);
       }
-    const Row r = row_of(s);
+    const Row r = row_of(Stats{m, f.total(f.s), f.total(f.t)});
     write_row(a, row, r, l);
 #pragma unroll
     for (int k = 0; k < K; ++k)
@@ -408,8 +444,8 @@ struct Best {
 // one row tell each other (in shared) what they have reached (which only spares
 // work: a value below what some wave has top_k values of is none of the row's best).
 // Short rows (NV 8) are loaded 4 bytes a lane, so that all lanes hold some of them.
-template <typename T, int NV>
-__device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1, Stats& s, Best& best, bool share,
+template <typename T, int NV, typename A>
+__device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1, Sums<A>& s, Best& best, bool share,
                                              lds_floats shared) {
   typedef Piece<T> P;
   constexpr int W = NV > 8 ? P::N : 4 / (int)sizeof(T);  // values a load brings a lane
@@ -448,7 +484,7 @@ __device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1,
     float top = v[0];
 #pragma unroll
     for (int i = 1; i < NV; ++i) top = fmaxf(top, v[i]);
-    add_values(s, top, v);
+    s.add(top, v);
     if (best.k > 0) {
       // k lanes reach x: what is smaller need not be gathered
       if (at == c0) best.last = fmaxf(best.last, below(reached_by(best.k, top)));
@@ -489,7 +525,7 @@ __device__ __forceinline__ void stream_range(const T* x, int64_t c0, int64_t c1,
 // its four ranges joined through LDS.  parts > 4 (a multiple of 4): every wave
 // leaves its range's sums and best to k_labels_join.
 template <typename T, int NV>
-__global__ __launch_bounds__(256) void k_labels_wide(LabelArgs a) {
+__global__ __launch_bounds__(256, 4) void k_labels_wide(LabelArgs a) {
   __shared__ float ls[3][4], reached[4];
   __shared__ u32x2 lists[4][kGather + 4];
   __shared__ int ln[4];
@@ -511,9 +547,10 @@ __global__ __launch_bounds__(256) void k_labels_wide(LabelArgs a) {
     const Label l = a.parts <= 4 && have ? load_label<T>(a, row) : Label{-1, 0.0f};
     if (have) {
       const int64_t c0 = part * a.range;
-      stream_range<T, NV>(static_cast<const T*>(a.logits) + row * a.ld, c0, min(a.C, c0 + a.range), s, best,
+      Sums<std::conditional_t<(NV > 8), double, float>> sums;  // (8: rows of one tile)
+      stream_range<T, NV>(static_cast<const T*>(a.logits) + row * a.ld, c0, min(a.C, c0 + a.range), sums, best,
                           a.parts == 4, (lds_floats)reached);
-      s = join_lanes<64>(s);
+      s = sums.join();
     }
     if (a.parts > 4) {
       float* p = a.part_stats + unit * 3;

@@ -1,0 +1,66 @@
+"""8-bit products, block norms and label log probabilities at the far ends of what
+their calls allow: long rows, rows without a number, large magnitudes, ordinary
+torch tensors, other streams."""
+import pytest
+import torch
+
+from gpu_util import device
+from test_gpu_operators import FLOATS, LY, U, gen, padded
+
+pytestmark = pytest.mark.gpu
+
+
+# --------------------------------------------------------------------------
+# long rows: the sums' error does not grow with the number of classes
+# --------------------------------------------------------------------------
+def long_rows(c):
+    """rows whose float32 sums go wrong if every term is added to the running sum (few
+    distinct values: all roundings to one side) or if the sum is rescaled often (a
+    largest value that grows all the time)"""
+    g = gen(c)
+    at = torch.arange(c, dtype=torch.float64)
+    two = torch.where(torch.rand(c, generator=g) < 0.1, 0.0, -1.1)
+    one_top = torch.full((c,), -3.3)
+    one_top[c - 7] = 0.5
+    three = torch.tensor([0.0, -0.7, -2.9])[torch.randint(0, 3, (c,), generator=g)]
+    return torch.stack([two, one_top, three, torch.full((c,), 0.3), (at * (8.0 / c) - 4).float(),
+                        (at * (60.0 / c) - 30).float(), (4 - at * (8.0 / c)).float(), torch.randn(c, generator=g) * 3])
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("times,c", [(64, 100003), (64, 1 << 18), (64, 1 << 20), (1, 1 << 20), (1, (1 << 22) + 5)])
+def test_labels_sums_of_long_rows(times, c, dtype):
+    """With D = sum p |x - m| and D2 = sum p (x - m)^2, in units of 2^-24.  The sums are
+    about a value r that is at most 2 below the largest so far.  A term e^(x - r): the
+    difference, its product with log2 e (rounded twice) and the function, 2.3 |x - r| + 4, at
+    most 2.3 |x - m| + 8.6.  A rescaling by e^-d, d >= 2: 2.3 d + 3, at most 3.8 d, over all of a
+    term's steps 3.8 |x - m|.  The joins of lanes, waves and ranges: 2.3 |x - m| again, scale
+    factors of 7.6 (from r to m), 3 and 3, and 22 additions.  A tile's terms are added in
+    float32, 8 additions at most, the tiles' sums in float64 and rounded once.  So S is within
+    9 D + 54 of itself, T within 9 D2 / D + 54; log S adds 3 of its own value, log p another
+    2 of its, and T / S one."""
+    x = long_rows(c).to(dtype)
+    patterns = x.shape[0]
+    m = times * patterns
+    to = (torch.arange(m, dtype=torch.int64) * 7919 % c).int()
+    xd = x.to(device())
+    big = padded(torch.empty(0, c, dtype=dtype))  # (its pitch)
+    big = torch.zeros((m, big.stride(0)), dtype=dtype, device=device())[:, :c]
+    for t in range(times):
+        big[t * patterns:(t + 1) * patterns] = xd
+    got = LY().label_log_probs(big, to.to(device()), top_k=2)
+    logp, ent = (v.double().cpu().view(times, patterns) for v in got[:2])
+    for r in range(patterns):
+        v = x[r].double()
+        d = v - v.max()
+        e = torch.exp(d)
+        s = e.sum()
+        log_s, dist = torch.log(s), -(e * d).sum() / s
+        dist2 = (e * d * d).sum() / s
+        want = (v - v.max() - log_s)[to.view(times, patterns)[:, r].long()]
+        tol = U * (9 * dist + 54 + 3 * log_s + 2 * want.abs() + 1)
+        assert ((logp[:, r] - want).abs() / tol).max() <= 1, (r, (logp[:, r] - want).abs().max() / U)
+        tol = U * ((9 * dist + 54) * (1 + dist) + 9 * dist2 + 54 * dist + 3 * log_s + dist + 2 * (log_s + dist))
+        assert ((ent[:, r] - log_s - dist).abs() / tol).max() <= 1, (r, (ent[:, r] - log_s - dist).abs().max() / U)
+        order = torch.sort(v, descending=True, stable=True).indices[:2]
+        assert bool((got[2].view(times, patterns, 2)[:, r].cpu().long() == order).all()), r
