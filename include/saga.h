@@ -579,7 +579,8 @@ saga_status saga_apply_vertex(const saga_gemm_op* op, saga_cmat a, saga_cmat w,
  *     q_k = x_k / s rounded to the nearest whole number, ties to even
  * so that x_k is about s q_k and |q_k| <= 127.  The quotient is judged exactly:
  * the same row gives the same q and s in every call that quantises.  A row that
- * holds a NaN or an infinity has s = NaN and q = 0 (every result of it is NaN).
+ * holds a NaN or an infinity has s = NaN and q = 0.  Every result of it is NaN, from
+ * SAGA_ACT_RELU too, which takes a NaN to itself here.
  *
  * saga_quantize_rows: x: M x K (dtype f32 or bf16); q: M x K int8 (16-byte base
  * and ld a multiple of 16; columns [K, ld) are not written); scale: float[M].

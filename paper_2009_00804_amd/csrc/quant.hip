@@ -168,8 +168,9 @@ __device__ __forceinline__ void store_quad(const QuantGemmArgs& g, int64_t m, in
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = (float)sum[j] * sa * tw[j] + tb[j];
   if (g.act == SAGA_ACT_RELU) {
+    // (a NaN stays: it is all that is left of a row that held no number)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = v[j] > 0.0f ? v[j] : 0.0f;
+    for (int j = 0; j < 4; ++j) v[j] = v[j] <= 0.0f ? 0.0f : v[j];
   } else if (g.act != SAGA_ACT_NONE) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = apply_act(g.act, v[j]);

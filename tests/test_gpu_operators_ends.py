@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from gpu_util import device
-from test_gpu_operators import FLOATS, LY, U, gen, padded
+from test_gpu_operators import ACTS, FLOATS, LY, U, gen, padded
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +64,36 @@ def test_labels_sums_of_long_rows(times, c, dtype):
         assert ((ent[:, r] - log_s - dist).abs() / tol).max() <= 1, (r, (ent[:, r] - log_s - dist).abs().max() / U)
         order = torch.sort(v, descending=True, stable=True).indices[:2]
         assert bool((got[2].view(times, patterns, 2)[:, r].cpu().long() == order).all()), r
+
+
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("m,k,n", [(7, 100, 50), (70, 1024, 1024), (17000, 602, 41), (17000, 200, 300), (65600, 100, 64),
+                                   (65600, 200, 128), (300, 1400, 600), (20000, 1300, 300)])
+def test_product_rows_without_a_number_in_every_activation(m, k, n, act):
+    """a row that holds a NaN or an infinity answers NaN, whatever the activation, from
+    every kernel: float rows, and the 8-bit rows and scales quantize_rows makes of them"""
+    L = LY()
+    bad = [0, m // 2, m - 1]
+    for dtype in FLOATS:
+        x = torch.randn(m, k, generator=gen(m + k)).to(dtype)
+        for i, v in zip(bad, (float("nan"), float("inf"), -float("inf"))):
+            x[i, (i * 7) % k] = v
+        x = padded(x)
+        w = padded(torch.randint(-9, 9, (n, k), generator=gen(n), dtype=torch.int8))
+        ws = torch.full((n,), 0.01, device=device())
+        q, s = L.quantize_rows(x)
+        for out in FLOATS:
+            for got in (L.quant_linear(x, w, ws, act=act, out_dtype=out),
+                        L.quant_linear(q, w, ws, x_scale=s, act=act, out_dtype=out)):
+                empty = torch.isnan(got)
+                assert empty.all(1).nonzero().flatten().tolist() == bad
+                assert empty.any(1).sum().item() == len(bad)
+
+
+def test_product_relu_of_zeros():
+    """+0 for what is not above 0, from -0 too"""
+    L = LY()
+    x = padded(torch.full((5, 40), -1.0))
+    w = padded(torch.cat([torch.zeros(20, 40), torch.ones(20, 40)]).to(torch.int8))
+    got = L.quant_linear(x, w, torch.full((40,), -0.0, device=device()), act="relu")
+    assert bool((got == 0).all()) and not bool(torch.signbit(got).any())
