@@ -591,7 +591,8 @@ saga_status saga_apply_vertex(const saga_gemm_op* op, saga_cmat a, saga_cmat w,
  * 8-bit rows of a and w, with a scale per vertex and one per channel:
  *     out[i, j] = act(rs_i * (a_scale[i] * w_scale[j] * sum_k a[i, k] w[j, k]) + bias[j])
  * rs_i = row_scale_deg ? (deg[i] > 0 ? deg[i]^-1/2 : 0) : 1.  The sums are exact
- * (32-bit whole numbers), the rest is float32.
+ * (32-bit whole numbers), the rest is float32.  No step overflows where the result
+ * does not; rs_i * a_scale[i] is formed first and has the bits of a float32 (fewer below 2^-126).
  * a: M x K: a_dtype I8: 8-bit rows with a_scale[M]; F32 / BF16: float rows,
  * which the call quantises as above (a_scale must be NULL).  w: N x K int8, one
  * channel a row, w_scale[N] (both any values; -128 is allowed).  out: M x N,

@@ -161,12 +161,24 @@ __device__ __forceinline__ i32x4 mask_bytes(i32x4 v, int left) {
   return v;
 }
 
+constexpr float kLargeScale = 0x1p64f;
+
 // four neighbouring channels n.. of row m: scales, bias, activation, rounding
 __device__ __forceinline__ void store_quad(const QuantGemmArgs& g, int64_t m, int64_t n, i32x4 sum, float sa,
                                            const f32x4& tw, const f32x4& tb) {
   float v[4];
+  // A sum is below 2^31, so its product with a row scale of up to kLargeScale is finite.
+  // A larger one comes last: a result that is finite has no infinite step.
 #pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = (float)sum[j] * sa * tw[j] + tb[j];
+  for (int j = 0; j < 4; ++j) v[j] = (float)sum[j] * sa;
+  if (__builtin_expect(__ballot(fabsf(sa) > kLargeScale) != 0, 0)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      v[j] = fabsf(sa) > kLargeScale ? (float)sum[j] * tw[j] * sa + tb[j] : v[j] * tw[j] + tb[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = v[j] * tw[j] + tb[j];
+  }
   if (g.act == SAGA_ACT_RELU) {
     // (a NaN stays: it is all that is left of a row that held no number)
 #pragma unroll

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from gpu_util import device
-from test_gpu_operators import ACTS, FLOATS, LY, U, gen, padded
+from test_gpu_operators import ACTS, FLOATS, LY, U, gen, padded, product_exact, rows_exact
 
 pytestmark = pytest.mark.gpu
 
@@ -97,3 +97,32 @@ def test_product_relu_of_zeros():
     w = padded(torch.cat([torch.zeros(20, 40), torch.ones(20, 40)]).to(torch.int8))
     got = L.quant_linear(x, w, torch.full((40,), -0.0, device=device()), act="relu")
     assert bool((got == 0).all()) and not bool(torch.signbit(got).any())
+
+
+@pytest.mark.parametrize("m,k,n", [(3, 100, 50), (70, 1024, 1024), (17000, 602, 41), (17000, 200, 300), (65600, 100, 64),
+                                   (65600, 200, 128), (300, 1400, 600), (20000, 1300, 300)])
+def test_product_of_rows_of_large_magnitude(m, k, n):
+    """Finite results are finite and within the product's roundings: large rows (up to
+    3e38) by small weights, whole numbers times the row's scale being past float32, and
+    small rows by large weights."""
+    L = LY()
+    g = gen(m + n)
+    w = torch.randint(-127, 128, (n, k), generator=g, dtype=torch.int8)
+    unit = (torch.rand(n, generator=g) + 0.5) / k
+    deg = torch.randint(0, 9, (m,), generator=g, dtype=torch.int32)
+    for dtype in FLOATS:
+        base = torch.randn(m, k, generator=g).clamp_(-4, 4)
+        for size, weight in ((6e37, 1e-6), (1e34, 1e-3), (1e30, 1.0), (1e-30, 1e30), (1e-34, 1e36), (1.0, 1e30)):
+            x = (base * size).to(dtype)
+            x[m // 2] = base[m // 2].to(dtype)  # an ordinary row between them
+            ws = unit * weight
+            q, s = rows_exact(x.double())
+            want, mag = product_exact(q, s, w, ws, None, "none", deg)
+            assert bool(torch.isfinite(want.float()).all())
+            xd, wd, wsd, degd = padded(x), padded(w), ws.to(device()), deg.to(device())
+            qd, sd = L.quantize_rows(xd)
+            for got in (L.quant_linear(xd, wd, wsd, row_scale_deg=degd, out_dtype=torch.float32),
+                        L.quant_linear(qd, wd, wsd, x_scale=sd, row_scale_deg=degd, out_dtype=torch.float32)):
+                err = (got.double().cpu() - want).abs()
+                # the sum to float32, two scales, the degree's root, quotient and product: seven roundings
+                assert bool((err <= 8 * U * mag + 2.0 ** -149).all()), (size, (err / (U * mag + 1e-45)).max())
