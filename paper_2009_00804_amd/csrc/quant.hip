@@ -180,9 +180,9 @@ __device__ __forceinline__ void store_quad(const QuantGemmArgs& g, int64_t m, in
     for (int j = 0; j < 4; ++j) v[j] = v[j] * tw[j] + tb[j];
   }
   if (g.act == SAGA_ACT_RELU) {
-    // (a NaN stays: it is all that is left of a row that held no number)
+    // (a NaN stays: it is all that is left of a row that held no number; -0 becomes +0)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = v[j] <= 0.0f ? 0.0f : v[j];
+    for (int j = 0; j < 4; ++j) v[j] = __builtin_elementwise_maximum(v[j], 0.0f);
   } else if (g.act != SAGA_ACT_NONE) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = apply_act(g.act, v[j]);
