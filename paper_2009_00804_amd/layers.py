@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import inspect
 
 import torch
 
@@ -137,16 +138,27 @@ def _placed(f):
     """Runs f on its first tensor's device and on ``stream`` (None: torch's
     current stream of that device).  Outputs and workspaces are allocated there,
     so calls on different streams or in different graphs share none."""
+    parameters = inspect.signature(f).parameters
+    first = next(iter(parameters))
+
     @functools.wraps(f)
-    def call(x, *args, stream=None, **kw):
+    def call(*args, stream=None, **kw):
+        if not args and first not in kw:
+            return f(*args, **kw)  # (Python's own TypeError)
+        x = args[0] if args else kw[first]
+        if not isinstance(x, torch.Tensor):
+            raise TypeError(f"{f.__name__}: {first}: a tensor is needed, got {type(x).__name__}")
         if not x.is_cuda:
             raise ValueError(f"{f.__name__}: tensors on the GPU are needed, got one on {x.device}")
         if stream is None and x.get_device() == torch._C._cuda_getDevice():
-            return f(x, *args, **kw)
+            return f(*args, **kw)
         with torch.cuda.device(x.device), torch.cuda.stream(stream):
             if torch.cuda.current_device() != x.device.index:
                 raise ValueError(f"{f.__name__}: the stream belongs to another device than {x.device}")
-            return f(x, *args, **kw)
+            return f(*args, **kw)
+
+    call.__signature__ = inspect.Signature(
+        [*parameters.values(), inspect.Parameter("stream", inspect.Parameter.KEYWORD_ONLY, default=None)])
     return call
 
 

@@ -126,3 +126,23 @@ def test_product_of_rows_of_large_magnitude(m, k, n):
                 err = (got.double().cpu() - want).abs()
                 # the sum to float32, two scales, the degree's root, quotient and product: seven roundings
                 assert bool((err <= 8 * U * mag + 2.0 ** -149).all()), (size, (err / (U * mag + 1e-45)).max())
+
+
+# --------------------------------------------------------------------------
+# the torch entry points
+# --------------------------------------------------------------------------
+def test_arguments_by_name():
+    """the same bits by name as by place"""
+    L = LY()
+    d = device()
+    x, block, gate = (padded(torch.randn(30, 50, generator=gen(i))) for i in range(3))
+    w = padded(torch.randint(-127, 128, (20, 50), generator=gen(4), dtype=torch.int8))
+    ws, to = torch.rand(20, generator=gen(5)).to(d), torch.randint(0, 50, (30,), generator=gen(6), dtype=torch.int32).to(d)
+    q, s = L.quantize_rows(x)
+    for a, b in ((L.quantize_rows(x=x), (q, s)),
+                 ([L.quant_linear(w_scale=ws, w=w, x=x, act="elu")], [L.quant_linear(x, w, ws, act="elu")]),
+                 ([L.quant_linear(x=q, x_scale=s, w=w, w_scale=ws)], [L.quant_linear(q, w, ws, s)]),
+                 (L.block_norm(block=block, x=x, pre="rms", gate=gate)[:2], L.block_norm(block, x, pre="rms", gate=gate)[:2]),
+                 (L.block_norm(block, x=x, pre="rms", quantize=True), L.block_norm(block, x, pre="rms", quantize=True)),
+                 (L.label_log_probs(logits=x, labels=to, top_k=3, entropy=True), L.label_log_probs(x, to, 3, True))):
+        assert len(a) == len(b) and all(torch.equal(g, h) for g, h in zip(a, b))

@@ -229,6 +229,35 @@ def test_tensor_checks():
     assert L._vector(None, "v", x, 4) is None and L._matrix(None, "x", x, ()).ptr is None
 
 
+def test_every_argument_by_its_name():
+    """the torch entry points take each argument by the name that they show"""
+    import inspect
+
+    from paper_2009_00804_amd import layers as L
+
+    x = torch.zeros(4, 16)
+    w, ws = torch.zeros(8, 16, dtype=torch.int8), torch.ones(8)
+    to = torch.zeros(4, dtype=torch.int32)
+    given = {"x": x, "w": w, "w_scale": ws, "x_scale": None, "bias": None, "act": "none", "row_scale_deg": None,
+             "out_dtype": None, "block": x, "post": "none", "post_weight": None, "post_bias": None, "gate": None,
+             "gate_act": "none", "channel_scale": None, "res_scale": 1.0, "pre": "none", "pre_weight": None,
+             "pre_bias": None, "eps": 1e-5, "quantize": False, "in_place": False, "x_dtype": None, "logits": x,
+             "labels": to, "top_k": 2, "entropy": True, "stream": None}
+    for f in (L.quantize_rows, L.quant_linear, L.block_norm, L.label_log_probs):
+        names = list(inspect.signature(f).parameters)
+        assert names[-1] == "stream"
+        with pytest.raises(ValueError, match="on the GPU"):  # (past the binding of the arguments)
+            f(**{n: given[n] for n in names})
+        with pytest.raises(ValueError, match="on the GPU"):
+            f(given[names[0]], **{n: given[n] for n in names[1:]})
+        with pytest.raises(TypeError, match=f"required positional argument.*'{names[0]}'"):
+            f()
+        with pytest.raises(TypeError, match="tensor"):
+            f(3)
+        with pytest.raises(TypeError, match="tensor"):
+            f(**{names[0]: None})
+
+
 @pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"),
                     reason="ROCm toolchain absent")
 def test_refusals_clean_under_asan_and_ubsan():
