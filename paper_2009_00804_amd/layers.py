@@ -137,7 +137,8 @@ def run(layers, x, edge_feat=None, stream=None):
 def _placed(f):
     """Runs f on its first tensor's device and on ``stream`` (None: torch's
     current stream of that device).  Outputs and workspaces are allocated there,
-    so calls on different streams or in different graphs share none."""
+    so calls on different streams or in different graphs share none.  The caller
+    orders ``stream`` with the work before and after, as for torch's own operators."""
     parameters = inspect.signature(f).parameters
     first = next(iter(parameters))
 
@@ -152,10 +153,18 @@ def _placed(f):
             raise ValueError(f"{f.__name__}: tensors on the GPU are needed, got one on {x.device}")
         if stream is None and x.get_device() == torch._C._cuda_getDevice():
             return f(*args, **kw)
+        here = torch.cuda.current_stream(x.device)
         with torch.cuda.device(x.device), torch.cuda.stream(stream):
             if torch.cuda.current_device() != x.device.index:
                 raise ValueError(f"{f.__name__}: the stream belongs to another device than {x.device}")
-            return f(*args, **kw)
+            out = f(*args, **kw)
+        if stream is not None and stream != here:
+            # memory freed by the caller waits for this call, results for the caller's reads
+            for ts, reader in (((*args, *kw.values()), stream), (out if isinstance(out, tuple) else (out,), here)):
+                for t in ts:
+                    if isinstance(t, torch.Tensor):
+                        t.record_stream(reader)
+        return out
 
     call.__signature__ = inspect.Signature(
         [*parameters.values(), inspect.Parameter("stream", inspect.Parameter.KEYWORD_ONLY, default=None)])

@@ -146,3 +146,85 @@ def test_arguments_by_name():
                  (L.block_norm(block, x=x, pre="rms", quantize=True), L.block_norm(block, x, pre="rms", quantize=True)),
                  (L.label_log_probs(logits=x, labels=to, top_k=3, entropy=True), L.label_log_probs(x, to, 3, True))):
         assert len(a) == len(b) and all(torch.equal(g, h) for g, h in zip(a, b))
+
+
+def test_memory_on_another_stream():
+    """What a call on ``stream`` still reads, and what it returned to work on the current
+    stream, is not handed out again while that work is under way"""
+    L = LY()
+    d = device()
+    torch.cuda.synchronize()
+    m, f, n = 400, 512, 256
+    side = torch.cuda.Stream()
+    w = padded(torch.randint(-127, 128, (n, f), generator=gen(1), dtype=torch.int8))
+    ws = torch.rand(n, generator=gen(2)).to(d)
+    host = torch.randn(m, f, generator=gen(3))
+    busy = torch.zeros(4096, 4096, dtype=torch.bfloat16, device=d)
+    sink = torch.empty_like(busy)
+    keep = host.to(d)
+    calls = [lambda x, **kw: (L.quant_linear(x, w, ws, **kw),), lambda x, **kw: (L.quant_linear(x=x, w=w, w_scale=ws, **kw),),
+             lambda x, **kw: L.quantize_rows(x, **kw), lambda x, **kw: L.block_norm(x, x=keep, gate=x, pre="rms", **kw)[:2],
+             lambda x, **kw: L.block_norm(keep, gate=x, pre="rms", **kw)[:2],
+             lambda x, **kw: L.label_log_probs(logits=x, **kw)[1:2]]
+    for call in calls:
+        want = call(keep.clone())
+        call(keep.clone(), stream=side)
+        with torch.cuda.stream(side):
+            torch.mm(busy, busy, out=sink)
+        torch.cuda.synchronize()
+        x = host.to(d)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for _ in range(100):
+                torch.mm(busy, busy, out=sink)
+        got = call(x, stream=side)
+        at = x.untyped_storage().data_ptr()
+        del x
+        others = [torch.empty(m, f, device=d) for _ in range(8)]
+        assert side.query() or at not in [t.untyped_storage().data_ptr() for t in others]
+        del others
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        del got, want
+    # a result, read on the current stream and dropped
+    want = L.quant_linear(keep, w, ws) * 2.0
+    torch.mm(busy, busy, out=sink)
+    torch.cuda.synchronize()
+    got = L.quant_linear(keep, w, ws, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(100):
+        torch.mm(busy, busy, out=sink)
+    total = got * 2.0
+    at = got.untyped_storage().data_ptr()
+    del got
+    with torch.cuda.stream(side):
+        others = [torch.empty(m, n, device=d) for _ in range(8)]
+    assert torch.cuda.current_stream().query() or at not in [t.untyped_storage().data_ptr() for t in others]
+    torch.cuda.synchronize()
+    assert torch.equal(total, want)
+
+
+def test_captured_with_the_stream_argument():
+    """a side stream inside a capture, joined again"""
+    L = LY()
+    d = device()
+    x = padded(torch.randn(40, 96, generator=gen(1)))
+    w = padded(torch.randint(-127, 128, (64, 96), generator=gen(2), dtype=torch.int8))
+    ws = torch.rand(64, generator=gen(3)).to(d)
+    L.quant_linear(x, w, ws)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    gph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gph):
+        side.wait_stream(torch.cuda.current_stream())
+        out = L.quant_linear(x, w, ws, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        top = L.label_log_probs(out, top_k=3)
+    for turn in range(3):
+        x.copy_(torch.randn(40, 96, generator=gen(5 + turn)).to(d))
+        want = L.quant_linear(x, w, ws)
+        tops = L.label_log_probs(want, top_k=3)
+        torch.cuda.synchronize()
+        gph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and all(torch.equal(a, b) for a, b in zip(top[1:], tops[1:]))
