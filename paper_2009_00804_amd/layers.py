@@ -133,6 +133,12 @@ def run(layers, x, edge_feat=None, stream=None):
 
 # --------------------------------------------------------------------------
 # operators of a deep network on torch tensors
+#
+# Matrices are 2-D, on one GPU, each row's columns neighbours; a matrix begins on 16 bytes
+# and its rows lie a multiple of 16 bytes apart (S.padded_empty makes such a buffer, and
+# every matrix returned here is one; a single row needs no pitch).  Others are
+# refused, not copied.  Vectors are contiguous: float32, labels and degrees int32.
+# Errors: ValueError for what the tensors give away, S.SagaError from the library.
 # --------------------------------------------------------------------------
 def _placed(f):
     """Runs f on its first tensor's device and on ``stream`` (None: torch's
@@ -185,6 +191,8 @@ def _matrix(t, name, like, dtypes, shape=None):
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError(f"{name}: the columns of a row have to be neighbours")
+    if rows <= 1:  # no pitch to speak of
+        ld = _whole(cols, t.dtype)
     return S.saga_cmat(t.data_ptr(), rows, cols, ld)
 
 
@@ -198,10 +206,15 @@ def _vector(t, name, like, n, dtype=torch.float32):
     return t.data_ptr()
 
 
+def _whole(cols, dtype):
+    """cols rounded up to whole 16 bytes"""
+    a = 16 // dtype.itemsize
+    return (cols + a - 1) // a * a
+
+
 def _out(rows, cols, dtype, like):
     """(view, saga_mat) of a new matrix with 16-byte rows"""
-    a = 16 // dtype.itemsize
-    ld = (cols + a - 1) // a * a
+    ld = _whole(cols, dtype)
     buf = like.new_empty((rows, ld), dtype=dtype)
     return (buf if ld == cols else buf[:, :cols]), S.saga_mat(buf.data_ptr(), rows, cols, ld)
 

@@ -4,7 +4,7 @@ torch tensors, other streams."""
 import pytest
 import torch
 
-from gpu_util import device
+from gpu_util import device, lib
 from test_gpu_operators import ACTS, FLOATS, LY, U, gen, padded, product_exact, rows_exact
 
 pytestmark = pytest.mark.gpu
@@ -228,3 +228,44 @@ def test_captured_with_the_stream_argument():
         gph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and all(torch.equal(a, b) for a, b in zip(top[1:], tops[1:]))
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("k", [1, 5, 41, 602, 5001])
+def test_single_and_no_rows_as_they_come(k, dtype):
+    """one row of any width, from the first or in the middle of a vector, and no row"""
+    L = LY()
+    d = device()
+    n = 21
+    flat = torch.randn(64 + k, generator=gen(k)).to(dtype).to(d)
+    x, block, gate = flat[:k][None], flat[16:16 + k].unsqueeze(0), flat[32:32 + k].view(1, k)
+    w = padded(torch.randint(-127, 128, (n, k), generator=gen(4), dtype=torch.int8))
+    ws, one = torch.rand(n, generator=gen(5)).to(d), torch.rand(1, generator=gen(6)).to(d)
+    to = torch.zeros(1, dtype=torch.int32, device=d)
+    wide, wb, wg = padded(x), padded(block), padded(gate)
+    q, s = L.quantize_rows(x)
+    byte = torch.randint(-127, 128, (1, k), generator=gen(7), dtype=torch.int8).to(d)  # w of one channel
+    for a, b in ((L.quantize_rows(x), L.quantize_rows(wide)),
+                 ([L.quant_linear(x, w, ws)], [L.quant_linear(wide, w, ws)]),
+                 ([L.quant_linear(q, w, ws, s)], [L.quant_linear(wide, w, ws, out_dtype=torch.float32)]),
+                 ([L.quant_linear(x, byte, one)], [L.quant_linear(wide, padded(byte), one)]),
+                 (L.block_norm(block, x, gate=gate, post="layer", pre="rms", quantize=True),
+                  L.block_norm(wb, wide, gate=wg, post="layer", pre="rms", quantize=True)),
+                 (L.label_log_probs(x, to, 4), L.label_log_probs(wide, to, 4))):
+        assert all(torch.equal(g.nan_to_num(3.0), h.nan_to_num(3.0)) for g, h in zip(a, b))
+    # in place: nothing behind the row is written
+    rest = flat[k:].clone()
+    y, z, _ = L.block_norm(wb, x, pre="rms", in_place=True)
+    y2, z2, _ = L.block_norm(wb, wide, pre="rms")
+    assert y.data_ptr() == x.data_ptr() and torch.equal(y, y2) and torch.equal(z, z2)
+    assert torch.equal(flat[k:], rest)
+    # no rows
+    none = torch.empty(0, k, dtype=dtype, device=d)
+    assert L.quantize_rows(none)[0].shape == (0, k) and L.quant_linear(none, w, ws).shape == (0, n)
+    assert L.block_norm(none, none, pre="rms")[1].shape == (0, k)
+    assert L.label_log_probs(none, top_k=2)[2].shape == (0, 2)
+    # more rows have a pitch, and it is checked
+    two = torch.empty(2 * k, dtype=dtype, device=d).view(2, k)
+    if k % (16 // dtype.itemsize):
+        with pytest.raises(lib().SagaError, match="multiple of 16"):
+            L.quantize_rows(two)

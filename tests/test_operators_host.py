@@ -258,6 +258,20 @@ def test_every_argument_by_its_name():
             f(**{names[0]: None})
 
 
+def test_a_single_row_has_no_pitch():
+    from paper_2009_00804_amd import layers as L
+
+    for t in (torch.zeros(1, 41), torch.zeros(41)[None], torch.zeros(41, 1).t(), torch.zeros(0, 41), torch.zeros(9, 41)[4:5]):
+        m = L._matrix(t, "x", t, (torch.float32,))
+        assert (m.rows, m.cols, m.ld) == (t.shape[0], 41, 44)
+    t = torch.zeros(1, 41, dtype=torch.bfloat16)
+    assert L._matrix(t, "x", t, (torch.bfloat16,)).ld == 48
+    t = torch.zeros(2, 41)
+    assert L._matrix(t, "x", t, (torch.float32,)).ld == 41  # (which the library refuses)
+    with pytest.raises(ValueError, match="neighbours"):
+        L._matrix(torch.zeros(1, 82)[:, ::2], "x", t, (torch.float32,))
+
+
 @pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"),
                     reason="ROCm toolchain absent")
 def test_refusals_clean_under_asan_and_ubsan():
