@@ -139,6 +139,9 @@ def run(layers, x, edge_feat=None, stream=None):
 # every matrix returned here is one; a single row needs no pitch).  Others are
 # refused, not copied.  Vectors are contiguous: float32, labels and degrees int32.
 # Errors: ValueError for what the tensors give away, S.SagaError from the library.
+#
+# Inference only, as the library: results have no history, whether the inputs require
+# grad or not.
 # --------------------------------------------------------------------------
 def _placed(f):
     """Runs f on its first tensor's device and on ``stream`` (None: torch's
@@ -302,12 +305,16 @@ def block_norm(block, x=None, *, post="none", post_weight=None, post_bias=None, 
     if in_place:
         if x is None:
             raise ValueError("in_place: there is no x")
+        if x.requires_grad and torch.is_grad_enabled():
+            raise ValueError("in_place: x requires grad, and no gradient passes through this call")
         y, my = x, S.saga_mat(cx.ptr, cx.rows, cx.cols, cx.ld)
     else:
         y, my = _out(m, f, x_dtype, block)
     z, mz = _out(m, f, torch.int8 if quantize else block.dtype, block)
     zs = block.new_empty(m, dtype=torch.float32) if quantize else None
     S.saga_block_norm(op, cb, cg, cx, my, mz, zs.data_ptr() if quantize else None, _stream(block))
+    if in_place:  # (a backward pass that saved x sees that it has changed)
+        torch.autograd.graph.increment_version(x)
     return y, z, zs
 
 

@@ -269,3 +269,30 @@ def test_single_and_no_rows_as_they_come(k, dtype):
     if k % (16 // dtype.itemsize):
         with pytest.raises(lib().SagaError, match="multiple of 16"):
             L.quantize_rows(two)
+
+
+def test_no_gradients():
+    """inference only: results without history, x in place neither part of a graph nor
+    changed behind a graph's back"""
+    L = LY()
+    x, block = (padded(torch.randn(6, 24, generator=gen(i))) for i in range(2))
+    want = L.block_norm(block, x, pre="rms")
+    leaf = block.detach().clone().requires_grad_()
+    got = L.block_norm(leaf, x, pre="rms")
+    assert not got[0].requires_grad and not got[1].requires_grad and torch.equal(got[0], want[0])
+    assert not L.label_log_probs(leaf)[1].requires_grad and not L.quantize_rows(leaf)[1].requires_grad
+    for t in (x.clone().requires_grad_(), x.clone().requires_grad_() * 1.0):
+        with pytest.raises(ValueError, match="requires grad"):
+            L.block_norm(block, t, pre="rms", in_place=True)
+        assert torch.equal(t, x)
+        with torch.no_grad():
+            assert torch.equal(L.block_norm(block, t, pre="rms", in_place=True)[0], want[0])
+    scale = torch.ones(24, device=x.device, requires_grad=True)
+    t = x.clone()
+    out = (t * scale).sum()  # its backward pass needs t
+    L.block_norm(block, t, pre="rms", in_place=True)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.backward()
+    with torch.inference_mode():
+        t = x.clone()
+        assert torch.equal(L.block_norm(block, t, pre="rms", in_place=True)[0], want[0])
