@@ -296,3 +296,22 @@ def test_no_gradients():
     with torch.inference_mode():
         t = x.clone()
         assert torch.equal(L.block_norm(block, t, pre="rms", in_place=True)[0], want[0])
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "elu", "sigmoid", "tanh"])
+def test_gates_to_their_last_places(act):
+    """Gates alone (y = act(gate)), relative to their own size, in units of 2^-24.  e^x by
+    the card's exponential: 2.3 |x| + 4 (argument, its product with log2 e, the function), a
+    reciprocal 2, an addition 1.  sigmoid: 2.3 |x| + 7.  tanh from 0.3 on, q = 2 / (e^2x + 1): a
+    share e / (e + 1) of 4.6 |x| + 4, and 3 more, times q, over tanh x: at x = -0.3, where q is
+    largest, (0.35 * 5.4 + 3) * 1.29 / 0.29 = 22, and 2 for the last difference over 0.29: 29
+    in all; falling from there on both sides; below, four multiply-adds and the term left
+    out (0.9): 6.  ELU: expm1f, 4.  What is below 2^-126 may be 0."""
+    L = LY()
+    sizes = torch.cat([torch.logspace(-8, 0, 3000), torch.linspace(0.25, 0.35, 2000), torch.linspace(1, 100, 3193)])
+    g = torch.cat([sizes, -sizes]).view(2, 8193)[:, :8192].contiguous()
+    y, _, _ = L.block_norm(torch.ones(2, 8192, device=device()), gate=g.to(device()), gate_act=act)
+    want = ACTS[act](g.double())
+    units = {"none": 0, "relu": 0, "elu": 4, "sigmoid": 7, "tanh": 32}[act] + (2.3 * g.double().abs() if act == "sigmoid" else 0)
+    err = (y.double().cpu() - want).abs()
+    assert bool((err <= U * units * want.abs() + 2.0 ** -126).all()), (err / (U * want.abs() + 1e-45)).max()
