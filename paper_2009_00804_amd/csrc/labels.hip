@@ -642,9 +642,9 @@ __global__ __launch_bounds__(64) void k_labels_join(LabelArgs a) {
   }
 }
 
-// Values a lane takes at a time: 32, fewer where a row has no more.  Waves per row:
-// one where rows alone fill the card, a workgroup's four where they do not, and so
-// many workgroups that all CUs have some where there are few.
+// Values a lane takes at a time: 16, 8 where a row has no more than 512.  Waves per row:
+// one where a row is less than four tiles, else a workgroup's four, and so many workgroups
+// that all CUs have some where there are few rows.
 struct Split {
   int parts;
   int64_t range;
@@ -675,7 +675,8 @@ hipError_t launch(LabelArgs a, hipStream_t st) {
   };
   a.parts = 1;
   // a lane a row from 16384 rows on: fewer do not fill the card
-  if (a.C <= kLaneC && a.M >= 16384 && a.top_k <= 32) {
+  static_assert(SAGA_MAX_TOP == 32, "the last list holds them");
+  if (a.C <= kLaneC && a.M >= 16384) {
     const int k = a.top_k;
     if (k == 0) return go(k_labels_lane<T, 0>, 256);
     if (k == 1) return go(k_labels_lane<T, 1>, 256);
