@@ -37,7 +37,8 @@
  * Conventions (all entry points):
  *   - Every pointer argument except the host-side structs (saga_plan_opts,
  *     saga_plan, saga_rel_plan, saga_edge_op, saga_edge_inputs, saga_gemm_op,
- *     saga_layer_desc) is a DEVICE pointer.  The caller allocates, owns and
+ *     saga_quant_op, saga_norm_desc, saga_block_op, saga_layer_desc) is a DEVICE
+ *     pointer.  The caller allocates, owns and
  *     frees all device memory; the library allocates nothing, ever.  Scratch
  *     space comes from a caller-provided workspace whose size the matching
  *     *_workspace_size call reports.
@@ -45,8 +46,8 @@
  *     Feature matrices must have a 16-byte-aligned base and ld*elem_size a
  *     multiple of 16 bytes; columns [cols, ld) are never read as data and
  *     never written.
- *   - float32 ("f32") or bfloat16 ("bf16") storage; accumulation is always
- *     float32.  Biases, attention vectors, gate weights and degree scalings
+ *   - float32 ("f32") or bfloat16 ("bf16") storage, 8-bit rows where a call
+ *     names them; accumulation is float32 or wider.  Biases, attention vectors, gate weights and degree scalings
  *     are float32.
  *   - All work is enqueued on `stream` (a hipStream_t; NULL = the null
  *     stream) and is asynchronous.  The returned status covers argument
@@ -633,7 +634,8 @@ saga_status saga_apply_vertex_quant(const saga_quant_op* op, saga_cmat a, const 
  *         LAYER (v - mean) / sqrt(mean((v - mean)^2) + eps) * weight + bias
  * over the F columns of a row, in float32 (weight, bias: nullable float[F];
  * eps > 0, finite).  The squares are summed in float32: rows of magnitudes from
- * 2^60 on overflow.  z is computed from y as summed, before y is rounded to its type.
+ * 2^60 on overflow.  LAYER's mean is a float32 too, good to a few 2^-24 of the row's
+ * mean magnitude: what that is to sqrt(variance + eps) shows in the result.  z is computed from y as summed, before y is rounded to its type.
  * block, gate: M x F, dtype; gate is absent (1) if its ptr is NULL; gate_act is
  * applied to it.  channel_scale: float[F], nullable (1).
  * x (the residual stream): M x F, x_dtype; absent (0) if its ptr is NULL.
@@ -683,7 +685,8 @@ saga_status saga_block_norm(const saga_block_op* op, saga_cmat block, saga_cmat 
  * A logit of -inf is a class that is not allowed: it has p = 0 and is no
  * alternative.  Where fewer than top_k classes are left the rest has index -1
  * and log probability -inf.  A row with nothing left has logp -inf and entropy
- * 0; a row with a NaN or +inf has NaN for all, and indices -1.
+ * 0; a row with a NaN or +inf has NaN for all (logp of an unknown label stays 0),
+ * and indices -1.
  * logits: M x C (dtype f32 or bf16; 16-byte base and row pitch), 1 <= C <= 2^30.
  * labels: int32[M], with logp: float[M] (both or neither); entropy: float[M],
  * nullable; top_index: int32[M * top_k] and top_logp: float[M * top_k] (both if

@@ -7,9 +7,10 @@
 // them in float64) and rescales them as m grows.  The classes come by value, equal ones
 // by index.
 //
-// Memory bounds the sums (4099 x 100003 in bfloat16 170 to 180 us without
-// alternatives, 4.6 to 4.8 TB/s); the alternatives add to it: top 5 10 us, top 20 60
-// to 70 us.  2^21 x 41 with top 3 takes 73 us (41 us without, 4.2 TB/s).
+// Memory bounds the sums (4099 x 100003 in bfloat16 147 to 158 us without alternatives, 5.2
+// to 5.6 TB/s), vector instructions what the alternatives add: top 3 15 us, top 10 40, top 20 85,
+// where they are issued in four fifths of the cycles.  2^21 x 41 with top 3 takes 68 to 73
+// us (40 us without, 4.3 TB/s), as much of it vector instructions.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

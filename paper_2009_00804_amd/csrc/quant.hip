@@ -20,8 +20,9 @@ constexpr int64_t kMostBlocks = 1 << 20;  // (a grid holds less than 2^32 thread
 
 // --------------------------------------------------------------------------
 // float rows to 8-bit rows: a row is read once into registers, its largest
-// magnitude taken over its lanes, and rounded from there.  Memory bounds it (100000
-// x 602 in bfloat16 32 us, 5.6 TB/s; 2^18 x 602 96 us, 4.9 TB/s).
+// magnitude taken over its lanes, and rounded from there.  Memory bounds it (2^20 x 602
+// in bfloat16 391 us, 4.9 TB/s, in float32 675 us, 4.7 TB/s; 100000 x 602 34 and 67 us).
+// Past 8192 columns a row is read twice (8000 x 12000 in bfloat16 75 us, 3.8 TB/s).
 // --------------------------------------------------------------------------
 template <typename T, int G, int U>
 __global__ __launch_bounds__(RowGroup<G>::THREADS) void k_quantize_rows(QuantRowsArgs a) {
@@ -127,7 +128,8 @@ hipError_t dispatch_rows(const QuantRowsArgs& a, hipStream_t st) {
 // each stage and the two thirds of the CU's LDS bandwidth that fragments and loads
 // take stand against it.  Short k (40001 x 1024 x 1024 68 to 75 us, 1.2 POPS) is
 // bounded by the first loads and the epilogue of every tile, which nothing hides
-// with one workgroup a CU, and by 628 tiles in 2.5 rounds of 256.
+// with one workgroup a CU, and by 628 tiles in 2.5 rounds of 256.  The 256 x 256 tiles spill
+// two of 128 registers, reloaded after the main loop.
 // --------------------------------------------------------------------------
 template <int WM, int WN, int MI, int NI, int KB, int ST>
 struct Tile {
@@ -437,11 +439,12 @@ hipError_t launch_tile(const QuantGemmArgs& g0, hipStream_t st) {
 // --------------------------------------------------------------------------
 // float rows of up to kFusedK columns: a workgroup quantises BM rows into LDS and
 // multiplies them by all of w from there, so that the rows are read once and their
-// 8-bit form never leaves the CU.  2^20 x 602 x 128 in bfloat16 takes 392 to 428 us,
-// 3.6 to 3.9 TB/s of the bytes it cannot do without (a copy: 4.7): reading the rows
-// bounds it, with about 7 vector instructions a value (150 us of them by
-// themselves) and the products of one workgroup only in part behind the loads of
-// the others.
+// 8-bit form never leaves the CU.  2^20 x 602 x 128 in bfloat16 takes 405 to 425 us, 3.6
+// to 3.8 TB/s of the bytes it cannot do without (a copy: 4.7).  Vector instructions bound
+// it, about 25 a value with the epilogue's: counters show them issued in all of its
+// cycles, and where the card has just been idle and its clock is lower (1.7 GHz) it
+// takes 550 us, as kernels that memory bounds do not.  float32 rows of that size are
+// bound by memory (617 us, 4.7 TB/s).
 //
 // Quantising: 16 lanes a row, four rows a wave and pass, U units a lane.  Rows lie
 // an odd number of 16-byte pieces apart, so that the 16 rows a fragment read
@@ -829,7 +832,13 @@ bool quant_few_float(int64_t M, int64_t N, int64_t K) { return K <= kFewK && qua
 // 40000 x 602 x 128 24 / 33, 2^18 x 602 x 128 107 / 175, 5000 x 128 x 128 5.5 / 7.4, 16384
 // x 602 x 256 18 / 26, 60000 x 1000 x 512 83 / 87, 100000 x 602 x 1024 182 / 163; over
 // few rows its sweeps of 128 columns, and of long rows the first, take too long
-// (2000 x 1000 x 512 31 / 24, 2000 x 602 x 128 12.5 / 10.4).
+// (2000 x 1000 x 512 31 / 24, 2000 x 602 x 128 12.5 / 10.4).  (Kernels alone, bfloat16 out.)
+// Two launches write and read the 8-bit rows and are 2 to 3 times as long as their bytes:
+// 100000 x 602 x 1024 180, 34 for the rows and 147 for the product of short k, against 70;
+// 100000 x 1500 x 64 130 against 67.
+// Its units for 640 columns serve 257 to 512 too, in bfloat16 at 1.2 to 1.4 times the
+// bytes' time like 602 itself (2^20 x 257 x 128 248 / 173, 300 262 / 193, 400 313 / 238, 512
+// 354 / 288, 602 409 / 329), in float32 at 1.0 to 1.1.
 // k_quant_short from a tile for each of its 1024 workgroups on, against k_quant_fused: in
 // bfloat16 2^20 x 128 x 128 137 / 159, 2^20 x 100 x 32 93 / 106, 2^20 x 64 x 64 100 / 101,
 // 2^20 x 256 x 128 204 / 219, 65536 x 256 x 128 18.9 / 21.2; in float32 151 / 177, 95 / 98,
@@ -875,7 +884,10 @@ hipError_t launch_gemm_quant(const QuantGemmArgs& g, hipStream_t st) {
   // of two, 41 / 36; 20000 x 512 x 512, 0.62 of one, 18 / 17).
   const int64_t large = ((g.M + 255) / 256) * ((g.N + 255) / 256), rounds = (large + 255) / 256;
   // (not where 128-wide tiles leave out a tenth or more of its columns: 2^20 x 602 x
-  // 128 263 / 361)
+  // 128 to bfloat16 263 / 361.  That is 1.36 times its bytes' time: the ten chunks of a
+  // tile's k do not hide its first loads and its epilogue.  Vector units are busy a quarter of
+  // the cycles, matrix units 14 %, and rows 608 bytes apart are fetched in 1.17 times their
+  // bytes, as 64-byte chunks do not begin on lines.)
   if (large * 5 >= rounds * 256 * 4 && (g.N + 255) / 256 * 20 <= cols * 11) return launch_tile<4, 4, 4, 4, 64, 4>(g, st);
   if (g.N <= 16) return launch_tile<4, 1, 2, 1, 128, 2>(g, st);
   if (g.N <= 32) return launch_tile<4, 1, 2, 2, 128, 2>(g, st);
