@@ -81,8 +81,9 @@ typedef enum saga_status {
   SAGA_EINTERNAL = 6
 } saga_status;
 
-/* SAGA_I8: 8-bit rows with a float32 scale each, only where a call names it. */
-typedef enum saga_dtype { SAGA_F32 = 0, SAGA_BF16 = 1, SAGA_I8 = 2 } saga_dtype;
+/* SAGA_I8: 8-bit rows with a float32 scale each; SAGA_MX4: 4-bit rows with a scale for
+ * every 32 columns.  Both only where a call names them. */
+typedef enum saga_dtype { SAGA_F32 = 0, SAGA_BF16 = 1, SAGA_I8 = 2, SAGA_MX4 = 3 } saga_dtype;
 
 /* Gather reductions (Table I "Gather" column; the simple sum/mean/max
  * reductions and the attention reduction of Sec. 2 "Survey Result"). */
@@ -620,6 +621,118 @@ saga_status saga_apply_vertex_quant(const saga_quant_op* op, saga_cmat a, const 
                                     saga_cmat w, const float* w_scale, const float* bias,
                                     saga_mat out, void* workspace, size_t workspace_bytes,
                                     void* stream);
+
+/* ======================================================================
+ * ApplyVertex in microscaled 4-bit floating point
+ * ======================================================================
+ * 32 neighbouring columns of a row (a block; the last one may be shorter) are held as
+ * numbers 0, 1/2, 1, 3/2, 2, 3, 4, 6 with a sign and one power of two:
+ *     e = max(floor(log2 A) - 2, -127), A the block's largest magnitude
+ *     q = x 2^-e rounded to the nearest of the numbers, ties to the even one (0, 1, 2, 4);
+ *         beyond 6 (A may be up to 8 scales): 6
+ * The scale is the byte e + 127.  A block that holds a NaN or an infinity has the byte 255,
+ * which stands for NaN, and zeros: every result of its row is NaN, from SAGA_ACT_RELU
+ * too, which takes a NaN to itself here.  A number is four bits: sign, two of exponent, one
+ * of mantissa; a byte holds two, the first column in its low half.  (The format and its
+ * conversion are those of the Open Compute Project's Microscaling Formats, MXFP4.)
+ *
+ * A 4-bit matrix of M x K is two: q, M x (K + 1) / 2 bytes (16-byte base and ld a
+ * multiple of 16) and scale, M x (K + 31) / 32 bytes (4-byte base and ld a multiple of 4);
+ * saga_cmat's cols and ld count bytes there.  What lies past a row's bytes is neither
+ * used nor written.  Where K is odd the last byte's high half is a column: the
+ * quantiser writes 0 there.
+ *
+ * saga_quantize_rows_mx: x: M x K (dtype f32 or bf16) to q and scale; K < 2^31.
+ * saga_dequantize_rows_mx: q and scale to the values they stand for, x: M x K, dtype f32 or
+ * bf16 (exact, but below bfloat16's normal range).
+ * Weights are quantised the same way, one output channel a row.
+ *
+ * saga_apply_vertex_mx: the transform of saga_apply_vertex (mode PLAIN) on 4-bit rows:
+ *     out[i, j] = act(rs_i * sum_k a[i, k] w[j, k] + bias[j])
+ * rs_i = row_scale_deg ? (deg[i] > 0 ? deg[i]^-1/2 : 0) : 1.  Products are exact, sums
+ * float32.  a: M x K: a_dtype MX4: 4-bit rows with a_scale, K twice its bytes; F32 / BF16: float
+ * rows, which the call quantises as above (a_scale absent: ptr NULL).  w: N x (K + 1) / 2
+ * bytes, one channel a row, with w_scale.  out: M x N, out_dtype F32 or BF16.  a and out: 16-byte
+ * base and row pitch; ld of a and w below 2^23.  1 <= K <= 2^20, 1 <= N <= 2^28.
+ * Workspace: saga_apply_vertex_mx_workspace_size() bytes (0: none, may be NULL),
+ * 256-byte aligned, scratch afterwards, not overlapping any argument.  Calls that
+ * share one workspace must be ordered.
+ * Errors: SAGA_EINVAL, SAGA_EUNSUPPORTED (K, N or ld too large), SAGA_EWORKSPACE,
+ * SAGA_EDEVICE. */
+saga_status saga_quantize_rows_mx(int32_t dtype, saga_cmat x, saga_mat q, saga_mat scale, void* stream);
+
+saga_status saga_dequantize_rows_mx(int32_t dtype, saga_cmat q, saga_cmat scale, saga_mat x, void* stream);
+
+typedef struct saga_mx_op {
+  int32_t a_dtype;                /* SAGA_MX4, SAGA_F32 or SAGA_BF16 */
+  int32_t out_dtype;              /* SAGA_F32 or SAGA_BF16 */
+  int32_t act;                    /* saga_act */
+  const int32_t* row_scale_deg;   /* nullable, int32[M] */
+} saga_mx_op;
+
+saga_status saga_apply_vertex_mx_workspace_size(const saga_mx_op* op, int64_t m, int64_t k, int64_t n,
+                                                size_t* bytes);
+
+saga_status saga_apply_vertex_mx(const saga_mx_op* op, saga_cmat a, saga_cmat a_scale, saga_cmat w,
+                                 saga_cmat w_scale, const float* bias, saga_mat out, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* ======================================================================
+ * ApplyVertex by a layer of experts
+ * ======================================================================
+ * For a few rows x of a batch (asked vertices) a router chooses top_k of E experts:
+ *     l_e = x . router_e + router_bias_e        (float64 sums)
+ *     index[i, 0..] = the experts of the largest l, equal ones by number
+ *     weight[i, j]  = e^(l_index - max l) / sum of the same over the chosen experts
+ *                     (renormalise) or over all of them
+ *     expert e: h = act(x up_e^T + up_bias_e), or, gated,
+ *               h = act(x gate_e^T + gate_bias_e) * (x up_e^T + up_bias_e)
+ *     out[i] = sum_j weight[i, j] * (h down_e^T + down_bias_e), e = index[i, j]
+ * An expert with l = -inf (by its bias) is closed: where fewer than top_k are open the
+ * rest has index -1 and weight 0, and a row with none open is 0.  A row that holds a NaN
+ * or an infinity, or has a logit that is NaN or +inf, has index -1, weight NaN and
+ * nothing but NaN in out; other rows do not see it.
+ * Sums are float32.  Rows and the values h enter the matrix cores as sums of bfloat16
+ * terms that hold them to 2^-24 (dtype F32) or, h of BF16 rows, 2^-16.
+ * x: M x F, out: M x N, of dtype F32 or BF16.  router: E x F, router_dtype F32 or BF16.
+ * Weights, one output channel a row, the experts' one below the other, weight_dtype BF16
+ * or MX4 (with scales, as saga_apply_vertex_mx takes them; absent otherwise: ptr NULL):
+ * up: E H x F, gated: E 2H x F, each expert's gate above its up; down: E N x H.  Biases
+ * (nullable, float32): router_bias[E], up_bias, one for each row of up, down_bias[E N].  Matrices:
+ * 16-byte base and row pitch.  1 <= E <= 1024, 1 <= top_k <= min(E, 16),
+ * F, H, N <= 65536.  1024 rows are worked on at a time: of more the weights are read again.
+ * Workspace: saga_apply_vertex_experts_workspace_size() bytes, 256-byte aligned, scratch
+ * afterwards, not overlapping any argument.  Calls that share one must be ordered.
+ * Errors: SAGA_EINVAL, SAGA_EUNSUPPORTED (sizes), SAGA_EWORKSPACE, SAGA_EDEVICE. */
+#define SAGA_MAX_EXPERTS 1024
+#define SAGA_MAX_CHOICES 16
+
+typedef struct saga_expert_op {
+  int32_t dtype;                  /* x, out */
+  int32_t router_dtype;           /* router */
+  int32_t weight_dtype;           /* up, down: SAGA_BF16 or SAGA_MX4 */
+  int32_t experts;                /* E */
+  int32_t top_k;
+  int32_t act;                    /* saga_act */
+  int32_t gated, renormalise;     /* 0 or 1 */
+} saga_expert_op;
+
+typedef struct saga_expert_weights {
+  saga_cmat router;
+  const float* router_bias;       /* nullable */
+  saga_cmat up, up_scale;
+  const float* up_bias;           /* nullable */
+  saga_cmat down, down_scale;
+  const float* down_bias;         /* nullable */
+} saga_expert_weights;
+
+/* f, h, n: columns of x, hidden channels of an expert, columns of out */
+saga_status saga_apply_vertex_experts_workspace_size(const saga_expert_op* op, int64_t m, int64_t f,
+                                                     int64_t h, int64_t n, size_t* bytes);
+
+saga_status saga_apply_vertex_experts(const saga_expert_op* op, const saga_expert_weights* weights,
+                                      saga_cmat x, saga_mat out, int32_t* index, float* weight,
+                                      void* workspace, size_t workspace_bytes, void* stream);
 
 /* ======================================================================
  * The end of a block in a deep network

@@ -18,7 +18,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libsaga.so")
 SOURCES = ["abi.hip", "plan.hip", "gather.hip", "gemm.hip", "gemm_split.hip", "gemm_stream.hip", "lstm.hip", "rel.hip",
-           "quant.hip", "block.hip", "labels.hip"]
+           "quant.hip", "block.hip", "labels.hip", "mx4.hip", "experts.hip"]
 
 
 def hipcc() -> str:

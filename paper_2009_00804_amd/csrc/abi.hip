@@ -672,6 +672,219 @@ saga_status run_quant(const saga_quant_op& op, const saga_cmat& a, const float* 
   return e == hipSuccess ? ok() : dev_fail(e, "8-bit product launch");
 }
 
+// -------------------------------------------------------------------------
+// 4-bit rows and products, layers of experts
+// -------------------------------------------------------------------------
+// the scales of a 4-bit matrix of rows x k
+saga_status check_scales(const void* ptr, int64_t rows, int64_t cols, int64_t ld, int64_t want_rows, int64_t k,
+                         const char* name) {
+  saga_status s = check_extent(rows, cols, ld, name);
+  if (s) return s;
+  if ((s = check_mat(ptr, rows, cols, ld, want_rows, (k + 31) / 32, 1, false, name))) return s;
+  if (rows <= 0) return SAGA_OK;
+  if ((uintptr_t)ptr % 4 != 0) return fail(SAGA_EINVAL, "%s: base not 4-byte aligned", name);
+  if (ld % 4 != 0) return fail(SAGA_EINVAL, "%s: row pitch %lld not a multiple of 4", name, (long long)ld);
+  return SAGA_OK;
+}
+
+// x: M x K floats, q and scale its 4-bit form
+saga_status check_rows_mx(int32_t dtype, const saga_cmat& x, const saga_cmat& q, const saga_cmat& scale) {
+  if (!float_dtype(dtype)) return fail(SAGA_EINVAL, "bad dtype");
+  saga_status s = check_extent(x.rows, x.cols, std::max(x.ld, q.ld), "x");
+  if (s) return s;
+  if (x.cols > INT32_MAX) return fail(SAGA_EUNSUPPORTED, "x: %lld columns", (long long)x.cols);
+  if ((s = check_mat(x.ptr, x.rows, x.cols, x.ld, x.rows, x.cols, esize(dtype), true, "x"))) return s;
+  if ((s = check_mat(q.ptr, q.rows, q.cols, q.ld, x.rows, (x.cols + 1) / 2, 1, true, "q"))) return s;
+  return check_scales(scale.ptr, scale.rows, scale.cols, scale.ld, x.rows, x.cols, "scale");
+}
+
+saga_status run_rows_mx(int32_t dtype, const saga_cmat& x, const saga_cmat& q, const saga_cmat& scale, bool back,
+                        hipStream_t st) {
+  saga_status s = check_rows_mx(dtype, x, q, scale);
+  if (s) return s;
+  if (back) {
+    const Span outs[] = {span(x, esize(dtype))}, ins[] = {span(q, 1), span(scale, 1)};
+    if ((s = check_apart(outs, ins))) return s;
+  } else {
+    const Span outs[] = {span(q, 1), span(scale, 1)}, ins[] = {span(x, esize(dtype))};
+    if ((s = check_apart(outs, ins))) return s;
+  }
+  saga::Mx4RowsArgs a;
+  a.dtype = dtype;
+  a.M = x.rows;
+  a.K = x.cols;
+  a.x = x.ptr;
+  a.ldx = x.ld;
+  a.q = static_cast<uint8_t*>(const_cast<void*>(q.ptr));
+  a.ldq = q.ld;
+  a.scale = static_cast<uint8_t*>(const_cast<void*>(scale.ptr));
+  a.lds = scale.ld;
+  const hipError_t e = saga::launch_rows_mx4(a, back, st);
+  return e == hipSuccess ? ok() : dev_fail(e, "4-bit rows launch");
+}
+
+saga_status check_mx_op(const saga_mx_op& op, int64_t m, int64_t k, int64_t n) {
+  if (op.a_dtype != SAGA_MX4 && !float_dtype(op.a_dtype)) return fail(SAGA_EINVAL, "bad a_dtype");
+  if (!float_dtype(op.out_dtype)) return fail(SAGA_EINVAL, "bad out_dtype");
+  if (op.act < SAGA_ACT_NONE || op.act > SAGA_ACT_TANH) return fail(SAGA_EINVAL, "bad activation");
+  if (m < 0 || k <= 0 || n <= 0) return fail(SAGA_EINVAL, "m must be >= 0, k and n > 0");
+  if (k > saga::kMx4MaxK) return fail(SAGA_EUNSUPPORTED, "4-bit product: k %lld too large", (long long)k);
+  if (n > saga::kMx4MaxN || m > ((int64_t)1 << 40)) return fail(SAGA_EUNSUPPORTED, "4-bit product: m or n too large");
+  return SAGA_OK;
+}
+
+saga_status run_mx(const saga_mx_op& op, const saga_cmat& a, const saga_cmat& a_scale, const saga_cmat& w,
+                   const saga_cmat& w_scale, const float* bias, const saga_mat& out, void* ws, size_t ws_bytes,
+                   hipStream_t st) {
+  const bool mx = op.a_dtype == SAGA_MX4;
+  const int64_t M = a.rows, N = w.rows;
+  if (a.cols > saga::kMx4MaxK) return fail(SAGA_EUNSUPPORTED, "4-bit product: k %lld too large", (long long)a.cols);
+  const int64_t K = mx ? 2 * a.cols : a.cols;
+  saga_status s = check_mx_op(op, M, K, N);
+  if (s) return s;
+  const size_t ea = mx ? 1 : esize(op.a_dtype), eo = esize(op.out_dtype);
+  if ((s = check_extent(M, a.cols, a.ld, "a"))) return s;
+  if ((s = check_extent(N, w.cols, w.ld, "w"))) return s;
+  if ((s = check_extent(M, N, out.ld, "out"))) return s;
+  if ((s = check_mat(a.ptr, M, a.cols, a.ld, M, a.cols, ea, true, "a"))) return s;
+  if ((s = check_mat(w.ptr, N, w.cols, w.ld, N, (K + 1) / 2, 1, true, "w"))) return s;
+  if ((s = check_mat(out.ptr, out.rows, out.cols, out.ld, M, N, eo, true, "out"))) return s;
+  if (a.ld >= saga::kMx4MaxLd || w.ld >= saga::kMx4MaxLd)
+    return fail(SAGA_EUNSUPPORTED, "4-bit product: ld of a and w must be below 2^23");
+  if (!mx && a_scale.ptr) return fail(SAGA_EINVAL, "a_scale is for 4-bit rows (a float a is quantised by the call)");
+  if (mx && (s = check_scales(a_scale.ptr, a_scale.rows, a_scale.cols, a_scale.ld, M, K, "a_scale"))) return s;
+  if ((s = check_scales(w_scale.ptr, w_scale.rows, w_scale.cols, w_scale.ld, N, K, "w_scale"))) return s;
+  if ((mx && a_scale.ld >= saga::kMx4MaxLd) || w_scale.ld >= saga::kMx4MaxLd)
+    return fail(SAGA_EUNSUPPORTED, "4-bit product: ld of the scales must be below 2^23");
+  if ((s = check_vec(bias, N, false, "bias"))) return s;
+  if ((s = check_vec(op.row_scale_deg, M, false, "row_scale_deg"))) return s;
+  const size_t need = saga::mx4_workspace_bytes(op.a_dtype, M, N, K);
+  if ((s = check_ws(ws, ws_bytes, need, "apply_vertex_mx"))) return s;
+  const Span outs[] = {span(out, eo), Span{ws, need}};
+  const Span ins[] = {span(a, ea), span(w, 1), mx ? span(a_scale, 1) : Span{nullptr, 0}, span(w_scale, 1),
+                      span(bias, N, 4), span(op.row_scale_deg, M, 4)};
+  if ((s = check_apart(outs, ins))) return s;
+  saga::Mx4GemmArgs g;
+  g.M = M;
+  g.N = N;
+  g.K = K;
+  g.a_dtype = op.a_dtype;
+  g.a = a.ptr;
+  g.lda = a.ld;
+  g.a_scale = mx ? static_cast<const uint8_t*>(a_scale.ptr) : nullptr;
+  g.lda_s = mx ? a_scale.ld : 0;
+  g.w = static_cast<const uint8_t*>(w.ptr);
+  g.ldw = w.ld;
+  g.w_scale = static_cast<const uint8_t*>(w_scale.ptr);
+  g.ldw_s = w_scale.ld;
+  g.bias = bias;
+  g.row_scale_deg = op.row_scale_deg;
+  g.act = op.act;
+  g.out_dtype = op.out_dtype;
+  g.out = out.ptr;
+  g.ldo = out.ld;
+  g.ws = ws;
+  const hipError_t e = saga::launch_gemm_mx4(g, st);
+  return e == hipSuccess ? ok() : dev_fail(e, "4-bit product launch");
+}
+
+saga_status check_expert_op(const saga_expert_op& op, int64_t m, int64_t f, int64_t h, int64_t n) {
+  if (!float_dtype(op.dtype)) return fail(SAGA_EINVAL, "bad dtype");
+  if (!float_dtype(op.router_dtype)) return fail(SAGA_EINVAL, "bad router_dtype");
+  if (op.weight_dtype != SAGA_BF16 && op.weight_dtype != SAGA_MX4) return fail(SAGA_EINVAL, "bad weight_dtype");
+  if (op.act < SAGA_ACT_NONE || op.act > SAGA_ACT_TANH) return fail(SAGA_EINVAL, "bad activation");
+  if (op.experts < 1 || op.experts > SAGA_MAX_EXPERTS)
+    return fail(SAGA_EINVAL, "experts must be 1 to %d", SAGA_MAX_EXPERTS);
+  if (op.top_k < 1 || op.top_k > std::min(op.experts, SAGA_MAX_CHOICES))
+    return fail(SAGA_EINVAL, "top_k must be 1 to %d and at most experts", SAGA_MAX_CHOICES);
+  if ((op.gated | op.renormalise) & ~1) return fail(SAGA_EINVAL, "gated and renormalise must be 0 or 1");
+  if (m < 0 || f <= 0 || h <= 0 || n <= 0) return fail(SAGA_EINVAL, "m must be >= 0, f, h and n > 0");
+  if (std::max(f, std::max(h, n)) > saga::kExpertMaxF || m > ((int64_t)1 << 40))
+    return fail(SAGA_EUNSUPPORTED, "experts: sizes too large");
+  return SAGA_OK;
+}
+
+saga_status run_experts(const saga_expert_op& op, const saga_expert_weights& w, const saga_cmat& x,
+                        const saga_mat& out, int32_t* index, float* weight, void* ws, size_t ws_bytes,
+                        hipStream_t st) {
+  const bool mx = op.weight_dtype == SAGA_MX4;
+  const int64_t M = x.rows, F = x.cols, N = out.cols, E = op.experts, per = E * (1 + (op.gated ? 1 : 0));
+  // (the hidden width is what up's rows give each expert)
+  const int64_t H = op.experts > 0 && w.up.rows > 0 && w.up.rows % per == 0 ? w.up.rows / per : 0;
+  saga_status s = check_expert_op(op, M, F, std::max<int64_t>(H, 1), N);
+  if (s) return s;
+  if (H == 0) return fail(SAGA_EINVAL, "up: %lld rows are no multiple of %lld", (long long)w.up.rows, (long long)per);
+  const size_t es = esize(op.dtype), er = esize(op.router_dtype), ew = mx ? 1 : 2;
+  const int64_t up_cols = mx ? (F + 1) / 2 : F, down_cols = mx ? (H + 1) / 2 : H;
+  const int64_t lds[] = {x.ld, out.ld, w.router.ld, w.up.ld, w.down.ld};
+  for (int64_t ld : lds)
+    if (ld >= (int64_t)1 << 40) return fail(SAGA_EINVAL, "experts: ld out of range");
+  if ((s = check_extent(M, F, std::max(x.ld, out.ld), "x"))) return s;
+  if ((s = check_mat(x.ptr, M, F, x.ld, M, F, es, true, "x"))) return s;
+  if ((s = check_mat(out.ptr, out.rows, N, out.ld, M, N, es, true, "out"))) return s;
+  if ((s = check_mat(w.router.ptr, w.router.rows, w.router.cols, w.router.ld, E, F, er, true, "router"))) return s;
+  if ((s = check_mat(w.up.ptr, w.up.rows, w.up.cols, w.up.ld, per * H, up_cols, ew, true, "up"))) return s;
+  if ((s = check_mat(w.down.ptr, w.down.rows, w.down.cols, w.down.ld, E * N, down_cols, ew, true, "down"))) return s;
+  if (mx) {
+    if ((s = check_scales(w.up_scale.ptr, w.up_scale.rows, w.up_scale.cols, w.up_scale.ld, per * H, F, "up_scale")))
+      return s;
+    if ((s = check_scales(w.down_scale.ptr, w.down_scale.rows, w.down_scale.cols, w.down_scale.ld, E * N, H,
+                          "down_scale")))
+      return s;
+  } else if (w.up_scale.ptr || w.down_scale.ptr) {
+    return fail(SAGA_EINVAL, "up_scale and down_scale are for 4-bit weights");
+  }
+  if ((s = check_vec(w.router_bias, E, false, "router_bias"))) return s;
+  if ((s = check_vec(w.up_bias, per * H, false, "up_bias"))) return s;
+  if ((s = check_vec(w.down_bias, E * N, false, "down_bias"))) return s;
+  if ((s = check_vec(index, M, true, "index"))) return s;
+  if ((s = check_vec(weight, M, true, "weight"))) return s;
+  const size_t need = saga::experts_workspace_bytes(op.dtype, M, F, H, N, op.top_k);
+  if ((s = check_ws(ws, ws_bytes, need, "apply_vertex_experts"))) return s;
+  const Span none = {nullptr, 0};
+  const Span outs[] = {span(out, es), span(index, M * op.top_k, 4), span(weight, M * op.top_k, 4), Span{ws, need}};
+  const Span ins[] = {span(x, es), span(w.router, er), span(w.up, ew), span(w.down, ew),
+                      mx ? span(w.up_scale, 1) : none, mx ? span(w.down_scale, 1) : none,
+                      span(w.router_bias, E, 4), span(w.up_bias, per * H, 4), span(w.down_bias, E * N, 4)};
+  if ((s = check_apart(outs, ins))) return s;
+  saga::ExpertArgs a;
+  memset(&a, 0, sizeof(a));
+  a.dtype = op.dtype;
+  a.router_dtype = op.router_dtype;
+  a.weight_dtype = op.weight_dtype;
+  a.act = op.act;
+  a.gated = op.gated;
+  a.top_k = op.top_k;
+  a.renormalise = op.renormalise;
+  a.E = op.experts;
+  a.M = M;
+  a.F = (int)F;
+  a.H = (int)H;
+  a.N = (int)N;
+  a.x = x.ptr;
+  a.ldx = x.ld;
+  a.router = w.router.ptr;
+  a.ld_router = w.router.ld;
+  a.router_bias = w.router_bias;
+  a.up = w.up.ptr;
+  a.ld_up = w.up.ld;
+  a.up_scale = mx ? static_cast<const uint8_t*>(w.up_scale.ptr) : nullptr;
+  a.lds_up = w.up_scale.ld;
+  a.up_bias = w.up_bias;
+  a.down = w.down.ptr;
+  a.ld_down = w.down.ld;
+  a.down_scale = mx ? static_cast<const uint8_t*>(w.down_scale.ptr) : nullptr;
+  a.lds_down = w.down_scale.ld;
+  a.down_bias = w.down_bias;
+  a.out = out.ptr;
+  a.ldo = out.ld;
+  a.index = index;
+  a.weight = weight;
+  a.ws = ws;
+  const hipError_t e = saga::launch_experts(a, st);
+  return e == hipSuccess ? ok() : dev_fail(e, "experts launch");
+}
+
 saga_status check_norm(const saga_norm_desc& d, int64_t F, const char* name) {
   if (d.kind < SAGA_NORM_NONE || d.kind > SAGA_NORM_LAYER) return fail(SAGA_EINVAL, "%s: bad norm", name);
   if (d.kind != SAGA_NORM_NONE && !(d.eps > 0.0f && d.eps < 1e30f))
@@ -1960,6 +2173,75 @@ saga_status saga_apply_vertex_quant(const saga_quant_op* op, saga_cmat a, const 
     if (!op) return fail(SAGA_EINVAL, "op is null");
     return run_quant(*op, a, a_scale, w, w_scale, bias, out, workspace, workspace_bytes,
                      static_cast<hipStream_t>(stream));
+  } catch (...) {
+    return fail(SAGA_EINTERNAL, "exception");
+  }
+}
+
+saga_status saga_quantize_rows_mx(int32_t dtype, saga_cmat x, saga_mat q, saga_mat scale, void* stream) {
+  try {
+    return run_rows_mx(dtype, x, saga_cmat{q.ptr, q.rows, q.cols, q.ld},
+                       saga_cmat{scale.ptr, scale.rows, scale.cols, scale.ld}, false,
+                       static_cast<hipStream_t>(stream));
+  } catch (...) {
+    return fail(SAGA_EINTERNAL, "exception");
+  }
+}
+
+saga_status saga_dequantize_rows_mx(int32_t dtype, saga_cmat q, saga_cmat scale, saga_mat x, void* stream) {
+  try {
+    return run_rows_mx(dtype, saga_cmat{x.ptr, x.rows, x.cols, x.ld}, q, scale, true,
+                       static_cast<hipStream_t>(stream));
+  } catch (...) {
+    return fail(SAGA_EINTERNAL, "exception");
+  }
+}
+
+saga_status saga_apply_vertex_mx_workspace_size(const saga_mx_op* op, int64_t m, int64_t k, int64_t n,
+                                                size_t* bytes) {
+  try {
+    if (!op || !bytes) return fail(SAGA_EINVAL, "null argument");
+    saga_status s = check_mx_op(*op, m, k, n);
+    if (s) return s;
+    *bytes = saga::mx4_workspace_bytes(op->a_dtype, m, n, k);
+    return ok();
+  } catch (...) {
+    return fail(SAGA_EINTERNAL, "exception");
+  }
+}
+
+saga_status saga_apply_vertex_mx(const saga_mx_op* op, saga_cmat a, saga_cmat a_scale, saga_cmat w,
+                                 saga_cmat w_scale, const float* bias, saga_mat out, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  try {
+    if (!op) return fail(SAGA_EINVAL, "op is null");
+    return run_mx(*op, a, a_scale, w, w_scale, bias, out, workspace, workspace_bytes,
+                  static_cast<hipStream_t>(stream));
+  } catch (...) {
+    return fail(SAGA_EINTERNAL, "exception");
+  }
+}
+
+saga_status saga_apply_vertex_experts_workspace_size(const saga_expert_op* op, int64_t m, int64_t f,
+                                                     int64_t h, int64_t n, size_t* bytes) {
+  try {
+    if (!op || !bytes) return fail(SAGA_EINVAL, "null argument");
+    saga_status s = check_expert_op(*op, m, f, h, n);
+    if (s) return s;
+    *bytes = saga::experts_workspace_bytes(op->dtype, m, f, h, n, op->top_k);
+    return ok();
+  } catch (...) {
+    return fail(SAGA_EINTERNAL, "exception");
+  }
+}
+
+saga_status saga_apply_vertex_experts(const saga_expert_op* op, const saga_expert_weights* weights,
+                                      saga_cmat x, saga_mat out, int32_t* index, float* weight,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+  try {
+    if (!op || !weights) return fail(SAGA_EINVAL, "null argument");
+    return run_experts(*op, *weights, x, out, index, weight, workspace, workspace_bytes,
+                       static_cast<hipStream_t>(stream));
   } catch (...) {
     return fail(SAGA_EINTERNAL, "exception");
   }

@@ -225,6 +225,66 @@ struct QuantFloatArgs {
 bool quant_fuses(int64_t M, int64_t N, int64_t K);
 hipError_t launch_quant_fused(int dtype, const QuantFloatArgs& f, hipStream_t st);
 
+// ---- mx4.hip: 4-bit rows and products ----
+struct Mx4RowsArgs {
+  int dtype;
+  int64_t M, K;
+  const void* x; int64_t ldx;       // written to where the 4-bit rows are read
+  uint8_t* q; int64_t ldq;          // M x (K + 1) / 2
+  uint8_t* scale; int64_t lds;      // M x (K + 31) / 32
+};
+hipError_t launch_rows_mx4(const Mx4RowsArgs& a, bool back, hipStream_t st);
+
+struct Mx4GemmArgs {
+  int64_t M, N, K;
+  int a_dtype;
+  const void* a; int64_t lda;       // M x K floats, or 4-bit rows with a_scale
+  const uint8_t* a_scale; int64_t lda_s;
+  const uint8_t* w; int64_t ldw;    // N x (K + 1) / 2
+  const uint8_t* w_scale; int64_t ldw_s;
+  const float* bias;                // nullable
+  const int32_t* row_scale_deg;     // nullable
+  int act, out_dtype;
+  void* out; int64_t ldo;
+  void* ws;
+};
+constexpr int64_t kMx4MaxK = 1 << 20;
+constexpr int64_t kMx4MaxN = 1 << 28;
+constexpr int64_t kMx4MaxLd = 1 << 23;  // a tile's rows within 32-bit offsets
+size_t mx4_workspace_bytes(int a_dtype, int64_t M, int64_t N, int64_t K);
+hipError_t launch_gemm_mx4(const Mx4GemmArgs& g, hipStream_t st);
+
+// ---- experts.hip ----
+constexpr int kExpertsMax = SAGA_MAX_EXPERTS;
+constexpr int kExpertRows = 1024;       // rows of one run of the kernels
+constexpr int64_t kExpertMaxF = 1 << 16;
+struct ExpertArgs {
+  int dtype, router_dtype, weight_dtype, act, gated, top_k, renormalise, E;
+  int64_t M;
+  int F, H, N;
+  const void* x; int64_t ldx;
+  const void* router; int64_t ld_router;
+  const float* router_bias;                     // nullable
+  const void* up; int64_t ld_up;
+  const uint8_t* up_scale; int64_t lds_up;
+  const float* up_bias;                         // nullable
+  const void* down; int64_t ld_down;
+  const uint8_t* down_scale; int64_t lds_down;
+  const float* down_bias;                       // nullable
+  void* out; int64_t ldo;
+  int32_t* index;                               // M x top_k
+  float* weight;
+  void* ws;
+  // set by launch_experts: x and the values between the products as planes of bfloat16
+  // terms, and the second products' results for each pair of a row and an expert
+  uint16_t *xt, *ht;
+  float* part;
+  int64_t ld_xt, ld_ht, ld_part;
+  int x_terms, h_terms;
+};
+size_t experts_workspace_bytes(int dtype, int64_t M, int64_t F, int64_t H, int64_t N, int top_k);
+hipError_t launch_experts(const ExpertArgs& a, hipStream_t st);
+
 // ---- block.hip ----
 constexpr int64_t kBlockMaxF = 16384;
 struct BlockArgs {

@@ -180,7 +180,7 @@ def _placed(f):
     return call
 
 
-def _matrix(t, name, like, dtypes, shape=None):
+def _matrix(t, name, like, dtypes, shape=None, unit=16):
     """saga_cmat of a 2-D tensor on the device of ``like``"""
     if t is None:
         return S.saga_cmat(None, 0, 0, 0)
@@ -195,7 +195,7 @@ def _matrix(t, name, like, dtypes, shape=None):
     if step != 1 and cols > 1:
         raise ValueError(f"{name}: the columns of a row have to be neighbours")
     if rows <= 1:  # no pitch to speak of
-        ld = _whole(cols, t.dtype)
+        ld = _whole(cols, t.dtype, unit)
     return S.saga_cmat(t.data_ptr(), rows, cols, ld)
 
 
@@ -209,15 +209,15 @@ def _vector(t, name, like, n, dtype=torch.float32):
     return t.data_ptr()
 
 
-def _whole(cols, dtype):
-    """cols rounded up to whole 16 bytes"""
-    a = 16 // dtype.itemsize
+def _whole(cols, dtype, unit=16):
+    """cols rounded up to whole 16 bytes (or ``unit``)"""
+    a = unit // dtype.itemsize
     return (cols + a - 1) // a * a
 
 
-def _out(rows, cols, dtype, like):
-    """(view, saga_mat) of a new matrix with 16-byte rows"""
-    ld = _whole(cols, dtype)
+def _out(rows, cols, dtype, like, unit=16):
+    """(view, saga_mat) of a new matrix with 16-byte rows (or a multiple of ``unit`` bytes)"""
+    ld = _whole(cols, dtype, unit)
     buf = like.new_empty((rows, ld), dtype=dtype)
     return (buf if ld == cols else buf[:, :cols]), S.saga_mat(buf.data_ptr(), rows, cols, ld)
 
@@ -242,8 +242,28 @@ def _label_bytes(dtype, m, c, top_k):
     return S.saga_label_log_probs_workspace_size(dtype, m, c, top_k)
 
 
+@functools.lru_cache(maxsize=1024)
+def _mx_bytes(a_dtype, out_dtype, m, k, n):
+    return S.saga_apply_vertex_mx_workspace_size(S.saga_mx_op(a_dtype, out_dtype, 0, None), m, k, n)
+
+
+@functools.lru_cache(maxsize=1024)
+def _expert_bytes(*sizes):
+    return S.saga_apply_vertex_experts_workspace_size(S.saga_expert_op(*sizes[:-4]), *sizes[-4:])
+
+
 _FLOATS = (torch.float32, torch.bfloat16)
 _BYTES = (torch.int8,)
+_NIBBLES = (torch.uint8,)
+_NONE = S.saga_cmat(None, 0, 0, 0)
+
+
+def _four_bit(q, scale, name, scale_name, like, shape=None):
+    """saga_cmats of 4-bit rows and their scales, whose rows lie a multiple of 4 bytes apart"""
+    cq = _matrix(q, name, like, _NIBBLES, shape)
+    if scale is None:
+        raise ValueError(f"{scale_name}: 4-bit rows need their scales")
+    return cq, _matrix(scale, scale_name, like, _NIBBLES, (cq.rows, (cq.cols + 15) // 16), 4)
 
 
 @_placed
@@ -277,6 +297,100 @@ def quant_linear(x, w, w_scale, x_scale=None, bias=None, act="none", row_scale_d
                               _vector(w_scale, "w_scale", x, n), _vector(bias, "bias", x, n), mo,
                               ws.data_ptr() if nbytes else None, nbytes, _stream(x))
     return out
+
+
+@_placed
+def quantize_rows_mx4(x):
+    """(q, scale): the 4-bit rows of x, two columns a byte, and a scale byte for every
+    32 columns."""
+    m, k = x.shape
+    cx = _matrix(x, "x", x, _FLOATS)
+    q, mq = _out(m, (k + 1) // 2, torch.uint8, x)
+    scale, ms = _out(m, (k + 31) // 32, torch.uint8, x, 4)
+    S.saga_quantize_rows_mx(S.dtype_code(x.dtype), cx, mq, ms, _stream(x))
+    return q, scale
+
+
+@_placed
+def dequantize_rows_mx4(q, scale, columns=None, dtype=torch.bfloat16):
+    """The values that 4-bit rows stand for, as float32 or bfloat16; columns: how many
+    (all that q's bytes hold, or one less)."""
+    if columns is None:
+        columns = 2 * q.shape[1]
+    cq, cs = _four_bit(q, scale, "q", "scale", q)
+    x, mx = _out(q.shape[0], columns, dtype, q)
+    S.saga_dequantize_rows_mx(S.dtype_code(dtype), cq, cs, mx, _stream(q))
+    return x
+
+
+@_placed
+def mx4_linear(x, w, w_scale, x_scale=None, bias=None, act="none", row_scale_deg=None, out_dtype=None):
+    """act(rs * (x w^T) + bias) on 4-bit rows: w and w_scale hold one output channel a
+    row; x is 4-bit rows with x_scale, or float rows that the call quantises.
+    out_dtype: x's own, float32 for 4-bit rows."""
+    m, k = x.shape
+    mx = x.dtype == torch.uint8
+    if mx:
+        k *= 2
+    if out_dtype is None:
+        out_dtype = torch.float32 if mx else x.dtype
+    n = w.shape[0]
+    if mx:
+        cx, cxs = _four_bit(x, x_scale, "x", "x_scale", x)
+    elif x_scale is not None:
+        raise ValueError("x_scale: for 4-bit rows (float rows are quantised by the call)")
+    else:
+        cx, cxs = _matrix(x, "x", x, _FLOATS), _NONE
+    cw, cws = _four_bit(w, w_scale, "w", "w_scale", x, (n, (k + 1) // 2))
+    op = S.saga_mx_op(S.SAGA_MX4 if mx else S.dtype_code(x.dtype), S.dtype_code(out_dtype), S.ACT[act],
+                      _vector(row_scale_deg, "row_scale_deg", x, m, torch.int32))
+    nbytes = _mx_bytes(op.a_dtype, op.out_dtype, m, k, n)
+    out, mo = _out(m, n, out_dtype, x)
+    ws = _space(nbytes, x)
+    S.saga_apply_vertex_mx(op, cx, cxs, cw, cws, _vector(bias, "bias", x, n), mo,
+                           ws.data_ptr() if nbytes else None, nbytes, _stream(x))
+    return out
+
+
+@_placed
+def expert_layer(x, router, up, down, *, up_scale=None, down_scale=None, router_bias=None, up_bias=None,
+                 down_bias=None, top_k=1, act="relu", gated=False, renormalise=True):
+    """(y, index, weight): y = sum over each row's top_k experts of weight *
+    (act(x up^T) down^T), the experts chosen by x router^T.  up and down hold the experts'
+    weights one below the other, an output channel a row, in bfloat16 or, with
+    up_scale and down_scale, in 4 bits; gated: up holds each expert's gate above its up, and
+    an expert is (act(x gate^T) * (x up^T)) down^T."""
+    m, f = x.shape
+    e = router.shape[0]
+    per = e * (2 if gated else 1)
+    mx = up.dtype == torch.uint8
+    h, n = (up.shape[0] // per, down.shape[0] // e) if e else (0, 0)
+    if not e or h * per != up.shape[0] or n * e != down.shape[0]:
+        raise ValueError(f"{up.shape[0]} rows of up and {down.shape[0]} of down are no multiple of {e} experts'")
+    w = S.saga_expert_weights()
+    cx = _matrix(x, "x", x, _FLOATS)
+    w.router = _matrix(router, "router", x, _FLOATS, (e, f))
+    if mx:
+        w.up, w.up_scale = _four_bit(up, up_scale, "up", "up_scale", x, (per * h, (f + 1) // 2))
+        w.down, w.down_scale = _four_bit(down, down_scale, "down", "down_scale", x, (e * n, (h + 1) // 2))
+    elif up_scale is not None or down_scale is not None:
+        raise ValueError("up_scale, down_scale: for 4-bit weights")
+    else:
+        w.up = _matrix(up, "up", x, (torch.bfloat16,), (per * h, f))
+        w.down = _matrix(down, "down", x, (torch.bfloat16,), (e * n, h))
+    w.router_bias = _vector(router_bias, "router_bias", x, e)
+    w.up_bias = _vector(up_bias, "up_bias", x, per * h)
+    w.down_bias = _vector(down_bias, "down_bias", x, e * n)
+    op = S.saga_expert_op(S.dtype_code(x.dtype), S.dtype_code(router.dtype), S.SAGA_MX4 if mx else S.SAGA_BF16, e,
+                          top_k, S.ACT[act], bool(gated), bool(renormalise))
+    nbytes = _expert_bytes(*(getattr(op, name) for name, _ in op._fields_), m, f, h, n)
+    y, my = _out(m, n, x.dtype, x)
+    index = x.new_empty((m, top_k), dtype=torch.int32)
+    weight = x.new_empty((m, top_k), dtype=torch.float32)
+    ws = _space(nbytes, x)
+    S.saga_apply_vertex_experts(op, w, cx, my, index.data_ptr(), weight.data_ptr(),
+                                ws.data_ptr() if nbytes else None, nbytes, _stream(x))
+    return y, index, weight
 
 
 @_placed

@@ -21,7 +21,7 @@ LIB_PATH = os.path.join(_PKG, "libsaga.so")
 
 # enums (saga.h)
 SAGA_OK, SAGA_EINVAL, SAGA_EGRAPH, SAGA_EUNSUPPORTED, SAGA_EDEVICE, SAGA_EWORKSPACE, SAGA_EINTERNAL = range(7)
-SAGA_F32, SAGA_BF16, SAGA_I8 = 0, 1, 2
+SAGA_F32, SAGA_BF16, SAGA_I8, SAGA_MX4 = 0, 1, 2, 3
 SAGA_RED_SUM, SAGA_RED_MEAN, SAGA_RED_MAX, SAGA_RED_SOFTMAX = range(4)
 SAGA_MSG_COPY, SAGA_MSG_SRC_NORM, SAGA_MSG_GAT, SAGA_MSG_GATED, SAGA_MSG_TYPED = range(5)
 SAGA_ACT_NONE, SAGA_ACT_RELU, SAGA_ACT_ELU, SAGA_ACT_SIGMOID, SAGA_ACT_TANH = range(5)
@@ -30,6 +30,8 @@ SAGA_GEMM_PLAIN, SAGA_GEMM_CONCAT, SAGA_GEMM_GRU = range(3)
  SAGA_LAYER_RGCN) = range(6)
 SAGA_NORM_NONE, SAGA_NORM_RMS, SAGA_NORM_LAYER = range(3)
 SAGA_MAX_TOP = 32
+SAGA_MAX_EXPERTS = 1024
+SAGA_MAX_CHOICES = 16
 SAGA_REL_TILE = 128
 SAGA_REL_MAX_RELATIONS = 2048
 
@@ -47,6 +49,8 @@ EXPORTS = [
     "saga_rel_transform_workspace_size", "saga_rel_transform",
     "saga_apply_vertex_workspace_size", "saga_apply_vertex",
     "saga_quantize_rows", "saga_apply_vertex_quant_workspace_size", "saga_apply_vertex_quant",
+    "saga_quantize_rows_mx", "saga_dequantize_rows_mx", "saga_apply_vertex_mx_workspace_size",
+    "saga_apply_vertex_mx", "saga_apply_vertex_experts_workspace_size", "saga_apply_vertex_experts",
     "saga_block_norm", "saga_label_log_probs_workspace_size", "saga_label_log_probs",
     "saga_layer_workspace_size", "saga_layer", "saga_trace_stages", "saga_sync_check",
     "saga_status_str", "saga_last_error", "saga_version",
@@ -126,6 +130,23 @@ class saga_quant_op(C.Structure):
                 ("row_scale_deg", C.c_void_p)]
 
 
+class saga_mx_op(C.Structure):
+    _fields_ = [("a_dtype", C.c_int), ("out_dtype", C.c_int), ("act", C.c_int),
+                ("row_scale_deg", C.c_void_p)]
+
+
+class saga_expert_op(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("router_dtype", C.c_int32), ("weight_dtype", C.c_int32),
+                ("experts", C.c_int32), ("top_k", C.c_int32), ("act", C.c_int32), ("gated", C.c_int32),
+                ("renormalise", C.c_int32)]
+
+
+class saga_expert_weights(C.Structure):
+    _fields_ = [("router", saga_cmat), ("router_bias", C.c_void_p), ("up", saga_cmat), ("up_scale", saga_cmat),
+                ("up_bias", C.c_void_p), ("down", saga_cmat), ("down_scale", saga_cmat),
+                ("down_bias", C.c_void_p)]
+
+
 class saga_norm_desc(C.Structure):
     _fields_ = [("kind", C.c_int), ("eps", C.c_float), ("weight", C.c_void_p), ("bias", C.c_void_p)]
 
@@ -203,6 +224,16 @@ def lib():
                                                        P(C.c_size_t)]),
         "saga_apply_vertex_quant": (S, [P(saga_quant_op), saga_cmat, C.c_void_p, saga_cmat, C.c_void_p,
                                         C.c_void_p, saga_mat, C.c_void_p, C.c_size_t, C.c_void_p]),
+        "saga_quantize_rows_mx": (S, [C.c_int, saga_cmat, saga_mat, saga_mat, C.c_void_p]),
+        "saga_dequantize_rows_mx": (S, [C.c_int, saga_cmat, saga_cmat, saga_mat, C.c_void_p]),
+        "saga_apply_vertex_mx_workspace_size": (S, [P(saga_mx_op), C.c_int64, C.c_int64, C.c_int64,
+                                                    P(C.c_size_t)]),
+        "saga_apply_vertex_mx": (S, [P(saga_mx_op), saga_cmat, saga_cmat, saga_cmat, saga_cmat, C.c_void_p,
+                                     saga_mat, C.c_void_p, C.c_size_t, C.c_void_p]),
+        "saga_apply_vertex_experts_workspace_size": (S, [P(saga_expert_op), C.c_int64, C.c_int64, C.c_int64,
+                                                         C.c_int64, P(C.c_size_t)]),
+        "saga_apply_vertex_experts": (S, [P(saga_expert_op), P(saga_expert_weights), saga_cmat, saga_mat,
+                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
         "saga_block_norm": (S, [P(saga_block_op), saga_cmat, saga_cmat, saga_cmat, saga_mat, saga_mat,
                                 C.c_void_p, C.c_void_p]),
         "saga_label_log_probs_workspace_size": (S, [C.c_int, C.c_int64, C.c_int64, C.c_int32,
@@ -398,6 +429,38 @@ def saga_apply_vertex_quant_workspace_size(op, m, k, n):
 def saga_apply_vertex_quant(op, a, a_scale, w, w_scale, bias, out, workspace, ws_bytes, stream):
     return _check(lib().saga_apply_vertex_quant(C.byref(op), a, a_scale, w, w_scale, bias, out, workspace,
                                                 ws_bytes, stream), "saga_apply_vertex_quant")
+
+
+def saga_quantize_rows_mx(dtype, x, q, scale, stream):
+    return _check(lib().saga_quantize_rows_mx(dtype, x, q, scale, stream), "saga_quantize_rows_mx")
+
+
+def saga_dequantize_rows_mx(dtype, q, scale, x, stream):
+    return _check(lib().saga_dequantize_rows_mx(dtype, q, scale, x, stream), "saga_dequantize_rows_mx")
+
+
+def saga_apply_vertex_mx_workspace_size(op, m, k, n):
+    out = C.c_size_t(0)
+    _check(lib().saga_apply_vertex_mx_workspace_size(C.byref(op), m, k, n, C.byref(out)),
+           "saga_apply_vertex_mx_workspace_size")
+    return out.value
+
+
+def saga_apply_vertex_mx(op, a, a_scale, w, w_scale, bias, out, workspace, ws_bytes, stream):
+    return _check(lib().saga_apply_vertex_mx(C.byref(op), a, a_scale, w, w_scale, bias, out, workspace,
+                                             ws_bytes, stream), "saga_apply_vertex_mx")
+
+
+def saga_apply_vertex_experts_workspace_size(op, m, f, h, n):
+    out = C.c_size_t(0)
+    _check(lib().saga_apply_vertex_experts_workspace_size(C.byref(op), m, f, h, n, C.byref(out)),
+           "saga_apply_vertex_experts_workspace_size")
+    return out.value
+
+
+def saga_apply_vertex_experts(op, weights, x, out, index, weight, workspace, ws_bytes, stream):
+    return _check(lib().saga_apply_vertex_experts(C.byref(op), C.byref(weights), x, out, index, weight,
+                                                  workspace, ws_bytes, stream), "saga_apply_vertex_experts")
 
 
 def saga_block_norm(op, block, gate, x, y, z, z_scale, stream):
