@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_device.h"
 #include "mx4_device.h"
@@ -14,62 +15,109 @@ namespace {
 constexpr int64_t kMostBlocks = 1 << 20;  // (a grid holds less than 2^32 threads)
 
 // --------------------------------------------------------------------------
-// float rows to 4-bit rows and back: G lanes a row, 8 columns a lane; the four lanes
-// of a block join their largest magnitudes.
+// float rows to 4-bit rows and back: G lanes a row, U units of 8 columns a lane at a time;
+// the four lanes of a block join their largest magnitudes.  Blocks know nothing of each
+// other, so a long row is divided among workgroups.
 // --------------------------------------------------------------------------
-template <typename T, int G>
+template <typename T, int G, int U>
 __global__ __launch_bounds__(256) void k_quantize_mx4(Mx4RowsArgs a) {
-  const int64_t bytes = (a.K + 1) / 2, end = (a.K + 31) / 32 * 32;
+  const int64_t bytes = (a.K + 1) / 2;
   for (int64_t row = blockIdx.x * (int64_t)(256 / G) + threadIdx.x / G; row < a.M;
        row += gridDim.x * (int64_t)(256 / G)) {
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
     uint8_t* q = a.q + row * a.ldq;
-    for (int64_t col = (threadIdx.x % G) * 8; col < end; col += G * 8) {
-      const int left = (int)min(a.K - col, (int64_t)8);
-      Raw<T> v;
-      v.load(x + col, left);
-      v.clear(left);
-      uint32_t top = v.top();
-      top = max(top, dpp_mov<0xB1>(top));  // quad_perm [1,0,3,2]
-      top = max(top, dpp_mov<0x4E>(top));  // quad_perm [2,3,0,1]
-      const BlockScale s = block_scale(top);
-      const uint32_t o = round_mx4(v, s);
-      const int64_t at = col / 2;
-      if (at + 4 <= bytes) {
-        *reinterpret_cast<uint32_t*>(q + at) = o;
-      } else {
+    uint8_t* scale = a.scale + row * a.lds;
+    for (int64_t col0 = blockIdx.y * (int64_t)(G * 8 * U) + (threadIdx.x % G) * 8; col0 < a.K + 24;
+         col0 += gridDim.y * (int64_t)(G * 8 * U)) {  // (+ 24: all four lanes of the last block)
+      Raw<T> v[U];
+      int left[U];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (at + j < bytes) q[at + j] = (uint8_t)(o >> (8 * j));
+      for (int u = 0; u < U; ++u) {
+        left[u] = (int)min(a.K - col0 - u * 8 * G, (int64_t)8);
+        v[u].load(x + col0 + u * 8 * G, left[u]);
       }
-      if ((threadIdx.x & 3) == 0) a.scale[row * a.lds + col / 32] = (uint8_t)s.byte;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        v[u].clear(left[u]);
+        uint32_t top = v[u].top();
+        top = max(top, dpp_mov<0xB1>(top));  // quad_perm [1,0,3,2]
+        top = max(top, dpp_mov<0x4E>(top));  // quad_perm [2,3,0,1]
+        const BlockScale s = block_scale(top);
+        const uint32_t o = round_mx4(v[u], s);
+        const int64_t at = (col0 + u * 8 * G) / 2;
+        if (at + 4 <= bytes) {
+          *reinterpret_cast<uint32_t*>(q + at) = o;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (at + j < bytes) q[at + j] = (uint8_t)(o >> (8 * j));
+        }
+        if ((threadIdx.x & 3) == 0 && left[u] > 0) scale[(col0 + u * 8 * G) / 32] = (uint8_t)s.byte;
+      }
     }
   }
 }
 
-template <typename T, int G>
+// the scale of a byte
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+  return __uint_as_float(byte == 255u ? 0x7fc00000u : byte ? byte << 23 : 0x00400000u);
+}
+
+template <typename T, int G, int U>
 __global__ __launch_bounds__(256) void k_dequantize_mx4(Mx4RowsArgs a) {
-  const int64_t bytes = (a.K + 1) / 2;
   for (int64_t row = blockIdx.x * (int64_t)(256 / G) + threadIdx.x / G; row < a.M;
        row += gridDim.x * (int64_t)(256 / G)) {
     T* x = static_cast<T*>(const_cast<void*>(a.x)) + row * a.ldx;
     const uint8_t* q = a.q + row * a.ldq;
-    for (int64_t col = (threadIdx.x % G) * 8; col < a.K; col += G * 8) {
-      uint32_t o = 0;
-      if (col / 2 < bytes) o = *reinterpret_cast<const uint32_t*>(q + col / 2);  // (rows are whole 16 bytes)
-      const uint32_t byte = a.scale[row * a.lds + col / 32];
-      const float s = byte == 255u ? __uint_as_float(0x7fc00000u)
-                                   : __uint_as_float(byte ? byte << 23 : 0x00400000u);
-      float v[8];
+    const uint8_t* scale = a.scale + row * a.lds;
+    for (int64_t col0 = blockIdx.y * (int64_t)(G * 8 * U) + (threadIdx.x % G) * 8; col0 < a.K;
+         col0 += gridDim.y * (int64_t)(G * 8 * U)) {
+      uint32_t o[U], byte[U];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t c = o >> (4 * j), e = (c >> 1) & 3u, m = c & 1u;
-        const float mag = e ? __uint_as_float((126u + e) << 23 | m << 22) : (m ? 0.5f : 0.0f);
-        v[j] = ((c & 8u) ? -mag : mag) * s;
+      for (int u = 0; u < U; ++u) {
+        const int64_t col = col0 + u * 8 * G;
+        o[u] = byte[u] = 0;
+        if (col < a.K) {  // (4 bytes of the last 16 of a row at most)
+          o[u] = *reinterpret_cast<const uint32_t*>(q + col / 2);
+          byte[u] = scale[col / 32];
+        }
       }
-      store_unit(x + col, a.K - col, v);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t col = col0 + u * 8 * G;
+        if (col >= a.K) break;
+        const float s = scale_value(byte[u]);
+        float v[8];
+        const auto pair = [&](auto p, float& lo, float& hi) { lo = p[0], hi = p[1]; };
+        pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(o[u], s, 0), v[0], v[1]);
+        pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(o[u], s, 1), v[2], v[3]);
+        pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(o[u], s, 2), v[4], v[5]);
+        pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(o[u], s, 3), v[6], v[7]);
+        store_unit(x + col, a.K - col, v);
+      }
     }
   }
+}
+
+// 16 lanes a row where a row fits them: less of its last unit is idle
+template <typename T, int G, int U>
+hipError_t launch_rows(const Mx4RowsArgs& a, bool back, hipStream_t st) {
+  const int64_t blocks = std::min<int64_t>((a.M + 256 / G - 1) / (256 / G), kMostBlocks / 4);
+  const int64_t parts = (a.K + G * 8 * U - 1) / (G * 8 * U);
+  const dim3 grid((unsigned)blocks, (unsigned)std::min(parts, std::max<int64_t>(1, 32768 / blocks)));
+  if (back) hipLaunchKernelGGL((k_dequantize_mx4<T, G, U>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_quantize_mx4<T, G, U>), grid, dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t rows_mx4(const Mx4RowsArgs& a, bool back, hipStream_t st) {
+  if (a.K <= 128) return launch_rows<T, 16, 1>(a, back, st);
+  if (a.K <= 256) return launch_rows<T, 16, 2>(a, back, st);
+  if (a.K <= 384) return launch_rows<T, 16, 3>(a, back, st);
+  if (a.K <= 512) return launch_rows<T, 16, 4>(a, back, st);
+  if (a.K <= 640) return launch_rows<T, 16, 5>(a, back, st);
+  if (a.K <= 768) return launch_rows<T, 16, 6>(a, back, st);
+  return launch_rows<T, 64, 2>(a, back, st);
 }
 
 // --------------------------------------------------------------------------
@@ -161,15 +209,302 @@ hipError_t launch_few(const Mx4GemmArgs& g, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <typename T>
-hipError_t rows_mx4(const Mx4RowsArgs& a, bool back, hipStream_t st) {
-  const auto go = [&](auto kernel, int rows) {
-    const int64_t blocks = std::min<int64_t>((a.M + rows - 1) / rows, kMostBlocks);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
-    return hipGetLastError();
+// --------------------------------------------------------------------------
+// large products of 4-bit rows: a workgroup of WM x WN waves holds BM rows of a and BN
+// rows of w, a wave MI x NI tiles of 32 x 32 sums.  64 bytes (128 k) of every row a stage
+// with their scales, ST stages in LDS filled by direct-to-LDS loads, which run between
+// the products of a stage rather than ahead of them.  The matrix instruction takes w as
+// its first operand: a lane then holds groups of four neighbouring channels of one row.
+// 32 x 32 x 64 and not 16 x 16 x 128: by itself it reaches 6.4 against 5.5 PFLOP/s on random
+// bytes, where power bounds both.
+//
+// A lane takes the pieces (16 bytes, a block) 2 (l / 32) and 2 (l / 32) + 1 of a stage in
+// its two steps, so that both scales are one 16-bit read.
+// --------------------------------------------------------------------------
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) uint4 lds_uint4;
+typedef const __attribute__((address_space(3))) u32x4 lds_cu32x4;
+
+template <int WM, int WN, int MI, int NI, int ST>
+struct Tile {
+  static constexpr int NW = WM * WN, THREADS = 64 * NW;
+  static constexpr int BM = 32 * MI * WM, BN = 32 * NI * WN, ROWS = BM + BN;
+  static constexpr int PR = 4;                                  // 16-byte pieces of a row
+  static constexpr int STAGE = ROWS * PR;                       // 16-byte slots
+  static constexpr int GROUPS = ROWS / 16;                      // load instructions per stage
+  static constexpr int LB = (GROUPS + NW - 1) / NW;             // of one wave
+  static constexpr int SR = (ROWS + NW - 1) / NW;               // rows whose scales a wave loads
+  static constexpr int LOADS = LB + 1;
+  static constexpr int NP = 8 * NI;                             // 16-byte pieces of a wave's row of sums
+  static constexpr int SLOTS = ST * STAGE > NW * 32 * NP ? ST * STAGE : NW * 32 * NP;
+  static_assert(SR <= 64, "one load instruction for a wave's scales");
+  static_assert(ST == 2 || (GROUPS % NW == 0 && ROWS % NW == 0), "a wait counts the same loads on every wave");
+  static constexpr int LDS = SLOTS * 16 + ST * NW * SR * 4 + ROWS * 4;
+  static constexpr int WAVES = 160 * 1024 / LDS * NW / 4;       // waves a SIMD that LDS has room for
+  static constexpr int WPE = WAVES < 4 ? WAVES : 4;             // (more would spill registers)
+  // slot of piece p of row r: the 16 rows of a fragment read fall on all banks
+  __device__ __forceinline__ static int slot(int r, int p) { return r * PR + (p ^ ((r >> 2) & 3)); }
+};
+
+template <int OPSEL>
+__device__ __forceinline__ f32x16 mma_tile(const u32x4& w, const u32x4& a, const f32x16& c, uint32_t sw, uint32_t sa) {
+  const i32x8 x = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+  const i32x8 y = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, OPSEL, (int)sw, OPSEL, (int)sa);
+}
+
+template <int WM, int WN, int MI, int NI, int ST>
+__global__ __launch_bounds__(64 * WM * WN)
+__attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_mx4(Mx4GemmArgs g, int tiles_m,
+                                                                                    int tiles_n) {
+  typedef Tile<WM, WN, MI, NI, ST> R;
+  __shared__ uint4 ring[R::SLOTS];
+  __shared__ uint32_t ring_scales[ST][R::NW * R::SR];
+  __shared__ f32x4 ends[R::ROWS / 4];  // degree scalings of the rows, bias of the channels
+  // Workgroup w runs on XCD w % 8: every XCD gets a run of tiles, and in it eight
+  // row tiles share each column tile.
+  const int total = tiles_m * tiles_n, per = (total + kXcds - 1) / kXcds;
+  const int t = (int)(blockIdx.x % kXcds) * per + (int)(blockIdx.x / kXcds);
+  if (t >= total || (int)(blockIdx.x / kXcds) >= per) return;
+  const int band = t / (8 * tiles_n), in = t % (8 * tiles_n), bm = min(8, tiles_m - band * 8);
+  const int64_t m0 = (int64_t)(band * 8 + in % bm) * R::BM, n0 = (int64_t)(in / bm) * R::BN;
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  lds_uint4* lds = (lds_uint4*)ring;
+
+  // this lane's share of the loads: row 16 (wave + j NW) + lane / 4 of the stage
+  // (rows past the last read the last one; their sums are not stored)
+  const uint8_t* const A = static_cast<const uint8_t*>(g.a) + m0 * g.lda;
+  const uint8_t* const W = g.w + n0 * g.ldw;
+  const int K = (int)g.K, bytes = (K + 1) / 2, kmax = (bytes - 1) / 16 * 16, last = (bytes - 1) / 64;
+  const auto row_of = [&](int r) {
+    return r < R::BM ? (int)min((int64_t)r, g.M - 1 - m0) : (int)min((int64_t)(r - R::BM), g.N - 1 - n0);
   };
-  if (a.K <= 1024) return back ? go(k_dequantize_mx4<T, 16>, 16) : go(k_quantize_mx4<T, 16>, 16);
-  return back ? go(k_dequantize_mx4<T, 256>, 1) : go(k_quantize_mx4<T, 256>, 1);
+  uint32_t off[R::LB];
+  int piece[R::LB];
+#pragma unroll
+  for (int j = 0; j < R::LB; ++j) {
+    const int r = 16 * (wave + j * R::NW) + lane / 4;
+    piece[j] = (R::slot(r, lane % 4) % 4) * 16;
+    off[j] = (uint32_t)row_of(r) * (uint32_t)(r < R::BM ? g.lda : g.ldw);
+  }
+  const int sr = min(wave * R::SR + lane, R::ROWS - 1);
+  const uint8_t* const scale_at = sr < R::BM ? g.a_scale + (m0 + row_of(sr)) * g.lda_s
+                                             : g.w_scale + (n0 + row_of(sr)) * g.ldw_s;
+  // load j of chunk c; only the last chunk can reach past the rows' ends, where it
+  // reads their last piece again (masked before use).  Load LB: the scales.
+  const auto issue = [&](int c, int j) {
+    if (j == R::LB) {
+      if (R::SR == 64 || lane < R::SR)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                     :
+                     : "s"(__builtin_amdgcn_readfirstlane(
+                           (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t*)ring_scales[c % ST] +
+                           wave * R::SR * 4)),
+                       "v"(scale_at + c * 4)
+                     : "memory", "m0");
+      return;
+    }
+    const int grp = wave + j * R::NW;
+    if (R::GROUPS % R::NW != 0 && grp >= R::GROUPS) return;
+    const uint8_t* base = grp * 16 < R::BM ? A : W;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds + (c % ST) * R::STAGE) + grp * 1024)),
+                   "v"(off[j] + (uint32_t)min(c * 64 + piece[j], kmax)), "s"(base)
+                 : "memory", "m0");
+  };
+#pragma unroll
+  for (int c = 0; c < ST; ++c)
+    if (c <= last)
+#pragma unroll
+      for (int j = 0; j < R::LOADS; ++j) issue(c, j);
+  {
+    float* e = reinterpret_cast<float*>(ends);
+    for (int i = threadIdx.x; i < R::BM; i += R::THREADS)
+      e[i] = g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[min(m0 + i, g.M - 1)]) : 1.0f;
+    for (int i = threadIdx.x; i < R::BN; i += R::THREADS)
+      e[R::BM + i] = g.bias ? g.bias[min(n0 + i, g.N - 1)] : 0.0f;
+  }
+
+  f32x16 acc[MI][NI];
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[mi][ni][i] = 0.0f;
+
+  const int half = lane >> 5, lr = lane & 31;
+  uint32_t at[2];  // this lane's piece of each step, in the row lr of a 32-row tile
+#pragma unroll
+  for (int s = 0; s < 2; ++s) at[s] = R::slot(lr, 2 * half + s);
+
+  // Fragments of a step are read into one half of a and w while those in the other
+  // half are multiplied; the scales of a chunk into one half of sa and sw.
+  u32x4 a[2][MI], w[2][NI];
+  uint32_t sa[2][MI], sw[2][NI];
+  const auto read_w = [&](int c, int s, int ni) {
+    w[s][ni] = *(lds_cu32x4*)(lds + (c % ST) * R::STAGE + at[s] + (R::BM + (wn * NI + ni) * 32) * R::PR);
+  };
+  const auto read_a = [&](int c, int s, int mi) {
+    a[s][mi] = *(lds_cu32x4*)(lds + (c % ST) * R::STAGE + at[s] + (wm * MI + mi) * 32 * R::PR);
+  };
+  const auto read_scales = [&](int c, int p) {
+    const uint16_t* const sc = reinterpret_cast<const uint16_t*>(ring_scales[c % ST]) + lr * 2 + half;
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) sa[p][mi] = sc[(wm * MI + mi) * 64];
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) sw[p][ni] = sc[(R::BM + (wn * NI + ni) * 32) * 2];
+  };
+  // Chunk c, its first fragments read, its scales in half p.  Before its last step chunk
+  // c + 1 has to have landed, for every wave; every wave then has chunk c's fragments in
+  // registers, and chunk c + ST takes its stage.  The reads of the next fragments and, where
+  // FILL, the loads go between the row tiles: in one run either would hold up the products
+  // behind it.
+  const auto chunk = [&](auto fill_tag, auto half_tag, int c) {
+    constexpr bool FILL = decltype(fill_tag)::value;
+    constexpr int P = decltype(half_tag)::value, WR = (NI + MI - 1) / MI;
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+#pragma unroll
+      for (int k = 0; k < WR; ++k)
+        if (mi * WR + k < NI) read_w(c, 1, mi * WR + k);
+      read_a(c, 1, mi);
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = mma_tile<0>(w[0][ni], a[0][mi], acc[mi][ni], sw[P][ni], sa[P][mi]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (FILL) wait_vm<(ST - 2) * R::LOADS>();
+    else wait_vm<0>();
+    ring_barrier();
+    read_scales(c + 1, P ^ 1);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+#pragma unroll
+      for (int k = 0; k < WR; ++k)
+        if (mi * WR + k < NI) read_w(c + 1, 0, mi * WR + k);
+      read_a(c + 1, 0, mi);
+      if constexpr (FILL) {
+#pragma unroll
+        for (int j = 0; j < R::LOADS; ++j)
+          if (j * MI / R::LOADS == mi) issue(c + ST, j);
+      }
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = mma_tile<1>(w[1][ni], a[1][mi], acc[mi][ni], sw[P][ni], sa[P][mi]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  typedef std::integral_constant<int, 0> P0;
+  typedef std::integral_constant<int, 1> P1;
+
+  wait_vm<0>();
+  ring_barrier();
+  read_scales(0, 0);
+#pragma unroll
+  for (int ni = 0; ni < NI; ++ni) read_w(0, 0, ni);
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi) read_a(0, 0, mi);
+  int c = 0;
+  const auto turn = [&] {  // the next chunk's scales to the first half
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) sa[0][mi] = sa[1][mi];
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) sw[0][ni] = sw[1][ni];
+  };
+  for (; c + 1 + ST <= last; c += 2) {
+    chunk(std::true_type{}, P0{}, c);
+    chunk(std::true_type{}, P1{}, c + 1);
+  }
+  if (c + ST <= last) {
+    chunk(std::true_type{}, P0{}, c);
+    ++c;
+    turn();
+  }
+  for (; c < last; ++c) {
+    chunk(std::false_type{}, P0{}, c);
+    turn();
+  }
+  // the last chunk: w's bytes past the rows' ends are zeros, scales past them 1 (they
+  // might stand for NaN)
+#pragma unroll
+  for (int ni = 0; ni < NI; ++ni) read_w(last, 1, ni);
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi) read_a(last, 1, mi);
+  const int left = bytes - last * 64 - half * 32;
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    if (left < 16 * (s + 1)) {
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) w[s][ni] = clear_bytes(w[s][ni], left - 16 * s);
+    }
+    if (left <= 16 * s) {
+      const uint32_t keep = s ? 0x00ffu : 0xff00u, one = s ? 0x7f00u : 0x007fu;
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) sw[0][ni] = (sw[0][ni] & keep) | one;
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) sa[0][mi] = (sa[0][mi] & keep) | one;
+    }
+  }
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+      acc[mi][ni] = mma_tile<0>(w[0][ni], a[0][mi], acc[mi][ni], sw[0][ni], sa[0][mi]);
+      acc[mi][ni] = mma_tile<1>(w[1][ni], a[1][mi], acc[mi][ni], sw[0][ni], sa[0][mi]);
+    }
+  ring_barrier();  // the stages are free
+
+  // 32 rows at a time go through LDS of this wave's own: a lane holds channels
+  // 8 i + 4 half + (0..3) of row lr, and takes back four channels of a row, so that
+  // a store covers whole rows of the wave's columns.
+  constexpr int NP = R::NP, RS = 64 / NP;
+  lds_uint4* const mine = lds + wave * 32 * NP;
+  const int p = lane % NP;
+  const int64_t n = n0 + (int64_t)wn * NI * 32 + 4 * p;
+  const f32x4 tb = ends[(R::BM + wn * NI * 32) / 4 + p];
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi) {
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(
+            mine + lr * NP + ((ni * 8 + i * 2 + half) ^ (lr & (NP - 1)))) =
+            f32x4{acc[mi][ni][4 * i], acc[mi][ni][4 * i + 1], acc[mi][ni][4 * i + 2], acc[mi][ni][4 * i + 3]};
+    asm volatile("" ::: "memory");
+#pragma unroll 2
+    for (int i = 0; i < 32 / RS; ++i) {
+      const int r = i * RS + lane / NP, rr = (wm * MI + mi) * 32 + r;
+      const f32x4 v =
+          *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(mine + r * NP + (p ^ (r & (NP - 1))));
+      const float rs = reinterpret_cast<const float*>(ends)[rr];
+      if (m0 + rr < g.M && n < g.N) store_quad(g, m0 + rr, n, v, rs, tb);
+    }
+  }
+}
+
+template <int WM, int WN, int MI, int NI, int ST>
+hipError_t launch_tile(const Mx4GemmArgs& g0, hipStream_t st) {
+  typedef Tile<WM, WN, MI, NI, ST> R;
+  const int64_t tn = (g0.N + R::BN - 1) / R::BN;
+  const int64_t slice = std::max<int64_t>(1, kMostBlocks / tn) * R::BM;  // rows per launch
+  for (int64_t m = 0; m < g0.M; m += slice) {
+    Mx4GemmArgs g = g0;
+    g.M = std::min(slice, g0.M - m);
+    g.a = static_cast<const uint8_t*>(g.a) + m * g.lda;
+    g.a_scale += m * g.lda_s;
+    if (g.row_scale_deg) g.row_scale_deg += m;
+    g.out = static_cast<char*>(g.out) + m * g.ldo * (g.out_dtype == SAGA_BF16 ? 2 : 4);
+    const int64_t tm = (g.M + R::BM - 1) / R::BM, blocks = (tm * tn + kXcds - 1) / kXcds * kXcds;
+    hipLaunchKernelGGL((k_gemm_mx4<WM, WN, MI, NI, ST>), dim3((unsigned)blocks), dim3(R::THREADS), 0, st, g, (int)tm,
+                       (int)tn);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
@@ -179,12 +514,55 @@ hipError_t launch_rows_mx4(const Mx4RowsArgs& a, bool back, hipStream_t st) {
   return a.dtype == SAGA_BF16 ? rows_mx4<uint16_t>(a, back, st) : rows_mx4<float>(a, back, st);
 }
 
-size_t mx4_workspace_bytes(int, int64_t, int64_t, int64_t) { return 0; }
+bool mx4_few(int64_t M, int64_t N, int64_t K) {
+  const int64_t wgs = ((M + 15) / 16) * ((N + 15) / 16);
+  return wgs <= 512 && wgs * ((K + 127) / 128) <= 8192;
+}
 
-hipError_t launch_gemm_mx4(const Mx4GemmArgs& g, hipStream_t st) {
-  if (g.M == 0) return hipSuccess;
-  if (g.a_dtype == SAGA_MX4) return launch_few<uint8_t>(g, st);
-  return g.a_dtype == SAGA_BF16 ? launch_few<uint16_t>(g, st) : launch_few<float>(g, st);
+// float rows for the tiles are quantised into the workspace: q, then their scales
+struct Mx4Space {
+  int64_t ldq, lds;
+  size_t scale, total;
+};
+Mx4Space mx4_space(int64_t M, int64_t K) {
+  Mx4Space s;
+  s.ldq = ((K + 1) / 2 + 15) / 16 * 16;
+  s.lds = ((K + 31) / 32 + 3) / 4 * 4;
+  s.scale = ((size_t)M * s.ldq + 255) & ~(size_t)255;
+  s.total = s.scale + (((size_t)M * s.lds + 255) & ~(size_t)255);
+  return s;
+}
+
+size_t mx4_workspace_bytes(int a_dtype, int64_t M, int64_t N, int64_t K) {
+  if (a_dtype == SAGA_MX4 || M == 0 || mx4_few(M, N, K)) return 0;
+  return mx4_space(M, K).total;
+}
+
+hipError_t launch_gemm_mx4(const Mx4GemmArgs& g0, hipStream_t st) {
+  if (g0.M == 0) return hipSuccess;
+  Mx4GemmArgs g = g0;
+  if (mx4_few(g.M, g.N, g.K)) {
+    if (g.a_dtype == SAGA_MX4) return launch_few<uint8_t>(g, st);
+    return g.a_dtype == SAGA_BF16 ? launch_few<uint16_t>(g, st) : launch_few<float>(g, st);
+  }
+  if (g.a_dtype != SAGA_MX4) {
+    const Mx4Space s = mx4_space(g.M, g.K);
+    uint8_t* const q = static_cast<uint8_t*>(g.ws);
+    const Mx4RowsArgs r = {g.a_dtype, g.M, g.K, g.a, g.lda, q, s.ldq, q + s.scale, s.lds};
+    const hipError_t e = launch_rows_mx4(r, false, st);
+    if (e != hipSuccess) return e;
+    g.a = q;
+    g.lda = s.ldq;
+    g.a_scale = q + s.scale;
+    g.lda_s = s.lds;
+  }
+  const int64_t cols = (g.N + 127) / 128, rows = (g.M + 127) / 128;
+  if (cols * rows <= 256) return launch_tile<2, 2, 1, 1, 8>(g, st);
+  const int64_t large = ((g.M + 255) / 256) * ((g.N + 255) / 256), rounds = (large + 255) / 256;
+  if (large * 5 >= rounds * 256 * 4 && (g.N + 255) / 256 * 20 <= cols * 11) return launch_tile<2, 4, 4, 2, 4>(g, st);
+  if (g.N <= 32) return launch_tile<4, 1, 1, 1, 2>(g, st);
+  if (g.N <= 64) return launch_tile<4, 1, 1, 2, 2>(g, st);
+  return launch_tile<2, 2, 2, 2, 3>(g, st);
 }
 
 }  // namespace saga
