@@ -126,20 +126,25 @@ hipError_t rows_mx4(const Mx4RowsArgs& a, bool back, hipStream_t st) {
 // its registers, since the 32 columns that a matrix instruction wants of a lane are
 // a block.
 // --------------------------------------------------------------------------
+template <int C>
+__device__ __forceinline__ void finish(int act, float (&v)[C]) {
+  if (act == SAGA_ACT_RELU) {
+    // (a NaN stays: it is all that is left of a row that held no number; -0 becomes +0)
+#pragma unroll
+    for (int j = 0; j < C; ++j) v[j] = __builtin_elementwise_maximum(v[j], 0.0f);
+  } else if (act != SAGA_ACT_NONE) {
+#pragma unroll
+    for (int j = 0; j < C; ++j) v[j] = apply_act(act, v[j]);
+  }
+}
+
 // four neighbouring channels n.. of row m: scale, bias, activation, rounding
 __device__ __forceinline__ void store_quad(const Mx4GemmArgs& g, int64_t m, int64_t n, const f32x4& sum, float rs,
                                            const f32x4& tb) {
   float v[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = sum[j] * rs + tb[j];
-  if (g.act == SAGA_ACT_RELU) {
-    // (a NaN stays: it is all that is left of a row that held no number; -0 becomes +0)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = __builtin_elementwise_maximum(v[j], 0.0f);
-  } else if (g.act != SAGA_ACT_NONE) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = apply_act(g.act, v[j]);
-  }
+  finish(g.act, v);
   if (g.out_dtype == SAGA_BF16) {
     uint16_t* o = static_cast<uint16_t*>(g.out) + m * g.ldo + n;
     if (n + 4 <= g.N) {
@@ -507,6 +512,181 @@ hipError_t launch_tile(const Mx4GemmArgs& g0, hipStream_t st) {
   return hipSuccess;
 }
 
+// --------------------------------------------------------------------------
+// many float rows by a narrow w: w stays in LDS in the order of its fragments, and a
+// wave takes 16 rows after 16 rows past it, 128 k at a time, with the next 128 on their
+// way.  Rows are loaded 16 lanes a row and rounded there; a piece of LDS of the wave's
+// own turns the four bytes that a lane then has into the block that the matrix
+// instruction wants of it.  The rows' 4-bit form never leaves the CU.
+//
+// A lane's channels of all NT column tiles are neighbours (tile t takes the channels
+// 4 NT q + 4 t + (0..3), q = 0..3), so that a store holds 16 bytes.
+// --------------------------------------------------------------------------
+// channels n.. of row m, 8 of them
+__device__ __forceinline__ void store_oct(const Mx4GemmArgs& g, int64_t m, int64_t n, const f32x4& lo, const f32x4& hi,
+                                          float rs, const f32x4& blo, const f32x4& bhi) {
+  if (g.out_dtype != SAGA_BF16 || n + 8 > g.N) {
+    if (n < g.N) store_quad(g, m, n, lo, rs, blo);
+    if (n + 4 < g.N) store_quad(g, m, n + 4, hi, rs, bhi);
+    return;
+  }
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = lo[j] * rs + blo[j], v[4 + j] = hi[j] * rs + bhi[j];
+  finish(g.act, v);
+  store_unit(static_cast<uint16_t*>(g.out) + m * g.ldo + n, 8, v);
+}
+
+constexpr int kStreamWaves = 8;
+// LDS: w's fragments, their scales (a byte for each of four steps), the bias, the waves' pieces
+struct StreamSpace {
+  int steps, w_scales, bias, turn, total;  // (bytes)
+  __host__ __device__ StreamSpace(int64_t K, int NT) {
+    steps = (int)((K + 127) / 128);
+    w_scales = steps * NT * 1024;
+    bias = w_scales + (steps + 3) / 4 * NT * 256;
+    turn = bias + NT * 64;
+    total = turn + kStreamWaves * (1024 + 64);
+  }
+};
+
+// waves a SIMD: float32 rows and eight column tiles would spill at four
+template <typename T, int NT>
+constexpr int kStreamPerSimd = sizeof(T) == 4 && NT == 8 ? 2 : 4;
+
+template <typename T, int NT>
+__global__ __launch_bounds__(64 * kStreamWaves)
+__attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, NT>))) void k_mx4_stream(
+    Mx4GemmArgs g, int64_t tiles) {
+  extern __shared__ uint4 space[];
+  const int K = (int)g.K;
+  const StreamSpace at(K, NT);
+  char* const base = reinterpret_cast<char*>(space);
+  u32x4* const lw = reinterpret_cast<u32x4*>(base);
+  uint32_t* const lws = reinterpret_cast<uint32_t*>(base + at.w_scales);
+  f32x4* const lb = reinterpret_cast<f32x4*>(base + at.bias);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int quarter = lane >> 4, lr = lane & 15;
+  uint32_t* const turn = reinterpret_cast<uint32_t*>(base + at.turn + wave * 1088);
+  uint8_t* const turn_scale = reinterpret_cast<uint8_t*>(turn) + 1024;
+  const int steps = at.steps;
+
+  for (int f = wave; f < steps * NT; f += kStreamWaves) {
+    const int s = f / NT, t = f % NT;
+    RowSource<uint8_t> w;
+    w.at(g.w, g.ldw, g.w_scale, g.ldw_s, min((int64_t)((lr >> 2) * 4 * NT + t * 4 + (lr & 3)), g.N - 1));
+    w.load(s * 4 + quarter, K);
+    const Mx4Block b = w.take(s * 4 + quarter, K);
+    lw[f * 64 + lane] = b.v;
+    reinterpret_cast<uint8_t*>(lws + ((s / 4) * NT + t) * 64 + lane)[s % 4] = (uint8_t)b.scale;
+  }
+  for (int i = threadIdx.x; i < NT * 4; i += 64 * kStreamWaves) lb[i] = bias_quad(g, i * 4);
+  __syncthreads();
+
+  const int64_t stride = (int64_t)gridDim.x * kStreamWaves;
+  int64_t tile = (int64_t)blockIdx.x * kStreamWaves + wave;
+  if (tile >= tiles) return;
+  // four rows a load: this lane's columns col.. of rows 4 j + lane / 16
+  Raw<T> v[4];
+  const T* x;
+  uint32_t off[4];
+  const auto rows_at = [&](int64_t t) {
+    x = static_cast<const T*>(g.a) + t * 16 * g.lda;
+    const int here = (int)min((int64_t)16, g.M - t * 16) - 1;  // (rows past the last: not stored)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) off[j] = (uint32_t)min(4 * j + quarter, here) * (uint32_t)g.lda + lr * 8;
+  };
+  const auto load = [&](int s) {
+    if (s * 128 + 128 <= K) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j].load(x + (off[j] + s * 128), 8);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j].load(x + (off[j] + s * 128), K - s * 128 - lr * 8);
+    }
+  };
+  rows_at(tile);
+  load(0);
+  for (; tile < tiles; tile += stride) {
+    const int64_t m = tile * 16 + lr;
+    const float rs = g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[min(m, g.M - 1)]) : 1.0f;
+    f32x4 acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = 0; s0 < steps; s0 += 4) {
+      const auto step = [&](auto opsel) {
+        constexpr int J = decltype(opsel)::value;
+        const int s = s0 + J;
+        if (s >= steps) return;
+        if (s * 128 + 128 > K) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j].clear(K - s * 128 - lr * 8);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t top = v[j].top();
+          top = max(top, dpp_mov<0xB1>(top));
+          top = max(top, dpp_mov<0x4E>(top));
+          const BlockScale b = block_scale(top);
+          turn[((4 * j + quarter) * 4 + ((lr >> 2) ^ j)) * 4 + (lr & 3)] = round_mx4(v[j], b);
+          if ((lr & 3) == 0) turn_scale[(lr >> 2) * 16 + 4 * j + quarter] = (uint8_t)b.byte;
+        }
+        if (s + 1 < steps) {
+          load(s + 1);
+        } else if (tile + stride < tiles) {
+          rows_at(tile + stride);
+          load(0);
+        }
+        asm volatile("" ::: "memory");
+        Mx4Block a;
+        a.v = *reinterpret_cast<const u32x4*>(turn + (lr * 4 + (quarter ^ (lr >> 2))) * 4);
+        a.scale = turn_scale[quarter * 16 + lr];
+        asm volatile("" ::: "memory");
+        const u32x4* const f = lw + s * NT * 64 + lane;
+        const uint32_t* const fs = lws + (s0 / 4) * NT * 64 + lane;
+        const i32x8 y = {(int)a.v[0], (int)a.v[1], (int)a.v[2], (int)a.v[3], 0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const u32x4 w = f[t * 64];
+          const i32x8 z = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+          acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(z, y, acc[t], 4, 4, J, (int)fs[t * 64], 0, (int)a.scale);
+        }
+      };
+      step(std::integral_constant<int, 0>{});
+      step(std::integral_constant<int, 1>{});
+      step(std::integral_constant<int, 2>{});
+      step(std::integral_constant<int, 3>{});
+    }
+    if (m < g.M) {
+      if constexpr (NT == 1) {
+        if (quarter * 4 < g.N) store_quad(g, m, quarter * 4, acc[0], rs, lb[quarter]);
+      } else {
+#pragma unroll
+        for (int t = 0; t < NT; t += 2) {
+          __builtin_amdgcn_sched_barrier(0);  // (two tiles' values at a time: registers)
+          store_oct(g, m, quarter * 4 * NT + t * 4, acc[t], acc[t + 1], rs, lb[quarter * NT + t], lb[quarter * NT + t + 1]);
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int NT>
+hipError_t launch_stream(const Mx4GemmArgs& g, hipStream_t st) {
+  const int64_t tiles = (g.M + 15) / 16;
+  const int lds = StreamSpace(g.K, NT).total, per = std::max(1, std::min(kStreamPerSimd<T, NT> / 2, 160 * 1024 / lds));
+  const int64_t blocks = std::min<int64_t>((tiles + kStreamWaves - 1) / kStreamWaves, 256 * per);
+  hipLaunchKernelGGL((k_mx4_stream<T, NT>), dim3((unsigned)blocks), dim3(64 * kStreamWaves), lds, st, g, tiles);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t dispatch_stream(const Mx4GemmArgs& g, hipStream_t st) {
+  if (g.N <= 16) return launch_stream<T, 1>(g, st);
+  if (g.N <= 32) return launch_stream<T, 2>(g, st);
+  if (g.N <= 64) return launch_stream<T, 4>(g, st);
+  return launch_stream<T, 8>(g, st);
+}
+
 }  // namespace
 
 hipError_t launch_rows_mx4(const Mx4RowsArgs& a, bool back, hipStream_t st) {
@@ -517,6 +697,10 @@ hipError_t launch_rows_mx4(const Mx4RowsArgs& a, bool back, hipStream_t st) {
 bool mx4_few(int64_t M, int64_t N, int64_t K) {
   const int64_t wgs = ((M + 15) / 16) * ((N + 15) / 16);
   return wgs <= 512 && wgs * ((K + 127) / 128) <= 8192;
+}
+
+bool mx4_streams(int64_t M, int64_t N, int64_t K) {
+  return M >= 4096 && N <= 128 && StreamSpace(K, N <= 16 ? 1 : N <= 32 ? 2 : N <= 64 ? 4 : 8).total <= 150 * 1024;
 }
 
 // float rows for the tiles are quantised into the workspace: q, then their scales
@@ -534,7 +718,7 @@ Mx4Space mx4_space(int64_t M, int64_t K) {
 }
 
 size_t mx4_workspace_bytes(int a_dtype, int64_t M, int64_t N, int64_t K) {
-  if (a_dtype == SAGA_MX4 || M == 0 || mx4_few(M, N, K)) return 0;
+  if (a_dtype == SAGA_MX4 || M == 0 || mx4_few(M, N, K) || mx4_streams(M, N, K)) return 0;
   return mx4_space(M, K).total;
 }
 
@@ -545,6 +729,8 @@ hipError_t launch_gemm_mx4(const Mx4GemmArgs& g0, hipStream_t st) {
     if (g.a_dtype == SAGA_MX4) return launch_few<uint8_t>(g, st);
     return g.a_dtype == SAGA_BF16 ? launch_few<uint16_t>(g, st) : launch_few<float>(g, st);
   }
+  if (g.a_dtype != SAGA_MX4 && mx4_streams(g.M, g.N, g.K))
+    return g.a_dtype == SAGA_BF16 ? dispatch_stream<uint16_t>(g, st) : dispatch_stream<float>(g, st);
   if (g.a_dtype != SAGA_MX4) {
     const Mx4Space s = mx4_space(g.M, g.K);
     uint8_t* const q = static_cast<uint8_t*>(g.ws);
