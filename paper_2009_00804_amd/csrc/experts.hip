@@ -16,16 +16,6 @@
 namespace saga {
 namespace {
 
-// --------------------------------------------------------------------------
-// router: a workgroup a row.  Logits are float64 sums: which expert a row takes hangs
-// on which of two close values is larger, so the products' rounding must not decide.
-// --------------------------------------------------------------------------
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  return v;
-}
-
 // x as terms bfloat16 values, each the rest cut to 8 bits of its mantissa: three hold a float32
 __device__ __forceinline__ uint32_t cut_term(float& rest) {
   const uint32_t hi = __float_as_uint(rest) & 0xffff0000u;
@@ -33,95 +23,147 @@ __device__ __forceinline__ uint32_t cut_term(float& rest) {
   return hi;
 }
 
-template <typename T, typename TR>
-__global__ __launch_bounds__(256) void k_route(ExpertArgs a) {
-  __shared__ double logits[kExpertsMax];
-  __shared__ int bad_row;
-  const int64_t row = blockIdx.x;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, F = a.F;
-  const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-  if (threadIdx.x == 0) bad_row = 0;
-  __syncthreads();
-
-  // the row's terms, and whether it holds numbers only
-  bool bad = false;
-  for (int c = threadIdx.x * 8; c < a.ld_xt; c += 2048) {
-    Raw<T> v;
-    v.load(x + c, F - c);
-    v.clear(F - c);
-    bad |= v.top() >= 0x7f800000u;
-    float f[8];
-    v.widen(f);
-    for (int t = 0; t < a.x_terms; ++t) {
-      u32x4 o;
+// the terms of 8 columns of a row
+template <typename T>
+__device__ __forceinline__ void store_terms(const ExpertArgs& a, int64_t row, int c, const Raw<T>& v) {
+  float f[8];
+  v.widen(f);
+  for (int t = 0; t < a.x_terms; ++t) {
+    u32x4 o;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t lo = cut_term(f[2 * j]), hi = cut_term(f[2 * j + 1]);
-        o[j] = lo >> 16 | hi;
-      }
-      *reinterpret_cast<u32x4*>(a.xt + (t * a.M + row) * a.ld_xt + c) = o;
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t lo = cut_term(f[2 * j]), hi = cut_term(f[2 * j + 1]);
+      o[j] = lo >> 16 | hi;
     }
+    *reinterpret_cast<u32x4*>(a.xt + (t * a.M + row) * a.ld_xt + c) = o;
   }
-  for (int e = wave; e < a.E; e += 4) {
-    const TR* r = static_cast<const TR*>(a.router) + e * a.ld_router;
-    double sum = 0.0;
+}
+
+// --------------------------------------------------------------------------
+// router: a workgroup a row.  Logits are float64 sums: which expert a row takes hangs
+// on which of two close values is larger, so the products' rounding must not decide.
+// A wave takes kTogether experts at a time, which share the row's values and whose loads
+// are on their way together; the choice is a rank by counting, a thread an expert.
+// --------------------------------------------------------------------------
+constexpr int kTogether = 4;
+
+// 64 lanes' sums of kTogether values; the steps of different values run side by side
+__device__ __forceinline__ void wave_sums(double (&v)[kTogether]) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2)
+#pragma unroll
+    for (int i = 0; i < kTogether; ++i) v[i] += __shfl_xor(v[i], d);
+}
+
+// logits[e] = x . router_e + bias_e for all experts; true: one that is NaN or +inf
+template <typename T, typename TR, int NW>
+__device__ __forceinline__ bool route_logits(const ExpertArgs& a, const T* x, double* logits) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, F = a.F;
+  bool bad = false;
+  for (int e0 = wave * kTogether; e0 < a.E; e0 += NW * kTogether) {
+    double sum[kTogether] = {};
     for (int c = lane * 8; c < F; c += 512) {
       Raw<T> v;
-      Raw<TR> w;
+      Raw<TR> w[kTogether];
       v.load(x + c, F - c);
-      w.load(r + c, F - c);
+#pragma unroll
+      for (int i = 0; i < kTogether; ++i)
+        w[i].load(static_cast<const TR*>(a.router) + min(e0 + i, a.E - 1) * a.ld_router + c, F - c);
       v.clear(F - c);
-      w.clear(F - c);
-      float f[8], g[8];
+      float f[8];
       v.widen(f);
-      w.widen(g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum = fma((double)f[j], (double)g[j], sum);
-    }
-    sum = wave_sum(sum);
-    if (a.router_bias) sum += (double)a.router_bias[e];
-    if (lane == 0) logits[e] = sum;
-    bad |= !(sum < (double)INFINITY);
-  }
-  if (bad) bad_row = 1;
-  __syncthreads();
-  if (wave != 0) return;
-  const double low = -(double)INFINITY;
-  double total = 0.0, top = 0.0;
-  float mine = 0.0f;      // lane j: of the j-th choice
-  int chosen = -1;
-  for (int k = 0; k < a.top_k; ++k) {
-    double best = low;
-    int at = -1;
-    for (int e = lane; e < a.E; e += 64) {
-      const double v = logits[e];
-      if (v > best) best = v, at = e;
-    }
+      for (int i = 0; i < kTogether; ++i) {
+        w[i].clear(F - c);
+        float g[8];
+        w[i].widen(g);
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const double v = __shfl_xor(best, d);
-      const int e = __shfl_xor(at, d);
-      if (v > best || (v == best && (uint32_t)e < (uint32_t)at)) best = v, at = e;
-    }
-    if (k == 0) {
-      top = at >= 0 ? best : 0.0;
-      if (!a.renormalise) {
-        for (int e = lane; e < a.E; e += 64) total += (double)expf((float)(logits[e] - top));
-        total = wave_sum(total);
+        for (int j = 0; j < 8; ++j) sum[i] = fma((double)f[j], (double)g[j], sum[i]);
       }
     }
-    const float p = at >= 0 ? expf((float)(best - top)) : 0.0f;
-    if (a.renormalise) total += (double)p;
-    if (lane == k) chosen = at, mine = p;
-    if (at >= 0 && lane == (at & 63)) logits[at] = low;
-    __builtin_amdgcn_wave_barrier();
+    wave_sums(sum);
+#pragma unroll
+    for (int i = 0; i < kTogether; ++i) {
+      if (e0 + i >= a.E) break;
+      if (a.router_bias) sum[i] += (double)a.router_bias[e0 + i];
+      if (lane == 0) logits[e0 + i] = sum[i];
+      bad |= !(sum[i] < (double)INFINITY);
+    }
   }
-  if (lane < a.top_k) {
-    float p = chosen >= 0 ? (float)((double)mine / total) : 0.0f;
-    if (bad_row) chosen = -1, p = __uint_as_float(0x7fc00000u);
-    a.index[row * a.top_k + lane] = chosen;
-    a.weight[row * a.top_k + lane] = p;
+  return bad;
+}
+
+// The choices of a row by its logits, with THREADS threads; the workgroup's own memory
+struct RouteSpace {
+  double logits[kExpertsMax];
+  double top, share[16];
+  double best[SAGA_MAX_CHOICES];
+  int chosen[SAGA_MAX_CHOICES];
+  int bad;
+};
+template <int THREADS>
+__device__ __forceinline__ void route_choose(const ExpertArgs& a, int64_t row, RouteSpace& s) {
+  const int tid = threadIdx.x;
+  if (tid < SAGA_MAX_CHOICES) s.chosen[tid] = -1;
+  __syncthreads();
+  for (int e = tid; e < a.E; e += THREADS) {
+    const double v = s.logits[e];
+    if (!(v > -(double)INFINITY)) continue;
+    int rank = 0;
+    for (int i = 0; i < a.E; ++i) {
+      const double o = s.logits[i];
+      rank += o > v || (o == v && i < e);
+    }
+    if (rank < a.top_k) s.chosen[rank] = e, s.best[rank] = v;
   }
+  __syncthreads();
+  const bool any = s.chosen[0] >= 0;
+  const double top = any ? s.best[0] : 0.0;
+  if (!a.renormalise) {
+    double part = 0.0;
+    for (int e = tid; e < a.E; e += THREADS) part += (double)expf((float)(s.logits[e] - top));
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) part += __shfl_xor(part, d);
+    if ((tid & 63) == 0) s.share[tid >> 6] = part;
+    __syncthreads();
+  }
+  if (tid < a.top_k) {
+    double total = 0.0;
+    if (a.renormalise) {
+      for (int k = 0; k < a.top_k; ++k)
+        if (s.chosen[k] >= 0) total += (double)expf((float)(s.best[k] - top));
+    } else {
+      for (int w = 0; w < THREADS / 64; ++w) total += s.share[w];
+    }
+    int chosen = s.chosen[tid];
+    float p = chosen >= 0 ? (float)((double)expf((float)(s.best[tid] - top)) / total) : 0.0f;
+    if (s.bad) chosen = -1, p = __uint_as_float(0x7fc00000u);
+    a.index[row * a.top_k + tid] = chosen;
+    a.weight[row * a.top_k + tid] = p;
+  }
+}
+
+constexpr int kRouteThreads = 1024;
+template <typename T, typename TR>
+__global__ __launch_bounds__(kRouteThreads) void k_route(ExpertArgs a) {
+  __shared__ RouteSpace s;
+  const int64_t row = blockIdx.x;
+  const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+  if (threadIdx.x == 0) s.bad = 0;
+  __syncthreads();
+  // the row's terms, and whether it holds numbers only
+  bool bad = false;
+  for (int c = threadIdx.x * 8; c < a.ld_xt; c += kRouteThreads * 8) {
+    Raw<T> v;
+    v.load(x + c, a.F - c);
+    v.clear(a.F - c);
+    bad |= v.top() >= 0x7f800000u;
+    store_terms(a, row, c, v);
+  }
+  bad |= route_logits<T, TR, kRouteThreads / 64>(a, x, s.logits);
+  if (bad) s.bad = 1;
+  __syncthreads();
+  route_choose<kRouteThreads>(a, row, s);
 }
 
 // --------------------------------------------------------------------------
@@ -173,32 +215,68 @@ struct WeightBlock<false> {
 
 // This workgroup's expert (-1: none) and its pairs (row * top_k + place), in order.
 // Up to E pairs a slot is a pair, which stands for its expert if no earlier pair does;
-// otherwise a slot is an expert.
+// otherwise a slot is an expert.  Each wave lists a run of the pairs.
+template <int NW>
 __device__ __forceinline__ int slot_expert(const ExpertArgs& a, int slot, int* list, int& count) {
+  __shared__ int found[NW], seen;
   const int pairs = (int)(a.M * a.top_k);
   const bool by_pair = pairs <= a.E;
   const int e = by_pair ? a.index[slot] : slot;
-  __shared__ int base, seen;
-  if (threadIdx.x == 0) base = 0, seen = 0;
-  __syncthreads();
   if (e < 0) return -1;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  for (int p0 = 0; p0 < pairs; p0 += blockDim.x) {
-    const int p = p0 + threadIdx.x;
-    const bool mine = p < pairs && a.index[p] == e;
-    if (by_pair && mine && p < slot) seen = 1;
-    const uint64_t all = __ballot(mine);
-    for (int w = 0; w < waves; ++w) {  // (in order, wave by wave)
-      if (w == wave) {
-        if (mine) list[base + __popcll(all & lanemask_lt())] = p;
-      }
-      __syncthreads();
-      if (w == wave && lane == 0) base += __popcll(all);
-      __syncthreads();
-    }
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int run = (pairs + NW * 64 - 1) / (NW * 64) * 64, p0 = wave * run, p1 = min(pairs, p0 + run);
+  if (threadIdx.x == 0) seen = 0;
+  __syncthreads();
+  int mine = 0;
+  for (int p = p0; p < p1; p += 64) {
+    const bool is = p + lane < p1 && a.index[p + lane] == e;
+    if (by_pair && is && p + lane < slot) seen = 1;
+    mine += __popcll(__ballot(is));
   }
-  count = base;
-  return seen || count == 0 ? -1 : e;
+  if (lane == 0) found[wave] = mine;
+  __syncthreads();
+  int base = 0;
+  count = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    if (w < wave) base += found[w];
+    count += found[w];
+  }
+  if (seen || count == 0) return -1;
+  for (int p = p0; p < p1; p += 64) {
+    const bool is = p + lane < p1 && a.index[p + lane] == e;
+    const uint64_t all = __ballot(is);
+    if (is) list[base + __popcll(all & lanemask_lt())] = p + lane;
+    base += __popcll(all);
+  }
+  __syncthreads();
+  return e;
+}
+
+// h of four channels n.. of a pair, to its terms
+__device__ __forceinline__ void store_hidden(const ExpertArgs& a, int e, int pair, int n, const f32x4& first,
+                                             const f32x4& second) {
+  if (n >= a.ld_ht) return;
+  uint32_t term[3][4];
+  const float* bias = a.up_bias ? a.up_bias + (int64_t)e * a.H * (a.gated ? 2 : 1) : nullptr;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float v = 0.0f;
+    if (n + j < a.H) {
+      v = apply_act(a.act, first[j] + (bias ? bias[n + j] : 0.0f));
+      if (a.gated) v *= second[j] + (bias ? bias[a.H + n + j] : 0.0f);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      // (the last term is rounded: of three it holds what is left)
+      if (t + 1 == a.h_terms) term[t][j] = (uint32_t)f32_to_bf16(v) << 16;
+      else term[t][j] = cut_term(v);
+    }
+    term[2][j] = (uint32_t)f32_to_bf16(v) << 16;
+  }
+  for (int t = 0; t < a.h_terms; ++t)
+    *reinterpret_cast<uint2*>(a.ht + (t * a.M * a.top_k + pair) * a.ld_ht + n) =
+        make_uint2(term[t][0] >> 16 | term[t][1], term[t][2] >> 16 | term[t][3]);
 }
 
 template <bool MX4, int TERMS, bool UP, bool GATED>
@@ -207,7 +285,7 @@ __global__ __launch_bounds__(256) void k_expert_product(ExpertArgs a) {
   __shared__ int list[kExpertRows];
   __shared__ f32x4 part[NW][NO][64];
   int count;
-  const int e = slot_expert(a, blockIdx.y, list, count);
+  const int e = slot_expert<NW>(a, blockIdx.y, list, count);
   if (e < 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int quarter = lane >> 4, lr = lane & 15;
@@ -260,33 +338,136 @@ __global__ __launch_bounds__(256) void k_expert_product(ExpertArgs a) {
         for (int k = 1; k < NW; ++k) acc[o] += part[k][o][lane];
       if (i0 + lr < count) {
         if constexpr (UP) {
-          uint32_t term[3][4];
-          const float* bias = a.up_bias ? a.up_bias + (int64_t)e * N * NO : nullptr;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float v = 0.0f;
-            if (n + j < N) {
-              v = apply_act(a.act, acc[0][j] + (bias ? bias[n + j] : 0.0f));
-              if constexpr (GATED) v *= acc[NO - 1][j] + (bias ? bias[N + n + j] : 0.0f);
-            }
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              // (the last term is rounded: of three it holds what is left)
-              if (t + 1 == a.h_terms) term[t][j] = (uint32_t)f32_to_bf16(v) << 16;
-              else term[t][j] = cut_term(v);
-            }
-            term[2][j] = (uint32_t)f32_to_bf16(v) << 16;
-          }
-          if (n < a.ld_ht)
-            for (int t = 0; t < a.h_terms; ++t)
-              *reinterpret_cast<uint2*>(a.ht + (t * a.M * a.top_k + pair) * a.ld_ht + n) =
-                  make_uint2(term[t][0] >> 16 | term[t][1], term[t][2] >> 16 | term[t][3]);
+          store_hidden(a, e, pair, n, acc[0], acc[NO - 1]);
         } else if (n < N) {
           *reinterpret_cast<f32x4*>(a.part + pair * a.ld_part + n) = acc[0];
         }
       }
     }
     __syncthreads();
+  }
+}
+
+// --------------------------------------------------------------------------
+// the same where the experts' weights take most of the time: a workgroup of NW waves
+// holds 32 NW rows of an expert's weights (32 a wave: gate and up of 16 channels, or 32
+// channels) and RT tiles of 16 rows of x.  A wave reads its weights from memory into
+// registers, AHEAD steps of 128 k ahead; the rows of x go through LDS, two steps in turn,
+// where all waves read them.  One barrier a step.
+// --------------------------------------------------------------------------
+template <bool MX4, int TERMS, bool UP, int RT, int NW>
+__global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
+  constexpr int AHEAD = RT == 1 && MX4 ? 4 : 2, ROWS = RT * 16;
+  constexpr int PIECES = (ROWS * 16 * TERMS + 64 * NW - 1) / (64 * NW);  // 16-byte pieces a thread stages a step
+  static_assert(ROWS * 16 * TERMS % (64 * NW) == 0, "whole pieces");
+  extern __shared__ uint4 space[];  // x: two steps of TERMS x ROWS x 16 pieces, then the list
+  u32x4* const xs = reinterpret_cast<u32x4*>(space);
+  constexpr int STEP = TERMS * ROWS * 16;
+  int* const list = reinterpret_cast<int*>(space + 2 * STEP);
+  int count;
+  const int e = slot_expert<NW>(a, blockIdx.y, list, count);
+  if (e < 0) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int quarter = lane >> 4, lr = lane & 15;
+  const int K = UP ? a.F : a.H, N = UP ? a.H : a.N;
+  const bool gated = UP && a.gated;
+  const int all = (K + 127) / 128, per = UP ? all : (all + a.splits - 1) / a.splits;
+  const int s0 = UP ? 0 : blockIdx.z * per, s1 = UP ? all : min(all, s0 + per);
+  const int64_t ld = UP ? a.ld_xt : a.ld_ht, plane = (UP ? a.M : a.M * a.top_k) * ld;
+  const uint16_t* const rows = UP ? a.xt : a.ht;
+  const int n0 = ((int)blockIdx.x * NW + wave) * (gated ? 16 : 32);
+  WeightBlock<MX4> w[AHEAD][2];
+#pragma unroll
+  for (int o = 0; o < 2; ++o) {
+    const int64_t r = gated ? ((int64_t)e * 2 + o) * N + min(n0 + lr, N - 1)
+                            : (int64_t)e * N + min(n0 + o * 16 + lr, N - 1);
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) {
+      if (UP) w[d][o].at(a.up, a.ld_up, a.up_scale, a.lds_up, r);
+      else w[d][o].at(a.down, a.ld_down, a.down_scale, a.lds_down, r);
+    }
+  }
+  for (int i0 = 0; i0 < count; i0 += ROWS) {
+    const int here = min(count - i0, ROWS), tiles = (here + 15) / 16;
+    // the pieces that this thread stages: term t, row r, piece p of the step
+    const uint16_t* from[PIECES];
+    u32x4 piece[PIECES];
+    int col[PIECES], to[PIECES];
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j) {
+      const int i = j * 64 * NW + threadIdx.x, p = i & 15, r = (i >> 4) % ROWS, t = (i >> 4) / ROWS;
+      const int pair = list[i0 + min(r, here - 1)];
+      from[j] = rows + t * plane + (UP ? pair / a.top_k : pair) * ld + p * 8;
+      col[j] = p * 8;
+      to[j] = (t * ROWS + r) * 16 + (p ^ (r & 15));
+    }
+    const auto fetch = [&](int s) {
+#pragma unroll
+      for (int j = 0; j < PIECES; ++j) {
+        piece[j] = u32x4{0u, 0u, 0u, 0u};
+        if (s * 128 + col[j] < ld) piece[j] = *reinterpret_cast<const u32x4*>(from[j] + s * 128);
+      }
+    };
+    const auto put = [&](int s) {
+#pragma unroll
+      for (int j = 0; j < PIECES; ++j) xs[(s & 1) * STEP + to[j]] = piece[j];
+    };
+    f32x4 acc[RT][2];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[r][0] = acc[r][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    fetch(s0);
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d)
+      if (s0 + d < s1) w[d][0].load((s0 + d) * 4 + quarter, K), w[d][1].load((s0 + d) * 4 + quarter, K);
+    put(s0);
+    if (s0 + 1 < s1) fetch(s0 + 1);
+    for (int sb = s0; sb < s1; sb += AHEAD) {
+#pragma unroll
+      for (int d = 0; d < AHEAD; ++d) {
+        const int s = sb + d;
+        if (s < s1) {
+          ring_barrier();  // step s is in LDS, and nobody reads step s - 1 any more
+          if (s + 1 < s1) put(s + 1);
+          if (s + 2 < s1) fetch(s + 2);
+          const int b = s * 4 + quarter;
+          bf16x8 wv[2][4];
+#pragma unroll
+          for (int o = 0; o < 2; ++o) w[d][o].take(b, K, wv[o]);
+          if (s + AHEAD < s1) w[d][0].load(b + 4 * AHEAD, K), w[d][1].load(b + 4 * AHEAD, K);
+          const u32x4* const x = xs + (s & 1) * STEP + lr * 16;
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            if (RT == 1 || r < tiles) {
+#pragma unroll
+              for (int p = 0; p < TERMS; ++p)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                  const u32x4 v = x[(p * ROWS + r * 16) * 16 + ((quarter * 4 + t) ^ lr)];
+                  bf16x8 xv;
+                  __builtin_memcpy(&xv, &v, 16);
+#pragma unroll
+                  for (int o = 0; o < 2; ++o)
+                    acc[r][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[o][t], xv, acc[r][o], 0, 0, 0);
+                }
+            }
+          }
+        }
+      }
+    }
+    ring_barrier();  // (the next rows' first step takes the place of one that may still be read)
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      if (r * 16 + lr >= here) continue;
+      const int pair = list[i0 + r * 16 + lr], n = n0 + quarter * 4;
+      if constexpr (UP) {
+        store_hidden(a, e, pair, n, acc[r][0], acc[r][1]);
+        if (!gated) store_hidden(a, e, pair, n + 16, acc[r][1], acc[r][1]);
+      } else {
+        float* const o = a.part + (blockIdx.z * a.M * a.top_k + pair) * a.ld_part + n;
+        if (n < N) *reinterpret_cast<f32x4*>(o) = acc[r][0];
+        if (n + 16 < N) *reinterpret_cast<f32x4*>(o + 16) = acc[r][1];
+      }
+    }
   }
 }
 
@@ -302,7 +483,9 @@ __global__ __launch_bounds__(256) void k_expert_sum(ExpertArgs a) {
       const int e = a.index[pair];
       const float p = a.weight[pair];
       f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (e >= 0) d = *reinterpret_cast<const f32x4*>(a.part + pair * a.ld_part + n);
+      if (e >= 0)
+        for (int z = 0; z < a.splits; ++z)
+          d += *reinterpret_cast<const f32x4*>(a.part + (z * a.M * a.top_k + pair) * a.ld_part + n);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (e >= 0 && a.down_bias && n + j < a.N) d[j] += a.down_bias[(int64_t)e * a.N + n + j];
@@ -318,15 +501,49 @@ __global__ __launch_bounds__(256) void k_expert_sum(ExpertArgs a) {
   }
 }
 
+// Whether the wide kernels take the products: their workgroups fill the CUs
+bool experts_wide(int64_t M, int64_t H, int64_t N, int E, int top_k, bool gated) {
+  const int64_t slots = std::min<int64_t>(M * top_k, E);
+  return slots * ((H * (gated ? 2 : 1) + 127) / 128) >= 256;
+}
+// parts of k of the second product, so that it has workgroups enough
+int expert_splits(int64_t M, int64_t H, int64_t N, int E, int top_k) {
+  const int64_t slots = std::min<int64_t>(M * top_k, E), wgs = slots * ((N + 127) / 128), steps = (H + 127) / 128;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({8, 512 / wgs, steps / 4}));
+}
+
+template <bool MX4, int TERMS, bool UP, int RT, int NW>
+hipError_t launch_wide(const ExpertArgs& a, hipStream_t st) {
+  const unsigned slots = (unsigned)std::min<int64_t>(a.M * a.top_k, a.E);
+  const int per = NW * (UP && a.gated ? 16 : 32), n = UP ? a.H : a.N;
+  const size_t lds = (size_t)2 * TERMS * RT * 16 * 16 * 16 + (size_t)a.M * 4;
+  hipLaunchKernelGGL((k_expert_wide<MX4, TERMS, UP, RT, NW>),
+                     dim3((unsigned)((n + per - 1) / per), slots, UP ? 1 : a.splits), dim3(64 * NW), lds, st, a);
+  return hipGetLastError();
+}
+template <bool MX4, int TERMS, bool UP>
+hipError_t dispatch_wide(const ExpertArgs& a, hipStream_t st) {
+  const int64_t mean = a.M * a.top_k / a.E;
+  if (a.M <= 16 || mean <= 8) return launch_wide<MX4, TERMS, UP, 1, 4>(a, st);
+  if constexpr (MX4 && TERMS < 3)
+    if (mean > 48) return launch_wide<MX4, TERMS, UP, 8, 8>(a, st);
+  return launch_wide<MX4, TERMS, UP, 4, 8>(a, st);
+}
+
 template <bool MX4>
 hipError_t products(const ExpertArgs& a, hipStream_t st) {
+  hipError_t e;
+  if (experts_wide(a.M, a.H, a.N, a.E, a.top_k, a.gated)) {
+    e = a.x_terms == 1 ? dispatch_wide<MX4, 1, true>(a, st) : dispatch_wide<MX4, 3, true>(a, st);
+    if (e != hipSuccess) return e;
+    return a.h_terms == 2 ? dispatch_wide<MX4, 2, false>(a, st) : dispatch_wide<MX4, 3, false>(a, st);
+  }
   const unsigned slots = (unsigned)std::min<int64_t>(a.M * a.top_k, a.E);
   const dim3 up((unsigned)((a.H + 15) / 16), slots), down((unsigned)((a.N + 15) / 16), slots);
   const auto go = [&](auto kernel, dim3 grid) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
     return hipGetLastError();
   };
-  hipError_t e;
   if (a.gated) e = a.x_terms == 1 ? go(k_expert_product<MX4, 1, true, true>, up) : go(k_expert_product<MX4, 3, true, true>, up);
   else e = a.x_terms == 1 ? go(k_expert_product<MX4, 1, true, false>, up) : go(k_expert_product<MX4, 3, true, false>, up);
   if (e != hipSuccess) return e;
@@ -338,10 +555,10 @@ size_t whole(size_t n) { return (n + 255) & ~(size_t)255; }
 // the parts of the workspace, of up to kExpertRows rows
 struct ExpertSpace {
   int64_t rows, ld_xt, ld_ht, ld_part;
-  int x_terms, h_terms;
+  int x_terms, h_terms, splits;
   size_t xt, ht, part, total;
 };
-ExpertSpace expert_space(int dtype, int64_t M, int64_t F, int64_t H, int64_t N, int top_k) {
+ExpertSpace expert_space(int dtype, int64_t M, int64_t F, int64_t H, int64_t N, int E, int top_k, bool gated) {
   ExpertSpace s;
   s.rows = std::min<int64_t>(M, kExpertRows);
   s.x_terms = dtype == SAGA_BF16 ? 1 : 3;
@@ -352,19 +569,20 @@ ExpertSpace expert_space(int dtype, int64_t M, int64_t F, int64_t H, int64_t N, 
   s.xt = 0;
   s.ht = s.xt + whole((size_t)s.x_terms * s.rows * s.ld_xt * 2);
   s.part = s.ht + whole((size_t)s.h_terms * s.rows * top_k * s.ld_ht * 2);
-  s.total = s.part + whole((size_t)s.rows * top_k * s.ld_part * 4);
+  s.splits = experts_wide(s.rows, H, N, E, top_k, gated) ? expert_splits(s.rows, H, N, E, top_k) : 1;
+  s.total = s.part + whole((size_t)s.splits * s.rows * top_k * s.ld_part * 4);
   return s;
 }
 
 }  // namespace
 
-size_t experts_workspace_bytes(int dtype, int64_t M, int64_t F, int64_t H, int64_t N, int top_k) {
-  return M == 0 ? 0 : expert_space(dtype, M, F, H, N, top_k).total;
+size_t experts_workspace_bytes(int dtype, int64_t M, int64_t F, int64_t H, int64_t N, int E, int top_k, bool gated) {
+  return M == 0 ? 0 : expert_space(dtype, M, F, H, N, E, top_k, gated).total;
 }
 
 hipError_t launch_experts(const ExpertArgs& a0, hipStream_t st) {
   if (a0.M == 0) return hipSuccess;
-  const ExpertSpace s = expert_space(a0.dtype, a0.M, a0.F, a0.H, a0.N, a0.top_k);
+  const ExpertSpace s = expert_space(a0.dtype, a0.M, a0.F, a0.H, a0.N, a0.E, a0.top_k, a0.gated);
   const size_t es = a0.dtype == SAGA_BF16 ? 2 : 4;
   for (int64_t m = 0; m < a0.M; m += s.rows) {
     ExpertArgs a = a0;
@@ -382,8 +600,12 @@ hipError_t launch_experts(const ExpertArgs& a0, hipStream_t st) {
     a.ld_part = s.ld_part;
     a.x_terms = s.x_terms;
     a.h_terms = s.h_terms;
+    a.splits = s.splits;
+    if (a.M < s.rows)  // (the rest of many rows: never more parts than there is room for)
+      a.splits = std::min(s.splits, experts_wide(a.M, a.H, a.N, a.E, a.top_k, a.gated)
+                                        ? expert_splits(a.M, a.H, a.N, a.E, a.top_k) : 1);
     const auto route = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)a.M), dim3(256), 0, st, a);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)a.M), dim3(kRouteThreads), 0, st, a);
       return hipGetLastError();
     };
     hipError_t e;

@@ -389,6 +389,18 @@ def test_experts(m, f, h, n, e, top_k, weights, dtype):
         layer.check(x, top_k, act, renorm=(i + f) % 3 != 0)
 
 
+@pytest.mark.parametrize("m,f,h,n,e,top_k", [(3, 130, 20000, 140, 4, 1), (40, 602, 1100, 300, 20, 2),
+                                             (200, 200, 2100, 130, 8, 2), (600, 1000, 700, 515, 24, 4),
+                                             (700, 129, 4500, 100, 4, 1), (1024, 64, 130, 1030, 256, 3)])
+@pytest.mark.parametrize("weights", ["mx4", "bf16"])
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("gated", [False, True])
+def test_large_layers(m, f, h, n, e, top_k, weights, dtype, gated):
+    """weights enough for the kernels that are bounded by them, one row to hundreds an expert"""
+    layer = Layer(m, f, h, n, e, weights, gated, biases=gated)
+    layer.check(torch.randn(m, f, generator=gen(m)).to(dtype), top_k, "sigmoid" if gated else "relu")
+
+
 def test_more_rows_than_one_run():
     """more than 1024 rows: the kernels run for each part, rows of one expert more than a tile"""
     layer = Layer(5, 40, 50, 24, 6, "mx4", True, True)
