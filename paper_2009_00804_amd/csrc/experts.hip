@@ -166,50 +166,71 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(ExpertArgs a) {
   route_choose<kRouteThreads>(a, row, s);
 }
 
-// --------------------------------------------------------------------------
-// an expert's product: 16 channels of one expert and the rows that take it, 16 at a
-// time, k divided among four waves.
-// --------------------------------------------------------------------------
-// 32 k of a channel as four groups of 8 bfloat16 values
+// where a lane reads its channel's weights
+template <bool MX4>
+struct WeightRow {
+  const uint8_t *q, *s;
+  __device__ __forceinline__ void at(const void* w, int64_t ld, const uint8_t* scale, int64_t lds, int64_t row) {
+    q = static_cast<const uint8_t*>(w) + row * ld * (MX4 ? 1 : 2);
+    s = MX4 ? scale + row * lds : nullptr;
+  }
+};
+template <bool MX4, bool UP>
+__device__ __forceinline__ WeightRow<MX4> weight_row(const ExpertArgs& a, int64_t row) {
+  WeightRow<MX4> r;
+  if (UP) r.at(a.up, a.ld_up, a.up_scale, a.lds_up, row);
+  else r.at(a.down, a.ld_down, a.down_scale, a.lds_down, row);
+  return r;
+}
+
+// 32 k of a channel (block b of K columns) as four groups of 8 bfloat16 values.  `load`
+// has no branch, so that many run ahead: past the row's end it reads the row's last
+// piece again, and `clear` has to follow in the last step of a row.
 template <bool MX4>
 struct WeightBlock;
 template <>
 struct WeightBlock<true> {
-  RowSource<uint8_t> s;
-  __device__ __forceinline__ void at(const void* w, int64_t ld, const uint8_t* scale, int64_t lds, int64_t row) {
-    s.at(w, ld, scale, lds, row);
+  u32x4 v;
+  uint32_t scale;
+  __device__ __forceinline__ void load(const WeightRow<true>& r, int b, int K) {
+    const int most = (K - 1) / 32;
+    b = min(b, most);
+    v = *reinterpret_cast<const u32x4*>(r.q + b * 16);
+    scale = r.s[b];
   }
-  __device__ __forceinline__ void load(int b, int K) { s.load(b, K); }
-  __device__ __forceinline__ void take(int b, int K, bf16x8 (&o)[4]) {
-    const Mx4Block m = s.take(b, K);
-    const float f = __uint_as_float(m.scale == 255u ? 0x7fc00000u : m.scale ? m.scale << 23 : 0x00400000u);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const bf16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(m.v[t], f, 0),
-                           __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(m.v[t], f, 1),
-                           __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(m.v[t], f, 2),
-                           __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(m.v[t], f, 3)};
-      __builtin_memcpy(&o[t], p, 16);
-    }
+  __device__ __forceinline__ void clear(int b, int K) {
+    const int left = (K + 1) / 2 - b * 16;
+    if (left < 16) v = clear_bytes(v, left);
+  }
+  // group t
+  __device__ __forceinline__ bf16x8 take(int t) const {
+    const float f = scale_value(scale);
+    const bf16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[t], f, 0),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[t], f, 1),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[t], f, 2),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[t], f, 3)};
+    bf16x8 o;
+    __builtin_memcpy(&o, p, 16);
+    return o;
   }
 };
 template <>
 struct WeightBlock<false> {
-  const uint16_t* p;
   Raw<uint16_t> v[4];
-  __device__ __forceinline__ void at(const void* w, int64_t ld, const uint8_t*, int64_t, int64_t row) {
-    p = static_cast<const uint16_t*>(w) + row * ld;
-  }
-  __device__ __forceinline__ void load(int b, int K) {
+  __device__ __forceinline__ void load(const WeightRow<false>& r, int b, int K) {
+    const int most = (K - 1) / 8 * 8;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) v[t].load(p + b * 32 + t * 8, K - b * 32 - t * 8);
+    for (int t = 0; t < 4; ++t)
+      v[t].load(reinterpret_cast<const uint16_t*>(r.q) + min(b * 32 + t * 8, most), 8);
   }
-  __device__ __forceinline__ void take(int b, int K, bf16x8 (&o)[4]) {
+  __device__ __forceinline__ void clear(int b, int K) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      v[t].clear(K - b * 32 - t * 8);
-      __builtin_memcpy(&o[t], &v[t].v, 16);
-    }
+    for (int t = 0; t < 4; ++t) v[t].clear(K - b * 32 - t * 8);
+  }
+  __device__ __forceinline__ bf16x8 take(int t) const {
+    bf16x8 o;
+    __builtin_memcpy(&o, &v[t].v, 16);
+    return o;
   }
 };
 
@@ -279,9 +300,15 @@ __device__ __forceinline__ void store_hidden(const ExpertArgs& a, int e, int pai
         make_uint2(term[t][0] >> 16 | term[t][1], term[t][2] >> 16 | term[t][3]);
 }
 
+// --------------------------------------------------------------------------
+// an expert's product: 16 channels of one expert and the rows that take it, 16 at a
+// time, k divided among eight waves.  A wave's loads, of the weights and of x, run AHEAD
+// steps of 128 k ahead.  The weights' zeros past a row's end make what x has there not
+// count.
+// --------------------------------------------------------------------------
 template <bool MX4, int TERMS, bool UP, bool GATED>
-__global__ __launch_bounds__(256) void k_expert_product(ExpertArgs a) {
-  constexpr int NW = 4, NO = GATED ? 2 : 1;
+__global__ __launch_bounds__(512) void k_expert_few(ExpertArgs a) {
+  constexpr int NW = 8, NO = GATED ? 2 : 1, AHEAD = TERMS == 1 && (MX4 || NO == 1) ? 4 : 2;
   __shared__ int list[kExpertRows];
   __shared__ f32x4 part[NW][NO][64];
   int count;
@@ -289,42 +316,61 @@ __global__ __launch_bounds__(256) void k_expert_product(ExpertArgs a) {
   if (e < 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int quarter = lane >> 4, lr = lane & 15;
-  const int K = UP ? a.F : a.H, N = UP ? a.H : a.N, n0 = blockIdx.x * 16, steps = (K + 127) / 128;
+  const int K = UP ? a.F : a.H, N = UP ? a.H : a.N, n0 = blockIdx.x * 16, all = (K + 127) / 128;
+  const int steps = (all - wave + NW - 1) / NW;  // of this wave: wave, wave + NW, ..
   const int64_t ld = UP ? a.ld_xt : a.ld_ht, plane = (UP ? a.M : a.M * a.top_k) * ld;
   const uint16_t* const rows = UP ? a.xt : a.ht;
-  WeightBlock<MX4> w[NO];
+  WeightRow<MX4> from[NO];
 #pragma unroll
-  for (int o = 0; o < NO; ++o) {
-    const int64_t r = (int64_t)e * N * NO + (int64_t)o * N + min(n0 + lr, N - 1);
-    if (UP) w[o].at(a.up, a.ld_up, a.up_scale, a.lds_up, r);
-    else w[o].at(a.down, a.ld_down, a.down_scale, a.lds_down, r);
-  }
+  for (int o = 0; o < NO; ++o)
+    from[o] = weight_row<MX4, UP>(a, (int64_t)e * N * NO + (int64_t)o * N + min(n0 + lr, N - 1));
   for (int i0 = 0; i0 < count; i0 += 16) {
     const int pair = list[min(i0 + lr, count - 1)];
     const uint16_t* const x = rows + (UP ? pair / a.top_k : pair) * ld;
+    WeightBlock<MX4> w[AHEAD][NO];
+    u32x4 xv[AHEAD][4][TERMS];
+    const auto load = [&](int d, int i) {
+      const int b = (wave + i * NW) * 4 + quarter;
+#pragma unroll
+      for (int o = 0; o < NO; ++o) w[d][o].load(from[o], b, K);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int p = 0; p < TERMS; ++p)
+          xv[d][t][p] = *reinterpret_cast<const u32x4*>(x + p * plane + min(b * 32 + t * 8, (int)ld - 8));
+    };
     f32x4 acc[NO];
 #pragma unroll
     for (int o = 0; o < NO; ++o) acc[o] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = wave; s < steps; s += NW) {
-      const int b = s * 4 + quarter;
-      bf16x8 wv[NO][4];
 #pragma unroll
-      for (int o = 0; o < NO; ++o) w[o].load(b, K);
+    for (int d = 0; d < AHEAD; ++d) load(d, d);
+    for (int ib = 0; ib < steps; ib += AHEAD) {
 #pragma unroll
-      for (int o = 0; o < NO; ++o) w[o].take(b, K, wv[o]);
+      for (int d = 0; d < AHEAD; ++d) {
+        const int i = ib + d;
+        if (i < steps) {
+          const int b = (wave + i * NW) * 4 + quarter;
+          if (wave + i * NW == all - 1)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int k = b * 32 + t * 8;
+            for (int o = 0; o < NO; ++o) w[d][o].clear(b, K);
 #pragma unroll
-        for (int p = 0; p < TERMS; ++p) {
-          u32x4 v = {0u, 0u, 0u, 0u};
-          if (k < ld) v = *reinterpret_cast<const u32x4*>(x + p * plane + k);
-          bf16x8 xv;
-          __builtin_memcpy(&xv, &v, 16);
+          for (int t = 0; t < 4; ++t) {
+            bf16x8 wv[NO];
 #pragma unroll
-          for (int o = 0; o < NO; ++o)
-            acc[o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[o][t], xv, acc[o], 0, 0, 0);
+            for (int o = 0; o < NO; ++o) wv[o] = w[d][o].take(t);
+#pragma unroll
+            for (int p = 0; p < TERMS; ++p) {
+              bf16x8 v;
+              __builtin_memcpy(&v, &xv[d][t][p], 16);
+#pragma unroll
+              for (int o = 0; o < NO; ++o) acc[o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[o], v, acc[o], 0, 0, 0);
+            }
+          }
         }
+      }
+      if (ib + AHEAD < steps) {
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d) load(d, ib + AHEAD + d);
       }
     }
 #pragma unroll
@@ -349,7 +395,8 @@ __global__ __launch_bounds__(256) void k_expert_product(ExpertArgs a) {
 }
 
 // --------------------------------------------------------------------------
-// the same where the experts' weights take most of the time: a workgroup of NW waves
+// the same where the experts' weights take most of the time and many rows take an expert: a
+// workgroup of NW waves
 // holds 32 NW rows of an expert's weights (32 a wave: gate and up of 16 channels, or 32
 // channels) and RT tiles of 16 rows of x.  A wave reads its weights from memory into
 // registers, AHEAD steps of 128 k ahead; the rows of x go through LDS, two steps in turn,
@@ -357,7 +404,7 @@ __global__ __launch_bounds__(256) void k_expert_product(ExpertArgs a) {
 // --------------------------------------------------------------------------
 template <bool MX4, int TERMS, bool UP, int RT, int NW>
 __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
-  constexpr int AHEAD = RT == 1 && MX4 ? 4 : 2, ROWS = RT * 16;
+  constexpr int AHEAD = 2, ROWS = RT * 16;
   constexpr int PIECES = (ROWS * 16 * TERMS + 64 * NW - 1) / (64 * NW);  // 16-byte pieces a thread stages a step
   static_assert(ROWS * 16 * TERMS % (64 * NW) == 0, "whole pieces");
   extern __shared__ uint4 space[];  // x: two steps of TERMS x ROWS x 16 pieces, then the list
@@ -377,16 +424,11 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
   const uint16_t* const rows = UP ? a.xt : a.ht;
   const int n0 = ((int)blockIdx.x * NW + wave) * (gated ? 16 : 32);
   WeightBlock<MX4> w[AHEAD][2];
+  WeightRow<MX4> weights[2];
 #pragma unroll
-  for (int o = 0; o < 2; ++o) {
-    const int64_t r = gated ? ((int64_t)e * 2 + o) * N + min(n0 + lr, N - 1)
-                            : (int64_t)e * N + min(n0 + o * 16 + lr, N - 1);
-#pragma unroll
-    for (int d = 0; d < AHEAD; ++d) {
-      if (UP) w[d][o].at(a.up, a.ld_up, a.up_scale, a.lds_up, r);
-      else w[d][o].at(a.down, a.ld_down, a.down_scale, a.lds_down, r);
-    }
-  }
+  for (int o = 0; o < 2; ++o)
+    weights[o] = weight_row<MX4, UP>(a, gated ? ((int64_t)e * 2 + o) * N + min(n0 + lr, N - 1)
+                                              : (int64_t)e * N + min(n0 + o * 16 + lr, N - 1));
   for (int i0 = 0; i0 < count; i0 += ROWS) {
     const int here = min(count - i0, ROWS), tiles = (here + 15) / 16;
     // the pieces that this thread stages: term t, row r, piece p of the step
@@ -397,16 +439,14 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
     for (int j = 0; j < PIECES; ++j) {
       const int i = j * 64 * NW + threadIdx.x, p = i & 15, r = (i >> 4) % ROWS, t = (i >> 4) / ROWS;
       const int pair = list[i0 + min(r, here - 1)];
-      from[j] = rows + t * plane + (UP ? pair / a.top_k : pair) * ld + p * 8;
+      from[j] = rows + t * plane + (UP ? pair / a.top_k : pair) * ld;
       col[j] = p * 8;
       to[j] = (t * ROWS + r) * 16 + (p ^ (r & 15));
     }
     const auto fetch = [&](int s) {
 #pragma unroll
-      for (int j = 0; j < PIECES; ++j) {
-        piece[j] = u32x4{0u, 0u, 0u, 0u};
-        if (s * 128 + col[j] < ld) piece[j] = *reinterpret_cast<const u32x4*>(from[j] + s * 128);
-      }
+      for (int j = 0; j < PIECES; ++j)
+        piece[j] = *reinterpret_cast<const u32x4*>(from[j] + min(s * 128 + col[j], (int)ld - 8));
     };
     const auto put = [&](int s) {
 #pragma unroll
@@ -417,27 +457,34 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
     for (int r = 0; r < RT; ++r) acc[r][0] = acc[r][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     fetch(s0);
 #pragma unroll
-    for (int d = 0; d < AHEAD; ++d)
-      if (s0 + d < s1) w[d][0].load((s0 + d) * 4 + quarter, K), w[d][1].load((s0 + d) * 4 + quarter, K);
+    for (int d = 0; d < AHEAD; ++d) {
+      w[d][0].load(weights[0], (s0 + d) * 4 + quarter, K);
+      w[d][1].load(weights[1], (s0 + d) * 4 + quarter, K);
+    }
     put(s0);
-    if (s0 + 1 < s1) fetch(s0 + 1);
+    fetch(s0 + 1);
     for (int sb = s0; sb < s1; sb += AHEAD) {
 #pragma unroll
       for (int d = 0; d < AHEAD; ++d) {
         const int s = sb + d;
         if (s < s1) {
           ring_barrier();  // step s is in LDS, and nobody reads step s - 1 any more
-          if (s + 1 < s1) put(s + 1);
-          if (s + 2 < s1) fetch(s + 2);
+          put(s + 1);
+          fetch(s + 2);
           const int b = s * 4 + quarter;
           bf16x8 wv[2][4];
 #pragma unroll
-          for (int o = 0; o < 2; ++o) w[d][o].take(b, K, wv[o]);
-          if (s + AHEAD < s1) w[d][0].load(b + 4 * AHEAD, K), w[d][1].load(b + 4 * AHEAD, K);
+          for (int o = 0; o < 2; ++o) {
+            if (s == all - 1) w[d][o].clear(b, K);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) wv[o][t] = w[d][o].take(t);
+          }
+          w[d][0].load(weights[0], b + 4 * AHEAD, K);
+          w[d][1].load(weights[1], b + 4 * AHEAD, K);
           const u32x4* const x = xs + (s & 1) * STEP + lr * 16;
 #pragma unroll
           for (int r = 0; r < RT; ++r) {
-            if (RT == 1 || r < tiles) {
+            if (r < tiles) {
 #pragma unroll
               for (int p = 0; p < TERMS; ++p)
 #pragma unroll
@@ -468,6 +515,133 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
         if (n + 16 < N) *reinterpret_cast<f32x4*>(o + 16) = acc[r][1];
       }
     }
+  }
+}
+
+// --------------------------------------------------------------------------
+// the same where the experts' weights take most of the time and few rows take an expert:
+// reading the weights is all that counts.  The rows of x (16 at a time) lie in LDS,
+// all of k if it fits, so that nothing but weights is loaded in the loop: loads come back in
+// their order, and a wait for x would be one for the weights that were asked for before.  A
+// workgroup takes `per` runs of 32 NW rows of weights one after the other, and a wave's
+// loads run AHEAD steps ahead across them.
+// --------------------------------------------------------------------------
+constexpr int kStreamPieces = 2176;  // (four workgroups a CU)
+
+template <bool MX4, int TERMS, bool UP>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k_expert_stream(ExpertArgs a, int runs,
+                                                                                              int per) {
+  constexpr int NW = 4, AHEAD = MX4 && TERMS < 3 ? 4 : 2;
+  static_assert(AHEAD * TERMS * 16 * 16 <= kStreamPieces, "a round of steps fits LDS");
+  __shared__ u32x4 xs[kStreamPieces];
+  __shared__ int list[kExpertRows];
+  int count;
+  const int e = slot_expert<NW>(a, blockIdx.y, list, count);
+  if (e < 0) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int quarter = lane >> 4, lr = lane & 15;
+  const int K = UP ? a.F : a.H, N = UP ? a.H : a.N;
+  const bool gated = UP && a.gated;
+  const int all = (K + 127) / 128, part = UP ? all : (all + a.splits - 1) / a.splits;
+  const int k0 = UP ? 0 : min(all, (int)blockIdx.z * part), steps = UP ? all : min(part, all - k0);  // from step k0 on
+  const int64_t ld = UP ? a.ld_xt : a.ld_ht, plane = (UP ? a.M : a.M * a.top_k) * ld;
+  const uint16_t* const rows = UP ? a.xt : a.ht;
+  const int run0 = blockIdx.x * per, run1 = min(runs, run0 + per);
+  const auto channel = [&](int run) { return (run * NW + wave) * (gated ? 16 : 32); };
+  WeightRow<MX4> from[2];
+  const auto rows_of = [&](int run) {
+    const int n = channel(run) + lr;
+    from[0] = weight_row<MX4, UP>(a, (int64_t)e * N * (gated ? 2 : 1) + min(n, N - 1));
+    from[1] = weight_row<MX4, UP>(a, gated ? ((int64_t)e * 2 + 1) * N + min(n, N - 1) : (int64_t)e * N + min(n + 16, N - 1));
+  };
+  WeightBlock<MX4> w[AHEAD][2];
+  const auto load = [&](int d, int s) {
+    w[d][0].load(from[0], (k0 + s) * 4 + quarter, K);
+    w[d][1].load(from[1], (k0 + s) * 4 + quarter, K);
+  };
+  for (int i0 = 0; i0 < count; i0 += 16) {
+    const int here = min(count - i0, 16), a_step = here * TERMS * 16;
+    const int fit = kStreamPieces / a_step, chunk = fit >= steps ? steps : fit / AHEAD * AHEAD;
+    const auto stage = [&](int first) {  // (what lies past a row's end does not count: weights are zeros there)
+      const int n = min(chunk, steps - first) * a_step;
+      for (int i = threadIdx.x; i < n; i += 4 * 256) {
+        u32x4 v[4];
+        int to[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int at = min(i + j * 256, n - 1), p = at & 15, q = at >> 4, r = q % here, st = q / here;
+          const int t = st % TERMS, k = (k0 + first + st / TERMS) * 128 + p * 8, pair = list[i0 + r];
+          v[j] = *reinterpret_cast<const u32x4*>(rows + t * plane + (UP ? pair / a.top_k : pair) * ld +
+                                                 min(k, (int)ld - 8));
+          to[j] = (q << 4) + (p ^ r);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) xs[to[j]] = v[j];
+      }
+    };
+    rows_of(run0);
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) load(d, d);
+    const bool whole = chunk >= steps;
+    if (whole) {
+      stage(0);
+      __syncthreads();
+    }
+    const int row = min(lr, here - 1);  // (rows past the last: not stored)
+    for (int run = run0; run < run1; ++run) {
+      f32x4 acc[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+      for (int sb = 0; sb < steps; sb += AHEAD) {
+        if (!whole && sb % chunk == 0) {
+          __syncthreads();
+          stage(sb);
+          __syncthreads();
+        }
+        // What the places of the ring hold next: of this run, or of the next one (of the
+        // last run again, unused).  Steps past a run's last have its last piece for weights,
+        // cleared: there is no branch around what is loaded, which would end in waits for it.
+        int next = sb + AHEAD;
+        if (next >= steps) {
+          next = 0;
+          rows_of(min(run + 1, run1 - 1));
+        }
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d) {
+          const int s = sb + d;
+          if (s >= steps || k0 + s == all - 1) {
+            const int b = s >= steps ? all * 4 : (k0 + s) * 4 + quarter;
+            w[d][0].clear(b, K);
+            w[d][1].clear(b, K);
+          }
+          const int at = min(s, steps - 1);
+          const u32x4* const x = xs + (whole ? at : at % chunk) * a_step + row * 16;
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const bf16x8 wv[2] = {w[d][0].take(t), w[d][1].take(t)};
+#pragma unroll
+            for (int p = 0; p < TERMS; ++p) {
+              const u32x4 v = x[p * here * 16 + ((quarter * 4 + t) ^ row)];
+              bf16x8 xv;
+              __builtin_memcpy(&xv, &v, 16);
+              acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[0], xv, acc[0], 0, 0, 0);
+              acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[1], xv, acc[1], 0, 0, 0);
+            }
+          }
+          load(d, next + d);
+        }
+      }
+      if (lr < here) {
+        const int pair = list[i0 + lr], n = channel(run) + quarter * 4;
+        if constexpr (UP) {
+          store_hidden(a, e, pair, n, acc[0], acc[1]);
+          if (!gated) store_hidden(a, e, pair, n + 16, acc[1], acc[1]);
+        } else {
+          float* const o = a.part + (blockIdx.z * a.M * a.top_k + pair) * a.ld_part + n;
+          if (n < N) *reinterpret_cast<f32x4*>(o) = acc[0];
+          if (n + 16 < N) *reinterpret_cast<f32x4*>(o + 16) = acc[1];
+        }
+      }
+    }
+    __syncthreads();  // (the next rows take x's place)
   }
 }
 
@@ -524,7 +698,14 @@ hipError_t launch_wide(const ExpertArgs& a, hipStream_t st) {
 template <bool MX4, int TERMS, bool UP>
 hipError_t dispatch_wide(const ExpertArgs& a, hipStream_t st) {
   const int64_t mean = a.M * a.top_k / a.E;
-  if (a.M <= 16 || mean <= 8) return launch_wide<MX4, TERMS, UP, 1, 4>(a, st);
+  if (a.M <= 16 || mean <= 8) {
+    const int64_t slots = std::min<int64_t>(a.M * a.top_k, a.E), rows = UP ? (int64_t)a.H * (a.gated ? 2 : 1) : a.N;
+    const int64_t z = UP ? 1 : a.splits, runs = (rows + 127) / 128, per = std::max<int64_t>(1, runs * slots * z / 1024);
+    hipLaunchKernelGGL((k_expert_stream<MX4, TERMS, UP>),
+                       dim3((unsigned)((runs + per - 1) / per), (unsigned)slots, (unsigned)z), dim3(256), 0, st, a,
+                       (int)runs, (int)per);
+    return hipGetLastError();
+  }
   if constexpr (MX4 && TERMS < 3)
     if (mean > 48) return launch_wide<MX4, TERMS, UP, 8, 8>(a, st);
   return launch_wide<MX4, TERMS, UP, 4, 8>(a, st);
@@ -541,13 +722,13 @@ hipError_t products(const ExpertArgs& a, hipStream_t st) {
   const unsigned slots = (unsigned)std::min<int64_t>(a.M * a.top_k, a.E);
   const dim3 up((unsigned)((a.H + 15) / 16), slots), down((unsigned)((a.N + 15) / 16), slots);
   const auto go = [&](auto kernel, dim3 grid) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(kernel, grid, dim3(512), 0, st, a);
     return hipGetLastError();
   };
-  if (a.gated) e = a.x_terms == 1 ? go(k_expert_product<MX4, 1, true, true>, up) : go(k_expert_product<MX4, 3, true, true>, up);
-  else e = a.x_terms == 1 ? go(k_expert_product<MX4, 1, true, false>, up) : go(k_expert_product<MX4, 3, true, false>, up);
+  if (a.gated) e = a.x_terms == 1 ? go(k_expert_few<MX4, 1, true, true>, up) : go(k_expert_few<MX4, 3, true, true>, up);
+  else e = a.x_terms == 1 ? go(k_expert_few<MX4, 1, true, false>, up) : go(k_expert_few<MX4, 3, true, false>, up);
   if (e != hipSuccess) return e;
-  return a.h_terms == 2 ? go(k_expert_product<MX4, 2, false, false>, down) : go(k_expert_product<MX4, 3, false, false>, down);
+  return a.h_terms == 2 ? go(k_expert_few<MX4, 2, false, false>, down) : go(k_expert_few<MX4, 3, false, false>, down);
 }
 
 size_t whole(size_t n) { return (n + 255) & ~(size_t)255; }

@@ -58,11 +58,6 @@ __global__ __launch_bounds__(256) void k_quantize_mx4(Mx4RowsArgs a) {
   }
 }
 
-// the scale of a byte
-__device__ __forceinline__ float scale_value(uint32_t byte) {
-  return __uint_as_float(byte == 255u ? 0x7fc00000u : byte ? byte << 23 : 0x00400000u);
-}
-
 template <typename T, int G, int U>
 __global__ __launch_bounds__(256) void k_dequantize_mx4(Mx4RowsArgs a) {
   for (int64_t row = blockIdx.x * (int64_t)(256 / G) + threadIdx.x / G; row < a.M;

@@ -54,7 +54,14 @@ __device__ __forceinline__ uint32_t round_mx4(const Raw<float>& r, const BlockSc
   return b.bad ? 0u : o;
 }
 
-// bytes past `left` cleared (left below 16, and above 0)
+// a scale byte's value: 2^(byte - 127), 0 below the normal numbers, 255 a NaN (both by the
+// bit that is set then: no branch)
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+  const uint32_t ends = ((byte + 1u) & 255u) < 2u ? 0x00400000u : 0u;
+  return __uint_as_float(byte << 23 | ends);
+}
+
+// bytes past `left` cleared (left below 16)
 __device__ __forceinline__ u32x4 clear_bytes(u32x4 v, int left) {
 #pragma unroll
   for (int d = 0; d < 4; ++d) {
