@@ -183,39 +183,47 @@ __device__ __forceinline__ WeightRow<MX4> weight_row(const ExpertArgs& a, int64_
   return r;
 }
 
-// 32 k of a channel (block b of K columns) as four groups of 8 bfloat16 values.  `load`
-// has no branch, so that many run ahead: past the row's end it reads the row's last
-// piece again, and `clear` has to follow in the last step of a row.
-template <bool MX4>
-struct WeightBlock;
-template <>
-struct WeightBlock<true> {
-  u32x4 v;
-  uint32_t scale;
+// A lane's weights of one step: J blocks of 32 k of a channel (b.. of K columns), each four
+// groups of 8 bfloat16 values.  `load` has no branch, so that many run ahead: past the
+// row's end it reads the row's last piece again, and `clear` has to follow in the last step
+// of a row.  Two blocks of 4-bit weights are 32 bytes: four lanes take a whole line, and
+// half as many loads of scales are needed.
+template <bool MX4, int J>
+struct WeightBlocks;
+template <int J>
+struct WeightBlocks<true, J> {
+  static_assert(J == 1 || J == 2, "one load for the scales");
+  u32x4 v[J];
+  uint32_t scale;  // a byte for each block
   __device__ __forceinline__ void load(const WeightRow<true>& r, int b, int K) {
     const int most = (K - 1) / 32;
-    b = min(b, most);
-    v = *reinterpret_cast<const u32x4*>(r.q + b * 16);
-    scale = r.s[b];
+#pragma unroll
+    for (int j = 0; j < J; ++j) v[j] = *reinterpret_cast<const u32x4*>(r.q + min(b + j, most) * 16);
+    if constexpr (J == 1) scale = r.s[min(b, most)];
+    else scale = *reinterpret_cast<const uint16_t*>(r.s + min(b, most / 2 * 2));  // (rows are whole 4 bytes)
   }
   __device__ __forceinline__ void clear(int b, int K) {
-    const int left = (K + 1) / 2 - b * 16;
-    if (left < 16) v = clear_bytes(v, left);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int left = (K + 1) / 2 - (b + j) * 16;
+      if (left < 16) v[j] = clear_bytes(v[j], left);
+      if (left <= 0) scale = (scale & ~(255u << (8 * j))) | 127u << (8 * j);
+    }
   }
-  // group t
-  __device__ __forceinline__ bf16x8 take(int t) const {
-    const float f = scale_value(scale);
-    const bf16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[t], f, 0),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[t], f, 1),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[t], f, 2),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[t], f, 3)};
+  __device__ __forceinline__ bf16x8 take(int j, int t) const {
+    const float f = scale_value(J == 1 ? scale : (scale >> (8 * j)) & 255u);
+    const uint32_t d = v[j][t];
+    const bf16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, f, 0),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, f, 1),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, f, 2),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, f, 3)};
     bf16x8 o;
     __builtin_memcpy(&o, p, 16);
     return o;
   }
 };
 template <>
-struct WeightBlock<false> {
+struct WeightBlocks<false, 1> {
   Raw<uint16_t> v[4];
   __device__ __forceinline__ void load(const WeightRow<false>& r, int b, int K) {
     const int most = (K - 1) / 8 * 8;
@@ -227,7 +235,7 @@ struct WeightBlock<false> {
 #pragma unroll
     for (int t = 0; t < 4; ++t) v[t].clear(K - b * 32 - t * 8);
   }
-  __device__ __forceinline__ bf16x8 take(int t) const {
+  __device__ __forceinline__ bf16x8 take(int, int t) const {
     bf16x8 o;
     __builtin_memcpy(&o, &v[t].v, 16);
     return o;
@@ -327,7 +335,7 @@ __global__ __launch_bounds__(512) void k_expert_few(ExpertArgs a) {
   for (int i0 = 0; i0 < count; i0 += 16) {
     const int pair = list[min(i0 + lr, count - 1)];
     const uint16_t* const x = rows + (UP ? pair / a.top_k : pair) * ld;
-    WeightBlock<MX4> w[AHEAD][NO];
+    WeightBlocks<MX4, 1> w[AHEAD][NO];
     u32x4 xv[AHEAD][4][TERMS];
     const auto load = [&](int d, int i) {
       const int b = (wave + i * NW) * 4 + quarter;
@@ -357,7 +365,7 @@ __global__ __launch_bounds__(512) void k_expert_few(ExpertArgs a) {
           for (int t = 0; t < 4; ++t) {
             bf16x8 wv[NO];
 #pragma unroll
-            for (int o = 0; o < NO; ++o) wv[o] = w[d][o].take(t);
+            for (int o = 0; o < NO; ++o) wv[o] = w[d][o].take(0, t);
 #pragma unroll
             for (int p = 0; p < TERMS; ++p) {
               bf16x8 v;
@@ -423,7 +431,7 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
   const int64_t ld = UP ? a.ld_xt : a.ld_ht, plane = (UP ? a.M : a.M * a.top_k) * ld;
   const uint16_t* const rows = UP ? a.xt : a.ht;
   const int n0 = ((int)blockIdx.x * NW + wave) * (gated ? 16 : 32);
-  WeightBlock<MX4> w[AHEAD][2];
+  WeightBlocks<MX4, 1> w[AHEAD][2];
   WeightRow<MX4> weights[2];
 #pragma unroll
   for (int o = 0; o < 2; ++o)
@@ -477,7 +485,7 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
           for (int o = 0; o < 2; ++o) {
             if (s == all - 1) w[d][o].clear(b, K);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) wv[o][t] = w[d][o].take(t);
+            for (int t = 0; t < 4; ++t) wv[o][t] = w[d][o].take(0, t);
           }
           w[d][0].load(weights[0], b + 4 * AHEAD, K);
           w[d][1].load(weights[1], b + 4 * AHEAD, K);
@@ -526,13 +534,13 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
 // workgroup takes `per` runs of 32 NW rows of weights one after the other, and a wave's
 // loads run AHEAD steps ahead across them.
 // --------------------------------------------------------------------------
-constexpr int kStreamPieces = 2176;  // (four workgroups a CU)
+constexpr int kStreamPieces = 3072;  // (three workgroups a CU)
 
 template <bool MX4, int TERMS, bool UP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k_expert_stream(ExpertArgs a, int runs,
                                                                                               int per) {
-  constexpr int NW = 4, AHEAD = MX4 && TERMS < 3 ? 4 : 2;
-  static_assert(AHEAD * TERMS * 16 * 16 <= kStreamPieces, "a round of steps fits LDS");
+  constexpr int NW = 4, J = MX4 ? 2 : 1, AHEAD = 2;
+  static_assert(AHEAD * TERMS * 16 * 16 * J <= kStreamPieces, "a round of steps fits LDS");
   __shared__ u32x4 xs[kStreamPieces];
   __shared__ int list[kExpertRows];
   int count;
@@ -542,7 +550,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   const int quarter = lane >> 4, lr = lane & 15;
   const int K = UP ? a.F : a.H, N = UP ? a.H : a.N;
   const bool gated = UP && a.gated;
-  const int all = (K + 127) / 128, part = UP ? all : (all + a.splits - 1) / a.splits;
+  const int all = (K + 128 * J - 1) / (128 * J), part = UP ? all : (all + a.splits - 1) / a.splits;
   const int k0 = UP ? 0 : min(all, (int)blockIdx.z * part), steps = UP ? all : min(part, all - k0);  // from step k0 on
   const int64_t ld = UP ? a.ld_xt : a.ld_ht, plane = (UP ? a.M : a.M * a.top_k) * ld;
   const uint16_t* const rows = UP ? a.xt : a.ht;
@@ -554,13 +562,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
     from[0] = weight_row<MX4, UP>(a, (int64_t)e * N * (gated ? 2 : 1) + min(n, N - 1));
     from[1] = weight_row<MX4, UP>(a, gated ? ((int64_t)e * 2 + 1) * N + min(n, N - 1) : (int64_t)e * N + min(n + 16, N - 1));
   };
-  WeightBlock<MX4> w[AHEAD][2];
+  WeightBlocks<MX4, J> w[AHEAD][2];
   const auto load = [&](int d, int s) {
-    w[d][0].load(from[0], (k0 + s) * 4 + quarter, K);
-    w[d][1].load(from[1], (k0 + s) * 4 + quarter, K);
+    w[d][0].load(from[0], ((k0 + s) * 4 + quarter) * J, K);
+    w[d][1].load(from[1], ((k0 + s) * 4 + quarter) * J, K);
   };
   for (int i0 = 0; i0 < count; i0 += 16) {
-    const int here = min(count - i0, 16), a_step = here * TERMS * 16;
+    const int here = min(count - i0, 16), a_step = here * TERMS * 16 * J;
     const int fit = kStreamPieces / a_step, chunk = fit >= steps ? steps : fit / AHEAD * AHEAD;
     const auto stage = [&](int first) {  // (what lies past a row's end does not count: weights are zeros there)
       const int n = min(chunk, steps - first) * a_step;
@@ -569,11 +577,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
         int to[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int at = min(i + j * 256, n - 1), p = at & 15, q = at >> 4, r = q % here, st = q / here;
-          const int t = st % TERMS, k = (k0 + first + st / TERMS) * 128 + p * 8, pair = list[i0 + r];
+          const int at = min(i + j * 256, n - 1), p = at % (16 * J), q = at / (16 * J), r = q % here, st = q / here;
+          const int t = st % TERMS, k = ((k0 + first + st / TERMS) * 16 * J + p) * 8, pair = list[i0 + r];
           v[j] = *reinterpret_cast<const u32x4*>(rows + t * plane + (UP ? pair / a.top_k : pair) * ld +
                                                  min(k, (int)ld - 8));
-          to[j] = (q << 4) + (p ^ r);
+          to[j] = q * 16 * J + (p ^ r);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) xs[to[j]] = v[j];
@@ -608,24 +616,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
         for (int d = 0; d < AHEAD; ++d) {
           const int s = sb + d;
           if (s >= steps || k0 + s == all - 1) {
-            const int b = s >= steps ? all * 4 : (k0 + s) * 4 + quarter;
+            const int b = s >= steps ? all * 4 * J : ((k0 + s) * 4 + quarter) * J;
             w[d][0].clear(b, K);
             w[d][1].clear(b, K);
           }
           const int at = min(s, steps - 1);
-          const u32x4* const x = xs + (whole ? at : at % chunk) * a_step + row * 16;
+          const u32x4* const x = xs + (whole ? at : at % chunk) * a_step + row * 16 * J;
 #pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const bf16x8 wv[2] = {w[d][0].take(t), w[d][1].take(t)};
+          for (int j = 0; j < J; ++j)
 #pragma unroll
-            for (int p = 0; p < TERMS; ++p) {
-              const u32x4 v = x[p * here * 16 + ((quarter * 4 + t) ^ row)];
-              bf16x8 xv;
-              __builtin_memcpy(&xv, &v, 16);
-              acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[0], xv, acc[0], 0, 0, 0);
-              acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[1], xv, acc[1], 0, 0, 0);
+            for (int t = 0; t < 4; ++t) {
+              const bf16x8 wv[2] = {w[d][0].take(j, t), w[d][1].take(j, t)};
+#pragma unroll
+              for (int p = 0; p < TERMS; ++p) {
+                const u32x4 v = x[p * here * 16 * J + (((quarter * J + j) * 4 + t) ^ row)];
+                bf16x8 xv;
+                __builtin_memcpy(&xv, &v, 16);
+                acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[0], xv, acc[0], 0, 0, 0);
+                acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[1], xv, acc[1], 0, 0, 0);
+              }
             }
-          }
           load(d, next + d);
         }
       }
