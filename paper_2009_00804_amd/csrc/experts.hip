@@ -404,21 +404,22 @@ __global__ __launch_bounds__(512) void k_expert_few(ExpertArgs a) {
 
 // --------------------------------------------------------------------------
 // the same where the experts' weights take most of the time and many rows take an expert: a
-// workgroup of NW waves
-// holds 32 NW rows of an expert's weights (32 a wave: gate and up of 16 channels, or 32
-// channels) and RT tiles of 16 rows of x.  A wave reads its weights from memory into
-// registers, AHEAD steps of 128 k ahead; the rows of x go through LDS, two steps in turn,
-// where all waves read them.  One barrier a step.
+// workgroup of NW waves holds 32 NW rows of an expert's weights (32 a wave: gate and up of
+// 16 channels, or 32 channels) and RT tiles of 16 rows of x.  A wave reads its weights from
+// memory into registers, two steps of J blocks a lane ahead; the rows of x go through
+// LDS, the 128 k of one block of all lanes at a time and two of them in turn, where all waves
+// read them.  One barrier for each.  Loads are not inside a branch: where one path has
+// loads and the other none, the compiler waits for all of them.
 // --------------------------------------------------------------------------
 template <bool MX4, int TERMS, bool UP, int RT, int NW>
 __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
-  constexpr int AHEAD = 2, ROWS = RT * 16;
-  constexpr int PIECES = (ROWS * 16 * TERMS + 64 * NW - 1) / (64 * NW);  // 16-byte pieces a thread stages a step
+  constexpr int J = MX4 ? 2 : 1, AHEAD = 2, ROWS = RT * 16;
+  constexpr int PIECES = (ROWS * 16 * TERMS + 64 * NW - 1) / (64 * NW);  // 16-byte pieces a thread stages at a time
   static_assert(ROWS * 16 * TERMS % (64 * NW) == 0, "whole pieces");
-  extern __shared__ uint4 space[];  // x: two steps of TERMS x ROWS x 16 pieces, then the list
+  extern __shared__ uint4 space[];  // x: twice TERMS x ROWS x 16 pieces, then the list
   u32x4* const xs = reinterpret_cast<u32x4*>(space);
-  constexpr int STEP = TERMS * ROWS * 16;
-  int* const list = reinterpret_cast<int*>(space + 2 * STEP);
+  constexpr int PART = TERMS * ROWS * 16;
+  int* const list = reinterpret_cast<int*>(space + 2 * PART);
   int count;
   const int e = slot_expert<NW>(a, blockIdx.y, list, count);
   if (e < 0) return;
@@ -426,73 +427,77 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
   const int quarter = lane >> 4, lr = lane & 15;
   const int K = UP ? a.F : a.H, N = UP ? a.H : a.N;
   const bool gated = UP && a.gated;
-  const int all = (K + 127) / 128, per = UP ? all : (all + a.splits - 1) / a.splits;
+  const int all = (K + 128 * J - 1) / (128 * J), per = UP ? all : (all + a.splits - 1) / a.splits;
   const int s0 = UP ? 0 : blockIdx.z * per, s1 = UP ? all : min(all, s0 + per);
   const int64_t ld = UP ? a.ld_xt : a.ld_ht, plane = (UP ? a.M : a.M * a.top_k) * ld;
   const uint16_t* const rows = UP ? a.xt : a.ht;
   const int n0 = ((int)blockIdx.x * NW + wave) * (gated ? 16 : 32);
-  WeightBlocks<MX4, 1> w[AHEAD][2];
+  WeightBlocks<MX4, J> w[AHEAD][2];
   WeightRow<MX4> weights[2];
 #pragma unroll
   for (int o = 0; o < 2; ++o)
     weights[o] = weight_row<MX4, UP>(a, gated ? ((int64_t)e * 2 + o) * N + min(n0 + lr, N - 1)
                                               : (int64_t)e * N + min(n0 + o * 16 + lr, N - 1));
+  const auto load = [&](int d, int s) {
+    w[d][0].load(weights[0], (s * 4 + quarter) * J, K);
+    w[d][1].load(weights[1], (s * 4 + quarter) * J, K);
+  };
   for (int i0 = 0; i0 < count; i0 += ROWS) {
     const int here = min(count - i0, ROWS), tiles = (here + 15) / 16;
-    // the pieces that this thread stages: term t, row r, piece p of the step
+    // the pieces that this thread stages: term t, row r, piece p (4 quarter + group)
     const uint16_t* from[PIECES];
     u32x4 piece[PIECES];
-    int col[PIECES], to[PIECES];
+    const int p = threadIdx.x & 15, col = (p >> 2) * 32 * J + (p & 3) * 8;
+    int to[PIECES];
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
-      const int i = j * 64 * NW + threadIdx.x, p = i & 15, r = (i >> 4) % ROWS, t = (i >> 4) / ROWS;
+      const int i = j * 4 * NW + (threadIdx.x >> 4), r = i % ROWS, t = i / ROWS;
       const int pair = list[i0 + min(r, here - 1)];
       from[j] = rows + t * plane + (UP ? pair / a.top_k : pair) * ld;
-      col[j] = p * 8;
       to[j] = (t * ROWS + r) * 16 + (p ^ (r & 15));
     }
-    const auto fetch = [&](int s) {
+    // part h: block h % J of step h / J
+    const auto fetch = [&](int h) {
+      const int k = min(h / J * 128 * J + h % J * 32 + col, (int)ld - 8);
 #pragma unroll
-      for (int j = 0; j < PIECES; ++j)
-        piece[j] = *reinterpret_cast<const u32x4*>(from[j] + min(s * 128 + col[j], (int)ld - 8));
+      for (int j = 0; j < PIECES; ++j) piece[j] = *reinterpret_cast<const u32x4*>(from[j] + k);
     };
-    const auto put = [&](int s) {
+    const auto put = [&](int h) {
 #pragma unroll
-      for (int j = 0; j < PIECES; ++j) xs[(s & 1) * STEP + to[j]] = piece[j];
+      for (int j = 0; j < PIECES; ++j) xs[(h & 1) * PART + to[j]] = piece[j];
     };
     f32x4 acc[RT][2];
 #pragma unroll
     for (int r = 0; r < RT; ++r) acc[r][0] = acc[r][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    fetch(s0);
+    fetch(s0 * J);
 #pragma unroll
-    for (int d = 0; d < AHEAD; ++d) {
-      w[d][0].load(weights[0], (s0 + d) * 4 + quarter, K);
-      w[d][1].load(weights[1], (s0 + d) * 4 + quarter, K);
-    }
-    put(s0);
-    fetch(s0 + 1);
+    for (int d = 0; d < AHEAD; ++d) load(d, s0 + d);
+    put(s0 * J);
+    fetch(s0 * J + 1);
     for (int sb = s0; sb < s1; sb += AHEAD) {
 #pragma unroll
       for (int d = 0; d < AHEAD; ++d) {
         const int s = sb + d;
-        if (s < s1) {
-          ring_barrier();  // step s is in LDS, and nobody reads step s - 1 any more
-          put(s + 1);
-          fetch(s + 2);
-          const int b = s * 4 + quarter;
+        if (s >= all - 1) {
+          w[d][0].clear((s * 4 + quarter) * J, K);
+          w[d][1].clear((s * 4 + quarter) * J, K);
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const int h = s * J + j;
+          ring_barrier();  // part h is in LDS, and nobody reads part h - 1 any more
+          put(h + 1);
+          fetch(h + 2);
           bf16x8 wv[2][4];
 #pragma unroll
-          for (int o = 0; o < 2; ++o) {
-            if (s == all - 1) w[d][o].clear(b, K);
+          for (int o = 0; o < 2; ++o)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) wv[o][t] = w[d][o].take(0, t);
-          }
-          w[d][0].load(weights[0], b + 4 * AHEAD, K);
-          w[d][1].load(weights[1], b + 4 * AHEAD, K);
-          const u32x4* const x = xs + (s & 1) * STEP + lr * 16;
+            for (int t = 0; t < 4; ++t) wv[o][t] = w[d][o].take(j, t);
+          if (j == J - 1) load(d, s + AHEAD);
+          const u32x4* const x = xs + (h & 1) * PART + lr * 16;
 #pragma unroll
           for (int r = 0; r < RT; ++r) {
-            if (r < tiles) {
+            if (r < tiles && s < s1) {
 #pragma unroll
               for (int p = 0; p < TERMS; ++p)
 #pragma unroll
@@ -509,7 +514,7 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
         }
       }
     }
-    ring_barrier();  // (the next rows' first step takes the place of one that may still be read)
+    ring_barrier();  // (the next rows' first part takes the place of one that may still be read)
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       if (r * 16 + lr >= here) continue;
@@ -523,6 +528,172 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
         if (n + 16 < N) *reinterpret_cast<f32x4*>(o + 16) = acc[r][1];
       }
     }
+  }
+}
+
+// --------------------------------------------------------------------------
+// 4-bit weights and many rows: 256 rows of an expert's weights and RT tiles of 16 rows of x
+// a workgroup.  Both come through LDS by direct-to-LDS loads, 128 k a stage, ST stages:
+// loads come back in their order, and the rows of x, which L2 has, must not wait for weights
+// that were asked for later.  A wave has 64 rows of weights (gate and up of 32 channels, or 64
+// channels) and every second tile of x.
+// --------------------------------------------------------------------------
+typedef __attribute__((address_space(3))) uint4 lds_uint4;
+
+// m0 + the lane's place <- 16 (or 4) bytes of each lane's address
+__device__ __forceinline__ void lds_load16(uint32_t to, const void* from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void lds_load4(uint32_t to, const void* from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
+               : "memory", "m0");
+}
+
+template <int TERMS, int RT, int ST>
+struct ExpertTile {
+  static constexpr int NW = 8, WROWS = 256, ROWS = RT * 16;
+  static constexpr int XL = TERMS * RT * 4 / NW;            // load instructions of a wave for x, 4 rows each
+  static constexpr int LOADS = 2 + 1 + XL;                  // and for weights and scales, a stage
+  static constexpr int W_BYTES = WROWS * 64, S_BYTES = WROWS * 4, X_BYTES = TERMS * ROWS * 256;
+  static constexpr int STAGE = W_BYTES + S_BYTES + X_BYTES;
+  static constexpr int PITCH = WROWS + 4;                   // of the sums on their way out, in floats
+  static constexpr int SUMS = ROWS * PITCH * 4;
+  static constexpr int RING = ST * STAGE > SUMS ? ST * STAGE : SUMS;
+  static constexpr int LDS = RING + kExpertRows * 4;
+  static_assert(TERMS * RT * 4 % NW == 0 && RT % 2 == 0, "the same loads and tiles on every wave");
+  static_assert(LDS <= 160 * 1024 - 64 && (ST - 2) * LOADS < 64, "LDS, waits");
+};
+
+template <int TERMS, bool UP, int RT, int ST>
+__global__ __launch_bounds__(512) void k_expert_tile(ExpertArgs a) {
+  typedef ExpertTile<TERMS, RT, ST> R;
+  extern __shared__ uint4 space[];
+  char* const base = reinterpret_cast<char*>(space);
+  int* const list = reinterpret_cast<int*>(base + R::RING);
+  int count;
+  const int e = slot_expert<R::NW>(a, blockIdx.y, list, count);
+  if (e < 0) return;
+  const uint32_t lds = (uint32_t)(uintptr_t)(lds_uint4*)space;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int quarter = lane >> 4, lr = lane & 15, wm = wave >> 1, wx = wave & 1;
+  const int K = UP ? a.F : a.H, N = UP ? a.H : a.N, bytes = (K + 1) / 2, kmax = (bytes - 1) / 16 * 16;
+  const bool gated = UP && a.gated;
+  const int all = (K + 127) / 128, per = UP ? all : (all + a.splits - 1) / a.splits;
+  const int s0 = UP ? 0 : min(all, (int)blockIdx.z * per), s1 = UP ? all : min(all, s0 + per);
+  const int64_t ld = UP ? a.ld_xt : a.ld_ht, plane = (UP ? a.M : a.M * a.top_k) * ld;
+  const uint16_t* const rows = UP ? a.xt : a.ht;
+  const int n0 = (int)blockIdx.x * (gated ? 128 : 256);
+  // row r of the stage's weights: 64 a wave; gated: gates of 32 channels, then ups
+  const auto weights = [&](int r) {
+    const int64_t row = gated ? ((int64_t)e * 2 + (r >> 5 & 1)) * N + min(n0 + (r >> 6) * 32 + (r & 31), N - 1)
+                              : (int64_t)e * N + min(n0 + r, N - 1);
+    return weight_row<true, UP>(a, row);
+  };
+  const uint8_t* w_at[2];
+  int w_piece[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int r = 16 * (wave + 8 * j) + lane / 4;
+    w_at[j] = weights(r).q;
+    w_piece[j] = ((lane & 3) ^ (r >> 2 & 3)) * 16;
+  }
+  const uint8_t* const s_at = weights(wave * 32 + (lane & 31)).s;
+
+  for (int i0 = 0; i0 < count; i0 += R::ROWS) {
+    const int here = min(count - i0, R::ROWS), tiles = (here + 15) / 16;
+    const uint16_t* x_at[R::XL];
+#pragma unroll
+    for (int j = 0; j < R::XL; ++j) {
+      const int i = (wave + 8 * j) * 4 + (lane >> 4), r = i % R::ROWS, t = i / R::ROWS;
+      const int pair = list[i0 + min(r, here - 1)];
+      x_at[j] = rows + t * plane + (UP ? pair / a.top_k : pair) * ld;
+    }
+    // (loads past a row's end are of its last piece: the weights' zeros make them not count)
+    const auto issue = [&](int s) {
+      const uint32_t to = lds + s % ST * R::STAGE;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) lds_load16(to + (wave + 8 * j) * 1024, w_at[j] + min(s * 64 + w_piece[j], kmax));
+      if (lane < 32) lds_load4(to + R::W_BYTES + wave * 128, s_at + s * 4);
+#pragma unroll
+      for (int j = 0; j < R::XL; ++j) {
+        const int r = (wave + 8 * j) * 4 + (lane >> 4);  // (16 rows a tile: r % 16 whatever the term)
+        lds_load16(to + R::W_BYTES + R::S_BYTES + (wave + 8 * j) * 1024,
+                   x_at[j] + min(s * 128 + ((lane & 15) ^ (r & 15)) * 8, (int)ld - 8));
+      }
+    };
+    f32x4 acc[4][RT / 2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < RT / 2; ++r) acc[i][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int d = 0; d < ST - 1; ++d)
+      if (s0 + d < s1) issue(s0 + d);
+    for (int s = s0; s < s1; ++s) {
+      if (s + ST - 2 < s1) wait_vm<(ST - 2) * R::LOADS>();
+      else wait_vm<0>();
+      ring_barrier();  // stage s is in LDS, and nobody reads stage s - 1 any more
+      if (s + ST - 1 < s1) issue(s + ST - 1);
+      const char* const stage = base + s % ST * R::STAGE;
+      WeightBlocks<true, 1> w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = wm * 64 + i * 16 + lr;
+        w[i].v[0] = *reinterpret_cast<const u32x4*>(stage + r * 64 + (quarter ^ (r >> 2 & 3)) * 16);
+        w[i].scale = *reinterpret_cast<const uint8_t*>(stage + R::W_BYTES + r * 4 + quarter);
+        if (s == all - 1) w[i].clear(s * 4 + quarter, K);
+      }
+      const u32x4* const x = reinterpret_cast<const u32x4*>(stage + R::W_BYTES + R::S_BYTES);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        bf16x8 wv[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) wv[i] = w[i].take(0, t);
+#pragma unroll
+        for (int r = 0; r < RT / 2; ++r) {
+          if (2 * r + wx < tiles) {
+#pragma unroll
+            for (int p = 0; p < TERMS; ++p) {
+              const u32x4 v = x[(p * R::ROWS + (2 * r + wx) * 16 + lr) * 16 + ((quarter * 4 + t) ^ lr)];
+              bf16x8 xv;
+              __builtin_memcpy(&xv, &v, 16);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                acc[i][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], xv, acc[i][r], 0, 0, 0);
+            }
+          }
+        }
+      }
+    }
+    ring_barrier();  // the stages are free: the sums go through them, to leave by whole rows
+    float* const sums = reinterpret_cast<float*>(base);
+#pragma unroll
+    for (int r = 0; r < RT / 2; ++r)
+      if (2 * r + wx < tiles)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<f32x4*>(sums + ((2 * r + wx) * 16 + lr) * R::PITCH + wm * 64 + i * 16 + quarter * 4) =
+              acc[i][r];
+    __syncthreads();
+    const int quads = gated ? 32 : 64;
+    for (int i = threadIdx.x; i < here * quads; i += 512) {
+      const int row = i / quads, q = i % quads, pair = list[i0 + row], n = n0 + q * 4;
+      const float* const v = sums + row * R::PITCH;
+      if constexpr (UP) {
+        const int c = gated ? (q >> 3) * 64 + (q & 7) * 4 : q * 4;
+        const f32x4 first = *reinterpret_cast<const f32x4*>(v + c);
+        store_hidden(a, e, pair, n, first, gated ? *reinterpret_cast<const f32x4*>(v + c + 32) : first);
+      } else if (n < N) {
+        *reinterpret_cast<f32x4*>(a.part + (blockIdx.z * a.M * a.top_k + pair) * a.ld_part + n) =
+            *reinterpret_cast<const f32x4*>(v + q * 4);
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -705,20 +876,32 @@ hipError_t launch_wide(const ExpertArgs& a, hipStream_t st) {
                      dim3((unsigned)((n + per - 1) / per), slots, UP ? 1 : a.splits), dim3(64 * NW), lds, st, a);
   return hipGetLastError();
 }
+template <int TERMS, bool UP, int RT, int ST>
+hipError_t launch_expert_tile(const ExpertArgs& a, hipStream_t st) {
+  const unsigned slots = (unsigned)std::min<int64_t>(a.M * a.top_k, a.E);
+  const int per = UP && a.gated ? 128 : 256, n = UP ? a.H : a.N;
+  constexpr size_t lds = ExpertTile<TERMS, RT, ST>::LDS;
+  hipLaunchKernelGGL((k_expert_tile<TERMS, UP, RT, ST>), dim3((unsigned)((n + per - 1) / per), slots, UP ? 1 : a.splits),
+                     dim3(512), lds, st, a);
+  return hipGetLastError();
+}
 template <bool MX4, int TERMS, bool UP>
 hipError_t dispatch_wide(const ExpertArgs& a, hipStream_t st) {
   const int64_t mean = a.M * a.top_k / a.E;
   if (a.M <= 16 || mean <= 8) {
     const int64_t slots = std::min<int64_t>(a.M * a.top_k, a.E), rows = UP ? (int64_t)a.H * (a.gated ? 2 : 1) : a.N;
-    const int64_t z = UP ? 1 : a.splits, runs = (rows + 127) / 128, per = std::max<int64_t>(1, runs * slots * z / 1024);
+    const int64_t z = UP ? 1 : a.splits, runs = (rows + 127) / 128, per = std::max<int64_t>(1, runs * slots * z / 640);
     hipLaunchKernelGGL((k_expert_stream<MX4, TERMS, UP>),
                        dim3((unsigned)((runs + per - 1) / per), (unsigned)slots, (unsigned)z), dim3(256), 0, st, a,
                        (int)runs, (int)per);
     return hipGetLastError();
   }
-  if constexpr (MX4 && TERMS < 3)
-    if (mean > 48) return launch_wide<MX4, TERMS, UP, 8, 8>(a, st);
-  return launch_wide<MX4, TERMS, UP, 4, 8>(a, st);
+  if constexpr (MX4) {
+    if (mean <= 40 || TERMS == 3) return launch_expert_tile<TERMS, UP, 4, TERMS == 1 ? 4 : TERMS == 2 ? 3 : 2>(a, st);
+    if constexpr (TERMS < 3) return launch_expert_tile<TERMS, UP, 6, TERMS == 1 ? 3 : 2>(a, st);
+  } else {
+    return launch_wide<MX4, TERMS, UP, 4, 8>(a, st);
+  }
 }
 
 template <bool MX4>
