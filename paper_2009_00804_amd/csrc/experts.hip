@@ -47,33 +47,34 @@ __device__ __forceinline__ void store_terms(const ExpertArgs& a, int64_t row, in
 // --------------------------------------------------------------------------
 constexpr int kTogether = 4;
 
-// 64 lanes' sums of kTogether values; the steps of different values run side by side
-__device__ __forceinline__ void wave_sums(double (&v)[kTogether]) {
+// 64 lanes' sums of C values; the steps of different values run side by side
+template <int C>
+__device__ __forceinline__ void wave_sums(double (&v)[C]) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2)
 #pragma unroll
-    for (int i = 0; i < kTogether; ++i) v[i] += __shfl_xor(v[i], d);
+    for (int i = 0; i < C; ++i) v[i] += __shfl_xor(v[i], d);
 }
 
 // logits[e] = x . router_e + bias_e for all experts; true: one that is NaN or +inf
-template <typename T, typename TR, int NW>
+template <typename T, typename TR, int NW, int C>
 __device__ __forceinline__ bool route_logits(const ExpertArgs& a, const T* x, double* logits) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, F = a.F;
   bool bad = false;
-  for (int e0 = wave * kTogether; e0 < a.E; e0 += NW * kTogether) {
-    double sum[kTogether] = {};
+  for (int e0 = wave * C; e0 < a.E; e0 += NW * C) {
+    double sum[C] = {};
     for (int c = lane * 8; c < F; c += 512) {
       Raw<T> v;
-      Raw<TR> w[kTogether];
+      Raw<TR> w[C];
       v.load(x + c, F - c);
 #pragma unroll
-      for (int i = 0; i < kTogether; ++i)
+      for (int i = 0; i < C; ++i)
         w[i].load(static_cast<const TR*>(a.router) + min(e0 + i, a.E - 1) * a.ld_router + c, F - c);
       v.clear(F - c);
       float f[8];
       v.widen(f);
 #pragma unroll
-      for (int i = 0; i < kTogether; ++i) {
+      for (int i = 0; i < C; ++i) {
         w[i].clear(F - c);
         float g[8];
         w[i].widen(g);
@@ -83,7 +84,7 @@ __device__ __forceinline__ bool route_logits(const ExpertArgs& a, const T* x, do
     }
     wave_sums(sum);
 #pragma unroll
-    for (int i = 0; i < kTogether; ++i) {
+    for (int i = 0; i < C; ++i) {
       if (e0 + i >= a.E) break;
       if (a.router_bias) sum[i] += (double)a.router_bias[e0 + i];
       if (lane == 0) logits[e0 + i] = sum[i];
@@ -102,7 +103,7 @@ struct RouteSpace {
   int bad;
 };
 template <int THREADS>
-__device__ __forceinline__ void route_choose(const ExpertArgs& a, int64_t row, RouteSpace& s) {
+__device__ __forceinline__ void route_choose(const ExpertArgs& a, RouteSpace& s, int32_t* index, float* weight) {
   const int tid = threadIdx.x;
   if (tid < SAGA_MAX_CHOICES) s.chosen[tid] = -1;
   __syncthreads();
@@ -138,8 +139,8 @@ __device__ __forceinline__ void route_choose(const ExpertArgs& a, int64_t row, R
     int chosen = s.chosen[tid];
     float p = chosen >= 0 ? (float)((double)expf((float)(s.best[tid] - top)) / total) : 0.0f;
     if (s.bad) chosen = -1, p = __uint_as_float(0x7fc00000u);
-    a.index[row * a.top_k + tid] = chosen;
-    a.weight[row * a.top_k + tid] = p;
+    index[tid] = chosen;
+    weight[tid] = p;
   }
 }
 
@@ -160,10 +161,10 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(ExpertArgs a) {
     bad |= v.top() >= 0x7f800000u;
     store_terms(a, row, c, v);
   }
-  bad |= route_logits<T, TR, kRouteThreads / 64>(a, x, s.logits);
+  bad |= route_logits<T, TR, kRouteThreads / 64, kTogether>(a, x, s.logits);
   if (bad) s.bad = 1;
   __syncthreads();
-  route_choose<kRouteThreads>(a, row, s);
+  route_choose<kRouteThreads>(a, s, a.index + row * a.top_k, a.weight + row * a.top_k);
 }
 
 // where a lane reads its channel's weights
@@ -242,44 +243,40 @@ struct WeightBlocks<false, 1> {
   }
 };
 
-// This workgroup's expert (-1: none) and its pairs (row * top_k + place), in order.
-// Up to E pairs a slot is a pair, which stands for its expert if no earlier pair does;
-// otherwise a slot is an expert.  Each wave lists a run of the pairs.
+// This workgroup's expert (-1: none) and its pairs (row * top_k + place), in some order (no
+// result depends on it).  Up to E pairs a slot is a pair, which stands for its expert if no
+// earlier pair does; otherwise a slot is an expert.
 template <int NW>
 __device__ __forceinline__ int slot_expert(const ExpertArgs& a, int slot, int* list, int& count) {
-  __shared__ int found[NW], seen;
+  __shared__ int found, seen;
   const int pairs = (int)(a.M * a.top_k);
   const bool by_pair = pairs <= a.E;
   const int e = by_pair ? a.index[slot] : slot;
   if (e < 0) return -1;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int run = (pairs + NW * 64 - 1) / (NW * 64) * 64, p0 = wave * run, p1 = min(pairs, p0 + run);
-  if (threadIdx.x == 0) seen = 0;
+  if (threadIdx.x == 0) found = seen = 0;
   __syncthreads();
-  int mine = 0;
-  for (int p = p0; p < p1; p += 64) {
-    const bool is = p + lane < p1 && a.index[p + lane] == e;
-    if (by_pair && is && p + lane < slot) seen = 1;
-    mine += __popcll(__ballot(is));
-  }
-  if (lane == 0) found[wave] = mine;
-  __syncthreads();
-  int base = 0;
-  count = 0;
+  const int lane = threadIdx.x & 63;
+  constexpr int TOGETHER = 4;  // (loads on their way)
+  for (int p0 = threadIdx.x - lane; p0 < pairs; p0 += NW * 64 * TOGETHER) {
+    int at[TOGETHER];
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    if (w < wave) base += found[w];
-    count += found[w];
-  }
-  if (seen || count == 0) return -1;
-  for (int p = p0; p < p1; p += 64) {
-    const bool is = p + lane < p1 && a.index[p + lane] == e;
-    const uint64_t all = __ballot(is);
-    if (is) list[base + __popcll(all & lanemask_lt())] = p + lane;
-    base += __popcll(all);
+    for (int j = 0; j < TOGETHER; ++j) at[j] = a.index[min(p0 + j * NW * 64 + lane, pairs - 1)];
+#pragma unroll
+    for (int j = 0; j < TOGETHER; ++j) {
+      const int p = p0 + j * NW * 64 + lane;
+      const bool mine = p < pairs && at[j] == e;
+      const uint64_t all = __ballot(mine);
+      if (all == 0) continue;
+      if (by_pair && mine && p < slot) seen = 1;
+      int base = 0;
+      if (lane == 0) base = atomicAdd(&found, __popcll(all));
+      base = __builtin_amdgcn_readfirstlane(base);
+      if (mine) list[base + __popcll(all & lanemask_lt())] = p;
+    }
   }
   __syncthreads();
-  return e;
+  count = found;
+  return seen || count == 0 ? -1 : e;
 }
 
 // h of four channels n.. of a pair, to its terms
@@ -400,6 +397,235 @@ __global__ __launch_bounds__(512) void k_expert_few(ExpertArgs a) {
     }
     __syncthreads();
   }
+}
+
+// --------------------------------------------------------------------------
+// a layer of few rows (at most 16, and 64 pairs) in two kernels: the latency of each counts.
+// The first chooses the experts itself where that is little work (FUSED; every workgroup
+// does, the first one's choice is the result), takes x as it is, and writes h.  The second
+// has 16 channels of out for all rows a workgroup: its waves share the k of all experts
+// that are taken, and sum by the choices' weights.
+// --------------------------------------------------------------------------
+constexpr int kFewRows = 16, kFewPairs = 64;
+
+// 8 columns of x as terms
+__device__ __forceinline__ void split_unit(const Raw<uint16_t>& x, bf16x8 (&o)[1]) { __builtin_memcpy(&o[0], &x.v, 16); }
+__device__ __forceinline__ void split_unit(const Raw<float>& x, bf16x8 (&o)[3]) {
+  float f[8];
+  x.widen(f);
+#pragma unroll
+  for (int t = 0; t < 3; ++t) {
+    u32x4 d;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t lo = cut_term(f[2 * j]), hi = cut_term(f[2 * j + 1]);
+      d[j] = lo >> 16 | hi;
+    }
+    __builtin_memcpy(&o[t], &d, 16);
+  }
+}
+
+template <bool MX4, typename T, bool GATED, bool FUSED>
+__global__ __launch_bounds__(512) void k_expert_up_few(ExpertArgs a) {
+  constexpr int NW = 8, NO = GATED ? 2 : 1, TERMS = sizeof(T) == 2 ? 1 : 3, AHEAD = 2;
+  __shared__ f32x4 part[NW][NO][64];
+  __shared__ int index[kFewPairs], list[NW][kFewRows];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int quarter = lane >> 4, lr = lane & 15, pairs = (int)a.M * a.top_k, slot = blockIdx.y;
+  if constexpr (FUSED) {
+    __shared__ RouteSpace s;
+    __shared__ float weight[kFewPairs];
+    for (int row = 0; row < (int)a.M; ++row) {
+      const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+      if (threadIdx.x == 0) s.bad = 0;
+      __syncthreads();
+      bool bad = false;
+      for (int c = threadIdx.x * 8; c < a.F; c += 512 * 8) {
+        Raw<T> v;
+        v.load(x + c, a.F - c);
+        v.clear(a.F - c);
+        bad |= v.top() >= 0x7f800000u;
+      }
+      bad |= a.router_dtype == SAGA_BF16 ? route_logits<T, uint16_t, NW, 1>(a, x, s.logits)
+                                         : route_logits<T, float, NW, 1>(a, x, s.logits);
+      if (bad) s.bad = 1;
+      __syncthreads();
+      route_choose<512>(a, s, index + row * a.top_k, weight + row * a.top_k);
+      __syncthreads();
+    }
+    if (blockIdx.x == 0 && slot == 0 && (int)threadIdx.x < pairs) {
+      a.index[threadIdx.x] = index[threadIdx.x];
+      a.weight[threadIdx.x] = weight[threadIdx.x];
+    }
+  } else {
+    if ((int)threadIdx.x < pairs) index[threadIdx.x] = a.index[threadIdx.x];
+    __syncthreads();
+  }
+  const bool by_pair = pairs <= a.E;
+  const int e = __builtin_amdgcn_readfirstlane(by_pair ? index[slot] : slot);
+  if (e < 0) return;
+  const bool mine = lane < pairs && index[lane] == e;
+  const uint64_t all_mine = __ballot(mine);
+  if (all_mine == 0 || (by_pair && __ffsll((unsigned long long)all_mine) - 1 < slot)) return;
+  const int count = __popcll(all_mine);
+  if (mine) list[wave][__popcll(all_mine & lanemask_lt())] = lane;
+  asm volatile("" ::: "memory");
+  const int pair = list[wave][min(lr, count - 1)];
+
+  const int K = a.F, n0 = blockIdx.x * 16, all = (K + 127) / 128, last = (K - 1) / 8 * 8;
+  const int steps = (all - wave + NW - 1) / NW;  // of this wave: wave, wave + NW, ..
+  const T* const x = static_cast<const T*>(a.x) + pair / a.top_k * a.ldx;
+  WeightRow<MX4> from[NO];
+#pragma unroll
+  for (int o = 0; o < NO; ++o)
+    from[o] = weight_row<MX4, true>(a, (int64_t)e * a.H * NO + (int64_t)o * a.H + min(n0 + lr, a.H - 1));
+  WeightBlocks<MX4, 1> w[AHEAD][NO];
+  Raw<T> xv[AHEAD][4];
+  const auto load = [&](int d, int i) {
+    const int b = (wave + i * NW) * 4 + quarter;
+#pragma unroll
+    for (int o = 0; o < NO; ++o) w[d][o].load(from[o], b, K);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) xv[d][t].load(x + min(b * 32 + t * 8, last), 8);
+  };
+  f32x4 acc[NO];
+#pragma unroll
+  for (int o = 0; o < NO; ++o) acc[o] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int ib = 0; ib < steps; ib += AHEAD) {
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) load(d, ib + d);
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) {
+      const int i = ib + d;
+      if (i >= steps) continue;
+      const int b = (wave + i * NW) * 4 + quarter;
+      if (wave + i * NW == all - 1) {
+#pragma unroll
+        for (int o = 0; o < NO; ++o) w[d][o].clear(b, K);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) xv[d][t].clear(K - min(b * 32 + t * 8, last));
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        bf16x8 term[TERMS];
+        split_unit(xv[d][t], term);
+#pragma unroll
+        for (int o = 0; o < NO; ++o) {
+          const bf16x8 wv = w[d][o].take(0, t);
+#pragma unroll
+          for (int p = 0; p < TERMS; ++p) acc[o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, term[p], acc[o], 0, 0, 0);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 0; o < NO; ++o) part[wave][o][lane] = acc[o];
+  __syncthreads();
+  if (wave != 0 || lr >= count) return;
+#pragma unroll
+  for (int o = 0; o < NO; ++o)
+#pragma unroll
+    for (int k = 1; k < NW; ++k) acc[o] += part[k][o][lane];
+  store_hidden(a, e, pair, n0 + quarter * 4, acc[0], acc[NO - 1]);
+}
+
+// four channels n.. of a row of out, from their sum without biases
+__device__ __forceinline__ void store_out(const ExpertArgs& a, int64_t row, int n, const float (&v)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (n + j >= a.N) continue;
+    if (a.dtype == SAGA_BF16) static_cast<uint16_t*>(a.out)[row * a.ldo + n + j] = f32_to_bf16(v[j]);
+    else static_cast<float*>(a.out)[row * a.ldo + n + j] = v[j];
+  }
+}
+
+template <bool MX4, int TERMS>
+__global__ __launch_bounds__(512) void k_expert_down_few(ExpertArgs a) {
+  constexpr int NW = 8, AHEAD = 2;
+  __shared__ f32x4 part[NW][64];
+  __shared__ int index[kFewPairs], expert[kFewPairs], pair_of[kFewPairs][kFewRows];
+  __shared__ float weight[kFewPairs];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int quarter = lane >> 4, lr = lane & 15, pairs = (int)a.M * a.top_k;
+  for (int i = threadIdx.x; i < kFewPairs * kFewRows; i += 512) pair_of[0][i] = -1;
+  const int mine = lane < pairs ? a.index[lane] : -1;
+  if ((int)threadIdx.x < pairs) index[threadIdx.x] = mine, weight[threadIdx.x] = a.weight[threadIdx.x];
+  __syncthreads();
+  // the experts that are taken, by their first pair, and each row's pair of them
+  int first = lane;
+  for (int p = 0; p < pairs; ++p)
+    if (p < first && index[p] == mine) first = p;
+  const uint64_t firsts = __ballot(mine >= 0 && first == lane);
+  const int taken = __popcll(firsts);
+  if (wave == 0 && mine >= 0) {
+    const int place = __popcll(firsts & ((1ull << first) - 1));
+    if (first == lane) expert[place] = mine;
+    pair_of[place][lane / a.top_k] = lane;
+  }
+  __syncthreads();
+
+  const int K = a.H, n0 = blockIdx.x * 16, all = (K + 127) / 128, ld = (int)a.ld_ht;
+  const int64_t plane = a.M * a.top_k * a.ld_ht;
+  const int steps = (all - wave + NW - 1) / NW, items = taken * steps;  // of this wave
+  WeightBlocks<MX4, 1> w[AHEAD];
+  u32x4 xv[AHEAD][4][TERMS];
+  const auto load = [&](int d, int item) {
+    item = min(item, items - 1);
+    const int u = item / steps, b = (wave + item % steps * NW) * 4 + quarter;
+    const WeightRow<MX4> from = weight_row<MX4, false>(a, (int64_t)expert[u] * a.N + min(n0 + lr, a.N - 1));
+    w[d].load(from, b, K);
+    const uint16_t* const x = a.ht + (int64_t)max(pair_of[u][lr], 0) * a.ld_ht;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int p = 0; p < TERMS; ++p)
+        xv[d][t][p] = *reinterpret_cast<const u32x4*>(x + p * plane + min(b * 32 + t * 8, ld - 8));
+  };
+  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (items > 0) {
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) load(d, d);
+    for (int ib = 0; ib < items; ib += AHEAD) {
+#pragma unroll
+      for (int d = 0; d < AHEAD; ++d) {
+        const int item = ib + d, u = min(item, items - 1) / steps, s = wave + item % steps * NW;
+        if (s == all - 1) w[d].clear(s * 4 + quarter, K);
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const bf16x8 wv = w[d].take(0, t);
+#pragma unroll
+          for (int p = 0; p < TERMS; ++p) {
+            bf16x8 v;
+            __builtin_memcpy(&v, &xv[d][t][p], 16);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, v, acc, 0, 0, 0);
+          }
+        }
+        load(d, item + AHEAD);
+        // (a row that does not take the expert has another row's values here)
+        const int pair = pair_of[u][lr];
+        const bool has = pair >= 0 && item < items;
+        const float p = has ? weight[max(pair, 0)] : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] = has ? fmaf(p, acc[j], sum[j]) : sum[j];
+      }
+    }
+  }
+  part[wave][lane] = sum;
+  __syncthreads();
+  if (wave != 0 || lr >= (int)a.M) return;
+#pragma unroll
+  for (int k = 1; k < NW; ++k) sum += part[k][lane];
+  const int n = n0 + quarter * 4;
+  float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+  for (int k = 0; k < a.top_k; ++k) {
+    const int e = index[lr * a.top_k + k];
+    const float p = weight[lr * a.top_k + k];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)  // (a row without numbers: p is NaN)
+      v[j] = fmaf(p, e >= 0 && a.down_bias && n + j < a.N ? a.down_bias[(int64_t)e * a.N + n + j] : 0.0f, v[j]);
+  }
+  store_out(a, lr, n, v);
 }
 
 // --------------------------------------------------------------------------
@@ -847,12 +1073,7 @@ __global__ __launch_bounds__(256) void k_expert_sum(ExpertArgs a) {
         v[j] = fmaf(p, d[j], v[j]);  // (a row without numbers: p is NaN)
       }
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (n + j >= a.N) continue;
-      if (a.dtype == SAGA_BF16) static_cast<uint16_t*>(a.out)[row * a.ldo + n + j] = f32_to_bf16(v[j]);
-      else static_cast<float*>(a.out)[row * a.ldo + n + j] = v[j];
-    }
+    store_out(a, row, n, v);
   }
 }
 
@@ -865,6 +1086,31 @@ bool experts_wide(int64_t M, int64_t H, int64_t N, int E, int top_k, bool gated)
 int expert_splits(int64_t M, int64_t H, int64_t N, int E, int top_k) {
   const int64_t slots = std::min<int64_t>(M * top_k, E), wgs = slots * ((N + 127) / 128), steps = (H + 127) / 128;
   return (int)std::max<int64_t>(1, std::min<int64_t>({8, 512 / wgs, steps / 4}));
+}
+
+// Whether the two kernels of few rows take the layer: the second one's workgroups, 16 channels
+// of out each, read their channels of all experts that are taken
+bool experts_few(int64_t M, int64_t H, int top_k, int E, bool mx4) {
+  return M <= kFewRows && M * top_k <= kFewPairs &&
+         std::min<int64_t>(M * top_k, E) * H * 16 * (mx4 ? 1 : 4) <= 2 * 256 * 1024;
+}
+// and whether the first one chooses: a float64 product of a few waves
+bool experts_fused(int64_t M, int64_t F, int E) { return M * E * F <= 16384; }
+
+template <bool MX4, typename T>
+hipError_t few_rows(const ExpertArgs& a, hipStream_t st) {
+  const dim3 up((unsigned)((a.H + 15) / 16), (unsigned)std::min<int64_t>(a.M * a.top_k, a.E));
+  const auto go = [&](auto kernel, dim3 grid) {
+    hipLaunchKernelGGL(kernel, grid, dim3(512), 0, st, a);
+    return hipGetLastError();
+  };
+  hipError_t e;
+  if (experts_fused(a.M, a.F, a.E))
+    e = a.gated ? go(k_expert_up_few<MX4, T, true, true>, up) : go(k_expert_up_few<MX4, T, false, true>, up);
+  else
+    e = a.gated ? go(k_expert_up_few<MX4, T, true, false>, up) : go(k_expert_up_few<MX4, T, false, false>, up);
+  if (e != hipSuccess) return e;
+  return go(k_expert_down_few<MX4, sizeof(T) == 2 ? 2 : 3>, dim3((unsigned)((a.N + 15) / 16)));
 }
 
 template <bool MX4, int TERMS, bool UP, int RT, int NW>
@@ -978,16 +1224,25 @@ hipError_t launch_experts(const ExpertArgs& a0, hipStream_t st) {
     if (a.M < s.rows)  // (the rest of many rows: never more parts than there is room for)
       a.splits = std::min(s.splits, experts_wide(a.M, a.H, a.N, a.E, a.top_k, a.gated)
                                         ? expert_splits(a.M, a.H, a.N, a.E, a.top_k) : 1);
+    const bool mx4 = a.weight_dtype == SAGA_MX4, few = experts_few(a.M, a.H, a.top_k, a.E, mx4);
     const auto route = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)a.M), dim3(kRouteThreads), 0, st, a);
       return hipGetLastError();
     };
-    hipError_t e;
-    if (a.dtype == SAGA_BF16)
-      e = a.router_dtype == SAGA_BF16 ? route(k_route<uint16_t, uint16_t>) : route(k_route<uint16_t, float>);
-    else
-      e = a.router_dtype == SAGA_BF16 ? route(k_route<float, uint16_t>) : route(k_route<float, float>);
-    if (e != hipSuccess) return e;
+    hipError_t e = hipSuccess;
+    if (!few || !experts_fused(a.M, a.F, a.E)) {
+      if (a.dtype == SAGA_BF16)
+        e = a.router_dtype == SAGA_BF16 ? route(k_route<uint16_t, uint16_t>) : route(k_route<uint16_t, float>);
+      else
+        e = a.router_dtype == SAGA_BF16 ? route(k_route<float, uint16_t>) : route(k_route<float, float>);
+      if (e != hipSuccess) return e;
+    }
+    if (few) {
+      if (a.dtype == SAGA_BF16) e = mx4 ? few_rows<true, uint16_t>(a, st) : few_rows<false, uint16_t>(a, st);
+      else e = mx4 ? few_rows<true, float>(a, st) : few_rows<false, float>(a, st);
+      if (e != hipSuccess) return e;
+      continue;
+    }
     e = a.weight_dtype == SAGA_MX4 ? products<true>(a, st) : products<false>(a, st);
     if (e != hipSuccess) return e;
     const int64_t quads = a.M * (a.ld_part / 4);
