@@ -151,6 +151,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(ExpertArgs a) {
   const int64_t row = blockIdx.x;
   const T* x = static_cast<const T*>(a.x) + row * a.ldx;
   if (threadIdx.x == 0) s.bad = 0;
+  if (row == 0 && threadIdx.x < 8) a.zeros[threadIdx.x] = 0;
   __syncthreads();
   // the row's terms, and whether it holds numbers only
   bool bad = false;
@@ -279,30 +280,70 @@ __device__ __forceinline__ int slot_expert(const ExpertArgs& a, int slot, int* l
   return seen || count == 0 ? -1 : e;
 }
 
-// h of four channels n.. of a pair, to its terms
+// e^x to about 2 units of 2^-24, x from -87 to 87: the product with log2 e has a second part
+__device__ __forceinline__ float exp_in_range(float x) {
+  constexpr float kLog2e = 1.44269504f, kRest = 1.92596299e-8f, kLn2 = 0.693147181f;
+  const float h = x * kLog2e, l = fmaf(x, kLog2e, -h) + x * kRest, e = __builtin_amdgcn_exp2f(h);
+  return fmaf(e, l * kLn2, e);
+}
+template <int C>
+__device__ __forceinline__ void activate(int act, float (&v)[C]) {
+  if (act == SAGA_ACT_SIGMOID) {  // (the values between the products are many: no call, no division)
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+      v[j] = __builtin_amdgcn_rcpf(1.0f + exp_in_range(-__builtin_elementwise_maximum(
+                                              -87.0f, __builtin_elementwise_minimum(v[j], 87.0f))));
+  } else if (act == SAGA_ACT_RELU) {
+#pragma unroll
+    for (int j = 0; j < C; ++j) v[j] = __builtin_elementwise_maximum(v[j], 0.0f);  // (a NaN stays)
+  } else if (act != SAGA_ACT_NONE) {
+#pragma unroll
+    for (int j = 0; j < C; ++j) v[j] = apply_act(act, v[j]);
+  }
+}
+
+// h of C channels n.. of a pair (C neighbours), to its terms
+template <int C>
+__device__ __forceinline__ void store_hidden(const ExpertArgs& a, int e, int pair, int n, float (&v)[C],
+                                             const float (&up)[C]) {
+  if (n >= a.ld_ht) return;
+  if (a.up_bias) {
+    const float* bias = a.up_bias + (int64_t)e * a.H * (a.gated ? 2 : 1);
+#pragma unroll
+    for (int j = 0; j < C; ++j) v[j] += bias[min(n + j, a.H - 1)];
+  }
+  activate(a.act, v);
+  if (a.gated) {
+    const float* bias = a.up_bias ? a.up_bias + ((int64_t)e * 2 + 1) * a.H : nullptr;
+#pragma unroll
+    for (int j = 0; j < C; ++j) v[j] *= up[j] + (bias ? bias[min(n + j, a.H - 1)] : 0.0f);
+  }
+  if (n + C > a.H)
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+      if (n + j >= a.H) v[j] = 0.0f;
+  for (int t = 0; t < a.h_terms; ++t) {
+    uint32_t o[C / 2];
+#pragma unroll
+    for (int j = 0; j < C; j += 2) {
+      // (the last term is rounded: of three it holds what is left)
+      if (t + 1 == a.h_terms) {
+        o[j / 2] = pack_bf16(v[j], v[j + 1]);
+      } else {
+        const uint32_t lo = cut_term(v[j]), hi = cut_term(v[j + 1]);
+        o[j / 2] = lo >> 16 | hi;
+      }
+    }
+    uint16_t* const to = a.ht + (t * a.M * a.top_k + pair) * a.ld_ht + n;
+    if constexpr (C == 8) *reinterpret_cast<u32x4*>(to) = u32x4{o[0], o[1], o[2], o[3]};
+    else *reinterpret_cast<uint2*>(to) = make_uint2(o[0], o[1]);
+  }
+}
 __device__ __forceinline__ void store_hidden(const ExpertArgs& a, int e, int pair, int n, const f32x4& first,
                                              const f32x4& second) {
-  if (n >= a.ld_ht) return;
-  uint32_t term[3][4];
-  const float* bias = a.up_bias ? a.up_bias + (int64_t)e * a.H * (a.gated ? 2 : 1) : nullptr;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    float v = 0.0f;
-    if (n + j < a.H) {
-      v = apply_act(a.act, first[j] + (bias ? bias[n + j] : 0.0f));
-      if (a.gated) v *= second[j] + (bias ? bias[a.H + n + j] : 0.0f);
-    }
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      // (the last term is rounded: of three it holds what is left)
-      if (t + 1 == a.h_terms) term[t][j] = (uint32_t)f32_to_bf16(v) << 16;
-      else term[t][j] = cut_term(v);
-    }
-    term[2][j] = (uint32_t)f32_to_bf16(v) << 16;
-  }
-  for (int t = 0; t < a.h_terms; ++t)
-    *reinterpret_cast<uint2*>(a.ht + (t * a.M * a.top_k + pair) * a.ld_ht + n) =
-        make_uint2(term[t][0] >> 16 | term[t][1], term[t][2] >> 16 | term[t][3]);
+  float v[4] = {first[0], first[1], first[2], first[3]};
+  const float up[4] = {second[0], second[1], second[2], second[3]};
+  store_hidden(a, e, pair, n, v, up);
 }
 
 // --------------------------------------------------------------------------
@@ -762,21 +803,22 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
 // a workgroup.  Both come through LDS by direct-to-LDS loads, 128 k a stage, ST stages:
 // loads come back in their order, and the rows of x, which L2 has, must not wait for weights
 // that were asked for later.  A wave has 64 rows of weights (gate and up of 32 channels, or 64
-// channels) and every second tile of x.
+// channels) and every second tile of x.  Past the rows' ends x is zeros and scales are 1,
+// whatever the weights' bits are there.
 // --------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) uint4 lds_uint4;
 
-// m0 + the lane's place <- 16 (or 4) bytes of each lane's address
-__device__ __forceinline__ void lds_load16(uint32_t to, const void* from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+// LDS at `to` + the lane's place <- 16 (or 4) bytes at the lane's offset from `base`
+__device__ __forceinline__ void lds_load16(uint32_t to, const void* base, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
-               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
+               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base)
                : "memory", "m0");
 }
-__device__ __forceinline__ void lds_load4(uint32_t to, const void* from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+__device__ __forceinline__ void lds_load4(uint32_t to, const void* base, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
                :
-               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
+               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base)
                : "memory", "m0");
 }
 
@@ -796,7 +838,7 @@ struct ExpertTile {
 };
 
 template <int TERMS, bool UP, int RT, int ST>
-__global__ __launch_bounds__(512) void k_expert_tile(ExpertArgs a) {
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_expert_tile(ExpertArgs a) {
   typedef ExpertTile<TERMS, RT, ST> R;
   extern __shared__ uint4 space[];
   char* const base = reinterpret_cast<char*>(space);
@@ -811,46 +853,43 @@ __global__ __launch_bounds__(512) void k_expert_tile(ExpertArgs a) {
   const bool gated = UP && a.gated;
   const int all = (K + 127) / 128, per = UP ? all : (all + a.splits - 1) / a.splits;
   const int s0 = UP ? 0 : min(all, (int)blockIdx.z * per), s1 = UP ? all : min(all, s0 + per);
-  const int64_t ld = UP ? a.ld_xt : a.ld_ht, plane = (UP ? a.M : a.M * a.top_k) * ld;
-  const uint16_t* const rows = UP ? a.xt : a.ht;
   const int n0 = (int)blockIdx.x * (gated ? 128 : 256);
-  // row r of the stage's weights: 64 a wave; gated: gates of 32 channels, then ups
-  const auto weights = [&](int r) {
-    const int64_t row = gated ? ((int64_t)e * 2 + (r >> 5 & 1)) * N + min(n0 + (r >> 6) * 32 + (r & 31), N - 1)
-                              : (int64_t)e * N + min(n0 + r, N - 1);
-    return weight_row<true, UP>(a, row);
-  };
-  const uint8_t* w_at[2];
-  int w_piece[2];
+  // row r of the stage's weights: 64 a wave; gated: gates of 32 channels, then ups.  A wave's
+  // loads are of rows whose r / 32 is even for all or odd for all: of gates or of ups.
+  const int64_t ld_w = UP ? a.ld_up : a.ld_down, ld_s = UP ? a.lds_up : a.lds_down;
+  const int64_t first = gated ? ((int64_t)e * 2 + (wave >> 1 & 1)) * N + n0 : (int64_t)e * N + n0;
+  const int64_t first_s = gated ? ((int64_t)e * 2 + (wave & 1)) * N + n0 : first;
+  const uint8_t* const w_base = static_cast<const uint8_t*>(UP ? a.up : a.down) + first * ld_w;
+  const uint8_t* const s_base = (UP ? a.up_scale : a.down_scale) + first_s * ld_s;
+  const auto local = [&](int r) { return min(gated ? (r >> 6) * 32 + (r & 31) : r, N - 1 - n0); };
+  uint32_t w_at[2];
+  const int w_piece = ((lane & 3) ^ (lane >> 4 & 3)) * 16;  // (row r = 16 i + lane / 4: r >> 2 & 3 = lane >> 4)
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int r = 16 * (wave + 8 * j) + lane / 4;
-    w_at[j] = weights(r).q;
-    w_piece[j] = ((lane & 3) ^ (r >> 2 & 3)) * 16;
-  }
-  const uint8_t* const s_at = weights(wave * 32 + (lane & 31)).s;
+  for (int j = 0; j < 2; ++j) w_at[j] = (uint32_t)local(16 * (wave + 8 * j) + lane / 4) * (uint32_t)ld_w;
+  const uint32_t s_at = (uint32_t)local(wave * 32 + (lane & 31)) * (uint32_t)ld_s;
+  const char* const rows = reinterpret_cast<const char*>(UP ? a.xt : a.ht);
+  const uint32_t ld = (uint32_t)(UP ? a.ld_xt : a.ld_ht) * 2, plane = (uint32_t)(UP ? a.M : a.M * a.top_k) * ld;
+  const uint32_t zeros = (uint32_t)(reinterpret_cast<const char*>(a.zeros) - rows);
+  const uint32_t x_piece = ((lane & 15) ^ ((wave * 4 + (lane >> 4)) & 15)) * 16;
 
   for (int i0 = 0; i0 < count; i0 += R::ROWS) {
     const int here = min(count - i0, R::ROWS), tiles = (here + 15) / 16;
-    const uint16_t* x_at[R::XL];
+    uint32_t x_at[R::XL];
 #pragma unroll
     for (int j = 0; j < R::XL; ++j) {
       const int i = (wave + 8 * j) * 4 + (lane >> 4), r = i % R::ROWS, t = i / R::ROWS;
       const int pair = list[i0 + min(r, here - 1)];
-      x_at[j] = rows + t * plane + (UP ? pair / a.top_k : pair) * ld;
+      x_at[j] = t * plane + (uint32_t)(UP ? pair / a.top_k : pair) * ld;
     }
-    // (loads past a row's end are of its last piece: the weights' zeros make them not count)
     const auto issue = [&](int s) {
       const uint32_t to = lds + s % ST * R::STAGE;
+      const uint32_t w_k = (uint32_t)min(s * 64 + w_piece, kmax), x_k = s * 256 + x_piece;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) lds_load16(to + (wave + 8 * j) * 1024, w_at[j] + min(s * 64 + w_piece[j], kmax));
-      if (lane < 32) lds_load4(to + R::W_BYTES + wave * 128, s_at + s * 4);
+      for (int j = 0; j < 2; ++j) lds_load16(to + (wave + 8 * j) * 1024, w_base, w_at[j] + w_k);
+      if (lane < 32) lds_load4(to + R::W_BYTES + wave * 128, s_base, s_at + s * 4);
 #pragma unroll
-      for (int j = 0; j < R::XL; ++j) {
-        const int r = (wave + 8 * j) * 4 + (lane >> 4);  // (16 rows a tile: r % 16 whatever the term)
-        lds_load16(to + R::W_BYTES + R::S_BYTES + (wave + 8 * j) * 1024,
-                   x_at[j] + min(s * 128 + ((lane & 15) ^ (r & 15)) * 8, (int)ld - 8));
-      }
+      for (int j = 0; j < R::XL; ++j)
+        lds_load16(to + R::W_BYTES + R::S_BYTES + (wave + 8 * j) * 1024, rows, x_k < ld ? x_at[j] + x_k : zeros);
     };
     f32x4 acc[4][RT / 2];
 #pragma unroll
@@ -866,26 +905,28 @@ __global__ __launch_bounds__(512) void k_expert_tile(ExpertArgs a) {
       ring_barrier();  // stage s is in LDS, and nobody reads stage s - 1 any more
       if (s + ST - 1 < s1) issue(s + ST - 1);
       const char* const stage = base + s % ST * R::STAGE;
+      const char* const wl = stage + (wm * 64 + lr) * 64 + (quarter ^ (lr >> 2)) * 16;
+      const char* const sl = stage + R::W_BYTES + (wm * 64 + lr) * 4 + quarter;
+      const bool past = (s * 4 + quarter) * 32 >= K;
       WeightBlocks<true, 1> w[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = wm * 64 + i * 16 + lr;
-        w[i].v[0] = *reinterpret_cast<const u32x4*>(stage + r * 64 + (quarter ^ (r >> 2 & 3)) * 16);
-        w[i].scale = *reinterpret_cast<const uint8_t*>(stage + R::W_BYTES + r * 4 + quarter);
-        if (s == all - 1) w[i].clear(s * 4 + quarter, K);
+        w[i].v[0] = *reinterpret_cast<const u32x4*>(wl + i * 1024);
+        w[i].scale = *reinterpret_cast<const uint8_t*>(sl + i * 64);
+        w[i].scale = past ? 127u : w[i].scale;
       }
-      const u32x4* const x = reinterpret_cast<const u32x4*>(stage + R::W_BYTES + R::S_BYTES);
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         bf16x8 wv[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) wv[i] = w[i].take(0, t);
+        const char* const xl = stage + R::W_BYTES + R::S_BYTES + (wx * 16 + lr) * 256 + ((quarter * 4 + t) ^ lr) * 16;
 #pragma unroll
         for (int r = 0; r < RT / 2; ++r) {
           if (2 * r + wx < tiles) {
 #pragma unroll
             for (int p = 0; p < TERMS; ++p) {
-              const u32x4 v = x[(p * R::ROWS + (2 * r + wx) * 16 + lr) * 16 + ((quarter * 4 + t) ^ lr)];
+              const u32x4 v = *reinterpret_cast<const u32x4*>(xl + (p * R::ROWS + r * 32) * 256);
               bf16x8 xv;
               __builtin_memcpy(&xv, &v, 16);
 #pragma unroll
@@ -906,17 +947,22 @@ __global__ __launch_bounds__(512) void k_expert_tile(ExpertArgs a) {
           *reinterpret_cast<f32x4*>(sums + ((2 * r + wx) * 16 + lr) * R::PITCH + wm * 64 + i * 16 + quarter * 4) =
               acc[i][r];
     __syncthreads();
-    const int quads = gated ? 32 : 64;
-    for (int i = threadIdx.x; i < here * quads; i += 512) {
-      const int row = i / quads, q = i % quads, pair = list[i0 + row], n = n0 + q * 4;
-      const float* const v = sums + row * R::PITCH;
-      if constexpr (UP) {
-        const int c = gated ? (q >> 3) * 64 + (q & 7) * 4 : q * 4;
-        const f32x4 first = *reinterpret_cast<const f32x4*>(v + c);
-        store_hidden(a, e, pair, n, first, gated ? *reinterpret_cast<const f32x4*>(v + c + 32) : first);
-      } else if (n < N) {
-        *reinterpret_cast<f32x4*>(a.part + (blockIdx.z * a.M * a.top_k + pair) * a.ld_part + n) =
-            *reinterpret_cast<const f32x4*>(v + q * 4);
+    if constexpr (UP) {
+      const int octs = gated ? 16 : 32;
+      for (int i = threadIdx.x; i < here * octs; i += 512) {
+        const int row = i / octs, q = i % octs;
+        const float* const from = sums + row * R::PITCH + (gated ? (q >> 2) * 64 + (q & 3) * 8 : q * 8);
+        float v[8], up[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = from[j], up[j] = from[j + (gated ? 32 : 0)];
+        store_hidden(a, e, list[i0 + row], n0 + q * 8, v, up);
+      }
+    } else {
+      for (int i = threadIdx.x; i < here * 64; i += 512) {
+        const int row = i / 64, q = i % 64;
+        if (n0 + q * 4 < N)
+          *reinterpret_cast<f32x4*>(a.part + (blockIdx.z * a.M * a.top_k + list[i0 + row]) * a.ld_part + n0 + q * 4) =
+              *reinterpret_cast<const f32x4*>(sums + row * R::PITCH + q * 4);
       }
     }
     __syncthreads();
@@ -1176,19 +1222,22 @@ size_t whole(size_t n) { return (n + 255) & ~(size_t)255; }
 struct ExpertSpace {
   int64_t rows, ld_xt, ld_ht, ld_part;
   int x_terms, h_terms, splits;
-  size_t xt, ht, part, total;
+  size_t xt, ht, zeros, part, total;
 };
 ExpertSpace expert_space(int dtype, int64_t M, int64_t F, int64_t H, int64_t N, int E, int top_k, bool gated) {
   ExpertSpace s;
-  s.rows = std::min<int64_t>(M, kExpertRows);
   s.x_terms = dtype == SAGA_BF16 ? 1 : 3;
   s.h_terms = dtype == SAGA_BF16 ? 2 : 3;
   s.ld_xt = (F + 15) / 16 * 16;
   s.ld_ht = (H + 15) / 16 * 16;
+  // (xt, ht and zeros lie within 32-bit offsets of each other)
+  const int64_t row_bytes = 2 * (s.x_terms * s.ld_xt + s.h_terms * top_k * s.ld_ht);
+  s.rows = std::min<int64_t>({M, kExpertRows, ((int64_t)1 << 31) / row_bytes});
   s.ld_part = (N + 3) / 4 * 4;
   s.xt = 0;
   s.ht = s.xt + whole((size_t)s.x_terms * s.rows * s.ld_xt * 2);
-  s.part = s.ht + whole((size_t)s.h_terms * s.rows * top_k * s.ld_ht * 2);
+  s.zeros = s.ht + whole((size_t)s.h_terms * s.rows * top_k * s.ld_ht * 2);
+  s.part = s.zeros + 256;
   s.splits = experts_wide(s.rows, H, N, E, top_k, gated) ? expert_splits(s.rows, H, N, E, top_k) : 1;
   s.total = s.part + whole((size_t)s.splits * s.rows * top_k * s.ld_part * 4);
   return s;
@@ -1214,6 +1263,7 @@ hipError_t launch_experts(const ExpertArgs& a0, hipStream_t st) {
     char* const ws = static_cast<char*>(a0.ws);
     a.xt = reinterpret_cast<uint16_t*>(ws + s.xt);
     a.ht = reinterpret_cast<uint16_t*>(ws + s.ht);
+    a.zeros = reinterpret_cast<uint16_t*>(ws + s.zeros);
     a.part = reinterpret_cast<float*>(ws + s.part);
     a.ld_xt = s.ld_xt;
     a.ld_ht = s.ld_ht;

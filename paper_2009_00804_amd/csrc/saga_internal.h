@@ -277,7 +277,7 @@ struct ExpertArgs {
   void* ws;
   // set by launch_experts: x and the values between the products as planes of bfloat16
   // terms, and the second products' results for each pair of a row and an expert
-  uint16_t *xt, *ht;
+  uint16_t *xt, *ht, *zeros;
   float* part;
   int64_t ld_xt, ld_ht, ld_part;
   int x_terms, h_terms;
