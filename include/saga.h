@@ -700,7 +700,8 @@ saga_status saga_apply_vertex_mx(const saga_mx_op* op, saga_cmat a, saga_cmat a_
  * up: E H x F, gated: E 2H x F, each expert's gate above its up; down: E N x H.  Biases
  * (nullable, float32): router_bias[E], up_bias, one for each row of up, down_bias[E N].  Matrices:
  * 16-byte base and row pitch.  1 <= E <= 1024, 1 <= top_k <= min(E, 16),
- * F, H, N <= 65536.  1024 rows are worked on at a time: of more the weights are read again.
+ * F, H, N <= 65536, ld of up and down below 2^23.  Up to 1024 rows are worked on at a time:
+ * of more the weights are read again.
  * Workspace: saga_apply_vertex_experts_workspace_size() bytes, 256-byte aligned, scratch
  * afterwards, not overlapping any argument.  Calls that share one must be ordered.
  * Errors: SAGA_EINVAL, SAGA_EUNSUPPORTED (sizes), SAGA_EWORKSPACE, SAGA_EDEVICE. */

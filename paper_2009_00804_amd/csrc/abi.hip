@@ -819,6 +819,8 @@ saga_status run_experts(const saga_expert_op& op, const saga_expert_weights& w, 
   const int64_t lds[] = {x.ld, out.ld, w.router.ld, w.up.ld, w.down.ld};
   for (int64_t ld : lds)
     if (ld >= (int64_t)1 << 40) return fail(SAGA_EINVAL, "experts: ld out of range");
+  if (w.up.ld >= saga::kMx4MaxLd || w.down.ld >= saga::kMx4MaxLd)
+    return fail(SAGA_EUNSUPPORTED, "experts: ld of the weights must be below 2^23");
   if ((s = check_extent(M, F, std::max(x.ld, out.ld), "x"))) return s;
   if ((s = check_mat(x.ptr, M, F, x.ld, M, F, es, true, "x"))) return s;
   if ((s = check_mat(out.ptr, out.rows, N, out.ld, M, N, es, true, "out"))) return s;

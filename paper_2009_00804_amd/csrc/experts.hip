@@ -800,46 +800,51 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
 
 // --------------------------------------------------------------------------
 // 4-bit weights and many rows: 256 rows of an expert's weights and RT tiles of 16 rows of x
-// a workgroup.  Both come through LDS by direct-to-LDS loads, 128 k a stage, ST stages:
-// loads come back in their order, and the rows of x, which L2 has, must not wait for weights
-// that were asked for later.  A wave has 64 rows of weights (gate and up of 32 channels, or 64
+// a workgroup.  Both come through LDS by direct-to-LDS loads, weights by whole lines (half
+// of them cost as much), each well ahead of its use.  A wave has 64 rows of weights (gate and up of 32 channels, or 64
 // channels) and every second tile of x.  Past the rows' ends x is zeros and scales are 1,
 // whatever the weights' bits are there.
 // --------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) uint4 lds_uint4;
 
-// LDS at `to` + the lane's place <- 16 (or 4) bytes at the lane's offset from `base`
+// LDS at `to` + the lane's place <- 16 bytes at the lane's offset from `base`, or 4 bytes of its address
 __device__ __forceinline__ void lds_load16(uint32_t to, const void* base, uint32_t offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
                : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base)
                : "memory", "m0");
 }
-__device__ __forceinline__ void lds_load4(uint32_t to, const void* base, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+__device__ __forceinline__ void lds_load4(uint32_t to, const void* from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
                :
-               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base)
+               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
                : "memory", "m0");
 }
 
-template <int TERMS, int RT, int ST>
+template <int TERMS, int RT>
 struct ExpertTile {
   static constexpr int NW = 8, WROWS = 256, ROWS = RT * 16;
-  static constexpr int XL = TERMS * RT * 4 / NW;            // load instructions of a wave for x, 4 rows each
-  static constexpr int LOADS = 2 + 1 + XL;                  // and for weights and scales, a stage
-  static constexpr int W_BYTES = WROWS * 64, S_BYTES = WROWS * 4, X_BYTES = TERMS * ROWS * 256;
-  static constexpr int STAGE = W_BYTES + S_BYTES + X_BYTES;
+  // weights: 256 k (whole lines) a slot, two slots; x: TC groups of 8 k of each lane's block, all
+  // terms, a part, three parts.  A slot is SL parts.
+  static constexpr int TC = TERMS == 1 ? 4 : TERMS == 2 ? 2 : 1, SL = 8 / TC;
+  static constexpr int PPR = 4 * TC;                        // pieces of a row and term in a part
+  static constexpr int XL = TERMS * ROWS * PPR / 64 / NW;   // load instructions of a wave for a part
+  static constexpr int WL = 4 + 1;                          // and for a slot: weights, scales
+  static constexpr int W_BYTES = WROWS * 128, S_BYTES = WROWS * 8, SLOT = W_BYTES + S_BYTES;
+  static constexpr int PART = TERMS * ROWS * PPR * 16;
   static constexpr int PITCH = WROWS + 4;                   // of the sums on their way out, in floats
-  static constexpr int SUMS = ROWS * PITCH * 4;
-  static constexpr int RING = ST * STAGE > SUMS ? ST * STAGE : SUMS;
-  static constexpr int LDS = RING + kExpertRows * 4;
-  static_assert(TERMS * RT * 4 % NW == 0 && RT % 2 == 0, "the same loads and tiles on every wave");
-  static_assert(LDS <= 160 * 1024 - 64 && (ST - 2) * LOADS < 64, "LDS, waits");
+  static constexpr int RING = 2 * SLOT + 3 * PART, LDS = RING + kExpertRows * 4;
+  static_assert(TERMS * ROWS * PPR % (64 * NW) == 0 && RT % 2 == 0, "the same loads and tiles on every wave");
+  static_assert(ROWS * PITCH * 4 <= RING && LDS <= 160 * 1024 - 64, "LDS");
+  // where piece p of row r is among its row's: 16 rows of a fragment read fall on all banks
+  __device__ __forceinline__ static int place(int r, int p) {
+    return p ^ (PPR == 16 ? r & 15 : PPR == 8 ? r >> 1 & 7 : r >> 2 & 3);
+  }
 };
 
-template <int TERMS, bool UP, int RT, int ST>
+template <int TERMS, bool UP, int RT>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_expert_tile(ExpertArgs a) {
-  typedef ExpertTile<TERMS, RT, ST> R;
+  typedef ExpertTile<TERMS, RT> R;
   extern __shared__ uint4 space[];
   char* const base = reinterpret_cast<char*>(space);
   int* const list = reinterpret_cast<int*>(base + R::RING);
@@ -850,88 +855,113 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int quarter = lane >> 4, lr = lane & 15, wm = wave >> 1, wx = wave & 1;
   const int K = UP ? a.F : a.H, N = UP ? a.H : a.N, bytes = (K + 1) / 2, kmax = (bytes - 1) / 16 * 16;
+  const int smax = (K - 1) / 128 * 4;  // the last scales' word
   const bool gated = UP && a.gated;
-  const int all = (K + 127) / 128, per = UP ? all : (all + a.splits - 1) / a.splits;
+  const int all = (K + 255) / 256, per = UP ? all : (all + a.splits - 1) / a.splits;
   const int s0 = UP ? 0 : min(all, (int)blockIdx.z * per), s1 = UP ? all : min(all, s0 + per);
   const int n0 = (int)blockIdx.x * (gated ? 128 : 256);
-  // row r of the stage's weights: 64 a wave; gated: gates of 32 channels, then ups.  A wave's
-  // loads are of rows whose r / 32 is even for all or odd for all: of gates or of ups.
+  // row r of the stage's weights: 64 a wave; gated: gates of 32 channels, then ups
   const int64_t ld_w = UP ? a.ld_up : a.ld_down, ld_s = UP ? a.lds_up : a.lds_down;
-  const int64_t first = gated ? ((int64_t)e * 2 + (wave >> 1 & 1)) * N + n0 : (int64_t)e * N + n0;
-  const int64_t first_s = gated ? ((int64_t)e * 2 + (wave & 1)) * N + n0 : first;
+  const auto row_of = [&](int r) {
+    return gated ? ((int64_t)e * 2 + (r >> 5 & 1)) * N + min(n0 + (r >> 6) * 32 + (r & 31), N - 1)
+                 : (int64_t)e * N + min(n0 + r, N - 1);
+  };
+  // a load of weights has 8 rows: of gates or of ups (from the first row of all of these)
+  const int64_t first = gated ? ((int64_t)e * 2 + (wave >> 2)) * N + n0 : (int64_t)e * N + n0;
   const uint8_t* const w_base = static_cast<const uint8_t*>(UP ? a.up : a.down) + first * ld_w;
-  const uint8_t* const s_base = (UP ? a.up_scale : a.down_scale) + first_s * ld_s;
-  const auto local = [&](int r) { return min(gated ? (r >> 6) * 32 + (r & 31) : r, N - 1 - n0); };
-  uint32_t w_at[2];
-  const int w_piece = ((lane & 3) ^ (lane >> 4 & 3)) * 16;  // (row r = 16 i + lane / 4: r >> 2 & 3 = lane >> 4)
+  const uint8_t* const s_base = UP ? a.up_scale : a.down_scale;
+  uint32_t w_at[4];
+  const int w_piece = ((lane & 7) ^ (lane >> 4 & 3 | (wave & 1) << 2)) * 16;  // (r >> 1 & 7 of row r = 8 i + lane / 8)
 #pragma unroll
-  for (int j = 0; j < 2; ++j) w_at[j] = (uint32_t)local(16 * (wave + 8 * j) + lane / 4) * (uint32_t)ld_w;
-  const uint32_t s_at = (uint32_t)local(wave * 32 + (lane & 31)) * (uint32_t)ld_s;
+  for (int j = 0; j < 4; ++j) w_at[j] = (uint32_t)(row_of(8 * (wave + 8 * j) + lane / 8) - first) * (uint32_t)ld_w;
+  const uint8_t* const s_at = s_base + row_of(wave * 32 + lane / 2) * ld_s;
   const char* const rows = reinterpret_cast<const char*>(UP ? a.xt : a.ht);
   const uint32_t ld = (uint32_t)(UP ? a.ld_xt : a.ld_ht) * 2, plane = (uint32_t)(UP ? a.M : a.M * a.top_k) * ld;
   const uint32_t zeros = (uint32_t)(reinterpret_cast<const char*>(a.zeros) - rows);
-  const uint32_t x_piece = ((lane & 15) ^ ((wave * 4 + (lane >> 4)) & 15)) * 16;
+  // this lane's piece of a row in every load of x: quarter p / TC, group p % TC
+  const int x_row = (wave * 64 + lane) / R::PPR % R::ROWS, p = R::place(x_row, lane % R::PPR);
+  const uint32_t x_piece = p / R::TC * 128 + p % R::TC * 16;
 
   for (int i0 = 0; i0 < count; i0 += R::ROWS) {
     const int here = min(count - i0, R::ROWS), tiles = (here + 15) / 16;
     uint32_t x_at[R::XL];
 #pragma unroll
     for (int j = 0; j < R::XL; ++j) {
-      const int i = (wave + 8 * j) * 4 + (lane >> 4), r = i % R::ROWS, t = i / R::ROWS;
+      const int i = ((wave + 8 * j) * 64 + lane) / R::PPR, r = i % R::ROWS, t = i / R::ROWS;
       const int pair = list[i0 + min(r, here - 1)];
       x_at[j] = t * plane + (uint32_t)(UP ? pair / a.top_k : pair) * ld;
     }
-    const auto issue = [&](int s) {
-      const uint32_t to = lds + s % ST * R::STAGE;
-      const uint32_t w_k = (uint32_t)min(s * 64 + w_piece, kmax), x_k = s * 256 + x_piece;
+    const auto issue_w = [&](int s) {
+      const uint32_t to = lds + (s & 1) * R::SLOT, k = (uint32_t)min(s * 128 + w_piece, kmax);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) lds_load16(to + (wave + 8 * j) * 1024, w_base, w_at[j] + w_k);
-      if (lane < 32) lds_load4(to + R::W_BYTES + wave * 128, s_base, s_at + s * 4);
+      for (int j = 0; j < 4; ++j) lds_load16(to + (wave + 8 * j) * 1024, w_base, w_at[j] + k);
+      lds_load4(to + R::W_BYTES + wave * 256, s_at + min(s * 8 + (lane & 1) * 4, smax));
+    };
+    const auto issue_x = [&](int v, int ring) {  // part v
+      const uint32_t to = lds + 2 * R::SLOT + ring * R::PART;
+      const int g = v % R::SL * R::TC;  // its first group: of block g / 4, groups g % 4..
+      const uint32_t k = v / R::SL * 512 + (g >> 2) * 64 + (g & 3) * 16 + x_piece;
 #pragma unroll
-      for (int j = 0; j < R::XL; ++j)
-        lds_load16(to + R::W_BYTES + R::S_BYTES + (wave + 8 * j) * 1024, rows, x_k < ld ? x_at[j] + x_k : zeros);
+      for (int j = 0; j < R::XL; ++j) lds_load16(to + (wave + 8 * j) * 1024, rows, k < ld ? x_at[j] + k : zeros);
     };
     f32x4 acc[4][RT / 2];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int r = 0; r < RT / 2; ++r) acc[i][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int d = 0; d < ST - 1; ++d)
-      if (s0 + d < s1) issue(s0 + d);
+    int ring = 0;  // where part v is; v + 1 and v + 2 follow
+    if (s0 < s1) {
+      issue_w(s0);
+      issue_x(s0 * R::SL, 0);
+      issue_x(s0 * R::SL + 1, 1);
+    }
     for (int s = s0; s < s1; ++s) {
-      if (s + ST - 2 < s1) wait_vm<(ST - 2) * R::LOADS>();
-      else wait_vm<0>();
-      ring_barrier();  // stage s is in LDS, and nobody reads stage s - 1 any more
-      if (s + ST - 1 < s1) issue(s + ST - 1);
-      const char* const stage = base + s % ST * R::STAGE;
-      const char* const wl = stage + (wm * 64 + lr) * 64 + (quarter ^ (lr >> 2)) * 16;
-      const char* const sl = stage + R::W_BYTES + (wm * 64 + lr) * 4 + quarter;
-      const bool past = (s * 4 + quarter) * 32 >= K;
-      WeightBlocks<true, 1> w[4];
+      const bool more = s + 1 < s1;
+      WeightBlocks<true, 2> w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w[i].v[0] = *reinterpret_cast<const u32x4*>(wl + i * 1024);
-        w[i].scale = *reinterpret_cast<const uint8_t*>(sl + i * 64);
-        w[i].scale = past ? 127u : w[i].scale;
-      }
+      for (int m = 0; m < R::SL; ++m) {
+        // Part v = s SL + m has to be there, and with m = 0 slot s: of what was asked for later,
+        // part v + 1 and (behind part s SL + 2) slot s + 1 may still be on their way.
+        const int v = s * R::SL + m;
+        if (m + 1 == R::SL && !more) wait_vm<0>();
+        else if ((m == 1 || (m == 2 && R::SL > 2)) && more) wait_vm<R::XL + R::WL>();
+        else wait_vm<R::XL>();
+        ring_barrier();  // and nobody reads part v - 1, or with m = 0 slot s - 1, any more
+        if (m + 2 < R::SL || more) issue_x(v + 2, ring == 0 ? 2 : ring - 1);
+        if (m == 0 && more) issue_w(s + 1);
+        const char* const slot = base + (s & 1) * R::SLOT;
+        const char* const part = base + 2 * R::SLOT + ring * R::PART;
+        ring = ring == 2 ? 0 : ring + 1;
+        const int j = m * R::TC / 4, t0 = m * R::TC % 4;
+        if (t0 == 0) {  // the lane's block 2 quarter + j of the slot
+          const int r0 = wm * 64 + lr;
+          const char* const wl = slot + r0 * 128 + ((quarter * 2 + j) ^ (r0 >> 1 & 7)) * 16;
+          const bool past = (s * 8 + quarter * 2 + j) * 32 >= K;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        bf16x8 wv[4];
+          for (int i = 0; i < 4; ++i) {
+            w[i].v[j] = *reinterpret_cast<const u32x4*>(wl + i * 16 * 128);
+            const uint32_t b = *reinterpret_cast<const uint8_t*>(slot + R::W_BYTES + r0 * 8 + i * 128 + quarter * 2 + j);
+            w[i].scale = (past ? 127u : b) << (8 * j);
+          }
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) wv[i] = w[i].take(0, t);
-        const char* const xl = stage + R::W_BYTES + R::S_BYTES + (wx * 16 + lr) * 256 + ((quarter * 4 + t) ^ lr) * 16;
+        for (int t = 0; t < R::TC; ++t) {
+          bf16x8 wv[4];
 #pragma unroll
-        for (int r = 0; r < RT / 2; ++r) {
-          if (2 * r + wx < tiles) {
+          for (int i = 0; i < 4; ++i) wv[i] = w[i].take(j, t0 + t);
+          const char* const xl = part + ((wx * 16 + lr) * R::PPR + R::place(lr, quarter * R::TC + t)) * 16;
 #pragma unroll
-            for (int p = 0; p < TERMS; ++p) {
-              const u32x4 v = *reinterpret_cast<const u32x4*>(xl + (p * R::ROWS + r * 32) * 256);
-              bf16x8 xv;
-              __builtin_memcpy(&xv, &v, 16);
+          for (int r = 0; r < RT / 2; ++r) {
+            if (2 * r + wx < tiles) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                acc[i][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], xv, acc[i][r], 0, 0, 0);
+              for (int p = 0; p < TERMS; ++p) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(xl + (p * R::ROWS + r * 32) * R::PPR * 16);
+                bf16x8 xv;
+                __builtin_memcpy(&xv, &x, 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  acc[i][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], xv, acc[i][r], 0, 0, 0);
+              }
             }
           }
         }
@@ -1168,12 +1198,12 @@ hipError_t launch_wide(const ExpertArgs& a, hipStream_t st) {
                      dim3((unsigned)((n + per - 1) / per), slots, UP ? 1 : a.splits), dim3(64 * NW), lds, st, a);
   return hipGetLastError();
 }
-template <int TERMS, bool UP, int RT, int ST>
+template <int TERMS, bool UP, int RT>
 hipError_t launch_expert_tile(const ExpertArgs& a, hipStream_t st) {
   const unsigned slots = (unsigned)std::min<int64_t>(a.M * a.top_k, a.E);
   const int per = UP && a.gated ? 128 : 256, n = UP ? a.H : a.N;
-  constexpr size_t lds = ExpertTile<TERMS, RT, ST>::LDS;
-  hipLaunchKernelGGL((k_expert_tile<TERMS, UP, RT, ST>), dim3((unsigned)((n + per - 1) / per), slots, UP ? 1 : a.splits),
+  constexpr size_t lds = ExpertTile<TERMS, RT>::LDS;
+  hipLaunchKernelGGL((k_expert_tile<TERMS, UP, RT>), dim3((unsigned)((n + per - 1) / per), slots, UP ? 1 : a.splits),
                      dim3(512), lds, st, a);
   return hipGetLastError();
 }
@@ -1189,8 +1219,7 @@ hipError_t dispatch_wide(const ExpertArgs& a, hipStream_t st) {
     return hipGetLastError();
   }
   if constexpr (MX4) {
-    if (mean <= 40 || TERMS == 3) return launch_expert_tile<TERMS, UP, 4, TERMS == 1 ? 4 : TERMS == 2 ? 3 : 2>(a, st);
-    if constexpr (TERMS < 3) return launch_expert_tile<TERMS, UP, 6, TERMS == 1 ? 3 : 2>(a, st);
+    return launch_expert_tile<TERMS, UP, TERMS == 3 ? 8 : 6>(a, st);
   } else {
     return launch_wide<MX4, TERMS, UP, 4, 8>(a, st);
   }

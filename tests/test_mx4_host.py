@@ -164,6 +164,8 @@ def test_expert_refusals(S):
     call(S.SAGA_EUNSUPPORTED, "too large", x=(A, 6, wide, wide))
     call(S.SAGA_EUNSUPPORTED, "too large", up=(G, 8 * wide, 20, 32))
     call(S.SAGA_EUNSUPPORTED, "too large", out=(B, 6, wide, wide))
+    call(S.SAGA_EUNSUPPORTED, "2^23", up=(G, 192, 20, 1 << 23))
+    call(S.SAGA_EUNSUPPORTED, "2^23", down=(H, 40, 12, 1 << 23))
     call(S.SAGA_EINVAL, "x: null", x=(None, 6, 40, 40))
     call(S.SAGA_EINVAL, "out: null", out=(None, 6, 10, 12))
     call(S.SAGA_EINVAL, "out: shape", out=(B, 5, 10, 12))
