@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_device.h"
 #include "mx4_device.h"
@@ -853,7 +854,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   if (e < 0) return;
   const uint32_t lds = (uint32_t)(uintptr_t)(lds_uint4*)space;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int quarter = lane >> 4, lr = lane & 15, wm = wave >> 1, wx = wave & 1;
+  const int quarter = lane >> 4, lr = lane & 15;
+  const int wm = wave & 3, wx = wave >> 2;  // (waves w and w + 4 share a SIMD: one of each half of x)
   const int K = UP ? a.F : a.H, N = UP ? a.H : a.N, bytes = (K + 1) / 2, kmax = (bytes - 1) / 16 * 16;
   const int smax = (K - 1) / 128 * 4;  // the last scales' word
   const bool gated = UP && a.gated;
@@ -909,12 +911,16 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int r = 0; r < RT / 2; ++r) acc[i][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    int ring = 0;  // where part v is; v + 1 and v + 2 follow
     if (s0 < s1) {
       issue_w(s0);
       issue_x(s0 * R::SL, 0);
       issue_x(s0 * R::SL + 1, 1);
     }
+    // (how many tiles the wave has is part of the code: a branch around each would keep the
+    // reads of the next one behind the products of the last)
+    const auto products = [&](auto count_tag) {
+    constexpr int NT = decltype(count_tag)::value;
+    int ring = 0;  // where part v is; v + 1 and v + 2 follow
     for (int s = s0; s < s1; ++s) {
       const bool more = s + 1 < s1;
       WeightBlocks<true, 2> w[4];
@@ -951,21 +957,27 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
           for (int i = 0; i < 4; ++i) wv[i] = w[i].take(j, t0 + t);
           const char* const xl = part + ((wx * 16 + lr) * R::PPR + R::place(lr, quarter * R::TC + t)) * 16;
 #pragma unroll
-          for (int r = 0; r < RT / 2; ++r) {
-            if (2 * r + wx < tiles) {
+          for (int r = 0; r < NT; ++r) {
 #pragma unroll
-              for (int p = 0; p < TERMS; ++p) {
-                const u32x4 x = *reinterpret_cast<const u32x4*>(xl + (p * R::ROWS + r * 32) * R::PPR * 16);
-                bf16x8 xv;
-                __builtin_memcpy(&xv, &x, 16);
+            for (int p = 0; p < TERMS; ++p) {
+              const u32x4 x = *reinterpret_cast<const u32x4*>(xl + (p * R::ROWS + r * 32) * R::PPR * 16);
+              bf16x8 xv;
+              __builtin_memcpy(&xv, &x, 16);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  acc[i][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], xv, acc[i][r], 0, 0, 0);
-              }
+              for (int i = 0; i < 4; ++i)
+                acc[i][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], xv, acc[i][r], 0, 0, 0);
             }
           }
         }
       }
+    }
+    };
+    switch ((tiles - wx + 1) / 2) {
+      case 0: products(std::integral_constant<int, 0>{}); break;
+      case 1: products(std::integral_constant<int, 1>{}); break;
+      case 2: products(std::integral_constant<int, 2>{}); break;
+      case 3: products(std::integral_constant<int, 3>{}); break;
+      default: products(std::integral_constant<int, RT / 2>{}); break;
     }
     ring_barrier();  // the stages are free: the sums go through them, to leave by whole rows
     float* const sums = reinterpret_cast<float*>(base);
