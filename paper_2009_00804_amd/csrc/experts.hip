@@ -245,6 +245,19 @@ struct WeightBlocks<false, 1> {
   }
 };
 
+// What a workgroup works on: `runs` parts of the weights' rows and `parts` of k for each slot.  Workgroup
+// w runs on XCD w % 8: all of a slot's go to one, whose L2 then has the rows of x that they share.
+struct Share {
+  int slot, run, part;
+};
+__device__ __forceinline__ Share share_of(int slots, int runs, int parts) {
+  const int i = blockIdx.x / kXcds, each = runs * parts;
+  return {i / each * kXcds + (int)(blockIdx.x % kXcds), i % each % runs, i % each / runs};
+}
+unsigned share_blocks(int64_t slots, int64_t runs, int64_t parts) {
+  return (unsigned)((slots + kXcds - 1) / kXcds * kXcds * runs * parts);
+}
+
 // This workgroup's expert (-1: none) and its pairs (row * top_k + place), in some order (no
 // result depends on it).  Up to E pairs a slot is a pair, which stands for its expert if no
 // earlier pair does; otherwise a slot is an expert.
@@ -689,17 +702,20 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
   constexpr int PART = TERMS * ROWS * 16;
   int* const list = reinterpret_cast<int*>(space + 2 * PART);
   int count;
-  const int e = slot_expert<NW>(a, blockIdx.y, list, count);
+  const int slots = min((int)a.M * a.top_k, a.E), width = NW * (UP && a.gated ? 16 : 32);
+  const Share me = share_of(slots, ((UP ? a.H : a.N) + width - 1) / width, UP ? 1 : a.splits);
+  if (me.slot >= slots) return;
+  const int e = slot_expert<NW>(a, me.slot, list, count);
   if (e < 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int quarter = lane >> 4, lr = lane & 15;
   const int K = UP ? a.F : a.H, N = UP ? a.H : a.N;
   const bool gated = UP && a.gated;
   const int all = (K + 128 * J - 1) / (128 * J), per = UP ? all : (all + a.splits - 1) / a.splits;
-  const int s0 = UP ? 0 : blockIdx.z * per, s1 = UP ? all : min(all, s0 + per);
+  const int s0 = UP ? 0 : me.part * per, s1 = UP ? all : min(all, s0 + per);
   const int64_t ld = UP ? a.ld_xt : a.ld_ht, plane = (UP ? a.M : a.M * a.top_k) * ld;
   const uint16_t* const rows = UP ? a.xt : a.ht;
-  const int n0 = ((int)blockIdx.x * NW + wave) * (gated ? 16 : 32);
+  const int n0 = me.run * width + wave * (gated ? 16 : 32);
   WeightBlocks<MX4, J> w[AHEAD][2];
   WeightRow<MX4> weights[2];
 #pragma unroll
@@ -791,7 +807,7 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
         store_hidden(a, e, pair, n, acc[r][0], acc[r][1]);
         if (!gated) store_hidden(a, e, pair, n + 16, acc[r][1], acc[r][1]);
       } else {
-        float* const o = a.part + (blockIdx.z * a.M * a.top_k + pair) * a.ld_part + n;
+        float* const o = a.part + (me.part * a.M * a.top_k + pair) * a.ld_part + n;
         if (n < N) *reinterpret_cast<f32x4*>(o) = acc[r][0];
         if (n + 16 < N) *reinterpret_cast<f32x4*>(o + 16) = acc[r][1];
       }
@@ -850,7 +866,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   char* const base = reinterpret_cast<char*>(space);
   int* const list = reinterpret_cast<int*>(base + R::RING);
   int count;
-  const int e = slot_expert<R::NW>(a, blockIdx.y, list, count);
+  const int slots = min((int)a.M * a.top_k, a.E), width = UP && a.gated ? 128 : 256;
+  const Share me = share_of(slots, ((UP ? a.H : a.N) + width - 1) / width, UP ? 1 : a.splits);
+  if (me.slot >= slots) return;
+  const int e = slot_expert<R::NW>(a, me.slot, list, count);
   if (e < 0) return;
   const uint32_t lds = (uint32_t)(uintptr_t)(lds_uint4*)space;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -860,8 +879,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   const int smax = (K - 1) / 128 * 4;  // the last scales' word
   const bool gated = UP && a.gated;
   const int all = (K + 255) / 256, per = UP ? all : (all + a.splits - 1) / a.splits;
-  const int s0 = UP ? 0 : min(all, (int)blockIdx.z * per), s1 = UP ? all : min(all, s0 + per);
-  const int n0 = (int)blockIdx.x * (gated ? 128 : 256);
+  const int s0 = UP ? 0 : min(all, me.part * per), s1 = UP ? all : min(all, s0 + per);
+  const int n0 = me.run * width;
   // row r of the stage's weights: 64 a wave; gated: gates of 32 channels, then ups
   const int64_t ld_w = UP ? a.ld_up : a.ld_down, ld_s = UP ? a.lds_up : a.lds_down;
   const auto row_of = [&](int r) {
@@ -1003,7 +1022,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
       for (int i = threadIdx.x; i < here * 64; i += 512) {
         const int row = i / 64, q = i % 64;
         if (n0 + q * 4 < N)
-          *reinterpret_cast<f32x4*>(a.part + (blockIdx.z * a.M * a.top_k + list[i0 + row]) * a.ld_part + n0 + q * 4) =
+          *reinterpret_cast<f32x4*>(a.part + (me.part * a.M * a.top_k + list[i0 + row]) * a.ld_part + n0 + q * 4) =
               *reinterpret_cast<const f32x4*>(sums + row * R::PITCH + q * 4);
       }
     }
@@ -1029,17 +1048,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   __shared__ u32x4 xs[kStreamPieces];
   __shared__ int list[kExpertRows];
   int count;
-  const int e = slot_expert<NW>(a, blockIdx.y, list, count);
+  const int slots = min((int)a.M * a.top_k, a.E);
+  const Share me = share_of(slots, (runs + per - 1) / per, UP ? 1 : a.splits);
+  if (me.slot >= slots) return;
+  const int e = slot_expert<NW>(a, me.slot, list, count);
   if (e < 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int quarter = lane >> 4, lr = lane & 15;
   const int K = UP ? a.F : a.H, N = UP ? a.H : a.N;
   const bool gated = UP && a.gated;
   const int all = (K + 128 * J - 1) / (128 * J), part = UP ? all : (all + a.splits - 1) / a.splits;
-  const int k0 = UP ? 0 : min(all, (int)blockIdx.z * part), steps = UP ? all : min(part, all - k0);  // from step k0 on
+  const int k0 = UP ? 0 : min(all, me.part * part), steps = UP ? all : min(part, all - k0);  // from step k0 on
   const int64_t ld = UP ? a.ld_xt : a.ld_ht, plane = (UP ? a.M : a.M * a.top_k) * ld;
   const uint16_t* const rows = UP ? a.xt : a.ht;
-  const int run0 = blockIdx.x * per, run1 = min(runs, run0 + per);
+  const int run0 = me.run * per, run1 = min(runs, run0 + per);
   const auto channel = [&](int run) { return (run * NW + wave) * (gated ? 16 : 32); };
   WeightRow<MX4> from[2];
   const auto rows_of = [&](int run) {
@@ -1130,7 +1152,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
           store_hidden(a, e, pair, n, acc[0], acc[1]);
           if (!gated) store_hidden(a, e, pair, n + 16, acc[1], acc[1]);
         } else {
-          float* const o = a.part + (blockIdx.z * a.M * a.top_k + pair) * a.ld_part + n;
+          float* const o = a.part + (me.part * a.M * a.top_k + pair) * a.ld_part + n;
           if (n < N) *reinterpret_cast<f32x4*>(o) = acc[0];
           if (n + 16 < N) *reinterpret_cast<f32x4*>(o + 16) = acc[1];
         }
@@ -1207,7 +1229,7 @@ hipError_t launch_wide(const ExpertArgs& a, hipStream_t st) {
   const int per = NW * (UP && a.gated ? 16 : 32), n = UP ? a.H : a.N;
   const size_t lds = (size_t)2 * TERMS * RT * 16 * 16 * 16 + (size_t)a.M * 4;
   hipLaunchKernelGGL((k_expert_wide<MX4, TERMS, UP, RT, NW>),
-                     dim3((unsigned)((n + per - 1) / per), slots, UP ? 1 : a.splits), dim3(64 * NW), lds, st, a);
+                     dim3(share_blocks(slots, (n + per - 1) / per, UP ? 1 : a.splits)), dim3(64 * NW), lds, st, a);
   return hipGetLastError();
 }
 template <int TERMS, bool UP, int RT>
@@ -1215,7 +1237,7 @@ hipError_t launch_expert_tile(const ExpertArgs& a, hipStream_t st) {
   const unsigned slots = (unsigned)std::min<int64_t>(a.M * a.top_k, a.E);
   const int per = UP && a.gated ? 128 : 256, n = UP ? a.H : a.N;
   constexpr size_t lds = ExpertTile<TERMS, RT>::LDS;
-  hipLaunchKernelGGL((k_expert_tile<TERMS, UP, RT>), dim3((unsigned)((n + per - 1) / per), slots, UP ? 1 : a.splits),
+  hipLaunchKernelGGL((k_expert_tile<TERMS, UP, RT>), dim3(share_blocks(slots, (n + per - 1) / per, UP ? 1 : a.splits)),
                      dim3(512), lds, st, a);
   return hipGetLastError();
 }
@@ -1226,8 +1248,7 @@ hipError_t dispatch_wide(const ExpertArgs& a, hipStream_t st) {
     const int64_t slots = std::min<int64_t>(a.M * a.top_k, a.E), rows = UP ? (int64_t)a.H * (a.gated ? 2 : 1) : a.N;
     const int64_t z = UP ? 1 : a.splits, runs = (rows + 127) / 128, per = std::max<int64_t>(1, runs * slots * z / 640);
     hipLaunchKernelGGL((k_expert_stream<MX4, TERMS, UP>),
-                       dim3((unsigned)((runs + per - 1) / per), (unsigned)slots, (unsigned)z), dim3(256), 0, st, a,
-                       (int)runs, (int)per);
+                       dim3(share_blocks(slots, (runs + per - 1) / per, z)), dim3(256), 0, st, a, (int)runs, (int)per);
     return hipGetLastError();
   }
   if constexpr (MX4) {
