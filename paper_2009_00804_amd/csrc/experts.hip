@@ -843,7 +843,7 @@ struct ExpertTile {
   static constexpr int NW = 8, WROWS = 256, ROWS = RT * 16;
   // weights: 256 k (whole lines) a slot, two slots; x: TC groups of 8 k of each lane's block, all
   // terms, a part, three parts.  A slot is SL parts.
-  static constexpr int TC = TERMS == 1 ? 4 : TERMS == 2 ? 2 : 1, SL = 8 / TC;
+  static constexpr int TC = TERMS == 1 || RT * TERMS <= 6 ? 4 : 2, SL = 8 / TC;
   static constexpr int PPR = 4 * TC;                        // pieces of a row and term in a part
   static constexpr int XL = TERMS * ROWS * PPR / 64 / NW;   // load instructions of a wave for a part
   static constexpr int WL = 4 + 1;                          // and for a slot: weights, scales
@@ -852,7 +852,7 @@ struct ExpertTile {
   static constexpr int PITCH = WROWS + 4;                   // of the sums on their way out, in floats
   static constexpr int RING = 2 * SLOT + 3 * PART, LDS = RING + kExpertRows * 4;
   static_assert(TERMS * ROWS * PPR % (64 * NW) == 0 && RT % 2 == 0, "the same loads and tiles on every wave");
-  static_assert(ROWS * PITCH * 4 <= RING && LDS <= 160 * 1024 - 64, "LDS");
+  static_assert(ROWS * PITCH * 4 <= RING && RT <= 6 && LDS <= 160 * 1024 - 64, "LDS");
   // where piece p of row r is among its row's: 16 rows of a fragment read fall on all banks
   __device__ __forceinline__ static int place(int r, int p) {
     return p ^ (PPR == 16 ? r & 15 : PPR == 8 ? r >> 1 & 7 : r >> 2 & 3);
@@ -994,8 +994,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     switch ((tiles - wx + 1) / 2) {
       case 0: products(std::integral_constant<int, 0>{}); break;
       case 1: products(std::integral_constant<int, 1>{}); break;
-      case 2: products(std::integral_constant<int, 2>{}); break;
-      case 3: products(std::integral_constant<int, 3>{}); break;
+      case 2: products(std::integral_constant<int, RT / 2 < 2 ? RT / 2 : 2>{}); break;
       default: products(std::integral_constant<int, RT / 2>{}); break;
     }
     ring_barrier();  // the stages are free: the sums go through them, to leave by whole rows
@@ -1252,7 +1251,9 @@ hipError_t dispatch_wide(const ExpertArgs& a, hipStream_t st) {
     return hipGetLastError();
   }
   if constexpr (MX4) {
-    return launch_expert_tile<TERMS, UP, TERMS == 3 ? 8 : 6>(a, st);
+    if (mean <= 20) return launch_expert_tile<TERMS, UP, 2>(a, st);
+    if (mean <= 40 || TERMS == 3) return launch_expert_tile<TERMS, UP, 4>(a, st);
+    if constexpr (TERMS < 3) return launch_expert_tile<TERMS, UP, 6>(a, st);
   } else {
     return launch_wide<MX4, TERMS, UP, 4, 8>(a, st);
   }
