@@ -1243,7 +1243,7 @@ hipError_t launch_expert_tile(const ExpertArgs& a, hipStream_t st) {
 template <bool MX4, int TERMS, bool UP>
 hipError_t dispatch_wide(const ExpertArgs& a, hipStream_t st) {
   const int64_t mean = a.M * a.top_k / a.E;
-  if (a.M <= 16 || mean <= 8) {
+  if (mean <= (MX4 ? 4 : 8)) {
     const int64_t slots = std::min<int64_t>(a.M * a.top_k, a.E), rows = UP ? (int64_t)a.H * (a.gated ? 2 : 1) : a.N;
     const int64_t z = UP ? 1 : a.splits, runs = (rows + 127) / 128, per = std::max<int64_t>(1, runs * slots * z / 640);
     hipLaunchKernelGGL((k_expert_stream<MX4, TERMS, UP>),
