@@ -233,13 +233,16 @@ struct Tile {
   static constexpr int STAGE = ROWS * PR;                       // 16-byte slots
   static constexpr int GROUPS = ROWS / 16;                      // load instructions per stage
   static constexpr int LB = (GROUPS + NW - 1) / NW;             // of one wave
-  static constexpr int SR = (ROWS + NW - 1) / NW;               // rows whose scales a wave loads
+  // Scales are loaded for four stages at a time, 16 bytes a row, a quarter of a wave's SR rows
+  // with each stage: a word a row for every stage asked for as many lines as the rows do.
+  // The four stages AHEAD of the present four are on their way.
+  static constexpr int SR = (ROWS + NW - 1) / NW / 4 * 4, AHEAD = (ST + 7) / 4, SETS = AHEAD + 1;
   static constexpr int LOADS = LB + 1;
   static constexpr int NP = 8 * NI;                             // 16-byte pieces of a wave's row of sums
   static constexpr int SLOTS = ST * STAGE > NW * 32 * NP ? ST * STAGE : NW * 32 * NP;
-  static_assert(SR <= 64, "one load instruction for a wave's scales");
+  static_assert(SR <= 64 && SR * NW == ROWS, "one load instruction for a quarter of a wave's scales");
   static_assert(ST == 2 || (GROUPS % NW == 0 && ROWS % NW == 0), "a wait counts the same loads on every wave");
-  static constexpr int LDS = SLOTS * 16 + ST * NW * SR * 4 + ROWS * 4;
+  static constexpr int LDS = SLOTS * 16 + SETS * ROWS * 16 + ROWS * 4;
   static constexpr int WAVES = 160 * 1024 / LDS * NW / 4;       // waves a SIMD that LDS has room for
   static constexpr int WPE = WAVES < 4 ? WAVES : 4;             // (more would spill registers)
   // slot of piece p of row r: the 16 rows of a fragment read fall on all banks
@@ -259,7 +262,7 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
                                                                                     int tiles_n) {
   typedef Tile<WM, WN, MI, NI, ST> R;
   __shared__ uint4 ring[R::SLOTS];
-  __shared__ uint32_t ring_scales[ST][R::NW * R::SR];
+  __shared__ uint32_t scales[R::SETS][R::ROWS * 4];
   __shared__ f32x4 ends[R::ROWS / 4];  // degree scalings of the rows, bias of the channels
   // Workgroup w runs on XCD w % 8: every XCD gets a run of tiles, and in it eight
   // row tiles share each column tile.
@@ -289,21 +292,28 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
     piece[j] = (R::slot(r, lane % 4) % 4) * 16;
     off[j] = (uint32_t)row_of(r) * (uint32_t)(r < R::BM ? g.lda : g.ldw);
   }
-  const int sr = min(wave * R::SR + lane, R::ROWS - 1);
-  const uint8_t* const scale_at = sr < R::BM ? g.a_scale + (m0 + row_of(sr)) * g.lda_s
-                                             : g.w_scale + (n0 + row_of(sr)) * g.ldw_s;
+  const int smax = (K - 1) / 128;  // the last scales' word
+  // a quarter of this wave's scales of the chunks 4 t.. : lane / 4 a row, lane % 4 a chunk
+  const auto issue_scales = [&](int t, int q) {
+    const int r = wave * R::SR + q * (R::SR / 4) + lane / 4;
+    const bool is_a = r < R::BM;
+    const uint32_t at = (uint32_t)row_of(r) * (uint32_t)(is_a ? g.lda_s : g.ldw_s) + min(t * 4 + (lane & 3), smax) * 4;
+    const uint8_t* const from = (is_a ? g.a_scale + m0 * g.lda_s : g.w_scale + n0 * g.ldw_s) + at;
+    if (R::SR == 64 || lane < R::SR)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                   :
+                   : "s"(__builtin_amdgcn_readfirstlane(
+                         (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t*)scales[t % R::SETS] +
+                         (wave * R::SR + q * (R::SR / 4)) * 16)),
+                     "v"(from)
+                   : "memory", "m0");
+  };
   // load j of chunk c; only the last chunk can reach past the rows' ends, where it
-  // reads their last piece again (masked before use).  Load LB: the scales.
+  // reads their last piece again (masked before use).  Load LB: scales, with chunk c = c' + ST
+  // those of the four chunks AHEAD of those of c'.
   const auto issue = [&](int c, int j) {
     if (j == R::LB) {
-      if (R::SR == 64 || lane < R::SR)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
-                     :
-                     : "s"(__builtin_amdgcn_readfirstlane(
-                           (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t*)ring_scales[c % ST] +
-                           wave * R::SR * 4)),
-                       "v"(scale_at + c * 4)
-                     : "memory", "m0");
+      issue_scales((c - ST) / 4 + R::AHEAD, (c - ST) & 3);
       return;
     }
     const int grp = wave + j * R::NW;
@@ -315,11 +325,13 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
                    "v"(off[j] + (uint32_t)min(c * 64 + piece[j], kmax)), "s"(base)
                  : "memory", "m0");
   };
+  for (int t = 0; t < R::AHEAD; ++t)
+    for (int q = 0; q < 4; ++q) issue_scales(t, q);
 #pragma unroll
   for (int c = 0; c < ST; ++c)
     if (c <= last)
 #pragma unroll
-      for (int j = 0; j < R::LOADS; ++j) issue(c, j);
+      for (int j = 0; j < R::LB; ++j) issue(c, j);
   {
     float* e = reinterpret_cast<float*>(ends);
     for (int i = threadIdx.x; i < R::BM; i += R::THREADS)
@@ -342,30 +354,37 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
   for (int s = 0; s < 2; ++s) at[s] = R::slot(lr, 2 * half + s);
 
   // Fragments of a step are read into one half of a and w while those in the other
-  // half are multiplied; the scales of a chunk into one half of sa and sw.
+  // half are multiplied.
   u32x4 a[2][MI], w[2][NI];
-  uint32_t sa[2][MI], sw[2][NI];
+  uint32_t sa[MI], sw[NI], sa_next[MI], sw_next[NI];
   const auto read_w = [&](int c, int s, int ni) {
     w[s][ni] = *(lds_cu32x4*)(lds + (c % ST) * R::STAGE + at[s] + (R::BM + (wn * NI + ni) * 32) * R::PR);
   };
   const auto read_a = [&](int c, int s, int mi) {
     a[s][mi] = *(lds_cu32x4*)(lds + (c % ST) * R::STAGE + at[s] + (wm * MI + mi) * 32 * R::PR);
   };
-  const auto read_scales = [&](int c, int p) {
-    const uint16_t* const sc = reinterpret_cast<const uint16_t*>(ring_scales[c % ST]) + lr * 2 + half;
+  const auto read_scales = [&](int c) {
+    const uint16_t* const sc =
+        reinterpret_cast<const uint16_t*>(scales[c / 4 % R::SETS]) + lr * 8 + (c & 3) * 2 + half;
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) sa[p][mi] = sc[(wm * MI + mi) * 64];
+    for (int mi = 0; mi < MI; ++mi) sa_next[mi] = sc[(wm * MI + mi) * 256];
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni) sw[p][ni] = sc[(R::BM + (wn * NI + ni) * 32) * 2];
+    for (int ni = 0; ni < NI; ++ni) sw_next[ni] = sc[(R::BM + (wn * NI + ni) * 32) * 8];
   };
-  // Chunk c, its first fragments read, its scales in half p.  Before its last step chunk
+  const auto turn = [&] {
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) sa[mi] = sa_next[mi];
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) sw[ni] = sw_next[ni];
+  };
+  // Chunk c, its first fragments and scales read.  Before its last step chunk
   // c + 1 has to have landed, for every wave; every wave then has chunk c's fragments in
   // registers, and chunk c + ST takes its stage.  The reads of the next fragments and, where
   // FILL, the loads go between the row tiles: in one run either would hold up the products
   // behind it.
-  const auto chunk = [&](auto fill_tag, auto half_tag, int c) {
+  const auto chunk = [&](auto fill_tag, int c) {
     constexpr bool FILL = decltype(fill_tag)::value;
-    constexpr int P = decltype(half_tag)::value, WR = (NI + MI - 1) / MI;
+    constexpr int WR = (NI + MI - 1) / MI;
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
 #pragma unroll
@@ -373,13 +392,13 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
         if (mi * WR + k < NI) read_w(c, 1, mi * WR + k);
       read_a(c, 1, mi);
 #pragma unroll
-      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = mma_tile<0>(w[0][ni], a[0][mi], acc[mi][ni], sw[P][ni], sa[P][mi]);
+      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = mma_tile<0>(w[0][ni], a[0][mi], acc[mi][ni], sw[ni], sa[mi]);
       __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (FILL) wait_vm<(ST - 2) * R::LOADS>();
     else wait_vm<0>();
     ring_barrier();
-    read_scales(c + 1, P ^ 1);
+    read_scales(c + 1);
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
 #pragma unroll
@@ -392,38 +411,26 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
           if (j * MI / R::LOADS == mi) issue(c + ST, j);
       }
 #pragma unroll
-      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = mma_tile<1>(w[1][ni], a[1][mi], acc[mi][ni], sw[P][ni], sa[P][mi]);
+      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = mma_tile<1>(w[1][ni], a[1][mi], acc[mi][ni], sw[ni], sa[mi]);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  typedef std::integral_constant<int, 0> P0;
-  typedef std::integral_constant<int, 1> P1;
 
   wait_vm<0>();
   ring_barrier();
-  read_scales(0, 0);
+  read_scales(0);
+  turn();
 #pragma unroll
   for (int ni = 0; ni < NI; ++ni) read_w(0, 0, ni);
 #pragma unroll
   for (int mi = 0; mi < MI; ++mi) read_a(0, 0, mi);
   int c = 0;
-  const auto turn = [&] {  // the next chunk's scales to the first half
-#pragma unroll
-    for (int mi = 0; mi < MI; ++mi) sa[0][mi] = sa[1][mi];
-#pragma unroll
-    for (int ni = 0; ni < NI; ++ni) sw[0][ni] = sw[1][ni];
-  };
-  for (; c + 1 + ST <= last; c += 2) {
-    chunk(std::true_type{}, P0{}, c);
-    chunk(std::true_type{}, P1{}, c + 1);
-  }
-  if (c + ST <= last) {
-    chunk(std::true_type{}, P0{}, c);
-    ++c;
+  for (; c + ST <= last; ++c) {
+    chunk(std::true_type{}, c);
     turn();
   }
   for (; c < last; ++c) {
-    chunk(std::false_type{}, P0{}, c);
+    chunk(std::false_type{}, c);
     turn();
   }
   // the last chunk: w's bytes past the rows' ends are zeros, scales past them 1 (they
@@ -442,17 +449,17 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
     if (left <= 16 * s) {
       const uint32_t keep = s ? 0x00ffu : 0xff00u, one = s ? 0x7f00u : 0x007fu;
 #pragma unroll
-      for (int ni = 0; ni < NI; ++ni) sw[0][ni] = (sw[0][ni] & keep) | one;
+      for (int ni = 0; ni < NI; ++ni) sw[ni] = (sw[ni] & keep) | one;
 #pragma unroll
-      for (int mi = 0; mi < MI; ++mi) sa[0][mi] = (sa[0][mi] & keep) | one;
+      for (int mi = 0; mi < MI; ++mi) sa[mi] = (sa[mi] & keep) | one;
     }
   }
 #pragma unroll
   for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) {
-      acc[mi][ni] = mma_tile<0>(w[0][ni], a[0][mi], acc[mi][ni], sw[0][ni], sa[0][mi]);
-      acc[mi][ni] = mma_tile<1>(w[1][ni], a[1][mi], acc[mi][ni], sw[0][ni], sa[0][mi]);
+      acc[mi][ni] = mma_tile<0>(w[0][ni], a[0][mi], acc[mi][ni], sw[ni], sa[mi]);
+      acc[mi][ni] = mma_tile<1>(w[1][ni], a[1][mi], acc[mi][ni], sw[ni], sa[mi]);
     }
   ring_barrier();  // the stages are free
 
