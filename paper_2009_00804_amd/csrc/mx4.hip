@@ -263,7 +263,7 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
   typedef Tile<WM, WN, MI, NI, ST> R;
   __shared__ uint4 ring[R::SLOTS];
   __shared__ uint32_t scales[R::SETS][R::ROWS * 4];
-  __shared__ f32x4 ends[R::ROWS / 4];  // degree scalings of the rows, bias of the channels
+  __shared__ f32x4 ends[R::ROWS / 4];  // the rows' degrees, the channels' bias
   // Workgroup w runs on XCD w % 8: every XCD gets a run of tiles, and in it eight
   // row tiles share each column tile.
   const int total = tiles_m * tiles_n, per = (total + kXcds - 1) / kXcds;
@@ -309,11 +309,12 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
                    : "memory", "m0");
   };
   // load j of chunk c; only the last chunk can reach past the rows' ends, where it
-  // reads their last piece again (masked before use).  Load LB: scales, with chunk c = c' + ST
-  // those of the four chunks AHEAD of those of c'.
+  // reads their last piece again (masked before use).  Load LB: scales, of a quarter of
+  // the rows for four chunks; the first ones come before all chunks.
   const auto issue = [&](int c, int j) {
     if (j == R::LB) {
-      issue_scales((c - ST) / 4 + R::AHEAD, (c - ST) & 3);
+      const int i = 4 * R::AHEAD - ST + c;
+      issue_scales(i >> 2, i & 3);
       return;
     }
     const int grp = wave + j * R::NW;
@@ -325,21 +326,29 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
                    "v"(off[j] + (uint32_t)min(c * 64 + piece[j], kmax)), "s"(base)
                  : "memory", "m0");
   };
-  for (int t = 0; t < R::AHEAD; ++t)
-    for (int q = 0; q < 4; ++q) issue_scales(t, q);
+  // (degrees and bias go first, straight to LDS too: a load into registers would be waited for
+  // with all that are under way)
+  const auto issue_ends = [&](const void* from, int64_t i0, int64_t count, int at, int n) {
+    for (int i = wave * 64; i < n; i += R::THREADS)
+      if (n % 64 == 0 || i + lane < n)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                     :
+                     : "s"(__builtin_amdgcn_readfirstlane(
+                           (uint32_t)(uintptr_t)(__attribute__((address_space(3))) f32x4*)ends + (at + i) * 4)),
+                       "v"(static_cast<const char*>(from) + min(i0 + i + lane, count - 1) * 4)
+                     : "memory", "m0");
+  };
+  if (g.row_scale_deg) issue_ends(g.row_scale_deg, m0, g.M, 0, R::BM);
+  if (g.bias) issue_ends(g.bias, n0, g.N, R::BM, R::BN);
+  else
+    for (int i = threadIdx.x; i < R::BN; i += R::THREADS) reinterpret_cast<float*>(ends)[R::BM + i] = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4 * R::AHEAD - ST; ++i) issue_scales(i >> 2, i & 3);
 #pragma unroll
   for (int c = 0; c < ST; ++c)
     if (c <= last)
 #pragma unroll
-      for (int j = 0; j < R::LB; ++j) issue(c, j);
-  {
-    float* e = reinterpret_cast<float*>(ends);
-    for (int i = threadIdx.x; i < R::BM; i += R::THREADS)
-      e[i] = g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[min(m0 + i, g.M - 1)]) : 1.0f;
-    for (int i = threadIdx.x; i < R::BN; i += R::THREADS)
-      e[R::BM + i] = g.bias ? g.bias[min(n0 + i, g.N - 1)] : 0.0f;
-  }
-
+      for (int j = 0; j < R::LOADS; ++j) issue(c, j);
   f32x16 acc[MI][NI];
 #pragma unroll
   for (int mi = 0; mi < MI; ++mi)
@@ -416,7 +425,8 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
     }
   };
 
-  wait_vm<0>();
+  if (last >= ST - 1 && R::GROUPS % R::NW == 0) wait_vm<(ST - 1) * R::LOADS>();
+  else wait_vm<0>();
   ring_barrier();
   read_scales(0);
   turn();
@@ -464,13 +474,60 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
   ring_barrier();  // the stages are free
 
   // 32 rows at a time go through LDS of this wave's own: a lane holds channels
-  // 8 i + 4 half + (0..3) of row lr, and takes back four channels of a row, so that
-  // a store covers whole rows of the wave's columns.
+  // 8 i + 4 half + (0..3) of row lr, and takes back eight channels of a row (four of
+  // float32 ones), so that a store covers whole rows of the wave's columns.
+  const auto row_scale = [&](int r) {
+    return g.row_scale_deg ? rsqrt_deg(reinterpret_cast<const int*>(ends)[r]) : 1.0f;
+  };
+  const f32x4* const bias = ends + (R::BM + wn * NI * 32) / 4;
+  // bfloat16 and no activation but ReLU: rounded before they go through LDS.  (Others after it,
+  // from a loop: their code for every value here would be longer than the rest.)
+  if (g.out_dtype == SAGA_BF16 && g.act <= SAGA_ACT_RELU) {
+    const float floor = g.act == SAGA_ACT_RELU ? 0.0f : -INFINITY;  // (a NaN stays; -0 becomes +0)
+    constexpr int NP = 4 * NI, RS = 64 / NP;
+    lds_uint4* const mine = lds + wave * 32 * NP;
+    const int p = lane % NP;
+    const int64_t n = n0 + (int64_t)wn * NI * 32 + 8 * p;
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      const float rs = row_scale((wm * MI + mi) * 32 + lr);
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 b = bias[ni * 8 + i * 2 + half];
+          float v[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = __builtin_elementwise_maximum(acc[mi][ni][4 * i + j] * rs + b[j], floor);
+          typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+          *(__attribute__((address_space(3))) u32x2*)(
+              (__attribute__((address_space(3))) char*)(mine + lr * NP + ((ni * 4 + i) ^ (lr & (NP - 1)))) + half * 8) =
+              u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        }
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < 32 / RS; ++i) {
+        const int r = i * RS + lane / NP, rr = (wm * MI + mi) * 32 + r;
+        const u32x4 v = *(lds_cu32x4*)(mine + r * NP + (p ^ (r & (NP - 1))));
+        if (m0 + rr >= g.M || n >= g.N) continue;
+        uint16_t* const o = static_cast<uint16_t*>(g.out) + (m0 + rr) * g.ldo + n;
+        if (n + 8 <= g.N) {
+          *reinterpret_cast<u32x4*>(o) = v;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (n + j < g.N) o[j] = (uint16_t)(v[j / 2] >> (16 * (j & 1)));
+        }
+      }
+    }
+    return;
+  }
   constexpr int NP = R::NP, RS = 64 / NP;
   lds_uint4* const mine = lds + wave * 32 * NP;
   const int p = lane % NP;
   const int64_t n = n0 + (int64_t)wn * NI * 32 + 4 * p;
-  const f32x4 tb = ends[(R::BM + wn * NI * 32) / 4 + p];
+  const f32x4 tb = bias[p];
 #pragma unroll
   for (int mi = 0; mi < MI; ++mi) {
     asm volatile("" ::: "memory");
@@ -487,7 +544,7 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
       const int r = i * RS + lane / NP, rr = (wm * MI + mi) * 32 + r;
       const f32x4 v =
           *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(mine + r * NP + (p ^ (r & (NP - 1))));
-      const float rs = reinterpret_cast<const float*>(ends)[rr];
+      const float rs = row_scale(rr);
       if (m0 + rr < g.M && n < g.N) store_quad(g, m0 + rr, n, v, rs, tb);
     }
   }
