@@ -116,7 +116,7 @@ hipError_t rows_mx4(const Mx4RowsArgs& a, bool back, hipStream_t st) {
 }
 
 // --------------------------------------------------------------------------
-// product: 16 rows and 16 channels a workgroup, k divided among its eight waves.  A
+// few rows: up to 64 of them and 16 channels a workgroup, k divided among its eight waves.  A
 // lane takes its blocks of a and w straight from memory; float rows are rounded in
 // its registers, since the 32 columns that a matrix instruction wants of a lane are
 // a block.
@@ -169,44 +169,84 @@ __device__ __forceinline__ f32x4 bias_quad(const Mx4GemmArgs& g, int64_t n) {
   return b;
 }
 
-template <typename T>
-__global__ __launch_bounds__(512) void k_mx4_few(Mx4GemmArgs g, int64_t tiles_m, int64_t tiles) {
+// (AHEAD steps' loads at a time: what registers hold, and not more than a wave has)
+template <typename T, int MI, int AHEAD>
+__global__ __launch_bounds__(512) void k_mx4_few(Mx4GemmArgs g, int64_t tiles_n, int64_t tiles) {
   constexpr int NW = 8;
-  __shared__ f32x4 part[NW][64];
+  __shared__ f32x4 part[NW][MI][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int quarter = lane >> 4, lr = lane & 15, K = (int)g.K;
-  const int steps = (K + 127) / 128, per = (steps + NW - 1) / NW, s0 = wave * per, s1 = min(steps, s0 + per);
-  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const int64_t m0 = t % tiles_m * 16, n0 = t / tiles_m * 16;
-    RowSource<T> a;
-    RowSource<uint8_t> w;
-    a.at(g.a, g.lda, g.a_scale, g.lda_s, min(m0 + lr, g.M - 1));  // (rows past the last: not stored)
-    w.at(g.w, g.ldw, g.w_scale, g.ldw_s, min(n0 + lr, g.N - 1));
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = s0; s < s1; ++s) {
-      const int b = s * 4 + quarter;
-      a.load(b, K);
-      w.load(b, K);
-      acc = mma_mx4(w.take(b, K), a.take(b, K), acc);
-    }
-    part[wave][lane] = acc;
-    __syncthreads();
-    if (wave == 0) {
+  const int all = (K + 127) / 128, steps = (all - wave + NW - 1) / NW;  // of this wave: wave, wave + NW, ..
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int64_t m0 = tile / tiles_n * (16 * MI), n0 = tile % tiles_n * 16;
+    RowSource<T> a[AHEAD][MI];
+    RowSource<uint8_t> w[AHEAD];
 #pragma unroll
-      for (int k = 1; k < NW; ++k) acc += part[k][lane];
-      const int64_t m = m0 + lr, n = n0 + quarter * 4;
+    for (int d = 0; d < AHEAD; ++d) {
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi)  // (rows past the last: not stored)
+        a[d][mi].at(g.a, g.lda, g.a_scale, g.lda_s, min(m0 + mi * 16 + lr, g.M - 1));
+      w[d].at(g.w, g.ldw, g.w_scale, g.ldw_s, min(n0 + lr, g.N - 1));
+    }
+    const auto load = [&](int d, int i) {
+      const int b = (wave + i * NW) * 4 + quarter;
+      w[d].load(b, K);
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) a[d][mi].load(b, K);
+    };
+    f32x4 acc[MI];
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) acc[mi] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int ib = 0; ib < steps; ib += AHEAD) {
+#pragma unroll
+      for (int d = 0; d < AHEAD; ++d) load(d, ib + d);
+#pragma unroll
+      for (int d = 0; d < AHEAD; ++d) {
+        const int i = ib + d, s = wave + i * NW, b = s * 4 + quarter;
+        if (i >= steps) continue;
+        const bool last = s == all - 1;
+        const Mx4Block wb = w[d].take(b, K, last);
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) acc[mi] = mma_mx4(wb, a[d][mi].take(b, K, last), acc[mi]);
+      }
+    }
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) part[wave][mi][lane] = acc[mi];
+    __syncthreads();
+    if (wave < MI) {
+      f32x4 sum = part[0][wave][lane];
+#pragma unroll
+      for (int k = 1; k < NW; ++k) sum += part[k][wave][lane];
+      const int64_t m = m0 + wave * 16 + lr, n = n0 + quarter * 4;
       if (m < g.M && n < g.N)
-        store_quad(g, m, n, acc, g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[m]) : 1.0f, bias_quad(g, n));
+        store_quad(g, m, n, sum, g.row_scale_deg ? rsqrt_deg(g.row_scale_deg[m]) : 1.0f, bias_quad(g, n));
     }
     __syncthreads();
   }
 }
 
+template <typename T, int MI, int AHEAD>
+hipError_t launch_few_steps(const Mx4GemmArgs& g, hipStream_t st) {
+  const int64_t tn = (g.N + 15) / 16, tiles = tn * ((g.M + 16 * MI - 1) / (16 * MI));
+  hipLaunchKernelGGL((k_mx4_few<T, MI, AHEAD>), dim3((unsigned)std::min(tiles, kMostBlocks)), dim3(512), 0, st, g, tn,
+                     tiles);
+  return hipGetLastError();
+}
+template <typename T, int MI>
+hipError_t launch_few_rows(const Mx4GemmArgs& g, hipStream_t st) {
+  constexpr int MOST = sizeof(T) == 1 ? 4 : std::min(4, 8 / (MI * (int)sizeof(T) / 2));
+  const int64_t steps = (g.K + 1023) / 1024;  // of a wave
+  if constexpr (MOST >= 4)
+    if (steps > 2) return launch_few_steps<T, MI, 4>(g, st);
+  if constexpr (MOST >= 2)
+    if (steps > 1) return launch_few_steps<T, MI, 2>(g, st);
+  return launch_few_steps<T, MI, 1>(g, st);
+}
 template <typename T>
 hipError_t launch_few(const Mx4GemmArgs& g, hipStream_t st) {
-  const int64_t tm = (g.M + 15) / 16, tiles = tm * ((g.N + 15) / 16);
-  hipLaunchKernelGGL((k_mx4_few<T>), dim3((unsigned)std::min(tiles, kMostBlocks)), dim3(512), 0, st, g, tm, tiles);
-  return hipGetLastError();
+  if (g.M <= 16) return launch_few_rows<T, 1>(g, st);
+  if (g.M <= 32) return launch_few_rows<T, 2>(g, st);
+  return launch_few_rows<T, 4>(g, st);
 }
 
 // --------------------------------------------------------------------------
@@ -635,7 +675,7 @@ __attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, NT>))) void k_mx4_stream(
     RowSource<uint8_t> w;
     w.at(g.w, g.ldw, g.w_scale, g.ldw_s, min((int64_t)((lr >> 2) * 4 * NT + t * 4 + (lr & 3)), g.N - 1));
     w.load(s * 4 + quarter, K);
-    const Mx4Block b = w.take(s * 4 + quarter, K);
+    const Mx4Block b = w.take(s * 4 + quarter, K, s == steps - 1);
     lw[f * 64 + lane] = b.v;
     reinterpret_cast<uint8_t*>(lws + ((s / 4) * NT + t) * 64 + lane)[s % 4] = (uint8_t)b.scale;
   }
@@ -753,9 +793,14 @@ hipError_t launch_rows_mx4(const Mx4RowsArgs& a, bool back, hipStream_t st) {
   return a.dtype == SAGA_BF16 ? rows_mx4<uint16_t>(a, back, st) : rows_mx4<float>(a, back, st);
 }
 
-bool mx4_few(int64_t M, int64_t N, int64_t K) {
-  const int64_t wgs = ((M + 15) / 16) * ((N + 15) / 16);
-  return wgs <= 512 && wgs * ((K + 127) / 128) <= 8192;
+// Which kernel takes a product (us of kernels alone, bfloat16 out).
+// k_mx4_few, whose workgroups each round the rows, while that is little, against 64 x 64 tiles: 4-bit
+// rows 1 x 1024 x 1024 3.6 / 5.4, 16 x 4096 x 4096 6.7 / 10.9, 32 8.8 / 11.0, 48 11.0 / 11.0, 64 12.3 / 11.1;
+// against a launch more for the rows' 4-bit form (about 4): bfloat16 1 x 1024 x 1024 4.0 / 7.8, 16 x 4096
+// x 4096 8.6 / 14.1, 32 13.5 / 14.7, 48 18.5 / 14.7, float32 16 12.6 / 14.1, 32 19.7 / 14.7.
+bool mx4_few(int a_dtype, int64_t M, int64_t N, int64_t K) {
+  const int64_t work = ((M + 15) / 16) * ((N + 15) / 16) * ((K + 127) / 128);
+  return M < 4096 && N <= 1 << 20 && work <= (a_dtype == SAGA_F32 ? 8192 : 16384);
 }
 
 bool mx4_streams(int64_t M, int64_t N, int64_t K) {
@@ -777,14 +822,14 @@ Mx4Space mx4_space(int64_t M, int64_t K) {
 }
 
 size_t mx4_workspace_bytes(int a_dtype, int64_t M, int64_t N, int64_t K) {
-  if (a_dtype == SAGA_MX4 || M == 0 || mx4_few(M, N, K) || mx4_streams(M, N, K)) return 0;
+  if (a_dtype == SAGA_MX4 || M == 0 || mx4_few(a_dtype, M, N, K) || mx4_streams(M, N, K)) return 0;
   return mx4_space(M, K).total;
 }
 
 hipError_t launch_gemm_mx4(const Mx4GemmArgs& g0, hipStream_t st) {
   if (g0.M == 0) return hipSuccess;
   Mx4GemmArgs g = g0;
-  if (mx4_few(g.M, g.N, g.K)) {
+  if (mx4_few(g.a_dtype, g.M, g.N, g.K)) {
     if (g.a_dtype == SAGA_MX4) return launch_few<uint8_t>(g, st);
     return g.a_dtype == SAGA_BF16 ? launch_few<uint16_t>(g, st) : launch_few<float>(g, st);
   }

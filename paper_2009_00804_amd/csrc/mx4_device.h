@@ -78,7 +78,9 @@ struct Mx4Block {
   uint32_t scale;  // in the low byte
 };
 
-// what a row's source is: 4-bit rows with their scales, or floats
+// What a row's source is: 4-bit rows with their scales, or floats.  Block b of the row of K
+// columns; `take` apart from `load`, so that loads run ahead, and without a branch in it: past
+// the row's end its last piece is read again, and `take` clears it (LAST: where that can be).
 template <typename T>
 struct RowSource {  // float or uint16_t
   const T* x;
@@ -86,18 +88,19 @@ struct RowSource {  // float or uint16_t
   __device__ __forceinline__ void at(const void* base, int64_t ld, const uint8_t*, int64_t, int64_t row) {
     x = static_cast<const T*>(base) + row * ld;
   }
-  // block b of the row of K columns; `take` apart, so that loads run ahead
   __device__ __forceinline__ void load(int b, int K) {
+    const int most = (K - 1) / 8 * 8;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) raw[u].load(x + b * 32 + u * 8, K - b * 32 - u * 8);
+    for (int u = 0; u < 4; ++u) raw[u].load(x + min(b * 32 + u * 8, most), 8);
   }
-  __device__ __forceinline__ Mx4Block take(int b, int K) {
+  __device__ __forceinline__ Mx4Block take(int b, int K, bool last) {
+    if (last) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) raw[u].clear(K - b * 32 - u * 8);
+    }
     uint32_t top = 0;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      raw[u].clear(K - b * 32 - u * 8);
-      top = max(top, raw[u].top());
-    }
+    for (int u = 0; u < 4; ++u) top = max(top, raw[u].top());
     const BlockScale s = block_scale(top);
     Mx4Block o;
 #pragma unroll
@@ -116,18 +119,17 @@ struct RowSource<uint8_t> {
     s = scales + row * lds;
   }
   __device__ __forceinline__ void load(int b, int K) {
-    v = u32x4{0u, 0u, 0u, 0u};
-    scale = 127u;
-    if (b * 32 < K) {
-      v = *reinterpret_cast<const u32x4*>(q + b * 16);
-      scale = s[b];
-    }
+    b = min(b, (K - 1) / 32);
+    v = *reinterpret_cast<const u32x4*>(q + b * 16);
+    scale = s[b];
   }
-  __device__ __forceinline__ Mx4Block take(int b, int K) {
-    const int left = (K + 1) / 2 - b * 16;
-    Mx4Block o = {v, scale};
-    if (left > 0 && left < 16) o.v = clear_bytes(v, left);
-    return o;
+  __device__ __forceinline__ Mx4Block take(int b, int K, bool last) {
+    if (last) {
+      const int left = (K + 1) / 2 - b * 16;
+      if (left < 16) v = clear_bytes(v, left);
+      if (left <= 0) scale = 127u;
+    }
+    return {v, scale};
   }
 };
 
