@@ -362,13 +362,13 @@ __device__ __forceinline__ void store_hidden(const ExpertArgs& a, int e, int pai
 
 // --------------------------------------------------------------------------
 // an expert's product: 16 channels of one expert and the rows that take it, 16 at a
-// time, k divided among eight waves.  A wave's loads, of the weights and of x, run AHEAD
-// steps of 128 k ahead.  The weights' zeros past a row's end make what x has there not
+// time, k divided among four waves.  A wave's loads, of the weights and of x, are AHEAD
+// steps of 128 k at a time.  The weights' zeros past a row's end make what x has there not
 // count.
 // --------------------------------------------------------------------------
-template <bool MX4, int TERMS, bool UP, bool GATED>
-__global__ __launch_bounds__(512) void k_expert_few(ExpertArgs a) {
-  constexpr int NW = 8, NO = GATED ? 2 : 1, AHEAD = TERMS == 1 && (MX4 || NO == 1) ? 4 : 2;
+template <bool MX4, int TERMS, bool UP, bool GATED, int AHEAD>
+__global__ __launch_bounds__(256) void k_expert_few(ExpertArgs a) {
+  constexpr int NW = 4, NO = GATED ? 2 : 1;
   __shared__ int list[kExpertRows];
   __shared__ f32x4 part[NW][NO][64];
   int count;
@@ -402,9 +402,9 @@ __global__ __launch_bounds__(512) void k_expert_few(ExpertArgs a) {
     f32x4 acc[NO];
 #pragma unroll
     for (int o = 0; o < NO; ++o) acc[o] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int d = 0; d < AHEAD; ++d) load(d, d);
     for (int ib = 0; ib < steps; ib += AHEAD) {
+#pragma unroll
+      for (int d = 0; d < AHEAD; ++d) load(d, ib + d);
 #pragma unroll
       for (int d = 0; d < AHEAD; ++d) {
         const int i = ib + d;
@@ -427,10 +427,6 @@ __global__ __launch_bounds__(512) void k_expert_few(ExpertArgs a) {
             }
           }
         }
-      }
-      if (ib + AHEAD < steps) {
-#pragma unroll
-        for (int d = 0; d < AHEAD; ++d) load(d, ib + AHEAD + d);
       }
     }
 #pragma unroll
@@ -1269,14 +1265,20 @@ hipError_t products(const ExpertArgs& a, hipStream_t st) {
   }
   const unsigned slots = (unsigned)std::min<int64_t>(a.M * a.top_k, a.E);
   const dim3 up((unsigned)((a.H + 15) / 16), slots), down((unsigned)((a.N + 15) / 16), slots);
-  const auto go = [&](auto kernel, dim3 grid) {
-    hipLaunchKernelGGL(kernel, grid, dim3(512), 0, st, a);
+  const auto go = [&](auto kernel, auto deep, dim3 grid, int k) {  // (deep: two steps at a time)
+    if (k > 512) hipLaunchKernelGGL(deep, grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
     return hipGetLastError();
   };
-  if (a.gated) e = a.x_terms == 1 ? go(k_expert_few<MX4, 1, true, true>, up) : go(k_expert_few<MX4, 3, true, true>, up);
-  else e = a.x_terms == 1 ? go(k_expert_few<MX4, 1, true, false>, up) : go(k_expert_few<MX4, 3, true, false>, up);
+  if (a.gated)
+    e = a.x_terms == 1 ? go(k_expert_few<MX4, 1, true, true, 1>, k_expert_few<MX4, 1, true, true, 2>, up, a.F)
+                       : go(k_expert_few<MX4, 3, true, true, 1>, k_expert_few<MX4, 3, true, true, 2>, up, a.F);
+  else
+    e = a.x_terms == 1 ? go(k_expert_few<MX4, 1, true, false, 1>, k_expert_few<MX4, 1, true, false, 2>, up, a.F)
+                       : go(k_expert_few<MX4, 3, true, false, 1>, k_expert_few<MX4, 3, true, false, 2>, up, a.F);
   if (e != hipSuccess) return e;
-  return a.h_terms == 2 ? go(k_expert_few<MX4, 2, false, false>, down) : go(k_expert_few<MX4, 3, false, false>, down);
+  return a.h_terms == 2 ? go(k_expert_few<MX4, 2, false, false, 1>, k_expert_few<MX4, 2, false, false, 2>, down, a.H)
+                        : go(k_expert_few<MX4, 3, false, false, 1>, k_expert_few<MX4, 3, false, false, 2>, down, a.H);
 }
 
 size_t whole(size_t n) { return (n + 255) & ~(size_t)255; }
