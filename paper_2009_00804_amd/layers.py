@@ -5,9 +5,10 @@ workspace and output, so a forward pass enqueues kernels and nothing else.
 The two-layer models of the workloads (GCN: ReLU then raw output; GAT:
 concat + ELU then head mean) are sequences of such layers.
 
-``quantize_rows``, ``quant_linear``, ``block_norm`` and ``label_log_probs`` call
-the operators of a deep network on torch tensors; ``ResidualGCN`` is such a
-network, served with 8-bit transforms.
+``quantize_rows``, ``quant_linear``, ``quantize_rows_mx4``, ``dequantize_rows_mx4``,
+``mx4_linear``, ``expert_layer``, ``block_norm`` and ``label_log_probs`` call the operators
+of a deep network on torch tensors; ``ResidualGCN`` is such a network, served with 8-bit
+or 4-bit transforms and, if it has them, a layer of experts for the vertices asked for.
 """
 from __future__ import annotations
 
@@ -137,7 +138,8 @@ def run(layers, x, edge_feat=None, stream=None):
 # Matrices are 2-D, on one GPU, each row's columns neighbours; a matrix begins on 16 bytes
 # and its rows lie a multiple of 16 bytes apart (S.padded_empty makes such a buffer, and
 # every matrix returned here is one; a single row needs no pitch).  Others are
-# refused, not copied.  Vectors are contiguous: float32, labels and degrees int32.
+# refused, not copied.  The scales of 4-bit rows lie a multiple of 4 bytes apart and begin
+# on 4.  Vectors are contiguous: float32, labels and degrees int32.
 # Errors: ValueError for what the tensors give away, S.SagaError from the library.
 #
 # Inference only, as the library: results have no history, whether the inputs require
@@ -454,31 +456,43 @@ def label_log_probs(logits, labels=None, top_k=0, entropy=True):
 
 
 class ResidualGCN:
-    """A deep GCN with a gated residual stream, its transforms in 8-bit integers.
+    """A deep GCN with a gated residual stream, its transforms in 8-bit integers (bits=8) or
+    microscaled 4-bit floating point (bits=4).
 
         h = x W_in + b_in
-        per block:  z = pre(h) in 8 bits;  [v | g] = z [W | W_g] + [0 | b_g]
+        per block:  z = pre(h) quantised;  [v | g] = z [W | W_g] + [0 | b_g]
                     m = relu(d_in^-1/2 A d_out^-1/2 v + b)
                     h = h + res_scale * sigmoid(g) * post(m)
+        experts:    h = h + res_scale * expert_layer(experts.norm(h))
         logits = norm(h) W_out + b_out
 
     weights: W_in (F_in x F), b_in, blocks: a list of dicts with W, W_g (F x F),
     b, b_g, pre, post (norm weights, F), then norm (F), W_out (F x classes), b_out;
     float32 tensors or arrays.  The weights are quantised once, one scale per
-    output channel.  F is a multiple of 8.  The stream h is float32, blocks are
-    ``dtype``; both norms are RMS norms."""
+    output channel (per 32 of its weights).  F is a multiple of 8.  The stream h is
+    float32, blocks are ``dtype``; all norms are RMS norms.
 
-    def __init__(self, graph: S.Graph, weights: dict, dtype=torch.bfloat16, res_scale=1.0, eps=1e-5):
+    experts (may be absent): a dict with norm (F), router (F x E), up (E x F x H), down
+    (E x H x F), top_k, act, and, each of which may be absent, gate (E x F x H: gated
+    experts), b_router (E), b_up, b_gate (E x H) and b_down (E x F).  They are kept in
+    bfloat16, or in 4 bits with the transforms."""
+
+    def __init__(self, graph: S.Graph, weights: dict, dtype=torch.bfloat16, res_scale=1.0, eps=1e-5, bits=8):
         dev = graph.row_ptr.device
-        self.graph, self.dtype, self.res_scale, self.eps = graph, dtype, res_scale, eps
+        if bits not in (4, 8):
+            raise ValueError(f"bits has to be 4 or 8, got {bits}")
+        self.graph, self.dtype, self.res_scale, self.eps, self.bits = graph, dtype, res_scale, eps, bits
+        quantise = quantize_rows if bits == 8 else quantize_rows_mx4
 
         def vector(v):
-            return _dev(v, dev, torch.float32)
+            return None if v is None else _dev(v, dev, torch.float32).reshape(-1)
+
+        def matrix(rows, dtype=torch.float32):
+            wide, _ = _out(rows.shape[0], rows.shape[1], dtype, rows)
+            return wide.copy_(rows)
 
         def transform(w, b):
-            rows = _dev(w, dev, torch.float32).t()
-            wide, _ = _out(rows.shape[0], rows.shape[1], torch.float32, rows)
-            return (*quantize_rows(wide.copy_(rows)), vector(b))
+            return (*quantise(matrix(_dev(w, dev, torch.float32).t())), vector(b))
 
         self.f = f = weights["blocks"][0]["W"].shape[0] if weights["blocks"] else weights["W_out"].shape[0]
         if f % 8:
@@ -492,6 +506,26 @@ class ResidualGCN:
                                     pre=vector(b["pre"]), post=vector(b["post"])))
         self.norm = vector(weights["norm"])
         self.last = transform(weights["W_out"], weights["b_out"])
+        self.experts = None
+        if weights.get("experts"):
+            x = weights["experts"]
+            up, down = (_dev(x[k], dev, torch.float32).transpose(1, 2) for k in ("up", "down"))
+            up_bias, gated = x.get("b_up"), x.get("gate") is not None
+            if gated:
+                up = torch.cat([_dev(x["gate"], dev, torch.float32).transpose(1, 2), up], 1)
+                if (up_bias is None) != (x.get("b_gate") is None):
+                    raise ValueError("experts: b_gate and b_up go together")
+                if up_bias is not None:
+                    up_bias = torch.cat([_dev(x[k], dev, torch.float32) for k in ("b_gate", "b_up")], 1)
+            kw = dict(router_bias=vector(x.get("b_router")), up_bias=vector(up_bias),
+                      down_bias=vector(x.get("b_down")), top_k=x["top_k"], act=x["act"], gated=gated)
+            up, down = up.reshape(-1, f), down.reshape(-1, down.shape[2])
+            if bits == 4:
+                (up, kw["up_scale"]), (down, kw["down_scale"]) = (quantize_rows_mx4(matrix(w)) for w in (up, down))
+            else:
+                up, down = (matrix(w, torch.bfloat16) for w in (up, down))
+            router = matrix(_dev(x["router"], dev, torch.float32).t())
+            self.experts = dict(norm=vector(x["norm"]), args=(router, up, down), kw=kw)
         self.op = S.saga_edge_op()
         self.op.msg, self.op.reduce, self.op.dtype = S.SAGA_MSG_SRC_NORM, S.SAGA_RED_SUM, S.dtype_code(dtype)
         self.op.heads, self.op.dst_norm, self.op.act = 1, 1, S.SAGA_ACT_RELU
@@ -508,26 +542,48 @@ class ResidualGCN:
                                          ws.numel(), S.stream_handle())
         return out
 
-    def logits(self, x):
-        """x: num_vertices x F_in (float32 or bfloat16) on the graph's device"""
+    def transform(self, x, weights, x_scale=None, out_dtype=torch.float32):
+        """x W + b in the network's bits; x: floats, or 8-bit rows with their scales"""
+        w, ws, b = weights
+        if self.bits == 4:
+            return mx4_linear(x, w, ws, bias=b, out_dtype=out_dtype)
+        return quant_linear(x, w, ws, x_scale=x_scale, bias=b, out_dtype=out_dtype)
+
+    def logits(self, x, vertices=None):
+        """x: num_vertices x F_in (float32 or bfloat16) on the graph's device; vertices: those
+        whose logits are wanted (int32 or int64; None: all)"""
         if x.device != self.graph.row_ptr.device:
             raise ValueError(f"x is on {x.device}, the graph on {self.graph.row_ptr.device}")
+
+        def asked(t):
+            if vertices is None or t is None:
+                return t
+            if t.dim() == 1:
+                return t.index_select(0, vertices)
+            return _out(vertices.numel(), t.shape[1], t.dtype, t)[0].copy_(t.index_select(0, vertices))
+
         with torch.cuda.device(x.device):
-            w, ws, b = self.first
-            h = quant_linear(x, w, ws, bias=b, out_dtype=self.dtype)
-            norms = [blk["pre"] for blk in self.blocks] + [self.norm]
+            # (4-bit transforms quantise on their way, experts take floats)
+            ends = [self.norm] if self.experts is None else [self.experts["norm"], self.norm]
+            norms = [blk["pre"] for blk in self.blocks] + ends
+            whole = [self.bits == 8] * len(self.blocks) + [self.bits == 8 and self.experts is None]
+            h = self.transform(x, self.first, out_dtype=self.dtype)
             h, z, zs = block_norm(h, None, x_dtype=torch.float32, pre="rms", pre_weight=norms[0], eps=self.eps,
-                                  quantize=True)
-            for blk, norm in zip(self.blocks, norms[1:]):
-                w, ws, b = blk["both"]
-                vg = quant_linear(z, w, ws, x_scale=zs, bias=b, out_dtype=self.dtype)
+                                  quantize=whole[0])
+            for i, blk in enumerate(self.blocks):
+                vg = self.transform(z, blk["both"], zs, self.dtype)
                 m = self.gather(vg[:, :self.f], blk["bias"])
                 h, z, zs = block_norm(m, h, post="rms", post_weight=blk["post"], gate=vg[:, self.f:],
-                                      gate_act="sigmoid", res_scale=self.res_scale, pre="rms", pre_weight=norm,
-                                      eps=self.eps, quantize=True, in_place=True)
-            w, ws, b = self.last
-            return quant_linear(z, w, ws, x_scale=zs, bias=b)
+                                      gate_act="sigmoid", res_scale=self.res_scale, pre="rms",
+                                      pre_weight=norms[i + 1], eps=self.eps, quantize=whole[i + 1], in_place=True)
+            z, zs = asked(z), asked(zs)
+            if self.experts is not None:
+                y, _, _ = expert_layer(z, *self.experts["args"], **self.experts["kw"])
+                _, z, zs = block_norm(y, asked(h), res_scale=self.res_scale, pre="rms", pre_weight=self.norm,
+                                      eps=self.eps, quantize=self.bits == 8)
+            return self.transform(z, self.last, zs)
 
-    def __call__(self, x, labels=None, top_k=1):
-        """(logp, entropy, top_index, top_logp) of every vertex"""
-        return label_log_probs(self.logits(x), labels, top_k)
+    def __call__(self, x, labels=None, top_k=1, vertices=None):
+        """(logp, entropy, top_index, top_logp) of every vertex, or of those asked for
+        (labels: one of each of them)"""
+        return label_log_probs(self.logits(x, vertices), labels, top_k)

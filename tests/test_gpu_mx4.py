@@ -529,3 +529,116 @@ def test_refused_tensors():
         L.expert_layer(x, layer.router_d, layer.up_d, layer.down_d)
     with pytest.raises(lib().SagaError, match="top_k"):
         layer(x, top_k=5)
+
+
+# --------------------------------------------------------------------------
+# in a network
+# --------------------------------------------------------------------------
+def network(bits, dtype, gated, seed=7, n=203, f_in=50, f=72, classes=11, depth=2, e=6, h=40):
+    import numpy as np
+
+    from gpu_util import graph
+    from helpers import edges_to_csr
+
+    rng = np.random.default_rng(seed)
+    rp, col, _ = edges_to_csr(n, rng.integers(0, n, n * 6).tolist(), rng.integers(0, n, n * 6).tolist())
+    g = gen(seed)
+    mat = lambda *s: torch.randn(*s, generator=g) / s[-2] ** 0.5  # noqa: E731
+    vec = lambda *s: torch.randn(*s, generator=g) * 0.1  # noqa: E731
+    w = dict(W_in=mat(f_in, f), b_in=vec(f), norm=vec(f) + 1, W_out=mat(f, classes), b_out=vec(classes),
+             blocks=[dict(W=mat(f, f), W_g=mat(f, f), b=vec(f), b_g=vec(f), pre=vec(f) + 1, post=vec(f) + 1)
+                     for _ in range(depth)],
+             experts=dict(norm=vec(f) + 1, router=mat(f, e), up=mat(e, f, h), down=mat(e, h, f), top_k=2, act="sigmoid",
+                          b_router=vec(e), b_up=vec(e, h), b_down=vec(e, f)))
+    if gated:
+        w["experts"].update(gate=mat(e, f, h), b_gate=vec(e, h))
+    gr = graph(rp, col)
+    x = torch.randn(n, f_in, generator=g)
+    return LY().ResidualGCN(gr, w, dtype=dtype, res_scale=0.5, bits=bits), w, padded(x)
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("bits,gated", [(4, True), (4, False), (8, True)])
+def test_network_of_experts(bits, dtype, gated):
+    """Each stage that a tested operator does is taken from it; the network has the stages' bits,
+    its experts' layer is the definition's on the rows that enter it, and vertices asked for
+    have the answers that they have among all."""
+    L = LY()
+    net, w, x = network(bits, dtype, gated)
+    f, n = net.f, x.shape[0]
+    seen = {}
+    real = L.expert_layer
+
+    def watch(z, *args, **kw):
+        seen["z"], seen["out"] = z, real(z, *args, **kw)
+        return seen["out"]
+
+    L.expert_layer = watch
+    try:
+        logits = net.logits(x)
+    finally:
+        L.expert_layer = real
+    # by hand
+    lin = (lambda z, t, zs, out: L.mx4_linear(z, t[0], t[1], bias=t[2], out_dtype=out)) if bits == 4 else (
+        lambda z, t, zs, out: L.quant_linear(z, t[0], t[1], x_scale=zs, bias=t[2], out_dtype=out))
+    norms = [b["pre"] for b in net.blocks] + [net.experts["norm"]]
+    h, z, zs = L.block_norm(lin(x, net.first, None, dtype), None, x_dtype=torch.float32, pre="rms",
+                            pre_weight=norms[0], quantize=bits == 8)
+    for i, b in enumerate(net.blocks):
+        vg = lin(z, b["both"], zs, dtype)
+        m = net.gather(vg[:, :f], b["bias"])
+        h, z, zs = L.block_norm(m, h, post="rms", post_weight=b["post"], gate=vg[:, f:], gate_act="sigmoid",
+                                res_scale=0.5, pre="rms", pre_weight=norms[i + 1],
+                                quantize=bits == 8 and i + 1 < len(net.blocks))
+    assert torch.equal(z, seen["z"])
+    # the experts, from the weights as given
+    ex = w["experts"]
+    up, down = ex["up"].transpose(1, 2), ex["down"].transpose(1, 2).reshape(-1, ex["up"].shape[2])
+    up_b = ex["b_up"]
+    if gated:
+        up, up_b = torch.cat([ex["gate"].transpose(1, 2), up], 1), torch.cat([ex["b_gate"], ex["b_up"]], 1)
+    up = up.reshape(-1, f)
+    up, down = (rows_exact(t.double())[2] if bits == 4 else t.bfloat16().double() for t in (up, down))
+    zc = z.cpu()
+    index, p = route_exact(zc, ex["router"].T, ex["b_router"], 2, True)
+    y, got_i, got_p = seen["out"]
+    assert torch.equal(got_i.cpu().long(), index)
+    want, tol = experts_exact(zc, index, p, up, down, up_b.reshape(-1), ex["b_down"].reshape(-1), ex["router"].shape[1],
+                              "sigmoid", gated, dtype)
+    assert ((y.cpu().double() - want).abs() / tol).max().item() <= 1
+    _, z, zs = L.block_norm(y, h, res_scale=0.5, pre="rms", pre_weight=net.norm, quantize=bits == 8)
+    assert torch.equal(lin(z, net.last, zs, torch.float32), logits)
+    # some vertices, one of them twice
+    to = torch.randint(0, 11, (5,), generator=gen(3), dtype=torch.int32).to(device())
+    ask = torch.tensor([n - 1, 0, 7, 7, 100], device=device())
+    some = net(x, to, 3, vertices=ask)
+    every = L.label_log_probs(net.logits(x, ask), to, 3)
+    for a, b in zip(some, every):
+        assert torch.equal(a, b)
+    # (few rows go through other kernels: the same values within the tolerances of both, through
+    # a norm and a quantiser that may turn them by a step)
+    near = net.logits(x, ask) - logits[ask]
+    assert near.abs().max().item() <= 0.25 * logits.abs().max().item()
+
+
+def test_network_in_four_bits_captured():
+    L = LY()
+    net, _, x = network(4, torch.bfloat16, True)
+    ask = torch.tensor([3, 50, 77], device=device())
+    net(x, top_k=2, vertices=ask)
+    torch.cuda.synchronize()
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        got = net(x, top_k=2, vertices=ask)
+    for turn in range(3):
+        x.copy_(torch.randn(x.shape, generator=gen(40 + turn)).to(device()))
+        want = net(x, top_k=2, vertices=ask)
+        torch.cuda.synchronize()
+        gr.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got[1:], want[1:]))
+
+
+def test_network_refusals():
+    with pytest.raises(ValueError, match="bits"):
+        network(6, torch.bfloat16, True)
