@@ -602,14 +602,16 @@ __global__ __launch_bounds__(512) void k_expert_down_few(ExpertArgs a) {
   const int mine = lane < pairs ? a.index[lane] : -1;
   if ((int)threadIdx.x < pairs) index[threadIdx.x] = mine, weight[threadIdx.x] = a.weight[threadIdx.x];
   __syncthreads();
-  // the experts that are taken, by their first pair, and each row's pair of them
+  // The experts that are taken, by number, and each row's pair of them.  (By number: a row's
+  // results are then summed in an order that no other row has a say in.)
   int first = lane;
   for (int p = 0; p < pairs; ++p)
     if (p < first && index[p] == mine) first = p;
   const uint64_t firsts = __ballot(mine >= 0 && first == lane);
   const int taken = __popcll(firsts);
   if (wave == 0 && mine >= 0) {
-    const int place = __popcll(firsts & ((1ull << first) - 1));
+    int place = 0;
+    for (int p = 0; p < pairs; ++p) place += (firsts >> p & 1) && index[p] < mine;
     if (first == lane) expert[place] = mine;
     pair_of[place][lane / a.top_k] = lane;
   }

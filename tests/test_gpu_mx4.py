@@ -446,6 +446,94 @@ def test_expert_rows_without_numbers(dtype):
         assert torch.equal(a[keep], b[keep])
 
 
+@pytest.mark.parametrize("m,f,e", [(5, 70, 6), (16, 600, 9), (1, 70, 3)])
+@pytest.mark.parametrize("weights", ["mx4", "bf16"])
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_few_rows_without_numbers_or_experts(m, f, e, weights, dtype):
+    """the kernels of few rows, with the choice in the first of them and without"""
+    layer = Layer(5, f, 33, 40, e, weights, True, biases=True, closed=[1])
+    x = torch.randn(m, f, generator=gen(6)).to(dtype)
+    want = layer(padded(x), top_k=2)
+    layer.check(x, 2, got=want)
+    bad = [0] if m == 1 else [0, m - 1]
+    x[0, f - 1] = NAN
+    if m > 1:
+        x[m - 1, 0] = -INF
+    y, index, weight = layer(padded(x), top_k=2)
+    assert bool(torch.isnan(y[bad]).all()) and bool(torch.isnan(weight[bad]).all()) and bool((index[bad] == -1).all())
+    keep = [i for i in range(m) if i not in bad]
+    for a, b in zip((y, index, weight), want):
+        assert torch.equal(a[keep], b[keep])
+    closed = Layer(5, f, 33, 40, e, weights, True, biases=True, closed=range(e))
+    y, index, weight = closed(padded(x[:0] if m == 1 else x[1:-1]), top_k=2)
+    assert bool((y == 0).all()) and bool((index == -1).all()) and bool((weight == 0).all())
+
+
+def test_a_router_without_numbers():
+    """a NaN in an expert's row of the router: no row has a choice"""
+    for m in (3, 50):
+        layer = Layer(5, 64, 32, 16, 5, "mx4")
+        layer.router_d[2, 7] = NAN
+        y, index, weight = layer(padded(torch.randn(m, 64, generator=gen(6))), top_k=2)
+        assert bool(torch.isnan(y).all()) and bool((index == -1).all()) and bool(torch.isnan(weight).all())
+
+
+@pytest.mark.parametrize("m,f,h,e", [(300, 200, 300, 60), (90, 300, 4000, 64), (200, 128, 3000, 12)])
+@pytest.mark.parametrize("weights", ["mx4", "bf16"])
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_all_rows_take_one_expert(m, f, h, e, weights, dtype):
+    """far more rows of one expert than of the mean: more tiles than one of it, none of others"""
+    layer = Layer(5, f, h, 70, e, weights, True, closed=[i for i in range(e) if i not in (1, 2)])
+    layer.check(torch.randn(m, f, generator=gen(6)).to(dtype), 2, "tanh")
+
+
+def test_hidden_values_beyond_float32():
+    """an expert whose values between the products overflow gives no number, others theirs"""
+    layer = Layer(5, 64, 40, 24, 4, "bf16")
+    layer.up_d[40:80] *= 1e38
+    x = torch.randn(50, 64, generator=gen(6))
+    y, index, _ = layer(padded(x), top_k=1)
+    took = (index[:, 0] == 1).cpu()
+    assert took.any() and not took.all()
+    assert bool(torch.isfinite(y.cpu()[~took]).all())
+
+
+def test_wide_pitches():
+    """rows far apart, and part of wider buffers, give what rows next to each other give"""
+    L = LY()
+    g = gen(4)
+    x, w = torch.randn(70, 200, generator=g), torch.randn(90, 200, generator=g)
+    q, s = L.quantize_rows_mx4(padded(w))
+    want = L.mx4_linear(padded(x), q, s)
+    far_q, far_s = padded(q.cpu(), extra=700), padded(s.cpu(), extra=900, unit=4)
+    assert torch.equal(L.mx4_linear(padded(x, extra=4001), far_q, far_s), want)
+    xq, xs = L.quantize_rows_mx4(padded(x, extra=33))
+    big_q = torch.full((140, 512), 0xff, dtype=torch.uint8, device=device())
+    big_s = torch.full((140, 64), 0xff, dtype=torch.uint8, device=device())
+    big_q[::2, 16:116], big_s[::2, 4:11] = xq, xs
+    assert torch.equal(L.mx4_linear(big_q[::2, 16:116], far_q, far_s, x_scale=big_s[::2, 4:11]), want)
+
+
+def test_two_calls_at_once():
+    """two streams, each with calls of its own sizes: the bits of one call alone"""
+    L = LY()
+    layer = Layer(5, 96, 130, 96, 8, "mx4", True, True)
+    q, s = L.quantize_rows_mx4(padded(torch.randn(96, 96, generator=gen(1)) / 10))
+    xs = [padded(torch.randn(m, 96, generator=gen(m))) for m in (9, 1500)]
+    want = [[t.clone() for t in chain(L, layer, x, q, s)] for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        got = []
+        for st, x in zip(streams, xs):
+            with torch.cuda.stream(st):
+                got.append(chain(L, layer, x, q, s))
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(p, r) for p, r in zip(a, b))
+
+
 def test_experts_that_no_row_takes_may_hold_anything():
     layer = Layer(5, 64, 48, 32, 4, "bf16", closed=[2])
     layer.up_d[2 * 48:3 * 48] = NAN

@@ -122,6 +122,15 @@ def test_product_refusals(S):
     call(S.SAGA_EINVAL, "a_scale is for", a_dtype=0, a=(A, 5, 39, 40))
     call(S.SAGA_EINVAL, "shape", a_dtype=0, a=(A, 5, 41, 44), sa=none)
     assert S.saga_apply_vertex_mx_workspace_size(S.saga_mx_op(3, 0, 0, None), 20000, 4096, 4096) == 0
+    m, k, n = 6000, 1300, 600
+    big = dict(a_dtype=0, sa=none, a=(A, m, k, 1312), w=(D, n, 650, 656), sw=(E, n, 41, 44), out=(F, m, n, 608))
+    need = S.saga_apply_vertex_mx_workspace_size(S.saga_mx_op(0, 0, 0, None), m, k, n)
+    assert need >= m * 656 + m * 44
+    call(S.SAGA_EWORKSPACE, "need", **big)
+    call(S.SAGA_EWORKSPACE, "need", **big, ws=G, nws=need - 1)
+    call(S.SAGA_EINVAL, "256", **big, ws=G + 16, nws=need)
+    for other in (A, D, E, F):
+        call(S.SAGA_EINVAL, "overlap", **big, ws=other, nws=need)
     with pytest.raises(S.SagaError):
         S.saga_apply_vertex_mx_workspace_size(S.saga_mx_op(0, 0, 0, None), 5, 0, 7)
     assert S.lib().saga_apply_vertex_mx_workspace_size(None, 1, 1, 1, None) == S.SAGA_EINVAL
