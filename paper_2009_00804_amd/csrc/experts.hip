@@ -1002,17 +1002,17 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
       if (2 * r + wx < tiles)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f32x4*>(sums + ((2 * r + wx) * 16 + lr) * R::PITCH + wm * 64 + i * 16 + quarter * 4) =
-              acc[i][r];
+          *reinterpret_cast<f32x4*>(sums + ((2 * r + wx) * 16 + lr) * R::PITCH + quarter * 4 +
+                                    (gated ? (i >> 1) * 128 + wm * 32 + (i & 1) * 16 : wm * 64 + i * 16)) = acc[i][r];
     __syncthreads();
     if constexpr (UP) {
       const int octs = gated ? 16 : 32;
       for (int i = threadIdx.x; i < here * octs; i += 512) {
         const int row = i / octs, q = i % octs;
-        const float* const from = sums + row * R::PITCH + (gated ? (q >> 2) * 64 + (q & 3) * 8 : q * 8);
+        const float* const from = sums + row * R::PITCH + q * 8;  // (gated: gates, then ups)
         float v[8], up[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = from[j], up[j] = from[j + (gated ? 32 : 0)];
+        for (int j = 0; j < 8; ++j) v[j] = from[j], up[j] = from[j + (gated ? 128 : 0)];
         store_hidden(a, e, list[i0 + row], n0 + q * 8, v, up);
       }
     } else {

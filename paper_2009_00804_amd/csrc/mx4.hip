@@ -528,6 +528,7 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
     lds_uint4* const mine = lds + wave * 32 * NP;
     const int p = lane % NP;
     const int64_t n = n0 + (int64_t)wn * NI * 32 + 8 * p;
+    const auto turned = [](int r) { return (r * NP / 16) & (NP - 1); };  // (16 rows fall on all banks)
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       const float rs = row_scale((wm * MI + mi) * 32 + lr);
@@ -542,14 +543,14 @@ __attribute__((amdgpu_waves_per_eu(Tile<WM, WN, MI, NI, ST>::WPE))) void k_gemm_
           for (int j = 0; j < 4; ++j) v[j] = __builtin_elementwise_maximum(acc[mi][ni][4 * i + j] * rs + b[j], floor);
           typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
           *(__attribute__((address_space(3))) u32x2*)(
-              (__attribute__((address_space(3))) char*)(mine + lr * NP + ((ni * 4 + i) ^ (lr & (NP - 1)))) + half * 8) =
+              (__attribute__((address_space(3))) char*)(mine + lr * NP + ((ni * 4 + i) ^ turned(lr))) + half * 8) =
               u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
         }
       asm volatile("" ::: "memory");
 #pragma unroll
       for (int i = 0; i < 32 / RS; ++i) {
         const int r = i * RS + lane / NP, rr = (wm * MI + mi) * 32 + r;
-        const u32x4 v = *(lds_cu32x4*)(mine + r * NP + (p ^ (r & (NP - 1))));
+        const u32x4 v = *(lds_cu32x4*)(mine + r * NP + (p ^ turned(r)));
         if (m0 + rr >= g.M || n >= g.N) continue;
         uint16_t* const o = static_cast<uint16_t*>(g.out) + (m0 + rr) * g.ldo + n;
         if (n + 8 <= g.N) {
