@@ -17,7 +17,8 @@ constexpr int64_t kMostBlocks = 1 << 20;  // (a grid holds less than 2^32 thread
 // --------------------------------------------------------------------------
 // float rows to 4-bit rows and back: G lanes a row, U units of 8 columns a lane at a time;
 // the four lanes of a block join their largest magnitudes.  Blocks know nothing of each
-// other, so a long row is divided among workgroups.
+// other, so a long row is divided among workgroups.  Memory bounds both: 2^20 x 602 of bfloat16
+// take 343 us to 4 bits (4.7 TB/s) and 363 back (4.4 TB/s), 4099 x 4096 of float32 15 and 17.
 // --------------------------------------------------------------------------
 template <typename T, int G, int U>
 __global__ __launch_bounds__(256) void k_quantize_mx4(Mx4RowsArgs a) {
@@ -58,7 +59,17 @@ __global__ __launch_bounds__(256) void k_quantize_mx4(Mx4RowsArgs a) {
   }
 }
 
-template <typename T, int G, int U>
+// 8 values, not to be read again here
+__device__ __forceinline__ void store_whole(float* p, const float (&v)[8]) {
+  __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4*>(p));
+  __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4*>(p + 4));
+}
+__device__ __forceinline__ void store_whole(uint16_t* p, const float (&v)[8]) {
+  __builtin_nontemporal_store(u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]),
+                                    pack_bf16(v[6], v[7])}, reinterpret_cast<u32x4*>(p));
+}
+
+template <typename T, int G, int U, bool PAST>
 __global__ __launch_bounds__(256) void k_dequantize_mx4(Mx4RowsArgs a) {
   for (int64_t row = blockIdx.x * (int64_t)(256 / G) + threadIdx.x / G; row < a.M;
        row += gridDim.x * (int64_t)(256 / G)) {
@@ -88,7 +99,8 @@ __global__ __launch_bounds__(256) void k_dequantize_mx4(Mx4RowsArgs a) {
         pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(o[u], s, 1), v[2], v[3]);
         pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(o[u], s, 2), v[4], v[5]);
         pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(o[u], s, 3), v[6], v[7]);
-        store_unit(x + col, a.K - col, v);
+        if (PAST && a.K - col >= 8) store_whole(x + col, v);
+        else store_unit(x + col, a.K - col, v);
       }
     }
   }
@@ -100,7 +112,11 @@ hipError_t launch_rows(const Mx4RowsArgs& a, bool back, hipStream_t st) {
   const int64_t blocks = std::min<int64_t>((a.M + 256 / G - 1) / (256 / G), kMostBlocks / 4);
   const int64_t parts = (a.K + G * 8 * U - 1) / (G * 8 * U);
   const dim3 grid((unsigned)blocks, (unsigned)std::min(parts, std::max<int64_t>(1, 32768 / blocks)));
-  if (back) hipLaunchKernelGGL((k_dequantize_mx4<T, G, U>), grid, dim3(256), 0, st, a);
+  // Values that the last cache (256 MiB) does not hold go past it: 2^20 x 602 of bfloat16 363 us
+  // against 407, but 4099 x 4096 of float32 28 against 17.
+  if (back && a.M * a.K > (int64_t)((256 << 20) / sizeof(T)))
+    hipLaunchKernelGGL((k_dequantize_mx4<T, G, U, true>), grid, dim3(256), 0, st, a);
+  else if (back) hipLaunchKernelGGL((k_dequantize_mx4<T, G, U, false>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((k_quantize_mx4<T, G, U>), grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
@@ -116,7 +132,8 @@ hipError_t rows_mx4(const Mx4RowsArgs& a, bool back, hipStream_t st) {
 }
 
 // --------------------------------------------------------------------------
-// few rows: up to 64 of them and 16 channels a workgroup, k divided among its eight waves.  A
+// few rows: up to 64 of them and 16 channels a workgroup, k divided among its eight waves.
+// Latency bounds it: 1 x 1024 x 1024 takes 3.6 to 4.2 us, 16 x 4096 x 4096 of 4-bit rows 6.7.  A
 // lane takes its blocks of a and w straight from memory; float rows are rounded in
 // its registers, since the 32 columns that a matrix instruction wants of a lane are
 // a block.
@@ -251,12 +268,18 @@ hipError_t launch_few(const Mx4GemmArgs& g, hipStream_t st) {
 
 // --------------------------------------------------------------------------
 // large products of 4-bit rows: a workgroup of WM x WN waves holds BM rows of a and BN
-// rows of w, a wave MI x NI tiles of 32 x 32 sums.  64 bytes (128 k) of every row a stage
-// with their scales, ST stages in LDS filled by direct-to-LDS loads, which run between
+// rows of w, a wave MI x NI tiles of 32 x 32 sums.  64 bytes (128 k) of every row a stage,
+// ST stages in LDS filled by direct-to-LDS loads, which run between
 // the products of a stage rather than ahead of them.  The matrix instruction takes w as
 // its first operand: a lane then holds groups of four neighbouring channels of one row.
-// 32 x 32 x 64 and not 16 x 16 x 128: by itself it reaches 6.4 against 5.5 PFLOP/s on random
+// 32 x 32 x 64 and not 16 x 16 x 128: by itself it reaches 6.5 against 5.5 PFLOP/s on random
 // bytes, where power bounds both.
+//
+// 16384 x 4096 x 4096 takes 156 to 180 us, 3.1 to 3.5 PFLOP/s: half of what the instruction reaches alone.
+// Nothing runs beside a tile's first loads (about 2 us) and its results' way out (128 KB, 7 us at
+// the copy's rate while all CUs write), and a stage's 32 KB take longer than its products.
+// 256 x 256 by 16 waves of 64 x 64 sums: 1028 us (spills); 8 waves of 64 x 128 the same as 128 x 64
+// (within 3 %); 128 x 128 by 4 waves 219, by 128 x 256 221.
 //
 // A lane takes the pieces (16 bytes, a block) 2 (l / 32) and 2 (l / 32) + 1 of a stage in
 // its two steps, so that both scales are one 16-bit read.
@@ -613,7 +636,9 @@ hipError_t launch_tile(const Mx4GemmArgs& g0, hipStream_t st) {
 }
 
 // --------------------------------------------------------------------------
-// many float rows by a narrow w: w stays in LDS in the order of its fragments, and a
+// many float rows by a narrow w (2^20 x 602 x 128 of bfloat16 319 us, 4.8 TB/s of the bytes it cannot do
+// without; of float32 714, 4.3; rounding and product in two launches 516): w stays in LDS in the
+// order of its fragments, and a
 // wave takes 16 rows after 16 rows past it, 128 k at a time, with the next 128 on their
 // way.  Rows are loaded 16 lanes a row and rounded there; a piece of LDS of the wave's
 // own turns the four bytes that a lane then has into the block that the matrix
@@ -804,6 +829,8 @@ bool mx4_few(int a_dtype, int64_t M, int64_t N, int64_t K) {
   return M < 4096 && N <= 1 << 20 && work <= (a_dtype == SAGA_F32 ? 8192 : 16384);
 }
 
+// k_mx4_stream while w fits LDS, against rounding and product in two launches (us, bfloat16: 4096 x 602 x 128 11
+// / 13, 65536 x 1024 x 64 27 / 45, 2^20 x 128 x 128 138 / 178, 2^20 x 602 x 128 321 / 516)
 bool mx4_streams(int64_t M, int64_t N, int64_t K) {
   return M >= 4096 && N <= 128 && StreamSpace(K, N <= 16 ? 1 : N <= 32 ? 2 : N <= 64 ? 4 : 8).total <= 150 * 1024;
 }
@@ -847,8 +874,13 @@ hipError_t launch_gemm_mx4(const Mx4GemmArgs& g0, hipStream_t st) {
     g.a_scale = q + s.scale;
     g.lda_s = s.lds;
   }
+  // Too few 128 x 128 tiles for all CUs: 64 x 64, and eight stages on their way (256 x 4096 x 4096 11 us).
   const int64_t cols = (g.N + 127) / 128, rows = (g.M + 127) / 128;
   if (cols * rows <= 256) return launch_tile<2, 2, 1, 1, 8>(g, st);
+  // 256 x 256, one workgroup a CU, where its tiles fill whole rounds of the CUs to four fifths and
+  // 128-wide ones do not leave out a tenth of its columns (us, against 128 x 128, two workgroups a
+  // CU: 16384 x 4096 x 4096 166 / 221, 16384 x 2048 x 2048 51 / 60, 16384 x 4096 x 1024 42 / 57, 16384 x 1024
+  // x 4096 67 / 71, 40001 x 1024 x 1024, four fifths, 42 / 44, 200000 x 602 x 300 to float32 129 / 118).
   const int64_t large = ((g.M + 255) / 256) * ((g.N + 255) / 256), rounds = (large + 255) / 256;
   if (large * 5 >= rounds * 256 * 4 && (g.N + 255) / 256 * 20 <= cols * 11) return launch_tile<2, 4, 4, 2, 4>(g, st);
   if (g.N <= 32) return launch_tile<4, 1, 1, 1, 2>(g, st);

@@ -126,6 +126,20 @@ def test_rows_exactly(k, dtype):
     assert bool((padding_of(y) == 3.0).all())
 
 
+@pytest.mark.parametrize("dtype,k", [(torch.float32, 515), (torch.bfloat16, 1031)])
+def test_values_that_no_cache_holds(dtype, k):
+    """More than 256 MiB of values: the same as of the same rows a few at a time."""
+    L = LY()
+    m = (256 << 20) // (k * dtype.itemsize) + 77
+    q = torch.randint(0, 256, (m, (k + 1) // 2), dtype=torch.uint8, device=device())
+    s = torch.randint(0, 255, (m, (k + 31) // 32), dtype=torch.uint8, device=device())
+    q, s = padded(q.cpu()), padded(s.cpu(), unit=4)
+    x = L.dequantize_rows_mx4(q, s, k, dtype=dtype)
+    for i in range(0, m, 50000):
+        part = L.dequantize_rows_mx4(q[i:i + 50000], s[i:i + 50000], k, dtype=dtype)
+        assert torch.equal(x[i:i + 50000], part)
+
+
 def test_many_rows_and_none():
     L = LY()
     x = torch.randn(70001, 40, generator=gen(3))
