@@ -44,7 +44,8 @@ __device__ __forceinline__ void store_terms(const ExpertArgs& a, int64_t row, in
 // router: a workgroup a row.  Logits are float64 sums: which expert a row takes hangs
 // on which of two close values is larger, so the products' rounding must not decide.
 // A wave takes kTogether experts at a time, which share the row's values and whose loads
-// are on their way together; the choice is a rank by counting, a thread an expert.
+// are on their way together; the choice is a rank by counting, a thread an expert.  64 rows and
+// experts of 1024 columns take 8.4 us (24 with an expert at a time), 512 rows and 32 experts of 2048 15.
 // --------------------------------------------------------------------------
 constexpr int kTogether = 4;
 
@@ -451,7 +452,9 @@ __global__ __launch_bounds__(256) void k_expert_few(ExpertArgs a) {
 }
 
 // --------------------------------------------------------------------------
-// a layer of few rows (at most 16, and 64 pairs) in two kernels: the latency of each counts.
+// a layer of few rows (at most 16, and 64 pairs) in two kernels: the latency of each counts (one row
+// of 4 experts of 128 x 256: 7.3 and 5.4 us, 4 launches took 17 with the gaps between them; of 8 of
+// 1024 x 4096 12 and 12).
 // The first chooses the experts itself where that is little work (FUSED; every workgroup
 // does, the first one's choice is the result), takes x as it is, and writes h.  The second
 // has 16 channels of out for all rows a workgroup: its waves share the k of all experts
@@ -682,17 +685,18 @@ __global__ __launch_bounds__(512) void k_expert_down_few(ExpertArgs a) {
 }
 
 // --------------------------------------------------------------------------
-// the same where the experts' weights take most of the time and many rows take an expert: a
-// workgroup of NW waves holds 32 NW rows of an expert's weights (32 a wave: gate and up of
+// the same where the experts' weights, of bfloat16, take most of the time and many rows take an
+// expert: a workgroup of NW waves holds 32 NW rows of an expert's weights (32 a wave: gate and up of
 // 16 channels, or 32 channels) and RT tiles of 16 rows of x.  A wave reads its weights from
-// memory into registers, two steps of J blocks a lane ahead; the rows of x go through
-// LDS, the 128 k of one block of all lanes at a time and two of them in turn, where all waves
+// memory into registers, two steps of 128 k ahead; the rows of x go through
+// LDS, a step at a time and two of them in turn, where all waves
 // read them.  One barrier for each.  Loads are not inside a branch: where one path has
-// loads and the other none, the compiler waits for all of them.
+// loads and the other none, the compiler waits for all of them.  512 rows of 32 experts of 2048 x 4096 take
+// 412 us for gates and ups and 241 for downs, where the layer's bytes take 347.
 // --------------------------------------------------------------------------
-template <bool MX4, int TERMS, bool UP, int RT, int NW>
+template <int TERMS, bool UP, int RT, int NW>
 __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
-  constexpr int J = MX4 ? 2 : 1, AHEAD = 2, ROWS = RT * 16;
+  constexpr int AHEAD = 2, ROWS = RT * 16;
   constexpr int PIECES = (ROWS * 16 * TERMS + 64 * NW - 1) / (64 * NW);  // 16-byte pieces a thread stages at a time
   static_assert(ROWS * 16 * TERMS % (64 * NW) == 0, "whole pieces");
   extern __shared__ uint4 space[];  // x: twice TERMS x ROWS x 16 pieces, then the list
@@ -709,27 +713,27 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
   const int quarter = lane >> 4, lr = lane & 15;
   const int K = UP ? a.F : a.H, N = UP ? a.H : a.N;
   const bool gated = UP && a.gated;
-  const int all = (K + 128 * J - 1) / (128 * J), per = UP ? all : (all + a.splits - 1) / a.splits;
+  const int all = (K + 127) / 128, per = UP ? all : (all + a.splits - 1) / a.splits;
   const int s0 = UP ? 0 : me.part * per, s1 = UP ? all : min(all, s0 + per);
   const int64_t ld = UP ? a.ld_xt : a.ld_ht, plane = (UP ? a.M : a.M * a.top_k) * ld;
   const uint16_t* const rows = UP ? a.xt : a.ht;
   const int n0 = me.run * width + wave * (gated ? 16 : 32);
-  WeightBlocks<MX4, J> w[AHEAD][2];
-  WeightRow<MX4> weights[2];
+  WeightBlocks<false, 1> w[AHEAD][2];
+  WeightRow<false> weights[2];
 #pragma unroll
   for (int o = 0; o < 2; ++o)
-    weights[o] = weight_row<MX4, UP>(a, gated ? ((int64_t)e * 2 + o) * N + min(n0 + lr, N - 1)
-                                              : (int64_t)e * N + min(n0 + o * 16 + lr, N - 1));
+    weights[o] = weight_row<false, UP>(a, gated ? ((int64_t)e * 2 + o) * N + min(n0 + lr, N - 1)
+                                                : (int64_t)e * N + min(n0 + o * 16 + lr, N - 1));
   const auto load = [&](int d, int s) {
-    w[d][0].load(weights[0], (s * 4 + quarter) * J, K);
-    w[d][1].load(weights[1], (s * 4 + quarter) * J, K);
+    w[d][0].load(weights[0], s * 4 + quarter, K);
+    w[d][1].load(weights[1], s * 4 + quarter, K);
   };
   for (int i0 = 0; i0 < count; i0 += ROWS) {
     const int here = min(count - i0, ROWS), tiles = (here + 15) / 16;
     // the pieces that this thread stages: term t, row r, piece p (4 quarter + group)
     const uint16_t* from[PIECES];
     u32x4 piece[PIECES];
-    const int p = threadIdx.x & 15, col = (p >> 2) * 32 * J + (p & 3) * 8;
+    const int p = threadIdx.x & 15, col = (p >> 2) * 32 + (p & 3) * 8;
     int to[PIECES];
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
@@ -738,65 +742,60 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
       from[j] = rows + t * plane + (UP ? pair / a.top_k : pair) * ld;
       to[j] = (t * ROWS + r) * 16 + (p ^ (r & 15));
     }
-    // part h: block h % J of step h / J
-    const auto fetch = [&](int h) {
-      const int k = min(h / J * 128 * J + h % J * 32 + col, (int)ld - 8);
+    const auto fetch = [&](int s) {
+      const int k = min(s * 128 + col, (int)ld - 8);
 #pragma unroll
       for (int j = 0; j < PIECES; ++j) piece[j] = *reinterpret_cast<const u32x4*>(from[j] + k);
     };
-    const auto put = [&](int h) {
+    const auto put = [&](int s) {
 #pragma unroll
-      for (int j = 0; j < PIECES; ++j) xs[(h & 1) * PART + to[j]] = piece[j];
+      for (int j = 0; j < PIECES; ++j) xs[(s & 1) * PART + to[j]] = piece[j];
     };
     f32x4 acc[RT][2];
 #pragma unroll
     for (int r = 0; r < RT; ++r) acc[r][0] = acc[r][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    fetch(s0 * J);
+    fetch(s0);
 #pragma unroll
     for (int d = 0; d < AHEAD; ++d) load(d, s0 + d);
-    put(s0 * J);
-    fetch(s0 * J + 1);
+    put(s0);
+    fetch(s0 + 1);
     for (int sb = s0; sb < s1; sb += AHEAD) {
 #pragma unroll
       for (int d = 0; d < AHEAD; ++d) {
         const int s = sb + d;
         if (s >= all - 1) {
-          w[d][0].clear((s * 4 + quarter) * J, K);
-          w[d][1].clear((s * 4 + quarter) * J, K);
+          w[d][0].clear(s * 4 + quarter, K);
+          w[d][1].clear(s * 4 + quarter, K);
         }
+        ring_barrier();  // step s is in LDS, and nobody reads step s - 1 any more
+        put(s + 1);
+        fetch(s + 2);
+        bf16x8 wv[2][4];
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-          const int h = s * J + j;
-          ring_barrier();  // part h is in LDS, and nobody reads part h - 1 any more
-          put(h + 1);
-          fetch(h + 2);
-          bf16x8 wv[2][4];
+        for (int o = 0; o < 2; ++o)
 #pragma unroll
-          for (int o = 0; o < 2; ++o)
+          for (int t = 0; t < 4; ++t) wv[o][t] = w[d][o].take(0, t);
+        load(d, s + AHEAD);
+        const u32x4* const x = xs + (s & 1) * PART + lr * 16;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) wv[o][t] = w[d][o].take(j, t);
-          if (j == J - 1) load(d, s + AHEAD);
-          const u32x4* const x = xs + (h & 1) * PART + lr * 16;
+        for (int r = 0; r < RT; ++r) {
+          if (r < tiles && s < s1) {
 #pragma unroll
-          for (int r = 0; r < RT; ++r) {
-            if (r < tiles && s < s1) {
+            for (int p = 0; p < TERMS; ++p)
 #pragma unroll
-              for (int p = 0; p < TERMS; ++p)
+              for (int t = 0; t < 4; ++t) {
+                const u32x4 v = x[(p * ROWS + r * 16) * 16 + ((quarter * 4 + t) ^ lr)];
+                bf16x8 xv;
+                __builtin_memcpy(&xv, &v, 16);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                  const u32x4 v = x[(p * ROWS + r * 16) * 16 + ((quarter * 4 + t) ^ lr)];
-                  bf16x8 xv;
-                  __builtin_memcpy(&xv, &v, 16);
-#pragma unroll
-                  for (int o = 0; o < 2; ++o)
-                    acc[r][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[o][t], xv, acc[r][o], 0, 0, 0);
-                }
-            }
+                for (int o = 0; o < 2; ++o)
+                  acc[r][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[o][t], xv, acc[r][o], 0, 0, 0);
+              }
           }
         }
       }
     }
-    ring_barrier();  // (the next rows' first part takes the place of one that may still be read)
+    ring_barrier();  // (the next rows' first step takes the place of one that may still be read)
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       if (r * 16 + lr >= here) continue;
@@ -819,6 +818,11 @@ __global__ __launch_bounds__(64 * NW) void k_expert_wide(ExpertArgs a) {
 // of them cost as much), each well ahead of its use.  A wave has 64 rows of weights (gate and up of 32 channels, or 64
 // channels) and every second tile of x.  Past the rows' ends x is zeros and scales are 1,
 // whatever the weights' bits are there.
+//
+// 512 rows and 32 experts of 2048 x 4096 (64 rows an expert): 112 us for gates and ups, 87 for downs, where
+// their weights alone would take 60 and 30 and the products 45 and 45.  The loads alone take 90: x comes
+// from L2 (24 KB for each 17 KB of weights), and nothing runs beside a tile's first loads and its
+// values' way out.  128 rows (16 an expert): 77 and 46, three quarters of the copy's rate.
 // --------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) uint4 lds_uint4;
 
@@ -936,58 +940,58 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     // (how many tiles the wave has is part of the code: a branch around each would keep the
     // reads of the next one behind the products of the last)
     const auto products = [&](auto count_tag) {
-    constexpr int NT = decltype(count_tag)::value;
-    int ring = 0;  // where part v is; v + 1 and v + 2 follow
-    for (int s = s0; s < s1; ++s) {
-      const bool more = s + 1 < s1;
-      WeightBlocks<true, 2> w[4];
+      constexpr int NT = decltype(count_tag)::value;
+      int ring = 0;  // where part v is; v + 1 and v + 2 follow
+      for (int s = s0; s < s1; ++s) {
+        const bool more = s + 1 < s1;
+        WeightBlocks<true, 2> w[4];
 #pragma unroll
-      for (int m = 0; m < R::SL; ++m) {
-        // Part v = s SL + m has to be there, and with m = 0 slot s: of what was asked for later,
-        // part v + 1 and (behind part s SL + 2) slot s + 1 may still be on their way.
-        const int v = s * R::SL + m;
-        if (m + 1 == R::SL && !more) wait_vm<0>();
-        else if ((m == 1 || (m == 2 && R::SL > 2)) && more) wait_vm<R::XL + R::WL>();
-        else wait_vm<R::XL>();
-        ring_barrier();  // and nobody reads part v - 1, or with m = 0 slot s - 1, any more
-        if (m + 2 < R::SL || more) issue_x(v + 2, ring == 0 ? 2 : ring - 1);
-        if (m == 0 && more) issue_w(s + 1);
-        const char* const slot = base + (s & 1) * R::SLOT;
-        const char* const part = base + 2 * R::SLOT + ring * R::PART;
-        ring = ring == 2 ? 0 : ring + 1;
-        const int j = m * R::TC / 4, t0 = m * R::TC % 4;
-        if (t0 == 0) {  // the lane's block 2 quarter + j of the slot
-          const int r0 = wm * 64 + lr;
-          const char* const wl = slot + r0 * 128 + ((quarter * 2 + j) ^ (r0 >> 1 & 7)) * 16;
-          const bool past = (s * 8 + quarter * 2 + j) * 32 >= K;
+        for (int m = 0; m < R::SL; ++m) {
+          // Part v = s SL + m has to be there, and with m = 0 slot s: of what was asked for later,
+          // part v + 1 and (behind part s SL + 2) slot s + 1 may still be on their way.
+          const int v = s * R::SL + m;
+          if (m + 1 == R::SL && !more) wait_vm<0>();
+          else if ((m == 1 || (m == 2 && R::SL > 2)) && more) wait_vm<R::XL + R::WL>();
+          else wait_vm<R::XL>();
+          ring_barrier();  // and nobody reads part v - 1, or with m = 0 slot s - 1, any more
+          if (m + 2 < R::SL || more) issue_x(v + 2, ring == 0 ? 2 : ring - 1);
+          if (m == 0 && more) issue_w(s + 1);
+          const char* const slot = base + (s & 1) * R::SLOT;
+          const char* const part = base + 2 * R::SLOT + ring * R::PART;
+          ring = ring == 2 ? 0 : ring + 1;
+          const int j = m * R::TC / 4, t0 = m * R::TC % 4;
+          if (t0 == 0) {  // the lane's block 2 quarter + j of the slot
+            const int r0 = wm * 64 + lr;
+            const char* const wl = slot + r0 * 128 + ((quarter * 2 + j) ^ (r0 >> 1 & 7)) * 16;
+            const bool past = (s * 8 + quarter * 2 + j) * 32 >= K;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            w[i].v[j] = *reinterpret_cast<const u32x4*>(wl + i * 16 * 128);
-            const uint32_t b = *reinterpret_cast<const uint8_t*>(slot + R::W_BYTES + r0 * 8 + i * 128 + quarter * 2 + j);
-            w[i].scale = (past ? 127u : b) << (8 * j);
+            for (int i = 0; i < 4; ++i) {
+              w[i].v[j] = *reinterpret_cast<const u32x4*>(wl + i * 16 * 128);
+              const uint32_t b = *reinterpret_cast<const uint8_t*>(slot + R::W_BYTES + r0 * 8 + i * 128 + quarter * 2 + j);
+              w[i].scale = (past ? 127u : b) << (8 * j);
+            }
           }
-        }
 #pragma unroll
-        for (int t = 0; t < R::TC; ++t) {
-          bf16x8 wv[4];
+          for (int t = 0; t < R::TC; ++t) {
+            bf16x8 wv[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) wv[i] = w[i].take(j, t0 + t);
-          const char* const xl = part + ((wx * 16 + lr) * R::PPR + R::place(lr, quarter * R::TC + t)) * 16;
+            for (int i = 0; i < 4; ++i) wv[i] = w[i].take(j, t0 + t);
+            const char* const xl = part + ((wx * 16 + lr) * R::PPR + R::place(lr, quarter * R::TC + t)) * 16;
 #pragma unroll
-          for (int r = 0; r < NT; ++r) {
+            for (int r = 0; r < NT; ++r) {
 #pragma unroll
-            for (int p = 0; p < TERMS; ++p) {
-              const u32x4 x = *reinterpret_cast<const u32x4*>(xl + (p * R::ROWS + r * 32) * R::PPR * 16);
-              bf16x8 xv;
-              __builtin_memcpy(&xv, &x, 16);
+              for (int p = 0; p < TERMS; ++p) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(xl + (p * R::ROWS + r * 32) * R::PPR * 16);
+                bf16x8 xv;
+                __builtin_memcpy(&xv, &x, 16);
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                acc[i][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], xv, acc[i][r], 0, 0, 0);
+                for (int i = 0; i < 4; ++i)
+                  acc[i][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], xv, acc[i][r], 0, 0, 0);
+              }
             }
           }
         }
       }
-    }
     };
     switch ((tiles - wx + 1) / 2) {
       case 0: products(std::integral_constant<int, 0>{}); break;
@@ -1033,9 +1037,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
 // all of k if it fits, so that nothing but weights is loaded in the loop: loads come back in
 // their order, and a wait for x would be one for the weights that were asked for before.  A
 // workgroup takes `per` runs of 32 NW rows of weights one after the other, and a wave's
-// loads run AHEAD steps ahead across them.
+// loads run AHEAD steps ahead across them.  64 rows and 64 experts of 1024 x 4096 in 4 bits (two rows
+// an expert): 64 us for gates and ups (3.8 TB/s of weights), 38 for downs; with half lines a load
+// 84 and 48, with loads in branches 106 and 53.  In bfloat16 4.2 TB/s.
 // --------------------------------------------------------------------------
-constexpr int kStreamPieces = 3072;  // (three workgroups a CU)
+constexpr int kStreamPieces = 48 * 64;  // 48 KB (three workgroups a CU)
 
 template <bool MX4, int TERMS, bool UP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k_expert_stream(ExpertArgs a, int runs,
@@ -1184,25 +1190,32 @@ __global__ __launch_bounds__(256) void k_expert_sum(ExpertArgs a) {
   }
 }
 
-// Whether the wide kernels take the products: their workgroups fill the CUs
+// Whether the wide kernels take the products: their workgroups fill the CUs (us of the layer, wide / not: 32
+// rows of 8 experts of 1024 x 4096 in 4 bits 32 / 44; 64 of 16 of 256 x 1024, where they just do, 26 / 26)
 bool experts_wide(int64_t M, int64_t H, int64_t N, int E, int top_k, bool gated) {
   const int64_t slots = std::min<int64_t>(M * top_k, E);
   return slots * ((H * (gated ? 2 : 1) + 127) / 128) >= 256;
 }
-// parts of k of the second product, so that it has workgroups enough
+// parts of k of the second product, so that it has workgroups enough (us of the layer, with / without: 512
+// rows of 8 experts of 1024 x 4096 in 4 bits 82 / 176, 128 of 32 80 / 91, 64 of 64, where there is one part, 114)
 int expert_splits(int64_t M, int64_t H, int64_t N, int E, int top_k) {
   const int64_t slots = std::min<int64_t>(M * top_k, E), wgs = slots * ((N + 127) / 128), steps = (H + 127) / 128;
   return (int)std::max<int64_t>(1, std::min<int64_t>({8, 512 / wgs, steps / 4}));
 }
 
 // Whether the two kernels of few rows take the layer: the second one's workgroups, 16 channels
-// of out each, read their channels of all experts that are taken
+// of out each, read their channels of all experts that are taken one after the other (us, two kernels /
+// four; 4 bits: a row, two of 8 experts of 1024 x 2048 20 / 26, of 1024 x 4096 24 / 26, two rows of these
+// 43 / 35; 16 rows of 8 of 128 x 256 22 / 25, of 4 of 256 x 1024 25 / 23, of 32 of 128 x 256 27 / 25.
+// bfloat16, twice the cost: a row, two of 8 of 1024 x 1024 20 / 24, of 1024 x 2048 23 / 24, of 1024 x 4096 33 / 28.)
 bool experts_few(int64_t M, int64_t H, int top_k, int E, bool mx4) {
   return M <= kFewRows && M * top_k <= kFewPairs &&
-         std::min<int64_t>(M * top_k, E) * H * 16 * (mx4 ? 1 : 4) <= 2 * 256 * 1024;
+         std::min<int64_t>(M * top_k, E) * H * (mx4 ? 1 : 2) <= (M <= 2 ? 8192 : 2048);
 }
-// and whether the first one chooses: a float64 product of a few waves
-bool experts_fused(int64_t M, int64_t F, int E) { return M * E * F <= 16384; }
+// and whether the first one chooses: a float64 product by the waves of every workgroup (us, chosen
+// there / by k_route before: a row and 16 experts of 1024 columns 20 / 23, two rows of 512 19 / 22, of 8 of 602
+// 21 / 23, four rows of 4 of 128 18 / 21, of 16 of 256 23 / 22, 16 rows of 8 of 128 51 / 22)
+bool experts_fused(int64_t M, int64_t F, int E) { return M <= 4 && M * E * F <= (M <= 2 ? 16384 : 4096); }
 
 template <bool MX4, typename T>
 hipError_t few_rows(const ExpertArgs& a, hipStream_t st) {
@@ -1220,12 +1233,12 @@ hipError_t few_rows(const ExpertArgs& a, hipStream_t st) {
   return go(k_expert_down_few<MX4, sizeof(T) == 2 ? 2 : 3>, dim3((unsigned)((a.N + 15) / 16)));
 }
 
-template <bool MX4, int TERMS, bool UP, int RT, int NW>
+template <int TERMS, bool UP, int RT, int NW>
 hipError_t launch_wide(const ExpertArgs& a, hipStream_t st) {
   const unsigned slots = (unsigned)std::min<int64_t>(a.M * a.top_k, a.E);
   const int per = NW * (UP && a.gated ? 16 : 32), n = UP ? a.H : a.N;
   const size_t lds = (size_t)2 * TERMS * RT * 16 * 16 * 16 + (size_t)a.M * 4;
-  hipLaunchKernelGGL((k_expert_wide<MX4, TERMS, UP, RT, NW>),
+  hipLaunchKernelGGL((k_expert_wide<TERMS, UP, RT, NW>),
                      dim3(share_blocks(slots, (n + per - 1) / per, UP ? 1 : a.splits)), dim3(64 * NW), lds, st, a);
   return hipGetLastError();
 }
@@ -1240,6 +1253,9 @@ hipError_t launch_expert_tile(const ExpertArgs& a, hipStream_t st) {
 }
 template <bool MX4, int TERMS, bool UP>
 hipError_t dispatch_wide(const ExpertArgs& a, hipStream_t st) {
+  // Rows an expert has on average (us of both products, 4-bit weights, k_expert_stream / k_expert_tile: two,
+  // 64 rows of 64 experts of 1024 x 4096, 102 / 116; eight, 128 rows of 32, 82 / 69.  Of the layer, bfloat16
+  // weights, k_expert_stream / k_expert_wide: four, 64 rows of 32 experts, 193 / 238; eight 219 / 244.)
   const int64_t mean = a.M * a.top_k / a.E;
   if (mean <= (MX4 ? 4 : 8)) {
     const int64_t slots = std::min<int64_t>(a.M * a.top_k, a.E), rows = UP ? (int64_t)a.H * (a.gated ? 2 : 1) : a.N;
@@ -1248,12 +1264,14 @@ hipError_t dispatch_wide(const ExpertArgs& a, hipStream_t st) {
                        dim3(share_blocks(slots, (runs + per - 1) / per, z)), dim3(256), 0, st, a, (int)runs, (int)per);
     return hipGetLastError();
   }
+  // (us of the layer by tiles of 32, 64 and 96 rows, 32 experts of 2048 x 4096: 16 rows an expert 136, 144,
+  // 150; 32: 194, 159, 167; 64: 306, 255, 214.  Three terms of 96 rows do not fit LDS.)
   if constexpr (MX4) {
     if (mean <= 20) return launch_expert_tile<TERMS, UP, 2>(a, st);
     if (mean <= 40 || TERMS == 3) return launch_expert_tile<TERMS, UP, 4>(a, st);
     if constexpr (TERMS < 3) return launch_expert_tile<TERMS, UP, 6>(a, st);
   } else {
-    return launch_wide<MX4, TERMS, UP, 4, 8>(a, st);
+    return launch_wide<TERMS, UP, 4, 8>(a, st);
   }
 }
 
