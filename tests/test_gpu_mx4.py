@@ -415,6 +415,20 @@ def test_large_layers(m, f, h, n, e, top_k, weights, dtype, gated):
     layer.check(torch.randn(m, f, generator=gen(m)).to(dtype), top_k, "sigmoid" if gated else "relu")
 
 
+@pytest.mark.parametrize("m,f,h,n,e,top_k", [(1, 2000, 4096, 33, 8, 2), (2, 1024, 1024, 40, 8, 4),
+                                             (2, 1032, 1032, 40, 8, 4), (2, 1024, 512, 40, 8, 4),
+                                             (3, 128, 100, 40, 9, 2), (4, 256, 250, 70, 4, 2),
+                                             (4, 264, 258, 70, 4, 2), (16, 130, 220, 50, 9, 4), (16, 130, 110, 50, 9, 4),
+                                             (16, 40, 64, 20, 40, 4), (16, 130, 230, 50, 9, 4)])
+@pytest.mark.parametrize("weights", ["mx4", "bf16"])
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_few_rows_two_kernels_or_four(m, f, h, n, e, top_k, weights, dtype):
+    """sizes on both sides of what the kernels of few rows take and of where they choose themselves"""
+    for gated in (False, True):
+        layer = Layer(m + h, f, h, n, e, weights, gated, biases=True)
+        layer.check(torch.randn(m, f, generator=gen(m + f)).to(dtype), top_k, "tanh")
+
+
 def test_more_rows_than_one_run():
     """more than 1024 rows: the kernels run for each part, rows of one expert more than a tile"""
     layer = Layer(5, 40, 50, 24, 6, "mx4", True, True)
