@@ -526,7 +526,7 @@ __global__ __launch_bounds__(512) void k_expert_up_few(ExpertArgs a) {
   asm volatile("" ::: "memory");
   const int pair = list[wave][min(lr, count - 1)];
 
-  const int K = a.F, n0 = blockIdx.x * 16, all = (K + 127) / 128, last = (K - 1) / 8 * 8;
+  const int K = a.F, n0 = blockIdx.x * 16, all = (K + 127) / 128;
   const int steps = (all - wave + NW - 1) / NW;  // of this wave: wave, wave + NW, ..
   const T* const x = static_cast<const T*>(a.x) + pair / a.top_k * a.ldx;
   WeightRow<MX4> from[NO];
@@ -540,7 +540,7 @@ __global__ __launch_bounds__(512) void k_expert_up_few(ExpertArgs a) {
 #pragma unroll
     for (int o = 0; o < NO; ++o) w[d][o].load(from[o], b, K);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) xv[d][t].load(x + min(b * 32 + t * 8, last), 8);
+    for (int t = 0; t < 4; ++t) load_clamped(xv[d][t], x, b * 32 + t * 8, K);
   };
   f32x4 acc[NO];
 #pragma unroll
@@ -557,7 +557,7 @@ __global__ __launch_bounds__(512) void k_expert_up_few(ExpertArgs a) {
 #pragma unroll
         for (int o = 0; o < NO; ++o) w[d][o].clear(b, K);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) xv[d][t].clear(K - min(b * 32 + t * 8, last));
+        for (int t = 0; t < 4; ++t) xv[d][t].clear(K - b * 32 - t * 8);
       }
 #pragma unroll
       for (int t = 0; t < 4; ++t) {

@@ -78,6 +78,17 @@ struct Mx4Block {
   uint32_t scale;  // in the low byte
 };
 
+// Columns col.. of a row of K floats, 8 of them and without a branch: past the row's end its last
+// 16 bytes are read again (each half by itself: rows are whole 16 bytes, not 32), to be cleared.
+__device__ __forceinline__ void load_clamped(Raw<float>& r, const float* x, int col, int K) {
+  const int most = (K - 1) / 4 * 4;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) r.v[h] = *reinterpret_cast<const u32x4*>(x + min(col + 4 * h, most));
+}
+__device__ __forceinline__ void load_clamped(Raw<uint16_t>& r, const uint16_t* x, int col, int K) {
+  r.v = *reinterpret_cast<const u32x4*>(x + min(col, (K - 1) / 8 * 8));
+}
+
 // What a row's source is: 4-bit rows with their scales, or floats.  Block b of the row of K
 // columns; `take` apart from `load`, so that loads run ahead, and without a branch in it: past
 // the row's end its last piece is read again, and `take` clears it (LAST: where that can be).
@@ -89,9 +100,8 @@ struct RowSource {  // float or uint16_t
     x = static_cast<const T*>(base) + row * ld;
   }
   __device__ __forceinline__ void load(int b, int K) {
-    const int most = (K - 1) / 8 * 8;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) raw[u].load(x + min(b * 32 + u * 8, most), 8);
+    for (int u = 0; u < 4; ++u) load_clamped(raw[u], x, b * 32 + u * 8, K);
   }
   __device__ __forceinline__ Mx4Block take(int b, int K, bool last) {
     if (last) {

@@ -429,6 +429,37 @@ def test_few_rows_two_kernels_or_four(m, f, h, n, e, top_k, weights, dtype):
         layer.check(torch.randn(m, f, generator=gen(m + f)).to(dtype), top_k, "tanh")
 
 
+def at_the_end(t):
+    """t on the GPU, pitch a multiple of 16 bytes, as the last rows of 24 MiB that are an allocation"""
+    ld = (t.shape[1] * t.element_size() + 15) // 16 * 16 // t.element_size()
+    buf = torch.empty((24 << 20) // t.element_size(), dtype=t.dtype, device=device())
+    rows = buf[buf.numel() - t.shape[0] * ld:].view(t.shape[0], ld)
+    rows.fill_(NAN)
+    rows[:, :t.shape[1]] = t.to(device())
+    return rows[:, :t.shape[1]]
+
+
+@pytest.mark.parametrize("k", [1, 3, 4, 12, 33, 36, 100, 129, 132])
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_last_rows_of_an_allocation(k, dtype):
+    """nothing past the last row's pitch is read: rows are whole 16 bytes, four columns of float32"""
+    L = LY()
+    for m in (1, 5, 20, 4099):
+        x = torch.randn(m, k, generator=gen(k + m)).to(dtype)
+        code, byte, value = rows_exact(x.double())
+        xd = at_the_end(x)
+        q, s = L.quantize_rows_mx4(xd)
+        assert torch.equal(s.cpu(), byte)
+        wq, ws, w = four_bits(torch.randn(70, k, generator=gen(k)))
+        y = L.mx4_linear(xd, wq, ws, out_dtype=torch.float32).cpu().double()
+        want, size = value @ w.double().t(), value.abs() @ w.double().abs().t()
+        assert ((y - want).abs() <= (k + 8) * U * size + 1e-30).all()  # (exact products, k float32 sums)
+    for m in (1, 3, 16, 40):
+        layer = Layer(m + k, k, 40, 24, 5, "mx4", True, True)
+        x = torch.randn(m, k, generator=gen(m)).to(dtype)
+        layer.check(x, 2, got=layer(at_the_end(x), top_k=2))
+
+
 def test_more_rows_than_one_run():
     """more than 1024 rows: the kernels run for each part, rows of one expert more than a tile"""
     layer = Layer(5, 40, 50, 24, 6, "mx4", True, True)
