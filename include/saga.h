@@ -694,6 +694,7 @@ saga_status saga_apply_vertex_mx(const saga_mx_op* op, saga_cmat a, saga_cmat a_
  * nothing but NaN in out; other rows do not see it.
  * Sums are float32.  Rows and the values h enter the matrix cores as sums of bfloat16
  * terms that hold them to 2^-24 (dtype F32) or, h of BF16 rows, 2^-16.
+ * A value h beyond float32's range makes its row of out NaN.
  * x: M x F, out: M x N, of dtype F32 or BF16.  router: E x F, router_dtype F32 or BF16.
  * Weights, one output channel a row, the experts' one below the other, weight_dtype BF16
  * or MX4 (with scales, as saga_apply_vertex_mx takes them; absent otherwise: ptr NULL):
