@@ -455,6 +455,26 @@ def label_log_probs(logits, labels=None, top_k=0, entropy=True):
     return lp, h, ti, tl
 
 
+def _asked(vertices, n, device):
+    """(at, off): the rows of n that ``vertices`` names, and which of its ids name none (at: any row).  Without a look
+    at the ids from the host, so that a call can be captured."""
+    if not isinstance(vertices, torch.Tensor) or vertices.dim() != 1 or vertices.dtype not in (
+            torch.int32, torch.int64) or vertices.device != device:
+        raise ValueError(f"vertices: a vector of int32 or int64 on {device} is needed, got " + (
+            f"{tuple(vertices.shape)} {vertices.dtype} on {vertices.device}" if isinstance(vertices, torch.Tensor)
+            else type(vertices).__name__))
+    if n == 0 and vertices.numel():
+        raise ValueError("vertices: the graph has none")
+    at = vertices.clamp(0, max(n - 1, 0))
+    return at, at != vertices
+
+
+def _rows_at(t, at):
+    """rows ``at`` of a matrix, in one with 16-byte rows; values ``at`` of a vector"""
+    rows = t.index_select(0, at)
+    return rows if t.dim() == 1 else _out(at.numel(), t.shape[1], t.dtype, t)[0].copy_(rows)
+
+
 class ResidualGCN:
     """A deep GCN with a gated residual stream, its transforms in 8-bit integers (bits=8) or
     microscaled 4-bit floating point (bits=4).
@@ -551,17 +571,10 @@ class ResidualGCN:
 
     def logits(self, x, vertices=None):
         """x: num_vertices x F_in (float32 or bfloat16) on the graph's device; vertices: those
-        whose logits are wanted (int32 or int64; None: all)"""
+        whose logits are wanted (int32 or int64; None: all), in their order; an id that is no vertex of
+        the graph has NaN for logits"""
         if x.device != self.graph.row_ptr.device:
             raise ValueError(f"x is on {x.device}, the graph on {self.graph.row_ptr.device}")
-
-        def asked(t):
-            if vertices is None or t is None:
-                return t
-            if t.dim() == 1:
-                return t.index_select(0, vertices)
-            return _out(vertices.numel(), t.shape[1], t.dtype, t)[0].copy_(t.index_select(0, vertices))
-
         with torch.cuda.device(x.device):
             # (4-bit transforms quantise on their way, experts take floats)
             ends = [self.norm] if self.experts is None else [self.experts["norm"], self.norm]
@@ -576,10 +589,15 @@ class ResidualGCN:
                 h, z, zs = block_norm(m, h, post="rms", post_weight=blk["post"], gate=vg[:, self.f:],
                                       gate_act="sigmoid", res_scale=self.res_scale, pre="rms",
                                       pre_weight=norms[i + 1], eps=self.eps, quantize=whole[i + 1], in_place=True)
-            z, zs = asked(z), asked(zs)
+            if vertices is not None:
+                at, off = _asked(vertices, h.shape[0], h.device)
+                h = _rows_at(h, at) if self.experts is not None else None
+                z, zs = _rows_at(z, at), None if zs is None else _rows_at(zs, at)
+                # (a row of NaN, or of 8-bit numbers whose scale is NaN, is NaN from here on)
+                (z if zs is None else zs[:, None]).masked_fill_(off[:, None], float("nan"))
             if self.experts is not None:
                 y, _, _ = expert_layer(z, *self.experts["args"], **self.experts["kw"])
-                _, z, zs = block_norm(y, asked(h), res_scale=self.res_scale, pre="rms", pre_weight=self.norm,
+                _, z, zs = block_norm(y, h, res_scale=self.res_scale, pre="rms", pre_weight=self.norm,
                                       eps=self.eps, quantize=self.bits == 8)
             return self.transform(z, self.last, zs)
 

@@ -786,6 +786,32 @@ def test_network_in_four_bits_captured():
         assert all(torch.equal(a, b) for a, b in zip(got[1:], want[1:]))
 
 
+@pytest.mark.parametrize("ids", [torch.int32, torch.int64])
+@pytest.mark.parametrize("bits,experts", [(4, True), (8, True), (4, False), (8, False)])
+def test_vertices_outside_the_graph(bits, experts, ids):
+    """an id that is no vertex's has NaN for logits, the others what they have without it"""
+    net, w, x = network(bits, torch.bfloat16, True)
+    if not experts:
+        net = LY().ResidualGCN(net.graph, {k: v for k, v in w.items() if k != "experts"}, res_scale=0.5, bits=bits)
+    n, far = x.shape[0], torch.iinfo(ids)
+    ask = torch.tensor([5, -1, n - 1, n, far.max, 0, far.min, 5], dtype=ids).to(device())
+    good = [0, 2, 5, 7]
+    bad = [1, 3, 4, 6]
+    got = net.logits(x, ask)
+    clean = ask.clone()
+    clean[bad] = 9
+    want = net.logits(x, clean)
+    assert bool(torch.isfinite(want).all())
+    assert torch.equal(got[good], want[good]) and bool(torch.isnan(got[bad]).all())
+    logp, entropy, index, top = net(x, torch.zeros(8, dtype=torch.int32, device=device()), 2, vertices=ask)
+    assert bool(torch.isnan(logp[bad]).all()) and bool((index[bad] == -1).all())
+    assert bool(torch.isfinite(logp[good]).all()) and bool((index[good] >= 0).all())
+    assert net.logits(x, ask[:0]).shape == (0, want.shape[1])
+    for wrong in (ask.cpu(), ask.float(), ask[None], [1, 2]):
+        with pytest.raises(ValueError, match="vertices"):
+            net.logits(x, wrong)
+
+
 def test_network_refusals():
     with pytest.raises(ValueError, match="bits"):
         network(6, torch.bfloat16, True)

@@ -241,6 +241,38 @@ def test_every_argument_by_its_name():
             f(3)
 
 
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+def test_vertices_outside_the_graph(dtype):
+    """ids that name no row get one of the rows there are, and are told apart"""
+    from paper_2009_00804_amd import layers as L
+
+    far = torch.iinfo(dtype)
+    ids = torch.tensor([3, -1, 0, 7, 6, far.max, far.min, 6], dtype=dtype)
+    at, off = L._asked(ids, 7, ids.device)
+    assert off.tolist() == [False, True, False, True, False, True, True, False]
+    assert int(at.min()) >= 0 and int(at.max()) <= 6
+    assert torch.equal(at[~off], ids[~off])
+    t = torch.arange(35).view(7, 5).float()
+    got = L._rows_at(t, at)
+    assert got.stride() == (8, 1) and torch.equal(got[~off], t[[3, 0, 6, 6]])
+    assert torch.equal(L._rows_at(t[:, 0], at)[~off], torch.tensor([15.0, 0, 30, 30]))
+    at, off = L._asked(ids[:0], 0, ids.device)  # (no vertex of none)
+    assert at.numel() == 0 and off.numel() == 0 and L._rows_at(t[:0], at).shape == (0, 5)
+
+
+def test_vertices_refused():
+    from paper_2009_00804_amd import layers as L
+
+    cpu = torch.device("cpu")
+    for bad in ([0, 1], 3, torch.tensor(3), torch.tensor([[1, 2]]), torch.tensor([True, False]), torch.tensor([1.0]),
+                torch.tensor([1], dtype=torch.int16), torch.tensor([1], dtype=torch.uint8),
+                torch.zeros(2, dtype=torch.int64, device="meta")):
+        with pytest.raises(ValueError, match="vertices"):
+            L._asked(bad, 7, cpu)
+    with pytest.raises(ValueError, match="vertices: the graph has none"):
+        L._asked(torch.tensor([0]), 0, cpu)
+
+
 def test_pitches_of_scales():
     from paper_2009_00804_amd import layers as L
 
