@@ -841,7 +841,8 @@ saga_status run_experts(const saga_expert_op& op, const saga_expert_weights& w, 
   if ((s = check_vec(w.down_bias, E * N, false, "down_bias"))) return s;
   if ((s = check_vec(index, M, true, "index"))) return s;
   if ((s = check_vec(weight, M, true, "weight"))) return s;
-  const size_t need = saga::experts_workspace_bytes(op.dtype, M, F, H, N, op.experts, op.top_k, op.gated != 0);
+  const size_t need =
+      saga::experts_workspace_bytes(op.dtype, op.weight_dtype, M, F, H, N, op.experts, op.top_k, op.gated != 0);
   if ((s = check_ws(ws, ws_bytes, need, "apply_vertex_experts"))) return s;
   const Span none = {nullptr, 0};
   const Span outs[] = {span(out, es), span(index, M * op.top_k, 4), span(weight, M * op.top_k, 4), Span{ws, need}};
@@ -2230,7 +2231,8 @@ saga_status saga_apply_vertex_experts_workspace_size(const saga_expert_op* op, i
     if (!op || !bytes) return fail(SAGA_EINVAL, "null argument");
     saga_status s = check_expert_op(*op, m, f, h, n);
     if (s) return s;
-    *bytes = saga::experts_workspace_bytes(op->dtype, m, f, h, n, op->experts, op->top_k, op->gated != 0);
+    *bytes = saga::experts_workspace_bytes(op->dtype, op->weight_dtype, m, f, h, n, op->experts, op->top_k,
+                                           op->gated != 0);
     return ok();
   } catch (...) {
     return fail(SAGA_EINTERNAL, "exception");

@@ -1190,11 +1190,18 @@ __global__ __launch_bounds__(256) void k_expert_sum(ExpertArgs a) {
   }
 }
 
-// Whether the wide kernels take the products: their workgroups fill the CUs (us of the layer, wide / not: 32
-// rows of 8 experts of 1024 x 4096 in 4 bits 32 / 44; 64 of 16 of 256 x 1024, where they just do, 26 / 26)
-bool experts_wide(int64_t M, int64_t H, int64_t N, int E, int top_k, bool gated) {
-  const int64_t slots = std::min<int64_t>(M * top_k, E);
-  return slots * ((H * (gated ? 2 : 1) + 127) / 128) >= 256;
+// Whether the wide kernels take the products: their workgroups fill the CUs (us of the layer, wide / k_expert_few: 32
+// rows of 8 experts of 1024 x 4096 in 4 bits 32 / 44; 64 of 16 of 256 x 1024, where they just do, 26 / 26; 42 of 5 of
+// 3872 x 1757, gated, 140 workgroups, 51 / 44).  k_expert_few reads an expert's weights again for every 16 rows: many
+// rows of 4-bit weights gain by fewer workgroups (all of 3 experts of 1761 x 3362, gated, 530 rows, 159 workgroups,
+// 336 / 709; both of 2 of 1656 x 5333, gated, 304, 168, 323 / 373; two of 6 of 1124 x 2530, 163, 120, 49 / 79; below the
+// rule: three of 22 of 2938 x 223, gated, 672, 88, 117 / 134; three of 11 of 279 x 591, 688, 55, 101 / 82; one of
+// 3043 x 4902, gated, 132, 77, 244 / 159).  bfloat16 ones do not always: four of 11 of 2621 x 1147, gated, 196 rows, 198
+// workgroups, 212 / 289, but four of 17 of 74 x 850, gated, 722, 238, 138 / 92; four of 7 of 1061 x 1005, gated, 153,
+// 112, 113 / 80; four of 4 of 3726 x 1697, 260, 56, 712 / 500.
+bool experts_wide(int64_t M, int64_t H, int E, int top_k, bool gated, bool mx4) {
+  const int64_t slots = std::min<int64_t>(M * top_k, E), mean = M * top_k / E;
+  return slots * ((H * (gated ? 2 : 1) + 127) / 128) >= (mx4 && mean >= 48 ? 96 : 256);
 }
 // parts of k of the second product, so that it has workgroups enough (us of the layer, with / without: 512
 // rows of 8 experts of 1024 x 4096 in 4 bits 82 / 176, 128 of 32 80 / 91, 64 of 64, where there is one part, 114)
@@ -1278,7 +1285,7 @@ hipError_t dispatch_wide(const ExpertArgs& a, hipStream_t st) {
 template <bool MX4>
 hipError_t products(const ExpertArgs& a, hipStream_t st) {
   hipError_t e;
-  if (experts_wide(a.M, a.H, a.N, a.E, a.top_k, a.gated)) {
+  if (experts_wide(a.M, a.H, a.E, a.top_k, a.gated, MX4)) {
     e = a.x_terms == 1 ? dispatch_wide<MX4, 1, true>(a, st) : dispatch_wide<MX4, 3, true>(a, st);
     if (e != hipSuccess) return e;
     return a.h_terms == 2 ? dispatch_wide<MX4, 2, false>(a, st) : dispatch_wide<MX4, 3, false>(a, st);
@@ -1309,7 +1316,7 @@ struct ExpertSpace {
   int x_terms, h_terms, splits;
   size_t xt, ht, zeros, part, total;
 };
-ExpertSpace expert_space(int dtype, int64_t M, int64_t F, int64_t H, int64_t N, int E, int top_k, bool gated) {
+ExpertSpace expert_space(int dtype, bool mx4, int64_t M, int64_t F, int64_t H, int64_t N, int E, int top_k, bool gated) {
   ExpertSpace s;
   s.x_terms = dtype == SAGA_BF16 ? 1 : 3;
   s.h_terms = dtype == SAGA_BF16 ? 2 : 3;
@@ -1323,20 +1330,22 @@ ExpertSpace expert_space(int dtype, int64_t M, int64_t F, int64_t H, int64_t N, 
   s.ht = s.xt + whole((size_t)s.x_terms * s.rows * s.ld_xt * 2);
   s.zeros = s.ht + whole((size_t)s.h_terms * s.rows * top_k * s.ld_ht * 2);
   s.part = s.zeros + 256;
-  s.splits = experts_wide(s.rows, H, N, E, top_k, gated) ? expert_splits(s.rows, H, N, E, top_k) : 1;
+  s.splits = experts_wide(s.rows, H, E, top_k, gated, mx4) ? expert_splits(s.rows, H, N, E, top_k) : 1;
   s.total = s.part + whole((size_t)s.splits * s.rows * top_k * s.ld_part * 4);
   return s;
 }
 
 }  // namespace
 
-size_t experts_workspace_bytes(int dtype, int64_t M, int64_t F, int64_t H, int64_t N, int E, int top_k, bool gated) {
-  return M == 0 ? 0 : expert_space(dtype, M, F, H, N, E, top_k, gated).total;
+size_t experts_workspace_bytes(int dtype, int weight_dtype, int64_t M, int64_t F, int64_t H, int64_t N, int E, int top_k,
+                               bool gated) {
+  return M == 0 ? 0 : expert_space(dtype, weight_dtype == SAGA_MX4, M, F, H, N, E, top_k, gated).total;
 }
 
 hipError_t launch_experts(const ExpertArgs& a0, hipStream_t st) {
   if (a0.M == 0) return hipSuccess;
-  const ExpertSpace s = expert_space(a0.dtype, a0.M, a0.F, a0.H, a0.N, a0.E, a0.top_k, a0.gated);
+  const bool mx4 = a0.weight_dtype == SAGA_MX4;
+  const ExpertSpace s = expert_space(a0.dtype, mx4, a0.M, a0.F, a0.H, a0.N, a0.E, a0.top_k, a0.gated);
   const size_t es = a0.dtype == SAGA_BF16 ? 2 : 4;
   for (int64_t m = 0; m < a0.M; m += s.rows) {
     ExpertArgs a = a0;
@@ -1357,9 +1366,9 @@ hipError_t launch_experts(const ExpertArgs& a0, hipStream_t st) {
     a.h_terms = s.h_terms;
     a.splits = s.splits;
     if (a.M < s.rows)  // (the rest of many rows: never more parts than there is room for)
-      a.splits = std::min(s.splits, experts_wide(a.M, a.H, a.N, a.E, a.top_k, a.gated)
+      a.splits = std::min(s.splits, experts_wide(a.M, a.H, a.E, a.top_k, a.gated, mx4)
                                         ? expert_splits(a.M, a.H, a.N, a.E, a.top_k) : 1);
-    const bool mx4 = a.weight_dtype == SAGA_MX4, few = experts_few(a.M, a.H, a.top_k, a.E, mx4);
+    const bool few = experts_few(a.M, a.H, a.top_k, a.E, mx4);
     const auto route = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)a.M), dim3(kRouteThreads), 0, st, a);
       return hipGetLastError();
@@ -1378,7 +1387,7 @@ hipError_t launch_experts(const ExpertArgs& a0, hipStream_t st) {
       if (e != hipSuccess) return e;
       continue;
     }
-    e = a.weight_dtype == SAGA_MX4 ? products<true>(a, st) : products<false>(a, st);
+    e = mx4 ? products<true>(a, st) : products<false>(a, st);
     if (e != hipSuccess) return e;
     const int64_t quads = a.M * (a.ld_part / 4);
     hipLaunchKernelGGL(k_expert_sum, dim3((unsigned)std::min<int64_t>((quads + 255) / 256, 1 << 16)), dim3(256), 0, st, a);

@@ -283,7 +283,8 @@ struct ExpertArgs {
   int x_terms, h_terms;
   int splits;             // parts of k of the second products
 };
-size_t experts_workspace_bytes(int dtype, int64_t M, int64_t F, int64_t H, int64_t N, int E, int top_k, bool gated);
+size_t experts_workspace_bytes(int dtype, int weight_dtype, int64_t M, int64_t F, int64_t H, int64_t N, int E, int top_k,
+                               bool gated);
 hipError_t launch_experts(const ExpertArgs& a, hipStream_t st);
 
 // ---- block.hip ----

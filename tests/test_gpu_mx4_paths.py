@@ -170,11 +170,13 @@ def test_the_same_bits_again(m, f, h, n, e, top_k, weights, dtype):
 
 
 @pytest.mark.parametrize("m,f,h,n,e,top_k", [(304, 602, 900, 400, 2, 2), (1024, 300, 520, 300, 1, 1), (260, 1000, 700, 1000, 4, 4),
-                                             (1500, 128, 256, 128, 2, 1), (130, 4096, 260, 33, 1, 1)])
+                                             (1500, 128, 256, 128, 2, 1), (130, 4096, 260, 33, 1, 1),
+                                             (304, 130, 3100, 130, 2, 2), (304, 130, 1530, 130, 8, 2),
+                                             (200, 100, 2000, 70, 12, 3), (150, 64, 4100, 50, 3, 1), (140, 64, 4100, 50, 3, 1)])
 @pytest.mark.parametrize("weights", ["mx4", "bf16"])
 @pytest.mark.parametrize("dtype", FLOATS)
 def test_few_experts_of_many_rows(m, f, h, n, e, top_k, weights, dtype):
-    """every row takes all experts, or one of two: hundreds of rows of each"""
+    """hundreds of rows of each expert, on both sides of where the kernels of many rows take them"""
     for gated in (False, True):
         layer = Layer(m + e, f, h, n, e, weights, gated, gated)
         layer.check(torch.randn(m, f, generator=gen(m)).to(dtype), top_k, "sigmoid" if gated else "relu")
