@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from gpu_util import device
-from test_gpu_mx4 import ACTS, FLOATS, HALF, LY, U, Layer, four_bits, gen, network, padded, route_exact
+from test_gpu_mx4 import ACTS, FLOATS, HALF, LY, U, Layer, experts_exact, four_bits, gen, network, padded, route_exact
 
 pytestmark = pytest.mark.gpu
 
@@ -194,3 +194,31 @@ def test_all_vertices_asked_for(bits, gated):
     order = torch.randperm(x.shape[0], generator=gen(2)).to(device())
     assert torch.equal(net.logits(x, order), every[order])
     assert torch.equal(net.logits(x, order.int()), every[order])
+
+
+@pytest.mark.parametrize("m,f,h,n,e", [(3, 64, 40, 24, 4), (16, 600, 33, 40, 4), (60, 70, 100, 50, 4), (64, 130, 1100, 140, 32),
+                                       (400, 130, 1100, 140, 32)])
+@pytest.mark.parametrize("weights", ["mx4", "bf16"])
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("power", [-100, -112, -122, -132])
+def test_tiny_rows(m, f, h, n, e, weights, dtype, power):
+    """Rows far below the numbers around 1: the terms that hold a float32 end at 2^-133, bfloat16's smallest number,
+    so a column is off by that at most.  (Large ups bring the values between the products back to normal ones.)"""
+    layer = Layer(m, f, h, n, e, weights)
+    large = min(-power, 120)
+    layer.up *= 2.0 ** large
+    if weights == "mx4":
+        layer.kw["up_scale"] += large
+    else:
+        layer.up_d *= 2.0 ** large
+    x = (torch.randn(m, f, generator=gen(m)) * 2.0 ** power).to(dtype)
+    y, index, weight = layer(padded(x), top_k=2, act="none")
+    want_i, want_p = route_exact(x, layer.router, None, 2, True)
+    assert torch.equal(index.cpu().long(), want_i)
+    want, tol = experts_exact(x, want_i, want_p, layer.up, layer.down, None, None, e, "none", False, dtype)
+    if dtype == torch.float32:
+        for i in range(e):
+            up, down = layer.up[i * h:(i + 1) * h].double().abs(), layer.down[i * n:(i + 1) * n].double().abs()
+            share = torch.where(want_i == i, want_p, 0.0).sum(1, keepdim=True)
+            tol += share * (2.0 ** -133 * up.sum(1) @ down.T)
+    assert ((y.cpu().double() - want).abs() <= tol).all()
