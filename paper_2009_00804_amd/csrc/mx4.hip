@@ -636,8 +636,8 @@ hipError_t launch_tile(const Mx4GemmArgs& g0, hipStream_t st) {
 }
 
 // --------------------------------------------------------------------------
-// many float rows by a narrow w (2^20 x 602 x 128 of bfloat16 319 us, 4.8 TB/s of the bytes it cannot do
-// without; of float32 714, 4.3; rounding and product in two launches 516): w stays in LDS in the
+// many float rows by a narrow w (2^20 x 602 x 128 of bfloat16 315 us, 4.9 TB/s of the bytes it cannot do
+// without; of float32 720, 4.3; rounding and product in two launches 516): w stays in LDS in the
 // order of its fragments, and a
 // wave takes 16 rows after 16 rows past it, 128 k at a time, with the next 128 on their
 // way.  Rows are loaded 16 lanes a row and rounded there; a piece of LDS of the wave's
@@ -675,13 +675,14 @@ struct StreamSpace {
   }
 };
 
-// waves a SIMD: float32 rows and eight column tiles would spill at four
-template <typename T, int NT>
-constexpr int kStreamPerSimd = sizeof(T) == 4 && NT == 8 ? 2 : 4;
+// waves a SIMD: eight column tiles spill at four (us, two / four: 2^20 x 602 x 128 of float32 720 / 973, of bfloat16,
+// which spill 18 registers, 315 / 329, 2^20 x 128 x 128 127 / 140, 65536 x 1024 x 128 32 / 38)
+template <int NT>
+constexpr int kStreamPerSimd = NT == 8 ? 2 : 4;
 
 template <typename T, int NT>
 __global__ __launch_bounds__(64 * kStreamWaves)
-__attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, NT>))) void k_mx4_stream(
+__attribute__((amdgpu_waves_per_eu(kStreamPerSimd<NT>))) void k_mx4_stream(
     Mx4GemmArgs g, int64_t tiles) {
   extern __shared__ uint4 space[];
   const int K = (int)g.K;
@@ -799,7 +800,7 @@ __attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, NT>))) void k_mx4_stream(
 template <typename T, int NT>
 hipError_t launch_stream(const Mx4GemmArgs& g, hipStream_t st) {
   const int64_t tiles = (g.M + 15) / 16;
-  const int lds = StreamSpace(g.K, NT).total, per = std::max(1, std::min(kStreamPerSimd<T, NT> / 2, 160 * 1024 / lds));
+  const int lds = StreamSpace(g.K, NT).total, per = std::max(1, std::min(kStreamPerSimd<NT> / 2, 160 * 1024 / lds));
   const int64_t blocks = std::min<int64_t>((tiles + kStreamWaves - 1) / kStreamWaves, 256 * per);
   hipLaunchKernelGGL((k_mx4_stream<T, NT>), dim3((unsigned)blocks), dim3(64 * kStreamWaves), lds, st, g, tiles);
   return hipGetLastError();
@@ -830,7 +831,7 @@ bool mx4_few(int a_dtype, int64_t M, int64_t N, int64_t K) {
 }
 
 // k_mx4_stream while w fits LDS, against rounding and product in two launches (us, bfloat16: 4096 x 602 x 128 11
-// / 13, 65536 x 1024 x 64 27 / 45, 2^20 x 128 x 128 138 / 178, 2^20 x 602 x 128 321 / 516)
+// / 13, 65536 x 1024 x 64 27 / 45, 2^20 x 128 x 128 127 / 178, 2^20 x 602 x 128 315 / 516)
 bool mx4_streams(int64_t M, int64_t N, int64_t K) {
   return M >= 4096 && N <= 128 && StreamSpace(K, N <= 16 ? 1 : N <= 32 ? 2 : N <= 64 ? 4 : 8).total <= 150 * 1024;
 }
