@@ -693,7 +693,8 @@ saga_status saga_apply_vertex_mx(const saga_mx_op* op, saga_cmat a, saga_cmat a_
  * or an infinity, or has a logit that is NaN or +inf, has index -1, weight NaN and
  * nothing but NaN in out; other rows do not see it.
  * Sums are float32.  Rows and the values h enter the matrix cores as sums of bfloat16
- * terms that hold them to 2^-24 (dtype F32) or, h of BF16 rows, 2^-16.
+ * terms that hold them to 2^-24 (dtype F32) or, h of BF16 rows, 2^-16 of themselves, and to
+ * 2^-133 where that is more.
  * A value h beyond float32's range makes its row of out NaN.
  * x: M x F, out: M x N, of dtype F32 or BF16.  router: E x F, router_dtype F32 or BF16.
  * Weights, one output channel a row, the experts' one below the other, weight_dtype BF16

@@ -495,7 +495,8 @@ class ResidualGCN:
     experts (may be absent): a dict with norm (F), router (F x E), up (E x F x H), down
     (E x H x F), top_k, act, and, each of which may be absent, gate (E x F x H: gated
     experts), b_router (E), b_up, b_gate (E x H) and b_down (E x F).  They are kept in
-    bfloat16, or in 4 bits with the transforms."""
+    bfloat16, or in 4 bits with the transforms.  They are meant for the vertices that are asked
+    for: every 1,024 rows read the experts' weights again."""
 
     def __init__(self, graph: S.Graph, weights: dict, dtype=torch.bfloat16, res_scale=1.0, eps=1e-5, bits=8):
         dev = graph.row_ptr.device
