@@ -72,6 +72,51 @@ def test_hidden_values_that_overflow(m, f, h, n, e, top_k, weights, dtype, gated
         assert torch.equal(y.cpu()[~took], want[0].cpu()[~took])
 
 
+FAMILIES = [(3, 64, 40, 24, 4), (16, 600, 33, 40, 4), (60, 70, 100, 50, 4), (64, 130, 1100, 140, 32),
+            (200, 130, 1100, 140, 32), (400, 130, 1100, 140, 32), (700, 130, 1100, 140, 32)]  # rows, f, h, n, experts
+
+
+@pytest.mark.parametrize("m,f,h,n,e", FAMILIES)
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("gated", [False, True])
+def test_blocks_of_weights_without_numbers(m, f, h, n, e, dtype, gated):
+    """the scale byte 255 in a 4-bit expert: in a down's row that channel of the rows that take the expert is NaN, in an
+    up's row all channels are; no other row sees it, nor does a byte behind the last block"""
+    layer = Layer(m, f, h, n, e, "mx4", gated)
+    x = padded(torch.randn(m, f, generator=gen(m)).to(dtype))
+    act = "sigmoid" if gated else "none"
+    want, index, weight = (t.cpu() for t in layer(x, top_k=2, act=act))
+    took = (index == 1).any(1)
+    assert took.any() and not took.all() and bool(torch.isfinite(want).all())
+    scale = layer.kw["down_scale"]
+    old = scale[n + 7, (h - 1) // 32].clone()
+    scale[n + 7, (h - 1) // 32] = 255
+    y = layer(x, top_k=2, act=act)[0].cpu()
+    assert bool(torch.isnan(y[took, 7]).all())
+    y[took, 7] = want[took, 7]
+    assert torch.equal(y, want)
+    scale[n + 7, (h - 1) // 32] = old
+    wide = h * (2 if gated else 1)
+    layer.kw["up_scale"][wide + wide - 1, 0] = 255
+    y, i2, w2 = (t.cpu() for t in layer(x, top_k=2, act=act))
+    assert torch.equal(i2, index) and torch.equal(w2, weight)
+    assert bool(torch.isnan(y[took]).all()) and torch.equal(y[~took], want[~took])
+
+
+@pytest.mark.parametrize("m,f,h,n,e", FAMILIES)
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_smallest_scales_of_weights(m, f, h, n, e, dtype):
+    """4-bit weights whose scales are at and next to the smallest, 2^-127, which no normal float32 is"""
+    layer = Layer(m, f, h, n, e, "mx4")
+    uq, us, up = four_bits(torch.randn(e * h, f, generator=gen(m)) * 2.0 ** -125)
+    assert int((us == 0).sum()) > 0 and int((us == 1).sum()) > 0
+    layer.up, layer.up_d, layer.kw["up_scale"] = up, uq, us
+    layer.router *= 2.0 ** -120
+    layer.router_d = padded(layer.router)
+    x = (torch.randn(m, f, generator=gen(m + 1)) * 2.0 ** 120).to(dtype)
+    layer.check(x, 2, "none")
+
+
 # --------------------------------------------------------------------------
 # products: every kernel with every epilogue
 # --------------------------------------------------------------------------
@@ -128,6 +173,26 @@ def test_tiles_and_their_epilogues(kind, m, k, n):
             got = L.mx4_linear(xd, q, s, x_scale=scale, bias=b, act=act, row_scale_deg=d, out_dtype=out)
             assert got.dtype == out and got.shape == (m, n)
             check_sums(got, v, mag, k, b, act, d)
+
+
+@pytest.mark.parametrize("m,k,n", [(3, 100, 40), (60, 1100, 130), (300, 1100, 2030), (4111, 333, 100), (40001, 333, 29),
+                                   (20011, 700, 130), (20011, 700, 700)])
+@pytest.mark.parametrize("kind", ["mx4", torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("power", [-125, 123])
+def test_scales_far_apart(kind, m, k, n, power):
+    """rows and weights at opposite ends of the scales, the smallest of which is 2^-127"""
+    L = LY()
+    g = torch.Generator(device=device()).manual_seed(m + k + n)
+    x = torch.randn(m, k, generator=g, device=device()) * 2.0 ** power
+    x = padded(x, dtype=torch.float32 if kind == "mx4" else kind)
+    q, s = L.quantize_rows_mx4(padded(torch.randn(n, k, generator=g, device=device()) * 2.0 ** -power))
+    xq, xs = L.quantize_rows_mx4(x)
+    assert power > 0 or m < 100 or int(xs.min()) == 0
+    x64 = L.dequantize_rows_mx4(xq, xs, k, dtype=torch.float32).double()
+    w64 = L.dequantize_rows_mx4(q, s, k, dtype=torch.float32).double()
+    xd, scale = (xq, xs) if kind == "mx4" else (x, None)
+    got = L.mx4_linear(xd, q, s, x_scale=scale, out_dtype=torch.float32)
+    check_sums(got, x64 @ w64.T, x64.abs() @ w64.abs().T, k, None, "none", None)
 
 
 # --------------------------------------------------------------------------
